@@ -127,7 +127,9 @@ enum kv_kernel_id {
     KV_KERNEL_PAGE_COPY = 2,      /* resume gather (cold -> hot) */
     KV_KERNEL_EVICT_COPY = 3,     /* eviction scatter and row clears (hot -> cold) */
     KV_KERNEL_PREFETCH_COPY = 4,  /* one layer's slices of spilled pages -> staging */
-    KV_KERNEL_COUNT = 5
+    KV_KERNEL_CHUNK = 5,          /* attention of prompt chunks and draft trees */
+    KV_KERNEL_CHUNK_MERGE = 6,    /* join of its partial results */
+    KV_KERNEL_COUNT = 7
 };
 
 typedef void* kv_stream_t;
@@ -205,8 +207,7 @@ int kv_pool_stats(const kv_pool* pool, kv_pool_stats_t* out);
 /* ----------------------------------------------------------------------- */
 
 /*
- * Create an ACTIVE session of seq_len tokens (a stand-in for prefill, which is
- * outside this library): allocates ceil(seq_len / 16) hot pages and writes the
+ * Create an ACTIVE session of seq_len tokens: allocates ceil(seq_len / 16) hot pages and writes the
  * session's page-table row.  hot_pages (host array, nullable) picks the exact
  * pages, which must be free and distinct.  NULL takes the lowest free ones; if
  * too few are free, least-recently-used pages of paused sessions are evicted
@@ -392,6 +393,32 @@ int kv_append_tokens_table(kv_pool* pool, int32_t layer_begin, int32_t num_layer
                            int64_t pt_stride, int32_t table_rows, const int32_t* rows,
                            const int32_t* positions, int32_t n, const void* k, const void* v,
                            kv_stream_t stream);
+
+/* Most drafted tokens per session in paged_tree_attention and kv_accept_drafts. */
+#define KV_MAX_DRAFTS 64
+
+/*
+ * The drafts that a verified step accepted become cached tokens (data path 3,
+ * Sec. III: fresh KV goes to the fast tier): for batch row b, row b of `table`
+ * (device int32 [batch][pt_stride]) and j < counts[b], token seq_lens[b] + j gets
+ * the K and V of draft path[b][j], for layers [layer_begin, layer_begin +
+ * num_layers) in one launch.  seq_lens and counts are device int32 [batch], path
+ * device int32 [batch][width], read when the kernel runs: the accepted counts
+ * never need to reach the host, and a captured call takes their current values.
+ * k and v are device arrays [num_layers][batch][width][num_kv_heads][head_dim] of
+ * the pool's dtype, 16-byte aligned: what paged_tree_attention read of every layer.
+ * A count above `width` counts as `width`, one below 0 as 0.  An entry that names
+ * no draft (outside [0, width)), whose position lies outside the table row or whose
+ * table entry names no page of either pool writes nothing.  The same draft may be
+ * named twice.  Rejected drafts are never written.
+ * As with kv_append_tokens_table the pool's bookkeeping is not read or changed:
+ * call kv_session_extend first, to the most tokens that may be accepted.
+ * Errors: KV_ERR_INVALID (layer range, batch, width, NULL or misaligned buffers,
+ * table shape, metadata-only pool), KV_ERR_HIP.
+ */
+int kv_accept_drafts(kv_pool* pool, int32_t layer_begin, int32_t num_layers, const int32_t* table,
+                     int64_t pt_stride, const int32_t* seq_lens, const int32_t* path, const int32_t* counts,
+                     int32_t batch, int32_t width, const void* k, const void* v, kv_stream_t stream);
 
 /*
  * Test and benchmark input: fill every slot of an ACTIVE session's pages, all
@@ -702,6 +729,94 @@ int paged_decode_attention_append(kv_pool* pool, int32_t layer, const void* q, c
 int paged_decode_attention_noalloc(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table,
                                    int64_t pt_stride, const int32_t* seq_lens, int32_t batch,
                                    int32_t num_q_heads, float scale, void* out, kv_stream_t stream);
+
+/* ----------------------------------------------------------------------- */
+/* Attention of several new tokens per session                              */
+/* ----------------------------------------------------------------------- */
+
+/* Device workspace bytes paged_prefill_attention needs (0: invalid arguments). */
+size_t paged_prefill_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t total_q, int32_t num_q_heads);
+
+/*
+ * Causal attention of prompt chunks for one layer: a new session's prompt, or the
+ * tool output or user text that a resumed session takes in (Sec. II, "Agentic AI
+ * Serving").  Row b brings n = q_starts[b + 1] - q_starts[b] queries, the last n of
+ * its L = seq_lens[b] tokens, whose K and V are already in its pages
+ * (kv_write_tokens, kv_append_tokens_table).  Query i of the row stands at position
+ * p = L - n + i and attends to tokens 0 .. p; for query head h (KV head
+ * g = h / (num_q_heads / num_kv_heads)):
+ *
+ *     out[q_starts[b] + i][h] = sum_t softmax_t(scale * q[q_starts[b] + i][h] . k_t) v_t,  t = 0 .. p,
+ *
+ * with token t in page page_table[b * pt_stride + t / 16], slot t % 16.
+ *
+ *   q          device [total_q][num_q_heads][head_dim], pool dtype: the rows' chunks
+ *              packed, of any lengths
+ *   q_starts   device int32 [batch + 1], ascending from 0 on to at most total_q;
+ *              a row without queries is fine.  A row whose range does not lie in
+ *              [0, total_q] or descends writes nothing
+ *   seq_lens   device int32 [batch], the new tokens included.  L < n or
+ *              L > 16 * pt_stride: the row's outputs are NaN and nothing is read
+ *   out        device, like q.  Only the rows' queries are written: queries before
+ *              q_starts[0] or from q_starts[batch] on are left as they were
+ *   workspace  device, >= paged_prefill_workspace_bytes(), 256-byte aligned
+ *
+ * A query sees its own tokens only: whatever later tokens of its row, other slots of the
+ * tail page and pages past it hold, NaN and infinities included, does not change it.
+ * A query that attends to a token on a page outside the pools (or on a staged copy,
+ * which only the decode reads) gets NaN.  Spilled pages (KV_PAGE_COLD) are read in place.
+ * q_starts, seq_lens and the page table are read when the kernels run: a call captured
+ * into a HIP graph (two kernels, nothing else) may be replayed after they change, for
+ * the same batch and total_q.  Concurrent calls need workspaces of their own.
+ * Numerics: float32 scores, maximum, sum and output; bf16 pools round the softmax
+ * weights to bf16 for the weighted sum of V, and the output once.  The result does not
+ * depend on where pages sit; it does depend, in float32 rounding, on the lengths of the
+ * batch's other rows, which move the cuts of the work split.
+ * num_q_heads / num_kv_heads must be an integer in 1 .. 16.
+ * Errors: KV_ERR_INVALID (shapes, sizes, layer, alignment to 16 bytes of q and out,
+ * workspace, metadata-only pool), KV_ERR_HIP.
+ */
+int paged_prefill_attention(kv_pool* pool, int32_t layer, const void* q, const int32_t* q_starts, int32_t total_q,
+                            const int32_t* page_table, int64_t pt_stride, const int32_t* seq_lens, int32_t batch,
+                            int32_t num_q_heads, float scale, void* out, void* workspace, size_t ws_bytes,
+                            kv_stream_t stream);
+
+/* Device workspace bytes paged_tree_attention needs (0: invalid arguments). */
+size_t paged_tree_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t width, int32_t num_q_heads);
+
+/*
+ * Attention of a tree of drafted tokens for one layer (the target model's check of a
+ * speculative draft: one read of the hot set serves several tokens of a session).  Row b
+ * has C = seq_lens[b] cached tokens and n = draft_lens[b] drafts (NULL: width of them).
+ * Draft i attends to tokens 0 .. C - 1 of the cache and to the drafts j < n whose bit j
+ * of masks[b][i] is set: itself and its ancestors, or whatever set the caller means (its
+ * own bit is not implied):
+ *
+ *     out[b][i][h] = sum_t softmax_t(scale * q[b][i][h] . k_t) v_t
+ *
+ * over those tokens and drafts.  The drafts' K and V are read from k_draft and v_draft
+ * and do not enter the cache: pages, page tables and cold copies stay as they are
+ * whatever is rejected, and kv_accept_drafts writes what was accepted.
+ *
+ *   q                 device [batch][width][num_q_heads][head_dim], pool dtype
+ *   k_draft, v_draft  device [batch][width][num_kv_heads][head_dim], pool dtype
+ *   masks             device uint64 [batch][width]; bits at or past n are ignored
+ *   draft_lens        device int32 [batch] or NULL; outside [0, width] it counts as the
+ *                     nearer end.  Drafts at or past n are neither read nor written
+ *   width             1 .. KV_MAX_DRAFTS
+ *   seq_lens          device int32 [batch]; C < 0 or C > 16 * pt_stride: NaN for the
+ *                     row's drafts, nothing is read
+ *   out               device, like q
+ *   workspace         device, >= paged_tree_workspace_bytes(), 256-byte aligned
+ *
+ * A draft that attends to nothing (C = 0 and an empty mask) gets zeros.  What a draft
+ * does not attend to does not change it, NaN and infinities included.  Page ids, spilled
+ * pages, capture, concurrent calls, numerics and errors as paged_prefill_attention.
+ */
+int paged_tree_attention(kv_pool* pool, int32_t layer, const void* q, const void* k_draft, const void* v_draft,
+                         const uint64_t* masks, const int32_t* draft_lens, int32_t width, const int32_t* page_table,
+                         int64_t pt_stride, const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, float scale,
+                         void* out, void* workspace, size_t ws_bytes, kv_stream_t stream);
 
 /*
  * The work split of paged_decode_attention, written out (device int32

@@ -1,0 +1,1006 @@
+// Attention of several new tokens per session over the paged cache, for gfx950:
+// prompt chunks (causal, the chunk's own K and V already in its pages) and trees of
+// drafted tokens (each draft sees its session's cached context and the drafts its mask
+// names; their K and V come dense and never enter the cache before they are accepted).
+//
+// Mathematics.  For a query at position p, out = sum_t w_t v_t / sum_t w_t with
+// w_t = 2^(c s_t - m), s_t = q . k_t over the tokens it attends to, c = scale log2(e).
+// One pass over the keys keeps the running maximum m, sum l and unnormalised output o of
+// every query; a new maximum rescales l and o.
+//
+// Tiles.  The query heads that share a KV head are rows of one product: a tile is `tok`
+// tokens x `group` heads of one (row b, KV head g), at most kRows rows, so each K/V
+// byte fetched serves all of them.  A wave owns 16 NT rows and computes
+//   S^T[t][row] = K[t][:] . Q[row][:]      v_mfma_f32_16x16x32_bf16 (f32: 16x16x4)
+//   O^T[d][row] += V^T[d][t] P^T[t][row]   the same instruction
+// Lane l of S^T holds row l % 16 and four tokens, so a row's maximum needs two cross-lane
+// steps and P goes into the second product without moving: for bf16 the tokens of a pair
+// of pages are assigned to the first product's A rows such that lane group l / 16 ends up
+// with 8 consecutive tokens, which are the 8 contraction slots it has in the second.
+//
+// Blocks of kBlock keys move from the pages to LDS by 16-byte direct loads (no
+// registers), STAGES - 1 blocks ahead.  A lane of such a load may fetch any 16 bytes
+// while its LDS place is fixed, so the order of 16-byte groups in LDS is chosen for the
+// fragment reads: every read is over 256 consecutive bytes per 16 lanes (no bank conflicts).
+//
+// Work split.  Tiles, with the keys they see as their cost, lie end to end in the order
+// (b, g, tile); `workers` workgroups take equal ranges, cut at block boundaries inside a
+// tile where need be, so prompts of any lengths, causal tiles and long contexts with few
+// queries all fill the GPU.  A tile cut between workers leaves partial results
+// (o, m, l) in the workspace, which chunk_merge_kernel joins.  Workgroups of one XCD
+// take neighbouring ranges: they read the same K/V through the same L2.
+
+#include "device_common.h"
+#include "kernels.h"
+
+#include <math.h>
+
+#include <type_traits>
+
+namespace hck {
+namespace {
+
+constexpr int kRsrcWord3 = 0x00020000;  // raw buffer, 32-bit data format (gfx9 family)
+constexpr int kXcds = 8;
+
+typedef const __attribute__((address_space(4))) int32_t* const_i32;  // read by scalar loads
+__device__ __forceinline__ const_i32 uniform_ptr(const int32_t* p) {
+    return (const_i32)(reinterpret_cast<uintptr_t>(p));
+}
+
+template <int D, bool BF16, int WAVES, int NT, int PAGES, int STAGES>
+struct Cfg {
+    static constexpr int kD = D, kWaves = WAVES, kNT = NT, kPages = PAGES, kStages = STAGES;
+    static constexpr bool kBf16 = BF16;
+    static constexpr int kElt = BF16 ? 2 : 4;
+    static constexpr int kX = 16 / kElt;                  // elements of a 16-byte group
+    static constexpr int kTile = kPageTokens * D * kElt;  // bytes of a K or V tile
+    static constexpr int kPage = 2 * kTile;               // a page's K and V tiles of one KV head
+    static constexpr int kBlock = PAGES * kPageTokens;    // keys per block
+    static constexpr int kStage = PAGES * kPage;          // LDS bytes of a block
+    static constexpr int kThreads = WAVES * kWave;
+    static constexpr int kWaveRows = 16 * NT;
+    static constexpr int kRows = WAVES * kWaveRows;
+    static constexpr int kTileLoads = kTile / 1024;       // 1 KiB loads of a tile
+    static constexpr int kLoads = PAGES * 2 * kTileLoads / WAVES;  // a wave's loads per block
+    static constexpr int kQ = D / (4 * kX);               // 16-byte Q fragments of a row per lane
+    static constexpr int kC = D / 16;                     // 16-dim output chunks
+    static_assert(kLoads >= 1 && (kLoads % kTileLoads == 0 || kTileLoads % kLoads == 0), "load split");
+    static_assert(!BF16 || PAGES % 2 == 0, "bf16 fragments take pages in pairs");
+};
+
+// What one row b brings: n tokens (or drafts), `ctx` tokens before them, the row's units.
+struct Row {
+    int start;     // first query of the row in q (tokens)
+    int n;         // queries
+    int ctx;       // cached tokens that every query sees
+    int bad;       // 1: lengths that do not fit, the row's outputs are NaN
+    int tiles;     // tiles per KV head
+    int64_t base;  // cost of tile i < tiles - 1: base + slope (i + 1)
+    int64_t slope;
+    int64_t last;  // cost of the last tile
+    __device__ int64_t tile_start(int64_t i) const { return i * base + slope * (i * (i + 1) / 2); }
+    __device__ int64_t head_units() const { return tiles ? tile_start(tiles - 1) + last : 0; }
+};
+
+// Fixed cost of a tile in keys: its queries' load, its output and the pipeline's start.
+constexpr int kTileCost = 64;
+
+template <class C, bool TREE>
+__device__ __forceinline__ Row row_info(const ChunkArgs& a, int b) {
+    Row r;
+    const int64_t most = static_cast<int64_t>(kPageTokens) * a.pt_stride;
+    const int32_t len = uniform_ptr(a.lens)[b];
+    if constexpr (TREE) {
+        int n = a.draft_lens ? uniform_ptr(a.draft_lens)[b] : a.width;
+        n = n < 0 ? 0 : (n > a.width ? a.width : n);
+        r.n = n;
+        r.start = b * a.width;
+        r.bad = len < 0 || len > most;
+        r.ctx = r.bad ? 0 : len;
+    } else {
+        const int s = uniform_ptr(a.starts)[b], e = uniform_ptr(a.starts)[b + 1];
+        const bool in = s >= 0 && e >= s && e <= a.total_q;
+        r.start = in ? s : 0;
+        r.n = in ? e - s : 0;
+        r.bad = len < r.n || len > most;
+        r.ctx = r.bad ? 0 : len - r.n;
+    }
+    r.tiles = (r.n + a.tile_tokens - 1) / a.tile_tokens;
+    if (r.bad) {
+        r.base = r.last = kTileCost;
+        r.slope = 0;
+    } else if constexpr (TREE) {
+        r.base = r.last = kTileCost + static_cast<int64_t>((r.n + C::kBlock - 1) / C::kBlock) * C::kBlock + r.ctx;
+        r.slope = 0;
+    } else {
+        r.base = kTileCost + static_cast<int64_t>(r.ctx);
+        r.slope = a.tile_tokens;
+        r.last = r.base + r.n;
+    }
+    return r;
+}
+
+// Blocks of tile i: the drafts' first (trees), then the context's.
+template <class C, bool TREE>
+__device__ __forceinline__ int draft_blocks(const Row& r) {
+    return TREE && !r.bad ? (r.n + C::kBlock - 1) / C::kBlock : 0;
+}
+template <class C, bool TREE>
+__device__ __forceinline__ int tile_keys(const ChunkArgs& a, const Row& r, int i) {
+    if (r.bad) return 0;
+    if (TREE) return r.ctx;
+    const int64_t hi = static_cast<int64_t>(i + 1) * a.tile_tokens;
+    return r.ctx + (hi < r.n ? static_cast<int>(hi) : r.n);
+}
+template <class C, bool TREE>
+__device__ __forceinline__ int tile_blocks(const ChunkArgs& a, const Row& r, int i) {
+    return draft_blocks<C, TREE>(r) + (tile_keys<C, TREE>(a, r, i) + C::kBlock - 1) / C::kBlock;
+}
+
+// A place in the order of blocks: block `blk` of tile `tile` of (row b, KV head g).
+struct Place {
+    int b, g, tile, blk;
+};
+
+// The place of unit `u` of row b (0 <= u < its units).  Both workers at a cut compute it
+// from the same numbers, so their ranges meet without a gap; a place past a tile's last
+// block is the next tile's first.  A tile without blocks belongs to the worker that has
+// its first unit.  Ranges of at least kTileCost + 2 kBlock units hold one block or more.
+template <class C, bool TREE>
+__device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int b, int64_t u) {
+    Place p;
+    p.b = b;
+    const int64_t h = r.head_units();
+    if (((u | h) >> 32) == 0) {
+        p.g = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(h));
+    } else {
+        p.g = static_cast<int>(u / h);
+    }
+    int64_t rem = u - p.g * h;
+    int lo = 0, hi = r.tiles - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (r.tile_start(mid) <= rem) lo = mid; else hi = mid - 1;
+    }
+    rem -= r.tile_start(lo);
+    p.tile = lo;
+    p.blk = 0;
+    if (rem > 0) {
+        const int64_t x = rem - kTileCost;
+        const int nb = tile_blocks<C, TREE>(a, r, lo);
+        const int64_t k = x <= 0 ? 0 : (x + C::kBlock - 1) / C::kBlock;
+        p.blk = k < nb ? static_cast<int>(k) : nb;
+        if (p.blk == nb) {
+            p.blk = 0;
+            if (++p.tile == r.tiles) {
+                p.tile = 0;
+                ++p.g;     // may be num_kv_heads: the walk moves on to the next row
+            }
+        }
+    }
+    return p;
+}
+
+__device__ __forceinline__ bool before(const Place& x, const Place& y) {
+    if (x.b != y.b) return x.b < y.b;
+    if (x.g != y.g) return x.g < y.g;
+    if (x.tile != y.tile) return x.tile < y.tile;
+    return x.blk < y.blk;
+}
+
+__device__ __forceinline__ int64_t wave_scan64(int64_t x) {
+    const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int64_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+
+// Worker k's range of places.  Every thread sums a run of rows; the two threads whose
+// runs hold the range's ends walk them.  Returns the number of workers with work.
+template <class C, bool TREE>
+__device__ int worker_range(const ChunkArgs& a, int k, Place& from, Place& to) {
+    __shared__ int64_t s_sum[C::kWaves];
+    __shared__ Place s_place[2];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int per = (a.batch + C::kThreads - 1) / C::kThreads;
+    const int lo = min(a.batch, tid * per), hi = min(a.batch, lo + per);
+    int64_t sum = 0;
+    for (int b = lo; b < hi; ++b) sum += a.num_kv_heads * row_info<C, TREE>(a, b).head_units();
+    const int64_t incl = wave_scan64(sum);
+    if (lane == kWave - 1) s_sum[wave] = incl;
+    if (tid < 2) s_place[tid] = Place{a.batch, 0, 0, 0};
+    __syncthreads();
+    int64_t total = 0, before_wave = 0;
+    for (int w = 0; w < C::kWaves; ++w) {
+        if (w == wave) before_wave = total;
+        total += s_sum[w];
+    }
+    const int64_t first = before_wave + incl - sum;
+    const int64_t least = kTileCost + 2 * C::kBlock;
+    int64_t n = total / least;
+    n = n < 1 ? 1 : (n > a.workers ? a.workers : n);
+    const int workers = total > 0 ? static_cast<int>(n) : 0;
+    if (k < workers) {
+        int64_t u[2];
+        if ((total >> 32) == 0) {   // k total / workers = k (total / workers) + k (total mod workers) / workers
+            const unsigned t = static_cast<unsigned>(total), w = static_cast<unsigned>(workers);
+            const unsigned q = t / w, m = t - q * w, kk = static_cast<unsigned>(k);
+            u[0] = static_cast<int64_t>(kk) * q + kk * m / w;
+            u[1] = static_cast<int64_t>(kk + 1) * q + (kk + 1) * m / w;
+        } else {
+            const int64_t q = total / workers, m = total % workers;
+            u[0] = k * q + k * m / workers;
+            u[1] = (k + 1) * q + (k + 1) * m / workers;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (u[j] < first || u[j] >= first + sum) continue;
+            int64_t at = first;
+            for (int b = lo; b < hi; ++b) {
+                const Row r = row_info<C, TREE>(a, b);
+                const int64_t units = a.num_kv_heads * r.head_units();
+                if (u[j] < at + units) {
+                    s_place[j] = place_of<C, TREE>(a, r, b, u[j] - at);
+                    break;
+                }
+                at += units;
+            }
+        }
+    }
+    __syncthreads();
+    from = s_place[0];
+    to = s_place[1];
+    int* f = reinterpret_cast<int*>(&from);
+    int* t = reinterpret_cast<int*>(&to);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = __builtin_amdgcn_readfirstlane(f[i]);
+        t[i] = __builtin_amdgcn_readfirstlane(t[i]);
+    }
+    return __builtin_amdgcn_readfirstlane(workers);
+}
+
+// Address of the tiles of page-table entry `pid` for a KV head; ok = 0 for an id outside
+// its pool (or a tag this call does not read).
+__device__ __forceinline__ const char* page_at(const ChunkArgs& a, int pid, unsigned head_off, bool& ok) {
+    const unsigned tag = static_cast<unsigned>(pid) >> 29;  // 0 hot, 2 cold, otherwise no page here
+    const unsigned id = static_cast<unsigned>(pid) & static_cast<unsigned>(kPageIdMask);
+    if (tag == 2 && a.tiered && id < static_cast<unsigned>(a.num_cold)) {
+        ok = true;
+        return a.cold + static_cast<int64_t>(id) * a.cold_stride + head_off;
+    }
+    ok = tag == 0 && id < static_cast<unsigned>(a.num_hot);
+    return a.hot + static_cast<int64_t>(ok ? id : 0) * a.hot_stride + head_off;
+}
+
+__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t rs, char* lds, unsigned voff) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(lds), 16, voff, 0, 0, 0);
+}
+
+// Waits until at most N of the wave's loads are in flight and its LDS reads are done,
+// then for the other waves.
+template <int N>
+__device__ __forceinline__ void wait_loads_and_sync() {
+    static_assert(N <= 63, "vmcnt");
+    __asm__ volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// A block's source for one wave: its page ids (context) or drafts.
+template <class C>
+struct Loader {
+    unsigned koff, voff;   // this lane's byte in a tile, first load
+    int wave, lane;
+    __device__ explicit Loader() {
+        lane = threadIdx.x & (kWave - 1);
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const int g = lane >> 4, x = lane & 15;
+        if constexpr (C::kBf16) {
+            // LDS place (dim group 4 i + g, x): x = 8 ab + 4 (t / 8) + t % 4 with ab = (t / 4) % 2
+            // (ab flipped in odd pages, so that the two pages of a pair fill all banks)
+            const int t = ((x >> 2) & 1) * 8 + (x >> 3) * 4 + (x & 3);
+            koff = (g * 16 + t) * 16;
+            // LDS place (16-dim chunk, half page, dim): dims of one half page side by side
+            voff = C::kTile + ((lane >> 5) * 16 + x) * 32 + (g & 1) * 16;
+        } else {
+            koff = lane * 16;
+            voff = C::kTile + x * 64 + g * 16;
+        }
+    }
+    // Loads of `lane`'s tiles of the block whose pages' ids are pid[0 .. PAGES).
+    __device__ __forceinline__ void pages(const ChunkArgs& a, const int (&pid)[C::kPages], unsigned head_off,
+                                          char* stage) const {
+#pragma unroll
+        for (int j = 0; j < (C::kLoads < C::kTileLoads ? 1 : C::kLoads / C::kTileLoads); ++j) {
+            int tile, first;
+            constexpr int kShare = C::kTileLoads > C::kLoads ? C::kTileLoads / C::kLoads : 1;  // waves of a tile
+            if constexpr (kShare > 1) {
+                tile = wave / kShare;
+                first = (wave % kShare) * C::kLoads;
+            } else {
+                tile = wave * (C::kLoads / C::kTileLoads) + j;
+                first = 0;
+            }
+            const int page = tile >> 1, kind = tile & 1;
+            int id = pid[0];
+#pragma unroll
+            for (int i = 1; i < C::kPages; ++i) id = page == i ? pid[i] : id;
+            bool ok;
+            const char* base = page_at(a, id, head_off, ok);
+            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                const_cast<char*>(base), static_cast<short>(0), ok ? C::kPage : 0, kRsrcWord3);
+            const unsigned off = kind ? voff : (C::kBf16 ? koff ^ ((page & 1) * 64) : koff);
+            char* dst = stage + tile * C::kTile + first * 1024;
+#pragma unroll
+            for (int i = 0; i < (C::kLoads < C::kTileLoads ? C::kLoads : C::kTileLoads); ++i)
+                load_lds16(rs, dst + i * 1024, off + (first + i) * 1024);
+        }
+    }
+    // The K of drafts [key0, key0 + kBlock) of a row, by the same kind of loads; drafts past n read zeros.
+    __device__ __forceinline__ void draft_keys(const ChunkArgs& a, int b, int g, int n, int key0, char* stage) const {
+        const unsigned row = a.num_kv_heads * D_bytes();
+        const char* base = static_cast<const char*>(a.k_new) +
+                           (static_cast<int64_t>(b) * a.width * a.num_kv_heads + g) * D_bytes();
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char*>(base), static_cast<short>(0), n > 0 ? (n - 1) * row + D_bytes() : 0, kRsrcWord3);
+        constexpr int kAll = C::kPages * C::kTileLoads;
+#pragma unroll
+        for (int j = 0; j < (kAll + C::kWaves - 1) / C::kWaves; ++j) {
+            const int idx = wave + j * C::kWaves;
+            if (idx < kAll) {
+                const int page = idx / C::kTileLoads, i = idx % C::kTileLoads;
+                const unsigned slot = (C::kBf16 ? koff ^ ((page & 1) * 64) : koff) / 16;  // (g, t)
+                const int key = key0 + page * kPageTokens + (slot & 15);
+                const unsigned dim_group = 4 * i + (slot >> 4);
+                // past the last draft the offset lies past the buffer's records: zeros, nothing is read
+                load_lds16(rs, stage + page * C::kPage + i * 1024, key < n ? key * row + dim_group * 16 : 0x7FFFFFF0u);
+            }
+        }
+    }
+    // The V of those drafts, transposed through registers.
+    __device__ __forceinline__ void draft_values(const ChunkArgs& a, int b, int g, int n, int key0, char* stage) const {
+        typedef typename std::conditional<C::kBf16, uint16_t, uint32_t>::type elt;
+        constexpr int kQuarters = kPageTokens / C::kX;            // 16-byte groups of a dim in a page
+        constexpr int kGroups = C::kPages * C::kD * kQuarters;    // of the block
+        const elt* base = static_cast<const elt*>(a.v_new) +
+                          (static_cast<int64_t>(b) * a.width * a.num_kv_heads + g) * C::kD;
+        const int64_t row = static_cast<int64_t>(a.num_kv_heads) * C::kD;
+#pragma unroll
+        for (int s = threadIdx.x; s < kGroups; s += C::kThreads) {
+            const int page = s / (C::kD * kQuarters), in = s % (C::kD * kQuarters);
+            const int c = in / (16 * kQuarters), q = in / 16 % kQuarters, dim = c * 16 + in % 16;
+            const int first = key0 + page * kPageTokens + q * C::kX;
+            elt e[C::kX];
+#pragma unroll
+            for (int j = 0; j < C::kX; ++j) e[j] = first + j < n ? base[(first + j) * row + dim] : elt(0);
+            u32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (C::kBf16) w[j] = e[2 * j] | (static_cast<unsigned>(e[2 * j + 1]) << 16);
+                else w[j] = e[j];
+            }
+            *reinterpret_cast<u32x4*>(stage + page * C::kPage + C::kTile + in * 16) = w;
+        }
+    }
+    static __device__ constexpr unsigned D_bytes() { return C::kD * C::kElt; }
+};
+
+template <class C>
+struct State {
+    u32x4 q[C::kNT][C::kQ];
+    f32x4 o[C::kNT][C::kC];
+    float m[C::kNT];   // running maximum of the raw scores
+    float l[C::kNT];   // this lane's part of the weights' sum
+};
+
+// What a block may show a wave's rows (only blocks that need it are masked).
+struct Mask {
+    int key0;                 // first key of the block
+    int len;                  // keys at or past it hold nothing of the row
+    unsigned ok;              // bit i: page i of the block exists
+    bool draft;
+};
+
+__device__ __forceinline__ unsigned nonfinite_code(unsigned h) {
+    // 1 for +inf, 2^8 for -inf, 2^16 for NaN, as bf16; 0 for a number.  A sum of up to 64
+    // of them tells which were there.
+    const unsigned e = h & 0x7FFFu;
+    if (e < 0x7F80u) return 0u;
+    return e > 0x7F80u ? 0x4780u : ((h & 0x8000u) ? 0x4380u : 0x3F80u);
+}
+__device__ __forceinline__ float nonfinite_code32(unsigned h) {
+    const unsigned e = h & 0x7FFFFFFFu;
+    if (e < 0x7F800000u) return 0.f;
+    return e > 0x7F800000u ? 65536.f : ((h >> 31) ? 256.f : 1.f);
+}
+__device__ __forceinline__ float nonfinite_value(float sum) {
+    if (sum == 0.f) return 0.f;
+    if (sum >= 65536.f) return NAN;
+    const float neg = floorf(sum * (1.f / 256.f));
+    const float pos = sum - 256.f * neg;
+    return neg == 0.f ? INFINITY : (pos == 0.f ? -INFINITY : NAN);
+}
+__device__ __forceinline__ bool any_nonfinite(const u32x4& v, bool bf16) {
+    bool hit = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (bf16) hit |= (v[j] & 0x7F80u) == 0x7F80u || (v[j] & 0x7F800000u) == 0x7F800000u;
+        else hit |= (v[j] & 0x7F800000u) == 0x7F800000u;
+    }
+    return hit;
+}
+
+// One block for one wave.  MASKED blocks hold keys that some row must not see: their
+// scores are left out, their weights are 0, and values at or past the row's length are
+// cleared.  `poison` (the block's V has infinities or NaN): a weight of 0 times such a
+// value would be NaN, so they are taken out of the product and put into the outputs of
+// the rows that attend to them.
+template <class C, bool TREE, bool MASKED>
+__device__ __forceinline__ void compute_block(State<C>& st, const char* stage, float scale, const Mask& mk,
+                                              const int (&lim)[C::kNT], const uint64_t (&seen)[C::kNT],
+                                              bool poison) {
+    const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, x = lane & 15;
+    f32x4 s[C::kPages][C::kNT];
+#pragma unroll
+    for (int t = 0; t < C::kPages; ++t)
+#pragma unroll
+        for (int n = 0; n < C::kNT; ++n) s[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // scores
+    if constexpr (C::kBf16) {
+        const char* kb = stage + (x >> 3) * C::kPage + g * 256 + (x & 7) * 16;
+        const unsigned flip = (x >> 3) * 128;
+#pragma unroll
+        for (int t = 0; t < C::kPages; ++t) {
+            const char* kt = kb + (t >> 1) * 2 * C::kPage + (((t & 1) * 128) ^ flip);
+#pragma unroll
+            for (int i = 0; i < C::kQ; ++i) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + i * 1024);
+#pragma unroll
+                for (int n = 0; n < C::kNT; ++n)
+                    s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, st.q[n][i]),
+                                                                      s[t][n], 0, 0, 0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < C::kPages; ++t) {
+            const char* kt = stage + t * C::kPage + lane * 16;
+#pragma unroll
+            for (int i = 0; i < C::kQ; ++i) {
+                const f32x4 kf = *reinterpret_cast<const f32x4*>(kt + i * 1024);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int n = 0; n < C::kNT; ++n)
+                        s[t][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j], __uint_as_float(st.q[n][i][j]),
+                                                                       s[t][n], 0, 0, 0);
+            }
+        }
+    }
+    // key of (t, r) in this lane, from the block's first
+    const auto key_of = [&](int t, int r) {
+        if constexpr (C::kBf16) return 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
+        else return 16 * t + 4 * g + r;
+    };
+    const auto page_of = [&](int t) { return C::kBf16 ? 2 * (t >> 1) + (g >> 1) : t; };
+    unsigned sees[C::kNT];   // bit 4 t + r: this row attends to that key
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int n = 0; n < C::kNT; ++n) {
+            unsigned bits = 0;
+#pragma unroll
+            for (int t = 0; t < C::kPages; ++t) {
+                const bool ok = (mk.ok >> page_of(t)) & 1u;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int key = mk.key0 + key_of(t, r);
+                    bool see = key < lim[n];
+                    if constexpr (TREE)
+                        if (mk.draft) see = key < mk.len && ((seen[n] >> (key & 63)) & 1u);
+                    bits |= see ? 1u << (4 * t + r) : 0u;
+                    s[t][n][r] = see ? (ok ? s[t][n][r] : NAN) : -INFINITY;
+                }
+            }
+            sees[n] = bits;
+        }
+    }
+    // running maximum
+    float mx[C::kNT];
+    bool rise = false;
+#pragma unroll
+    for (int n = 0; n < C::kNT; ++n) {
+        mx[n] = st.m[n];
+#pragma unroll
+        for (int t = 0; t < C::kPages; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx[n] = fmaxf(mx[n], s[t][n][r]);
+        rise |= mx[n] > st.m[n];
+    }
+    if (__builtin_amdgcn_ballot_w64(rise)) {
+#pragma unroll
+        for (int n = 0; n < C::kNT; ++n) {
+            float v = fmaxf(mx[n], __shfl_xor(mx[n], 16));
+            v = fmaxf(v, __shfl_xor(v, 32));
+            const float f = st.m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((st.m[n] - v) * scale);
+            st.l[n] *= f;
+#pragma unroll
+            for (int c = 0; c < C::kC; ++c) st.o[n][c] *= f;
+            st.m[n] = v;
+        }
+    }
+    // weights
+    u32x4 pb[C::kBf16 ? C::kPages / 2 : 1][C::kNT];
+#pragma unroll
+    for (int n = 0; n < C::kNT; ++n) {
+        const float ms = st.m[n] == -INFINITY ? 0.f : st.m[n] * scale;
+#pragma unroll
+        for (int t = 0; t < C::kPages; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][r], scale, -ms));
+                if constexpr (MASKED) w = (sees[n] >> (4 * t + r)) & 1u ? w : 0.f;
+                s[t][n][r] = w;
+                st.l[n] += w;
+            }
+            if constexpr (C::kBf16) {
+                // the weights round to bf16 for the product, as the matrix cores take them;
+                // their sum stays in float32
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                    const bf16x2 two = {static_cast<__bf16>(s[t][n][2 * h]), static_cast<__bf16>(s[t][n][2 * h + 1])};
+                    pb[t >> 1][n][2 * (t & 1) + h] = __builtin_bit_cast(unsigned, two);
+                }
+            }
+        }
+    }
+    // output
+    const char* vb;
+    if constexpr (C::kBf16) vb = stage + (g >> 1) * C::kPage + C::kTile + (g & 1) * 256 + x * 16;
+    else vb = stage + C::kTile + lane * 16;
+    constexpr int kSteps = C::kBf16 ? C::kPages / 2 : C::kPages;
+    u32x4 keep[MASKED ? kSteps : 1];
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int p = 0; p < kSteps; ++p)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (C::kBf16) {
+                    const int key = mk.key0 + 32 * p + 8 * g + 2 * j;
+                    const bool ok = (mk.ok >> (2 * p + (g >> 1))) & 1u;
+                    keep[p][j] = (ok && key < mk.len ? 0xFFFFu : 0u) | (ok && key + 1 < mk.len ? 0xFFFF0000u : 0u);
+                } else {
+                    const bool ok = (mk.ok >> p) & 1u;
+                    keep[p][j] = ok && mk.key0 + 16 * p + 4 * g + j < mk.len ? 0xFFFFFFFFu : 0u;
+                }
+            }
+        if (poison) {
+#pragma unroll
+            for (int c = 0; c < C::kC; ++c) {
+                f32x4 codes[C::kNT];
+#pragma unroll
+                for (int n = 0; n < C::kNT; ++n) codes[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int p = 0; p < kSteps; ++p) {
+                    u32x4 v, code;
+                    if constexpr (C::kBf16) v = *reinterpret_cast<const u32x4*>(vb + p * 2 * C::kPage + c * 512);
+                    else v = *reinterpret_cast<const u32x4*>(vb + p * C::kPage + c * 1024);
+                    v &= keep[p];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (C::kBf16) {
+                            const unsigned lo = nonfinite_code(v[j] & 0xFFFFu), hi = nonfinite_code(v[j] >> 16);
+                            code[j] = lo | (hi << 16);
+                            v[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+                        } else {
+                            const float f = nonfinite_code32(v[j]);
+                            code[j] = __float_as_uint(f);
+                            v[j] = f != 0.f ? 0u : v[j];
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < C::kNT; ++n) {
+                        if constexpr (C::kBf16) {
+                            u32x4 one;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int bit = 4 * (2 * p + (j >> 1)) + 2 * (j & 1);
+                                one[j] = ((sees[n] >> bit) & 1u ? 0x3F80u : 0u) |
+                                         ((sees[n] >> (bit + 1)) & 1u ? 0x3F800000u : 0u);
+                            }
+                            st.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pb[p][n]), st.o[n][c], 0, 0, 0);
+                            codes[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                __builtin_bit_cast(bf16x8, code), __builtin_bit_cast(bf16x8, one), codes[n], 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                st.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[j]), s[p][n][j],
+                                                                                  st.o[n][c], 0, 0, 0);
+                                codes[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                    __uint_as_float(code[j]), (sees[n] >> (4 * p + j)) & 1u ? 1.f : 0.f, codes[n], 0,
+                                    0, 0);
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < C::kNT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) st.o[n][c][r] += nonfinite_value(codes[n][r]);
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < C::kC; ++c) {
+#pragma unroll
+        for (int p = 0; p < kSteps; ++p) {
+            if constexpr (C::kBf16) {
+                u32x4 v = *reinterpret_cast<const u32x4*>(vb + p * 2 * C::kPage + c * 512);
+                if constexpr (MASKED) v &= keep[p];
+#pragma unroll
+                for (int n = 0; n < C::kNT; ++n)
+                    st.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pb[p][n]), st.o[n][c], 0, 0, 0);
+            } else {
+                u32x4 v = *reinterpret_cast<const u32x4*>(vb + p * C::kPage + c * 1024);
+                if constexpr (MASKED) v &= keep[p];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int n = 0; n < C::kNT; ++n)
+                        st.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[j]), s[p][n][j], st.o[n][c],
+                                                                          0, 0, 0);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void store4(const ChunkArgs& a, bool bf16, char* out, const f32x4& v) {
+    if (bf16) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        const bf16x4 w = {static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]),
+                          static_cast<__bf16>(v[3])};
+        *reinterpret_cast<u32x2*>(out) = __builtin_bit_cast(u32x2, w);
+    } else {
+        *reinterpret_cast<f32x4*>(out) = v;
+    }
+}
+
+template <class C, bool TREE>
+__global__ __launch_bounds__(C::kThreads, 2) void chunk_attend_kernel(const ChunkArgs a) {
+    extern __shared__ __align__(1024) char s_kv[];
+    __shared__ int s_poison;
+    const int lane = threadIdx.x & (kWave - 1), gq = lane >> 4, x = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    // neighbouring ranges to one XCD (blocks go to the XCDs in turn)
+    int k = blockIdx.x;
+    if (gridDim.x % kXcds == 0) k = (k % kXcds) * (gridDim.x / kXcds) + k / kXcds;
+    Place at, end;
+    const int workers = worker_range<C, TREE>(a, k, at, end);
+    int first_rec = -1, last_rec = -1;   // tiles this worker shares with the one before, the ones after
+    const Loader<C> ld;
+    const unsigned head_bytes = 2 * C::kTile;
+    bool first_piece = true;
+    if (k < workers) {
+        while (before(at, end)) {
+            if (at.b >= a.batch) break;
+            const Row row = row_info<C, TREE>(a, at.b);
+            if (at.g >= a.num_kv_heads || row.tiles == 0) {   // on to the next row with queries
+                int b = at.b + 1;
+                while (b < a.batch) {
+                    const uint64_t some = __builtin_amdgcn_ballot_w64(
+                        b + lane < a.batch && row_info<C, TREE>(a, min(b + lane, a.batch - 1)).tiles > 0);
+                    if (some) {
+                        b += __builtin_ctzll(some);
+                        break;
+                    }
+                    b += kWave;
+                }
+                at = Place{b, 0, 0, 0};
+                continue;
+            }
+            const int nb = tile_blocks<C, TREE>(a, row, at.tile);
+            const bool to_end = end.b == at.b && end.g == at.g && end.tile == at.tile;
+            const int k0 = at.blk, k1 = to_end ? end.blk : nb;
+            const int nd = draft_blocks<C, TREE>(row);
+            const int keys = tile_keys<C, TREE>(a, row, at.tile);
+            const int tok0 = at.tile * a.tile_tokens;
+            const int toks = min(a.tile_tokens, row.n - tok0);
+            const unsigned head_off = at.g * head_bytes;
+            const const_i32 pt = uniform_ptr(a.page_table + static_cast<int64_t>(at.b) * a.pt_stride);
+            const int last_page = (keys + kPageTokens - 1) / kPageTokens - 1;
+
+            if (!first_piece) wait_loads_and_sync<63>();   // the last piece's reads of the stages are over
+            first_piece = false;
+            if (threadIdx.x == 0) s_poison = 0;
+
+            // this wave's rows
+            State<C> st;
+            int lim[C::kNT], tok[C::kNT];
+            uint64_t seen[C::kNT];
+            bool live[C::kNT];
+            int64_t qrow[C::kNT];
+            const int w0 = wave * C::kWaveRows;
+            const bool wave_live = w0 < toks * a.group;
+            const int wtok0 = w0 / a.group;                                               // its first token
+            const int wtok1 = min(toks - 1, (w0 + C::kWaveRows - 1) / a.group);           // and last
+#pragma unroll
+            for (int n = 0; n < C::kNT; ++n) {
+                const int r = w0 + n * 16 + x;
+                tok[n] = r / a.group;
+                live[n] = tok[n] < toks;
+                const int t = live[n] ? tok0 + tok[n] : 0;
+                const int h = live[n] ? r % a.group : 0;
+                qrow[n] = ((static_cast<int64_t>(row.start) + t) * a.num_q_heads + at.g * a.group + h) * C::kD;
+                lim[n] = TREE ? row.ctx : (live[n] ? row.ctx + t + 1 : 0);
+                seen[n] = 0;
+                if constexpr (TREE)
+                    if (live[n]) seen[n] = a.masks[static_cast<int64_t>(at.b) * a.width + t];
+                const char* qp = static_cast<const char*>(a.q) + qrow[n] * C::kElt + gq * 16;
+#pragma unroll
+                for (int i = 0; i < C::kQ; ++i) {
+                    u32x4 v = {0u, 0u, 0u, 0u};
+                    if (live[n]) v = *reinterpret_cast<const u32x4*>(qp + i * 64);
+                    if (a.negate) v ^= C::kBf16 ? 0x80008000u : 0x80000000u;
+                    st.q[n][i] = v;
+                }
+                st.m[n] = -INFINITY;
+                st.l[n] = 0.f;
+#pragma unroll
+                for (int c = 0; c < C::kC; ++c) st.o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            const auto ids_of = [&](int blk, int (&pid)[C::kPages]) {
+                const int p0 = (blk - nd) * C::kPages;
+#pragma unroll
+                for (int i = 0; i < C::kPages; ++i) {
+                    // a page past the row's last holds no key that a row sees: no page
+                    const int p = p0 + i;
+                    const int e = pt[p <= last_page ? p : last_page];
+                    pid[i] = p <= last_page ? e : -1;
+                }
+            };
+            const auto ok_of = [&](const int (&pid)[C::kPages]) {
+                unsigned m = 0;
+#pragma unroll
+                for (int i = 0; i < C::kPages; ++i) {
+                    bool ok;
+                    (void)page_at(a, pid[i], 0, ok);
+                    m |= ok ? 1u << i : 0u;
+                }
+                return m;
+            };
+            unsigned oks = 0;   // page bits of the blocks in flight, the next one lowest
+            static_assert(C::kPages * C::kStages <= 32, "page bits");
+            const auto fetch = [&](int blk) {   // blk in [k0, k1): into its stage
+                char* stage = s_kv + ((blk - k0) % C::kStages) * C::kStage;
+                unsigned ok = (1u << C::kPages) - 1;
+                if (TREE && blk < nd) {
+                    ld.draft_keys(a, at.b, at.g, row.n, blk * C::kBlock, stage);
+                    ld.draft_values(a, at.b, at.g, row.n, blk * C::kBlock, stage);
+                } else {
+                    int pid[C::kPages];
+                    ids_of(blk, pid);
+                    ld.pages(a, pid, head_off, stage);
+                    ok = ok_of(pid);
+                }
+                return ok;
+            };
+#pragma unroll
+            for (int j = 0; j < C::kStages - 1; ++j)
+                if (k0 + j < k1) oks |= fetch(k0 + j) << (C::kPages * j);
+
+            for (int blk = k0; blk < k1; ++blk) {
+                const bool draft = TREE && blk < nd;
+                const int key0 = (draft ? blk : blk - nd) * C::kBlock;
+                char* stage = s_kv + ((blk - k0) % C::kStages) * C::kStage;
+                const unsigned ok = oks & ((1u << C::kPages) - 1);
+                oks >>= C::kPages;
+                // rows of this tile that do not see all of the block's keys
+                const bool partly = TREE ? draft : key0 + C::kBlock - 1 > row.ctx + tok0;
+                // the loads of this block are done; those of later blocks may go on
+                if (draft || k1 - 1 - blk < C::kStages - 2)
+                    wait_loads_and_sync<0>();
+                else
+                    wait_loads_and_sync<(C::kStages - 2) * C::kLoads>();
+                if (partly) {
+                    // an infinity or NaN among values that some row must not see?
+                    bool hit = false;
+                    constexpr int kVec = C::kPages * C::kTile / 16;
+                    for (int i = threadIdx.x; i < kVec; i += C::kThreads)
+                        hit |= any_nonfinite(*reinterpret_cast<const u32x4*>(stage + (i / (C::kTile / 16)) * C::kPage +
+                                                                            C::kTile + i % (C::kTile / 16) * 16),
+                                             C::kBf16);
+                    if (__builtin_amdgcn_ballot_w64(hit) && lane == 0) s_poison = 1;
+                    wait_loads_and_sync<63>();
+                }
+                if (blk + C::kStages - 1 < k1)
+                    oks |= fetch(blk + C::kStages - 1) << (C::kPages * (C::kStages - 2));
+                if (!wave_live) continue;
+                if (!TREE && key0 > row.ctx + tok0 + wtok1) continue;   // no row of this wave sees the block
+                const int len = draft ? row.n : keys;
+                const Mask mk{key0, len, ok, draft};
+                const bool masked = draft || key0 + C::kBlock > len || ok != (1u << C::kPages) - 1 ||
+                                    (!TREE && key0 + C::kBlock - 1 > row.ctx + tok0 + wtok0);
+                if (masked)
+                    compute_block<C, TREE, true>(st, stage, a.scale_log2, mk, lim, seen, partly && s_poison);
+                else
+                    compute_block<C, TREE, false>(st, stage, a.scale_log2, mk, lim, seen, false);
+            }
+
+            // the rows' sums over their four lanes
+            float l[C::kNT];
+#pragma unroll
+            for (int n = 0; n < C::kNT; ++n) {
+                l[n] = st.l[n] + __shfl_xor(st.l[n], 16);
+                l[n] += __shfl_xor(l[n], 32);
+                if (row.bad) l[n] = NAN;
+            }
+            if (k0 == 0 && k1 == nb) {
+#pragma unroll
+                for (int n = 0; n < C::kNT; ++n) {
+                    // l = 0: nothing to attend to, the output is zero; NaN stays NaN
+                    const float inv = l[n] == 0.f ? 0.f : 1.f / l[n];
+                    char* out = static_cast<char*>(a.out) + (qrow[n] + 4 * gq) * C::kElt;
+                    if (live[n]) {
+#pragma unroll
+                        for (int c = 0; c < C::kC; ++c) store4(a, C::kBf16, out + c * 16 * C::kElt, st.o[n][c] * inv);
+                    }
+                }
+            } else {
+                const int slot = 2 * k + (k0 == 0 ? 1 : 0);
+                float* po = a.part_o + static_cast<int64_t>(slot) * C::kRows * C::kD;
+                float* pm = a.part_ml + static_cast<int64_t>(slot) * 2 * C::kRows;
+#pragma unroll
+                for (int n = 0; n < C::kNT; ++n) {
+                    if (!live[n]) continue;
+                    const int r = w0 + n * 16 + x;
+#pragma unroll
+                    for (int c = 0; c < C::kC; ++c)
+                        *reinterpret_cast<f32x4*>(po + r * C::kD + c * 16 + 4 * gq) = st.o[n][c];
+                    if (gq == 0) {
+                        pm[r] = st.m[n] == -INFINITY ? -INFINITY : st.m[n] * a.scale_log2;
+                        pm[C::kRows + r] = l[n];
+                    }
+                }
+                if (k0 == 0) last_rec = 1; else first_rec = 1;
+            }
+            if (threadIdx.x == 0 && (last_rec == 1 || first_rec == 1)) {
+                ChunkRec* rec = a.recs + 2 * k + (last_rec == 1 ? 1 : 0);
+                *rec = ChunkRec{at.b, at.g, at.tile, 1};
+            }
+            if (last_rec == 1) last_rec = 2;
+            if (first_rec == 1) first_rec = 2;
+            if (to_end) break;
+            at.blk = 0;
+            if (++at.tile == row.tiles) {
+                at.tile = 0;
+                ++at.g;
+            }
+        }
+    }
+    if (threadIdx.x == 0) {
+        if (first_rec < 0) a.recs[2 * k] = ChunkRec{-1, -1, -1, 0};
+        if (last_rec < 0) a.recs[2 * k + 1] = ChunkRec{-1, -1, -1, 0};
+    }
+}
+
+// Joins the partial results of the tiles cut between workers: with M the largest of the
+// parts' maxima, out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Block (k, y) takes
+// rows of the tile whose first part worker k left in slot 2 k + 1; its other parts are
+// slots 2 (k + 1), 2 (k + 2), .. as long as they name the same tile.  A wave per row, a
+// float4 per lane, kWave / (D / 4) parts at a time.
+constexpr int kMergeRows = 16;
+
+template <class C, bool TREE>
+__global__ __launch_bounds__(kBlockThreads) void chunk_merge_kernel(const ChunkArgs a) {
+    const int k = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    ChunkRec rec = a.recs[2 * k + 1];
+    if (!rec.used) return;
+    rec.b = __builtin_amdgcn_readfirstlane(rec.b);
+    const Row row = row_info<C, TREE>(a, rec.b);
+    const int tok0 = rec.tile * a.tile_tokens;
+    const int rows = min(a.tile_tokens, row.n - tok0) * a.group;
+    if (static_cast<int>(blockIdx.y) * kMergeRows >= rows) return;
+    int parts = 1;   // slots 2 k + 1, 2 (k + 1), ..
+    for (int j = k + 1; j < a.workers; j += kWave) {
+        bool same = false;
+        if (j + lane < a.workers) {
+            const ChunkRec r = a.recs[2 * (j + lane)];
+            same = r.used && r.b == rec.b && r.g == rec.g && r.tile == rec.tile;
+        }
+        const uint64_t m = __builtin_amdgcn_ballot_w64(same);
+        const int run = m == ~0ull ? kWave : __builtin_ctzll(~m);
+        parts += run;
+        if (run < kWave) break;
+    }
+    constexpr int kLanes = C::kD / 4, kAtOnce = kWave / kLanes;
+    const int sub = lane / kLanes, col = lane % kLanes;
+    for (int i = wave; i < kMergeRows; i += kBlockWaves) {
+        const int r = blockIdx.y * kMergeRows + i;
+        if (r >= rows) break;
+        const auto slot_of = [&](int p) { return p == 0 ? 2 * k + 1 : 2 * (k + p); };
+        float top = -INFINITY;
+        for (int p = lane; p < parts; p += kWave)
+            top = fmaxf(top, a.part_ml[static_cast<int64_t>(slot_of(p)) * 2 * C::kRows + r]);
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        float den = 0.f;
+#pragma unroll 4
+        for (int p = sub; p < parts; p += kAtOnce) {
+            const int64_t slot = slot_of(p);
+            const float m = a.part_ml[slot * 2 * C::kRows + r], l = a.part_ml[slot * 2 * C::kRows + C::kRows + r];
+            const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + (slot * C::kRows + r) * C::kD + col * 4);
+            const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+            acc += o * w;
+            // a part whose scores were all NaN has no maximum: its sum is NaN
+            den += l * w;
+        }
+#pragma unroll
+        for (int d = kLanes; d < kWave; d <<= 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], d);
+            den += __shfl_xor(den, d);
+        }
+        if (sub == 0) {
+            const int t = tok0 + r / a.group, h = r % a.group;
+            const float inv = den == 0.f ? 0.f : 1.f / den;
+            char* out = static_cast<char*>(a.out) +
+                        (((static_cast<int64_t>(row.start) + t) * a.num_q_heads + rec.g * a.group + h) * C::kD + col * 4) *
+                            C::kElt;
+            store4(a, C::kBf16, out, acc * inv);
+        }
+    }
+}
+
+template <class C, bool TREE>
+hipError_t launch_cfg(ChunkArgs a, int workers, hipStream_t s, const LaunchEvents& ev, const LaunchEvents& ev_merge) {
+    a.tile_tokens = C::kRows / a.group;
+    a.workers = workers;
+    chunk_workspace_layout(a, C::kRows, C::kD);
+    const size_t lds = static_cast<size_t>(C::kStages) * C::kStage;
+    const void* kern = reinterpret_cast<const void*>(&chunk_attend_kernel<C, TREE>);
+    hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+    if (e != hipSuccess) return e;
+    void* args[] = {&a};
+    e = launch_kernel(kern, dim3(workers), dim3(C::kThreads), args, lds, s, ev);
+    if (e != hipSuccess) return e;
+    const void* merge = reinterpret_cast<const void*>(&chunk_merge_kernel<C, TREE>);
+    return launch_kernel(merge, dim3(workers, (C::kRows + kMergeRows - 1) / kMergeRows), dim3(kBlockThreads), args, 0,
+                         s, ev_merge);
+}
+
+template <int D, bool BF16, bool TREE>
+hipError_t launch_shape(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s, const LaunchEvents& ev,
+                        const LaunchEvents& ev_merge) {
+    constexpr int kPages = BF16 ? 4 : 2;
+    if (p.rows == 64) return launch_cfg<Cfg<D, BF16, 4, 1, kPages, 2>, TREE>(a, p.workers, s, ev, ev_merge);
+    return launch_cfg<Cfg<D, BF16, 8, 2, kPages, 3>, TREE>(a, p.workers, s, ev, ev_merge);
+}
+
+}  // namespace
+
+// Rows of a tile: 64 where a row's queries fit into them, else 256.
+ChunkPlan chunk_plan(int cus, int group, int64_t rows_per_seq) {
+    ChunkPlan p;
+    p.rows = rows_per_seq <= 64 ? 64 : 256;
+    p.workers = p.rows == 64 ? 2 * cus : cus;
+    return p;
+}
+
+hipError_t launch_chunk_attention(const ChunkArgs& a, const ChunkPlan& p, int head_dim, int dtype, bool tree,
+                                  hipStream_t s, const LaunchEvents& ev, const LaunchEvents& ev_merge) {
+    if (a.batch <= 0) return hipSuccess;
+#define HCK_CHUNK(DD, BB) \
+    (tree ? launch_shape<DD, BB, true>(a, p, s, ev, ev_merge) : launch_shape<DD, BB, false>(a, p, s, ev, ev_merge))
+    if (head_dim == 128) return dtype == kDtypeBf16 ? HCK_CHUNK(128, true) : HCK_CHUNK(128, false);
+    return dtype == kDtypeBf16 ? HCK_CHUNK(64, true) : HCK_CHUNK(64, false);
+#undef HCK_CHUNK
+}
+
+}  // namespace hck

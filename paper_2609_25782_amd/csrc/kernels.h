@@ -276,4 +276,74 @@ struct AppendTableArgs {
 };
 hipError_t launch_append_table(const AppendTableArgs& a, hipStream_t s);
 
+// Attention of several new tokens per row (prompt chunks, draft trees).
+struct ChunkRec {   // a part of a tile left in the workspace
+    int32_t b, g, tile, used;
+};
+struct ChunkArgs {
+    const char* hot;           // slice of hot page 0 for the layer
+    int64_t hot_stride;
+    const char* cold;          // the same of the cold pool (entries tagged KV_PAGE_COLD, if `tiered`)
+    int64_t cold_stride;
+    int32_t num_hot, num_cold, tiered;
+    int32_t num_kv_heads, group, num_q_heads;
+    const void* q;             // prompt chunks: [total_q][num_q_heads][D]; trees: [batch][width][num_q_heads][D]
+    void* out;                 // like q
+    const int32_t* page_table;
+    int64_t pt_stride;
+    const int32_t* lens;       // [batch] tokens in the pages (prompt chunks: the new ones included)
+    int32_t batch;
+    // prompt chunks
+    const int32_t* starts;     // [batch + 1] row b's queries are starts[b] .. starts[b + 1]
+    int32_t total_q;
+    // trees
+    int32_t width;             // drafts per row, at most 64
+    const int32_t* draft_lens; // [batch], or null: width
+    const uint64_t* masks;     // [batch][width]
+    const void* k_new;         // [batch][width][num_kv_heads][D]
+    const void* v_new;
+    float scale_log2;          // |scale| log2(e)
+    int32_t negate;            // 1: the scale is negative, the queries change sign
+    void* workspace;
+    // set by the launch
+    int32_t tile_tokens, workers;
+    float* part_o;             // [2 workers][rows of a tile][D]
+    float* part_ml;            // [2 workers][2][rows of a tile]
+    ChunkRec* recs;            // [2 workers]
+};
+struct ChunkPlan {
+    int32_t rows;      // rows of a tile
+    int32_t workers;   // workgroups
+};
+ChunkPlan chunk_plan(int cus, int group, int64_t rows_per_seq);
+inline size_t chunk_workspace_bytes(const ChunkPlan& p, int head_dim) {
+    const size_t n = static_cast<size_t>(2) * p.workers * (static_cast<size_t>(p.rows) * (head_dim + 2) * 4 + sizeof(ChunkRec));
+    return (n + 255) & ~static_cast<size_t>(255);
+}
+inline void chunk_workspace_layout(ChunkArgs& a, int rows, int head_dim) {
+    a.part_o = static_cast<float*>(a.workspace);
+    a.part_ml = a.part_o + static_cast<int64_t>(2) * a.workers * rows * head_dim;
+    a.recs = reinterpret_cast<ChunkRec*>(a.part_ml + static_cast<int64_t>(4) * a.workers * rows);
+}
+hipError_t launch_chunk_attention(const ChunkArgs& a, const ChunkPlan& p, int head_dim, int dtype, bool tree,
+                                  hipStream_t s, const LaunchEvents& ev = {}, const LaunchEvents& ev_merge = {});
+
+// Accepted drafts into the pages: token lens[b] + j of table row b gets draft path[b][j],
+// j < counts[b], for layers [layer, layer + num_layers).
+struct AcceptArgs {
+    PoolGeom hot;
+    PoolGeom cold;
+    int32_t num_hot, num_cold;
+    const int32_t* table;        // device [batch][pt_stride]
+    int64_t pt_stride;
+    const int32_t* lens;         // device [batch]
+    const int32_t* path;         // device [batch][width]
+    const int32_t* counts;       // device [batch]
+    int32_t batch, width;
+    int32_t num_kv_heads, head_dim, dtype, layer, num_layers;
+    const void* k;               // [num_layers][batch][width][kv_heads][head_dim]
+    const void* v;
+};
+hipError_t launch_accept_drafts(const AcceptArgs& a, hipStream_t s);
+
 }  // namespace hck

@@ -1167,6 +1167,49 @@ int kv_append_tokens_table(kv_pool* pool, int32_t layer_begin, int32_t num_layer
     return KV_OK;
 }
 
+int kv_accept_drafts(kv_pool* pool, int32_t layer_begin, int32_t num_layers, const int32_t* table,
+                     int64_t pt_stride, const int32_t* seq_lens, const int32_t* path, const int32_t* counts,
+                     int32_t batch, int32_t width, const void* k, const void* v, kv_stream_t stream) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (pool->meta) return fail(KV_ERR_INVALID, "metadata-only pool has no pages");
+    if (layer_begin < 0 || num_layers < 1 || layer_begin + static_cast<int64_t>(num_layers) > pool->d.num_layers)
+        return fail(KV_ERR_INVALID, "layers from %d, %d of them, outside the pool's %d", layer_begin, num_layers,
+                    pool->d.num_layers);
+    if (batch < 0 || batch > kMaxDecodeBatch)
+        return fail(KV_ERR_INVALID, "batch %d outside [0, %d]", batch, kMaxDecodeBatch);
+    if (width < 1 || width > KV_MAX_DRAFTS)
+        return fail(KV_ERR_INVALID, "width %d outside [1, %d]", width, KV_MAX_DRAFTS);
+    if (batch == 0) return KV_OK;
+    if (!table || !seq_lens || !path || !counts || !k || !v) return fail(KV_ERR_INVALID, "NULL buffer");
+    if (pt_stride < 1 || static_cast<int64_t>(batch) * pt_stride >= (int64_t(1) << 31))
+        return fail(KV_ERR_INVALID, "bad page-table stride");
+    if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15)
+        return fail(KV_ERR_INVALID, "k and v must be 16-byte aligned");
+    DeviceGuard g(pool->d.device);
+    hck::AcceptArgs a;
+    a.hot = pool->hot_geom;
+    a.cold = pool->cold_geom;
+    a.num_hot = pool->d.num_hot_pages;
+    a.num_cold = pool->cold ? pool->d.num_cold_pages : 0;
+    a.table = table;
+    a.pt_stride = pt_stride;
+    a.lens = seq_lens;
+    a.path = path;
+    a.counts = counts;
+    a.batch = batch;
+    a.width = width;
+    a.num_kv_heads = pool->d.num_kv_heads;
+    a.head_dim = pool->d.head_dim;
+    a.dtype = pool->d.dtype;
+    a.layer = layer_begin;
+    a.num_layers = num_layers;
+    a.k = k;
+    a.v = v;
+    hipError_t e = hck::launch_accept_drafts(a, pool->strm(stream));
+    if (e != hipSuccess) return hip_fail(e, "accept launch");
+    return KV_OK;
+}
+
 int kv_fill_synthetic_pages(kv_pool* pool, int32_t sid, int32_t gen_sid, uint64_t seed,
                             float value_mult, int32_t first_page, int32_t num_pages,
                             kv_stream_t stream) {
@@ -1539,6 +1582,143 @@ int paged_decode_attention_append(kv_pool* pool, int32_t layer, const void* q, c
     if (!k_new || !v_new) return fail(KV_ERR_INVALID, "NULL k_new or v_new");
     return hck::decode_impl(pool, layer, q, page_table, pt_stride, seq_lens, batch, num_q_heads, scale,
                             out, workspace, ws_bytes, stream, /*no_alloc=*/false, k_new, v_new);
+}
+
+}  // extern "C"
+
+namespace {
+
+// Checks and arguments that prompt chunks and draft trees share.  rows_per_seq: queries of
+// a row times the query heads of a KV head, the average (prompt chunks) or the most (trees).
+int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
+               const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, float scale, void* out, hck::ChunkArgs& a) {
+    if (pool->meta) return fail(KV_ERR_INVALID, "metadata-only pool has no pages");
+    if (layer < 0 || layer >= pool->d.num_layers) return fail(KV_ERR_INVALID, "bad layer %d", layer);
+    if (!q || !page_table || !seq_lens || !out) return fail(KV_ERR_INVALID, "NULL buffer");
+    if (num_q_heads <= 0 || num_q_heads % pool->d.num_kv_heads)
+        return fail(KV_ERR_INVALID, "query heads %d not a multiple of KV heads %d", num_q_heads,
+                    pool->d.num_kv_heads);
+    if (num_q_heads / pool->d.num_kv_heads > 16) return fail(KV_ERR_INVALID, "more than 16 query heads per KV head");
+    if (pt_stride < 1 || static_cast<int64_t>(batch) * pt_stride >= (int64_t(1) << 31))
+        return fail(KV_ERR_INVALID, "bad page-table stride");
+    if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15)
+        return fail(KV_ERR_INVALID, "q and out must be 16-byte aligned");
+    a = hck::ChunkArgs{};
+    a.hot = hck::slice_at(pool->hot_geom, 0, layer);
+    a.hot_stride = pool->hot_geom.page_stride;
+    a.num_hot = pool->d.num_hot_pages;
+    a.cold = pool->cold ? hck::slice_at(pool->cold_geom, 0, layer) : nullptr;
+    a.cold_stride = pool->cold_geom.page_stride;
+    a.num_cold = pool->cold ? pool->d.num_cold_pages : 0;
+    a.tiered = pool->tiered() ? 1 : 0;
+    a.num_kv_heads = pool->d.num_kv_heads;
+    a.group = num_q_heads / pool->d.num_kv_heads;
+    a.num_q_heads = num_q_heads;
+    a.q = q;
+    a.out = out;
+    a.page_table = page_table;
+    a.pt_stride = pt_stride;
+    a.lens = seq_lens;
+    a.batch = batch;
+    a.scale_log2 = (scale < 0.f ? -scale : scale) * 1.4426950408889634f;
+    a.negate = scale < 0.f ? 1 : 0;
+    return KV_OK;
+}
+
+int64_t prefill_rows(const kv_pool* pool, int32_t batch, int32_t total_q, int32_t num_q_heads) {
+    const int64_t group = num_q_heads / pool->d.num_kv_heads;
+    return (static_cast<int64_t>(total_q) * group + batch - 1) / batch;
+}
+
+int chunk_launch(kv_pool* pool, hck::ChunkArgs& a, int64_t rows_per_seq, bool tree, void* workspace, size_t ws_bytes,
+                 kv_stream_t stream) {
+    const hck::ChunkPlan plan = hck::chunk_plan(pool->cus, a.group, rows_per_seq);
+    const size_t need = hck::chunk_workspace_bytes(plan, pool->d.head_dim);
+    if (!workspace) return fail(KV_ERR_INVALID, "NULL workspace");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KV_ERR_INVALID, "workspace must be 256-byte aligned");
+    if (ws_bytes < need) return fail(KV_ERR_INVALID, "workspace %zu bytes, need %zu", ws_bytes, need);
+    a.workspace = workspace;
+    DeviceGuard g(pool->d.device);
+    hipStream_t st = pool->strm(stream);
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    const hipError_t ce = hipStreamIsCapturing(st, &cap);
+    if (ce != hipSuccess) return hip_fail(ce, "hipStreamIsCapturing");
+    // under capture the call records its two kernels only, without profiling events
+    const bool prof = cap == hipStreamCaptureStatusNone;
+    hck::LaunchEvents ev = prof ? pool->prof_events() : hck::LaunchEvents{};
+    hck::LaunchEvents evm = prof ? pool->prof_events() : hck::LaunchEvents{};
+    const hipError_t e =
+        hck::launch_chunk_attention(a, plan, pool->d.head_dim, pool->d.dtype, tree, st, ev, evm);
+    pool->prof_done(KV_KERNEL_CHUNK, ev, e);
+    pool->prof_done(KV_KERNEL_CHUNK_MERGE, evm, e);
+    if (e != hipSuccess) return hip_fail(e, tree ? "tree attention launch" : "prompt attention launch");
+    return KV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t paged_prefill_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t total_q, int32_t num_q_heads) {
+    if (!pool || pool->meta || batch < 0 || total_q < 0 || num_q_heads <= 0 || num_q_heads % pool->d.num_kv_heads)
+        return 0;
+    if (batch == 0) return 256;
+    const hck::ChunkPlan plan = hck::chunk_plan(pool->cus, num_q_heads / pool->d.num_kv_heads,
+                                                prefill_rows(pool, batch, total_q, num_q_heads));
+    return hck::chunk_workspace_bytes(plan, pool->d.head_dim);
+}
+
+int paged_prefill_attention(kv_pool* pool, int32_t layer, const void* q, const int32_t* q_starts, int32_t total_q,
+                            const int32_t* page_table, int64_t pt_stride, const int32_t* seq_lens, int32_t batch,
+                            int32_t num_q_heads, float scale, void* out, void* workspace, size_t ws_bytes,
+                            kv_stream_t stream) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (batch < 0 || batch > kMaxDecodeBatch)
+        return fail(KV_ERR_INVALID, "batch %d outside [0, %d]", batch, kMaxDecodeBatch);
+    if (total_q < 0) return fail(KV_ERR_INVALID, "total_q %d is negative", total_q);
+    if (batch == 0 || total_q == 0) return KV_OK;
+    hck::ChunkArgs a;
+    const int rc = chunk_args(pool, layer, q, page_table, pt_stride, seq_lens, batch, num_q_heads, scale, out, a);
+    if (rc != KV_OK) return rc;
+    if (!q_starts) return fail(KV_ERR_INVALID, "NULL q_starts");
+    a.starts = q_starts;
+    a.total_q = total_q;
+    return chunk_launch(pool, a, prefill_rows(pool, batch, total_q, num_q_heads), /*tree=*/false, workspace, ws_bytes,
+                        stream);
+}
+
+size_t paged_tree_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t width, int32_t num_q_heads) {
+    if (!pool || pool->meta || batch < 0 || width < 1 || width > KV_MAX_DRAFTS || num_q_heads <= 0 ||
+        num_q_heads % pool->d.num_kv_heads)
+        return 0;
+    const int32_t group = num_q_heads / pool->d.num_kv_heads;
+    return hck::chunk_workspace_bytes(hck::chunk_plan(pool->cus, group, static_cast<int64_t>(width) * group),
+                                      pool->d.head_dim);
+}
+
+int paged_tree_attention(kv_pool* pool, int32_t layer, const void* q, const void* k_draft, const void* v_draft,
+                         const uint64_t* masks, const int32_t* draft_lens, int32_t width, const int32_t* page_table,
+                         int64_t pt_stride, const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, float scale,
+                         void* out, void* workspace, size_t ws_bytes, kv_stream_t stream) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (batch < 0 || batch > kMaxDecodeBatch)
+        return fail(KV_ERR_INVALID, "batch %d outside [0, %d]", batch, kMaxDecodeBatch);
+    if (width < 1 || width > KV_MAX_DRAFTS)
+        return fail(KV_ERR_INVALID, "width %d outside [1, %d]", width, KV_MAX_DRAFTS);
+    if (batch == 0) return KV_OK;
+    hck::ChunkArgs a;
+    const int rc = chunk_args(pool, layer, q, page_table, pt_stride, seq_lens, batch, num_q_heads, scale, out, a);
+    if (rc != KV_OK) return rc;
+    if (!k_draft || !v_draft || !masks) return fail(KV_ERR_INVALID, "NULL k_draft, v_draft or masks");
+    if ((reinterpret_cast<uintptr_t>(k_draft) | reinterpret_cast<uintptr_t>(v_draft)) & 15)
+        return fail(KV_ERR_INVALID, "k_draft and v_draft must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(masks) & 7) return fail(KV_ERR_INVALID, "masks must be 8-byte aligned");
+    a.k_new = k_draft;
+    a.v_new = v_draft;
+    a.masks = masks;
+    a.draft_lens = draft_lens;
+    a.width = width;
+    return chunk_launch(pool, a, static_cast<int64_t>(width) * a.group, /*tree=*/true, workspace, ws_bytes, stream);
 }
 
 }  // extern "C"

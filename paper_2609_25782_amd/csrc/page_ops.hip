@@ -488,6 +488,35 @@ __global__ __launch_bounds__(kAppendThreads) void append_table_kernel(const Appe
     }
 }
 
+// Accepted drafts into the pages: block (b * width + j, y) writes accepted draft j of row b
+// for layers y, y + gridDim.y, ..
+__global__ __launch_bounds__(kAppendThreads) void accept_drafts_kernel(const AcceptArgs a) {
+    const int elt = a.dtype == kDtypeBf16 ? 2 : 4;
+    const int x = 16 / elt;
+    const int groups = a.head_dim / x;
+    const int64_t tile = static_cast<int64_t>(kPageTokens) * a.head_dim * elt;
+    const int b = static_cast<int>(blockIdx.x) / a.width, j = static_cast<int>(blockIdx.x) % a.width;
+    if (j >= a.counts[b]) return;
+    const int32_t src = a.path[blockIdx.x], len = a.lens[b];
+    if (src < 0 || src >= a.width || len < 0) return;
+    const int64_t pos = static_cast<int64_t>(len) + j;
+    if (pos / kPageTokens >= a.pt_stride) return;
+    const int32_t pid = a.table[static_cast<int64_t>(b) * a.pt_stride + pos / kPageTokens];
+    const unsigned id = static_cast<unsigned>(pid) & static_cast<unsigned>(kPageIdMask);
+    const unsigned tag = static_cast<unsigned>(pid) >> 29;   // 0 hot, 2 cold; others name no page
+    if (!((tag == 0 && id < static_cast<unsigned>(a.num_hot)) || (tag == 2 && id < static_cast<unsigned>(a.num_cold))))
+        return;
+    const AppendThread w = append_thread(static_cast<int>(threadIdx.x), groups);
+    if (w.head >= a.num_kv_heads) return;
+    for (int li = static_cast<int>(blockIdx.y); li < a.num_layers; li += static_cast<int>(gridDim.y)) {
+        char* lh = entry_slice(a.hot, a.cold, pid, a.layer + li) + static_cast<int64_t>(w.head) * 2 * tile;
+        const int64_t from = ((((static_cast<int64_t>(li) * a.batch + b) * a.width + src) * a.num_kv_heads + w.head) *
+                                  a.head_dim + w.cd * x) * elt;
+        write_token_group(lh, tile, static_cast<int>(pos % kPageTokens), w.cd, x, elt,
+                          static_cast<const char*>(a.k) + from, static_cast<const char*>(a.v) + from, true);
+    }
+}
+
 __global__ __launch_bounds__(kBlockThreads) void partition_holes_kernel(int32_t* slots, int64_t n) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlockThreads + threadIdx.x; i < n;
          i += static_cast<int64_t>(gridDim.x) * kBlockThreads) {
@@ -678,6 +707,16 @@ hipError_t launch_append_table(const AppendTableArgs& a, hipStream_t s) {
     const unsigned threads = append_threads(a.num_kv_heads, a.head_dim, a.dtype);
     if (threads > kAppendThreads) return hipErrorInvalidValue;
     hipLaunchKernelGGL(append_table_kernel, dim3(static_cast<unsigned>(a.n), layers), dim3(threads), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_accept_drafts(const AcceptArgs& a, hipStream_t s) {
+    if (a.batch <= 0 || a.width <= 0 || a.num_layers <= 0) return hipSuccess;
+    const unsigned layers = a.num_layers < 65535 ? static_cast<unsigned>(a.num_layers) : 65535u;
+    const unsigned threads = append_threads(a.num_kv_heads, a.head_dim, a.dtype);
+    if (threads > kAppendThreads) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(accept_drafts_kernel, dim3(static_cast<unsigned>(a.batch * a.width), layers), dim3(threads), 0,
+                       s, a);
     return hipGetLastError();
 }
 

@@ -26,7 +26,8 @@ KV_COLD_DEVICE, KV_COLD_PINNED_HOST = 0, 1
 KV_SESSION_FREE, KV_SESSION_ACTIVE, KV_SESSION_PAUSED = 0, 1, 2
 KV_POOL_METADATA_ONLY = 1
 KV_KERNEL_DECODE_SPLIT, KV_KERNEL_DECODE_COMBINE, KV_KERNEL_PAGE_COPY, KV_KERNEL_EVICT_COPY = 0, 1, 2, 3
-KV_KERNEL_PREFETCH_COPY, KV_KERNEL_COUNT = 4, 5
+KV_KERNEL_PREFETCH_COPY, KV_KERNEL_CHUNK, KV_KERNEL_CHUNK_MERGE, KV_KERNEL_COUNT = 4, 5, 6, 7
+KV_MAX_DRAFTS = 64
 KV_PAGE_COLD, KV_PAGE_STAGED = 1 << 30, 1 << 29
 KV_COMBINE_SEPARATE, KV_COMBINE_FUSED = 0, 1
 KV_DECODE_MATRIX, KV_DECODE_VECTOR = 0, 1
@@ -86,6 +87,7 @@ _SIGS = {
     "kv_append_tokens": (ctypes.c_int, [_P, _I32, _P, _P, _I32, _P, _P, _P]),
     "kv_write_tokens_layers": (ctypes.c_int, [_P, _I32, _I32, _I32, _I32, _I32, _P, _P, _P]),
     "kv_append_tokens_table": (ctypes.c_int, [_P, _I32, _I32, _P, _I64, _I32, _P, _P, _I32, _P, _P, _P]),
+    "kv_accept_drafts": (ctypes.c_int, [_P, _I32, _I32, _P, _I64, _P, _P, _P, _I32, _I32, _P, _P, _P]),
     "kv_fill_synthetic": (ctypes.c_int, [_P, _I32, _I32, _U64, ctypes.c_float, _P]),
     "kv_fill_synthetic_pages": (ctypes.c_int, [_P, _I32, _I32, _U64, ctypes.c_float, _I32, _I32, _P]),
     "kv_evict_session": (ctypes.c_int, [_P, _I32, _P]),
@@ -115,6 +117,12 @@ _SIGS = {
                                                      ctypes.c_float, _P, _P, _SZ, _P]),
     "paged_decode_attention_noalloc": (ctypes.c_int, [_P, _I32, _P, _P, _I64, _P, _I32, _I32,
                                                       ctypes.c_float, _P, _P]),
+    "paged_prefill_workspace_bytes": (_SZ, [_P, _I32, _I32, _I32]),
+    "paged_prefill_attention": (ctypes.c_int, [_P, _I32, _P, _P, _I32, _P, _I64, _P, _I32, _I32,
+                                               ctypes.c_float, _P, _P, _SZ, _P]),
+    "paged_tree_workspace_bytes": (_SZ, [_P, _I32, _I32, _I32]),
+    "paged_tree_attention": (ctypes.c_int, [_P, _I32, _P, _P, _P, _P, _P, _I32, _P, _I64, _P, _I32, _I32,
+                                            ctypes.c_float, _P, _P, _SZ, _P]),
     "paged_decode_partition": (ctypes.c_int, [_P, _P, _I32, _I32, _P, _P]),
     "paged_decode_gather_table": (ctypes.c_int, [_P, _P, _I32, _P, _P]),
     "kv_strerror": (ctypes.c_char_p, [ctypes.c_int]),
@@ -257,6 +265,14 @@ def kv_append_tokens_table(pool: int, layer_begin: int, num_layers: int, table_p
     _check(_lib.kv_append_tokens_table(pool, layer_begin, num_layers, table_ptr or None, pt_stride, table_rows,
                                        rows_ptr or None, positions_ptr or None, n, k_ptr or None, v_ptr or None,
                                        stream or None), "kv_append_tokens_table")
+
+
+def kv_accept_drafts(pool: int, layer_begin: int, num_layers: int, table_ptr: int, pt_stride: int,
+                     seq_lens_ptr: int, path_ptr: int, counts_ptr: int, batch: int, width: int, k_ptr: int,
+                     v_ptr: int, stream: int = 0) -> None:
+    _check(_lib.kv_accept_drafts(pool, layer_begin, num_layers, table_ptr or None, pt_stride, seq_lens_ptr or None,
+                                 path_ptr or None, counts_ptr or None, batch, width, k_ptr or None, v_ptr or None,
+                                 stream or None), "kv_accept_drafts")
 
 
 def kv_fill_synthetic(pool: int, sid: int, gen_sid: int, seed: int, value_mult: float,
@@ -404,6 +420,33 @@ def paged_decode_attention_noalloc(pool: int, layer: int, q_ptr: int, page_table
                                                seq_lens_ptr or None, batch, num_q_heads, scale,
                                                out_ptr or None, stream or None),
            "paged_decode_attention_noalloc")
+
+
+def paged_prefill_workspace_bytes(pool: int, batch: int, total_q: int, num_q_heads: int) -> int:
+    return int(_lib.paged_prefill_workspace_bytes(pool, batch, total_q, num_q_heads))
+
+
+def paged_prefill_attention(pool: int, layer: int, q_ptr: int, q_starts_ptr: int, total_q: int, page_table_ptr: int,
+                            pt_stride: int, seq_lens_ptr: int, batch: int, num_q_heads: int, scale: float,
+                            out_ptr: int, workspace_ptr: int, ws_bytes: int, stream: int = 0) -> None:
+    _check(_lib.paged_prefill_attention(pool, layer, q_ptr or None, q_starts_ptr or None, total_q,
+                                        page_table_ptr or None, pt_stride, seq_lens_ptr or None, batch, num_q_heads,
+                                        scale, out_ptr or None, workspace_ptr or None, ws_bytes, stream or None),
+           "paged_prefill_attention")
+
+
+def paged_tree_workspace_bytes(pool: int, batch: int, width: int, num_q_heads: int) -> int:
+    return int(_lib.paged_tree_workspace_bytes(pool, batch, width, num_q_heads))
+
+
+def paged_tree_attention(pool: int, layer: int, q_ptr: int, k_draft_ptr: int, v_draft_ptr: int, masks_ptr: int,
+                         draft_lens_ptr: int, width: int, page_table_ptr: int, pt_stride: int, seq_lens_ptr: int,
+                         batch: int, num_q_heads: int, scale: float, out_ptr: int, workspace_ptr: int,
+                         ws_bytes: int, stream: int = 0) -> None:
+    _check(_lib.paged_tree_attention(pool, layer, q_ptr or None, k_draft_ptr or None, v_draft_ptr or None,
+                                     masks_ptr or None, draft_lens_ptr or None, width, page_table_ptr or None,
+                                     pt_stride, seq_lens_ptr or None, batch, num_q_heads, scale, out_ptr or None,
+                                     workspace_ptr or None, ws_bytes, stream or None), "paged_tree_attention")
 
 
 def paged_decode_gather_table(pool: int, sids_ptr: int, n: int, table_ptr: int, stream: int = 0) -> None:

@@ -1,0 +1,111 @@
+"""Prompt chunks, draft trees and accepted drafts on the host: calls that must be refused before
+any device is touched, and the work split's arithmetic (CPU only)."""
+
+import random
+
+import pytest
+
+from paper_2609_25782_amd import hotcold_kv as kv
+
+
+@pytest.fixture
+def meta():
+    d = kv.kv_pool_desc(2, 2, 64, 16, kv.KV_DTYPE_BF16, 8, 8, 0, 4, 4, 0, kv.KV_POOL_METADATA_ONLY)
+    p = kv.kv_pool_create(d, 0, 0, 0, 0, 0)
+    yield p
+    kv.kv_pool_destroy(p)
+
+
+def test_metadata_only_pools_are_refused(meta):
+    for pool in (meta, 0):
+        for call in (lambda: kv.paged_prefill_attention(pool, 0, 16, 16, 4, 16, 4, 16, 1, 4, 0.1, 16, 256, 1 << 30),
+                     lambda: kv.paged_tree_attention(pool, 0, 16, 16, 16, 16, 0, 4, 16, 4, 16, 1, 4, 0.1, 16, 256,
+                                                     1 << 30),
+                     lambda: kv.kv_accept_drafts(pool, 0, 1, 16, 4, 16, 16, 16, 1, 4, 16, 16)):
+            with pytest.raises(kv.KVError) as e:
+                call()
+            assert e.value.status == kv.KV_ERR_INVALID
+        assert kv.paged_prefill_workspace_bytes(pool, 1, 4, 4) == 0
+        assert kv.paged_tree_workspace_bytes(pool, 1, 4, 4) == 0
+
+
+# -- the work split: tiles laid end to end, cut into equal ranges --------------
+# The same arithmetic as the kernel's (kTileCost, places of units), on plain integers.
+
+COST = 64
+
+
+def row_units(ctx, n, tok, block, tree):
+    """Costs of a row's tiles of one KV head, and their numbers of blocks."""
+    tiles = -(-n // tok)
+    cost, blocks = [], []
+    for i in range(tiles):
+        if tree:
+            nd = -(-n // block)
+            cost.append(COST + nd * block + ctx)
+            blocks.append(nd + -(-ctx // block))
+        else:
+            keys = ctx + min((i + 1) * tok, n)
+            cost.append(COST + keys)
+            blocks.append(-(-keys // block))
+    return cost, blocks
+
+
+def place(tiles, u, block):
+    """Block that unit u begins with: (tile, block) over the flat list of (cost, blocks)."""
+    for i, (cost, nb) in enumerate(tiles):
+        if u < cost:
+            if u == 0:
+                return i, 0
+            x = u - COST
+            k = min(nb, 0 if x <= 0 else -(-x // block))
+            return (i, k) if k < nb else (i + 1, 0)
+        u -= cost
+    return len(tiles), 0
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_every_block_belongs_to_one_worker(tree):
+    rng = random.Random(5)
+    for trial in range(300):
+        block = rng.choice([32, 64])
+        group = rng.choice([1, 2, 3, 5, 8, 16])
+        tok = rng.choice([64, 256]) // group
+        heads = rng.choice([1, 2, 4])
+        tiles = []
+        for _ in range(rng.randint(1, 6)):
+            ctx = rng.choice([0, 1, rng.randint(0, 100), rng.randint(0, 5000)])
+            n = rng.choice([0, 1, rng.randint(1, 64)] if tree else [0, 1, rng.randint(1, 3000)])
+            tiles += list(zip(*row_units(ctx, n, tok, block, tree))) * heads
+        total = sum(c for c, _ in tiles)
+        most = rng.choice([1, 7, 256, 512])
+        workers = max(1, min(most, total // (COST + 2 * block))) if total else 0
+        cuts = [place(tiles, k * total // workers, block) for k in range(workers)] + [(len(tiles), 0)]
+        assert not workers or cuts[0] == (0, 0)
+        done = []
+        for k in range(workers):
+            at, end = cuts[k], cuts[k + 1]
+            assert at < end, "worker %d of %d has nothing" % (k, workers)
+            heads_cut = 0
+            while at < end:
+                tile, k0 = at
+                nb = tiles[tile][1]
+                k1 = end[1] if end[0] == tile else nb
+                done.append((tile, k0, k1))
+                heads_cut += k0 > 0
+                if end[0] == tile:
+                    break
+                at = (tile + 1, 0)
+            assert heads_cut <= 1           # one slot for a tile begun by another worker
+        want = 0
+        flat = iter(done)
+        for tile, (_, nb) in enumerate(tiles):
+            upto = 0
+            while True:
+                t, k0, k1 = next(flat)
+                assert t == tile and k0 == upto and (k1 > k0 or nb == 0)
+                upto = k1
+                if upto == nb:
+                    break
+            want += 1
+        assert next(flat, None) is None
