@@ -59,6 +59,7 @@ struct Cfg {
     static constexpr int kBlock = PAGES * kPageTokens;    // keys per block
     static constexpr int kStage = PAGES * kPage;          // LDS bytes of a block
     static constexpr int kThreads = WAVES * kWave;
+    static constexpr int kPerSimd = 2;                    // waves per SIMD the registers are made for
     static constexpr int kWaveRows = 16 * NT;
     static constexpr int kRows = WAVES * kWaveRows;
     static constexpr int kTileLoads = kTile / 1024;       // 1 KiB loads of a tile
@@ -182,6 +183,11 @@ __device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int 
     return p;
 }
 
+__device__ __forceinline__ Place uniform_place(const Place& p) {
+    return Place{__builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.g),
+                 __builtin_amdgcn_readfirstlane(p.tile), __builtin_amdgcn_readfirstlane(p.blk)};
+}
+
 __device__ __forceinline__ bool before(const Place& x, const Place& y) {
     if (x.b != y.b) return x.b < y.b;
     if (x.g != y.g) return x.g < y.g;
@@ -252,29 +258,18 @@ __device__ int worker_range(const ChunkArgs& a, int k, Place& from, Place& to) {
         }
     }
     __syncthreads();
-    from = s_place[0];
-    to = s_place[1];
-    int* f = reinterpret_cast<int*>(&from);
-    int* t = reinterpret_cast<int*>(&to);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[i] = __builtin_amdgcn_readfirstlane(f[i]);
-        t[i] = __builtin_amdgcn_readfirstlane(t[i]);
-    }
+    from = uniform_place(s_place[0]);
+    to = uniform_place(s_place[1]);
     return __builtin_amdgcn_readfirstlane(workers);
 }
 
-// Address of the tiles of page-table entry `pid` for a KV head; ok = 0 for an id outside
-// its pool (or a tag this call does not read).
-__device__ __forceinline__ const char* page_at(const ChunkArgs& a, int pid, unsigned head_off, bool& ok) {
-    const unsigned tag = static_cast<unsigned>(pid) >> 29;  // 0 hot, 2 cold, otherwise no page here
-    const unsigned id = static_cast<unsigned>(pid) & static_cast<unsigned>(kPageIdMask);
-    if (tag == 2 && a.tiered && id < static_cast<unsigned>(a.num_cold)) {
-        ok = true;
-        return a.cold + static_cast<int64_t>(id) * a.cold_stride + head_off;
-    }
-    ok = tag == 0 && id < static_cast<unsigned>(a.num_hot);
-    return a.hot + static_cast<int64_t>(ok ? id : 0) * a.hot_stride + head_off;
+// Page-table entry `pid`: a hot page, a cold page (num_cold is 0 where the pool reads no
+// tagged entries), or no page that this call reads.
+__device__ __forceinline__ bool is_hot(const ChunkArgs& a, int pid) {
+    return static_cast<unsigned>(pid) < static_cast<unsigned>(a.num_hot);
+}
+__device__ __forceinline__ bool is_cold(const ChunkArgs& a, int pid) {
+    return static_cast<unsigned>(pid ^ kPageCold) < static_cast<unsigned>(a.num_cold);
 }
 
 __device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t rs, char* lds, unsigned voff) {
@@ -328,10 +323,12 @@ struct Loader {
             int id = pid[0];
 #pragma unroll
             for (int i = 1; i < C::kPages; ++i) id = page == i ? pid[i] : id;
-            bool ok;
-            const char* base = page_at(a, id, head_off, ok);
+            id = __builtin_amdgcn_readfirstlane(id);
+            const bool hot = is_hot(a, id), cold = is_cold(a, id);
+            const char* base = cold ? a.cold + static_cast<int64_t>(id ^ kPageCold) * a.cold_stride
+                                    : a.hot + static_cast<int64_t>(hot ? id : 0) * a.hot_stride;
             const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-                const_cast<char*>(base), static_cast<short>(0), ok ? C::kPage : 0, kRsrcWord3);
+                const_cast<char*>(base + head_off), static_cast<short>(0), hot || cold ? C::kPage : 0, kRsrcWord3);
             const unsigned off = kind ? voff : (C::kBf16 ? koff ^ ((page & 1) * 64) : koff);
             char* dst = stage + tile * C::kTile + first * 1024;
 #pragma unroll
@@ -439,7 +436,7 @@ __device__ __forceinline__ bool any_nonfinite(const u32x4& v, bool bf16) {
 // value would be NaN, so they are taken out of the product and put into the outputs of
 // the rows that attend to them.
 template <class C, bool TREE, bool MASKED>
-__device__ __forceinline__ void compute_block(State<C>& st, const char* stage, float scale, const Mask& mk,
+__device__ __forceinline__ void compute_block(State<C>& st, const char* stage, float scale, float slack, const Mask& mk,
                                               const int (&lim)[C::kNT], const uint64_t (&seen)[C::kNT],
                                               bool poison) {
     const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, x = lane & 15;
@@ -507,9 +504,11 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
             sees[n] = bits;
         }
     }
-    // running maximum
-    float mx[C::kNT];
+    // Running maximum.  It is raised only where a score exceeds it by more than 2^8 in the
+    // weights (`slack` in raw scores): a weight may then be up to 2^8, which float32 sums and
+    // bf16 weights hold as well as weights up to 1, and most blocks leave l and o alone.
     bool rise = false;
+    float mx[C::kNT];
 #pragma unroll
     for (int n = 0; n < C::kNT; ++n) {
         mx[n] = st.m[n];
@@ -517,7 +516,7 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
         for (int t = 0; t < C::kPages; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) mx[n] = fmaxf(mx[n], s[t][n][r]);
-        rise |= mx[n] > st.m[n];
+        rise |= mx[n] > st.m[n] + slack;
     }
     if (__builtin_amdgcn_ballot_w64(rise)) {
 #pragma unroll
@@ -672,7 +671,7 @@ __device__ __forceinline__ void store4(const ChunkArgs& a, bool bf16, char* out,
 }
 
 template <class C, bool TREE>
-__global__ __launch_bounds__(C::kThreads, 2) void chunk_attend_kernel(const ChunkArgs a) {
+__global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(const ChunkArgs a) {
     extern __shared__ __align__(1024) char s_kv[];
     __shared__ int s_poison;
     const int lane = threadIdx.x & (kWave - 1), gq = lane >> 4, x = lane & 15;
@@ -754,60 +753,68 @@ __global__ __launch_bounds__(C::kThreads, 2) void chunk_attend_kernel(const Chun
 #pragma unroll
                 for (int c = 0; c < C::kC; ++c) st.o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
-            const auto ids_of = [&](int blk, int (&pid)[C::kPages]) {
-                const int p0 = (blk - nd) * C::kPages;
+            // Order of a tile's blocks: the drafts', then the context's from its end down, so that the
+            // blocks that need masks come first (they are the ones at the end of what a row sees).
+            const int nc = nb - nd;                              // context blocks
+            const auto page_of_block = [&](int j) { return (nc - 1 - (j - nd)) * C::kPages; };
+            const auto load_ids = [&](int j, int (&pid)[C::kPages]) {
+                const int p0 = j >= nd && j < k1 ? page_of_block(j) : 0;
 #pragma unroll
                 for (int i = 0; i < C::kPages; ++i) {
                     // a page past the row's last holds no key that a row sees: no page
                     const int p = p0 + i;
-                    const int e = pt[p <= last_page ? p : last_page];
+                    const int e = last_page < 0 ? -1 : pt[p <= last_page ? p : last_page];
                     pid[i] = p <= last_page ? e : -1;
                 }
             };
-            const auto ok_of = [&](const int (&pid)[C::kPages]) {
-                unsigned m = 0;
-#pragma unroll
-                for (int i = 0; i < C::kPages; ++i) {
-                    bool ok;
-                    (void)page_at(a, pid[i], 0, ok);
-                    m |= ok ? 1u << i : 0u;
-                }
-                return m;
-            };
             unsigned oks = 0;   // page bits of the blocks in flight, the next one lowest
             static_assert(C::kPages * C::kStages <= 32, "page bits");
-            const auto fetch = [&](int blk) {   // blk in [k0, k1): into its stage
-                char* stage = s_kv + ((blk - k0) % C::kStages) * C::kStage;
+            int ids[C::kPages];   // of the block that is fetched next
+            const auto fetch = [&](int j) {   // block j of [k0, k1) into its stage
+                char* stage = s_kv + ((j - k0) % C::kStages) * C::kStage;
                 unsigned ok = (1u << C::kPages) - 1;
-                if (TREE && blk < nd) {
-                    ld.draft_keys(a, at.b, at.g, row.n, blk * C::kBlock, stage);
-                    ld.draft_values(a, at.b, at.g, row.n, blk * C::kBlock, stage);
+                if (TREE && j < nd) {
+                    ld.draft_keys(a, at.b, at.g, row.n, j * C::kBlock, stage);
+                    ld.draft_values(a, at.b, at.g, row.n, j * C::kBlock, stage);
                 } else {
-                    int pid[C::kPages];
-                    ids_of(blk, pid);
-                    ld.pages(a, pid, head_off, stage);
-                    ok = ok_of(pid);
+                    ld.pages(a, ids, head_off, stage);
+                    ok = 0;
+#pragma unroll
+                    for (int i = 0; i < C::kPages; ++i) ok |= is_hot(a, ids[i]) || is_cold(a, ids[i]) ? 1u << i : 0u;
                 }
+                load_ids(j + 1, ids);
                 return ok;
             };
+            load_ids(k0, ids);
 #pragma unroll
             for (int j = 0; j < C::kStages - 1; ++j)
                 if (k0 + j < k1) oks |= fetch(k0 + j) << (C::kPages * j);
 
-            for (int blk = k0; blk < k1; ++blk) {
-                const bool draft = TREE && blk < nd;
-                const int key0 = (draft ? blk : blk - nd) * C::kBlock;
-                char* stage = s_kv + ((blk - k0) % C::kStages) * C::kStage;
-                const unsigned ok = oks & ((1u << C::kPages) - 1);
+            // blocks that some row of the tile does not see whole; of this wave's rows; that none of them sees
+            int partly, masked, unseen = 0;
+            if constexpr (TREE) {
+                partly = nd;
+                masked = nd + (row.ctx % C::kBlock != 0);
+            } else {
+                partly = nb - (row.ctx + tok0 + 1) / C::kBlock;
+                masked = nb - (row.ctx + tok0 + wtok0 + 1) / C::kBlock;
+                unseen = nb - ((row.ctx + tok0 + wtok1) / C::kBlock + 1);
+            }
+            if (!wave_live) masked = unseen = nb;
+            int j = k0;
+            unsigned ok = 0;
+            char* stage = nullptr;
+            // Block j has arrived for every wave, and the block STAGES - 1 later is on its way.
+            const auto turn = [&]() {
+                stage = s_kv + ((j - k0) % C::kStages) * C::kStage;
+                ok = oks & ((1u << C::kPages) - 1);
                 oks >>= C::kPages;
-                // rows of this tile that do not see all of the block's keys
-                const bool partly = TREE ? draft : key0 + C::kBlock - 1 > row.ctx + tok0;
-                // the loads of this block are done; those of later blocks may go on
-                if (draft || k1 - 1 - blk < C::kStages - 2)
+                // loads of later blocks may go on: 1 KiB each, kLoads per block and wave
+                if ((TREE && j < nd) || k1 - 1 - j < C::kStages - 2)
                     wait_loads_and_sync<0>();
                 else
                     wait_loads_and_sync<(C::kStages - 2) * C::kLoads>();
-                if (partly) {
+                if (j < partly) {
                     // an infinity or NaN among values that some row must not see?
                     bool hit = false;
                     constexpr int kVec = C::kPages * C::kTile / 16;
@@ -818,18 +825,22 @@ __global__ __launch_bounds__(C::kThreads, 2) void chunk_attend_kernel(const Chun
                     if (__builtin_amdgcn_ballot_w64(hit) && lane == 0) s_poison = 1;
                     wait_loads_and_sync<63>();
                 }
-                if (blk + C::kStages - 1 < k1)
-                    oks |= fetch(blk + C::kStages - 1) << (C::kPages * (C::kStages - 2));
-                if (!wave_live) continue;
-                if (!TREE && key0 > row.ctx + tok0 + wtok1) continue;   // no row of this wave sees the block
-                const int len = draft ? row.n : keys;
-                const Mask mk{key0, len, ok, draft};
-                const bool masked = draft || key0 + C::kBlock > len || ok != (1u << C::kPages) - 1 ||
-                                    (!TREE && key0 + C::kBlock - 1 > row.ctx + tok0 + wtok0);
-                if (masked)
-                    compute_block<C, TREE, true>(st, stage, a.scale_log2, mk, lim, seen, partly && s_poison);
-                else
-                    compute_block<C, TREE, false>(st, stage, a.scale_log2, mk, lim, seen, false);
+                if (j + C::kStages - 1 < k1) oks |= fetch(j + C::kStages - 1) << (C::kPages * (C::kStages - 2));
+            };
+            for (; j < k1 && j < masked; ++j) {
+                turn();
+                if (j < unseen) continue;
+                const bool draft = TREE && j < nd;
+                const int key0 = draft ? j * C::kBlock : page_of_block(j) * kPageTokens;
+                const Mask mk{key0, draft ? row.n : keys, ok, draft};
+                compute_block<C, TREE, true>(st, stage, a.scale_log2, a.slack, mk, lim, seen, j < partly && s_poison);
+            }
+            bool bad = row.bad;
+            for (; j < k1; ++j) {
+                turn();
+                // every row of this wave attends to every token here: a missing page is NaN for all
+                bad |= ok != (1u << C::kPages) - 1;
+                compute_block<C, TREE, false>(st, stage, a.scale_log2, a.slack, Mask{}, lim, seen, false);
             }
 
             // the rows' sums over their four lanes
@@ -838,7 +849,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void chunk_attend_kernel(const Chun
             for (int n = 0; n < C::kNT; ++n) {
                 l[n] = st.l[n] + __shfl_xor(st.l[n], 16);
                 l[n] += __shfl_xor(l[n], 32);
-                if (row.bad) l[n] = NAN;
+                if (bad) l[n] = NAN;
             }
             if (k0 == 0 && k1 == nb) {
 #pragma unroll

@@ -283,9 +283,9 @@ struct ChunkRec {   // a part of a tile left in the workspace
 struct ChunkArgs {
     const char* hot;           // slice of hot page 0 for the layer
     int64_t hot_stride;
-    const char* cold;          // the same of the cold pool (entries tagged KV_PAGE_COLD, if `tiered`)
+    const char* cold;          // the same of the cold pool (entries tagged KV_PAGE_COLD)
     int64_t cold_stride;
-    int32_t num_hot, num_cold, tiered;
+    int32_t num_hot, num_cold; // num_cold 0: tagged entries name no page
     int32_t num_kv_heads, group, num_q_heads;
     const void* q;             // prompt chunks: [total_q][num_q_heads][D]; trees: [batch][width][num_q_heads][D]
     void* out;                 // like q
@@ -303,6 +303,7 @@ struct ChunkArgs {
     const void* k_new;         // [batch][width][num_kv_heads][D]
     const void* v_new;
     float scale_log2;          // |scale| log2(e)
+    float slack;               // how far a raw score may pass a row's maximum before that is raised
     int32_t negate;            // 1: the scale is negative, the queries change sign
     void* workspace;
     // set by the launch

@@ -1609,8 +1609,7 @@ int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_
     a.num_hot = pool->d.num_hot_pages;
     a.cold = pool->cold ? hck::slice_at(pool->cold_geom, 0, layer) : nullptr;
     a.cold_stride = pool->cold_geom.page_stride;
-    a.num_cold = pool->cold ? pool->d.num_cold_pages : 0;
-    a.tiered = pool->tiered() ? 1 : 0;
+    a.num_cold = pool->cold && pool->tiered() ? pool->d.num_cold_pages : 0;
     a.num_kv_heads = pool->d.num_kv_heads;
     a.group = num_q_heads / pool->d.num_kv_heads;
     a.num_q_heads = num_q_heads;
@@ -1621,6 +1620,8 @@ int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_
     a.lens = seq_lens;
     a.batch = batch;
     a.scale_log2 = (scale < 0.f ? -scale : scale) * 1.4426950408889634f;
+    // 2^8 in the weights; finite, so that a row's first score always raises its maximum
+    a.slack = a.scale_log2 > 1e-30f ? 8.f / a.scale_log2 : 8e30f;
     a.negate = scale < 0.f ? 1 : 0;
     return KV_OK;
 }
