@@ -59,7 +59,10 @@ struct Cfg {
     static constexpr int kBlock = PAGES * kPageTokens;    // keys per block
     static constexpr int kStage = PAGES * kPage;          // LDS bytes of a block
     static constexpr int kThreads = WAVES * kWave;
-    static constexpr int kPerSimd = 2;                    // waves per SIMD the registers are made for
+#ifndef PERSIMD
+#define PERSIMD 2
+#endif
+    static constexpr int kPerSimd = NT == 1 ? 2 : PERSIMD;                    // waves per SIMD the registers are made for
     static constexpr int kWaveRows = 16 * NT;
     static constexpr int kRows = WAVES * kWaveRows;
     static constexpr int kTileLoads = kTile / 1024;       // 1 KiB loads of a tile
@@ -287,7 +290,8 @@ __device__ __forceinline__ void wait_loads_and_sync() {
 // A block's source for one wave: its page ids (context) or drafts.
 template <class C>
 struct Loader {
-    unsigned koff, voff;   // this lane's byte in a tile, first load
+    unsigned koff, voff;   // this lane's byte in a tile, first load (an even page's K; V)
+    unsigned koff_page;    // the same for the K of the wave's page
     int wave, lane;
     __device__ explicit Loader() {
         lane = threadIdx.x & (kWave - 1);
@@ -304,37 +308,33 @@ struct Loader {
             koff = lane * 16;
             voff = C::kTile + x * 64 + g * 16;
         }
+        koff_page = C::kBf16 ? koff ^ ((page() & 1) * 64) : koff;
     }
-    // Loads of `lane`'s tiles of the block whose pages' ids are pid[0 .. PAGES).
-    __device__ __forceinline__ void pages(const ChunkArgs& a, const int (&pid)[C::kPages], unsigned head_off,
-                                          char* stage) const {
+    // This wave's share of a block is in one page: its tiles (K, V or both), or a part of one.
+    static constexpr int kShare = C::kTileLoads > C::kLoads ? C::kTileLoads / C::kLoads : 1;  // waves of a tile
+    static constexpr int kTiles = C::kLoads > C::kTileLoads ? C::kLoads / C::kTileLoads : 1;  // tiles of a wave
+    static_assert(kTiles <= 2, "a wave's tiles are one page's");
+    __device__ __forceinline__ int tile() const { return kShare > 1 ? wave / kShare : wave * kTiles; }
+    __device__ __forceinline__ int page() const { return tile() >> 1; }
+    // Its loads, from the page that entry `id` names; an id that names none reads zeros.
+    __device__ __forceinline__ bool load_page(const ChunkArgs& a, int id, unsigned head_off, char* stage) const {
+        const bool hot = is_hot(a, id), cold = is_cold(a, id);
+        const char* pool = cold ? a.cold : a.hot;
+        const int64_t stride = cold ? a.cold_stride : a.hot_stride;
+        const int64_t n = cold ? id ^ kPageCold : (hot ? id : 0);
+        const __amdgpu_buffer_rsrc_t rs =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool + n * stride + head_off), static_cast<short>(0),
+                                              hot || cold ? C::kPage : 0, kRsrcWord3);
 #pragma unroll
-        for (int j = 0; j < (C::kLoads < C::kTileLoads ? 1 : C::kLoads / C::kTileLoads); ++j) {
-            int tile, first;
-            constexpr int kShare = C::kTileLoads > C::kLoads ? C::kTileLoads / C::kLoads : 1;  // waves of a tile
-            if constexpr (kShare > 1) {
-                tile = wave / kShare;
-                first = (wave % kShare) * C::kLoads;
-            } else {
-                tile = wave * (C::kLoads / C::kTileLoads) + j;
-                first = 0;
-            }
-            const int page = tile >> 1, kind = tile & 1;
-            int id = pid[0];
+        for (int j = 0; j < kTiles; ++j) {
+            const int t = tile() + j;
+            const int first = kShare > 1 ? (wave % kShare) * C::kLoads : 0;
+            const unsigned off = (t & 1) ? voff : koff_page;
+            char* dst = stage + t * C::kTile + first * 1024;
 #pragma unroll
-            for (int i = 1; i < C::kPages; ++i) id = page == i ? pid[i] : id;
-            id = __builtin_amdgcn_readfirstlane(id);
-            const bool hot = is_hot(a, id), cold = is_cold(a, id);
-            const char* base = cold ? a.cold + static_cast<int64_t>(id ^ kPageCold) * a.cold_stride
-                                    : a.hot + static_cast<int64_t>(hot ? id : 0) * a.hot_stride;
-            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-                const_cast<char*>(base + head_off), static_cast<short>(0), hot || cold ? C::kPage : 0, kRsrcWord3);
-            const unsigned off = kind ? voff : (C::kBf16 ? koff ^ ((page & 1) * 64) : koff);
-            char* dst = stage + tile * C::kTile + first * 1024;
-#pragma unroll
-            for (int i = 0; i < (C::kLoads < C::kTileLoads ? C::kLoads : C::kTileLoads); ++i)
-                load_lds16(rs, dst + i * 1024, off + (first + i) * 1024);
+            for (int i = 0; i < C::kLoads / kTiles; ++i) load_lds16(rs, dst + i * 1024, off + (first + i) * 1024);
         }
+        return hot || cold;
     }
     // The K of drafts [key0, key0 + kBlock) of a row, by the same kind of loads; drafts past n read zeros.
     __device__ __forceinline__ void draft_keys(const ChunkArgs& a, int b, int g, int n, int key0, char* stage) const {
@@ -430,15 +430,152 @@ __device__ __forceinline__ bool any_nonfinite(const u32x4& v, bool bf16) {
     return hit;
 }
 
+#ifndef QKAHEAD
+#define QKAHEAD 8
+#endif
+#ifndef PVAHEAD
+#define PVAHEAD 8
+#endif
+// Order of a section's LDS reads and matrix instructions: `AHEAD` reads first, then one per
+// MFMAS matrix instructions, so that a read's latency lies under AHEAD * MFMAS of them.
+template <int READS, int MFMAS, int AHEAD>
+__device__ __forceinline__ void schedule_reads() {
+    constexpr int kFirst = AHEAD < READS ? AHEAD : READS;
+    __builtin_amdgcn_sched_group_barrier(0x100, kFirst, 0);
+#pragma unroll
+    for (int i = kFirst; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, MFMAS * kFirst, 0);
+}
+
+// Key that this lane's register (t, r) of S^T stands for, from the block's first, and its page.
+template <class C>
+__device__ __forceinline__ int lane_key(int t, int r) {
+    const int g = (threadIdx.x & (kWave - 1)) >> 4;
+    return C::kBf16 ? 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r : 16 * t + 4 * g + r;
+}
+template <class C>
+__device__ __forceinline__ int lane_page(int t) {
+    const int g = (threadIdx.x & (kWave - 1)) >> 4;
+    return C::kBf16 ? 2 * (t >> 1) + (g >> 1) : t;
+}
+
+// Bit 4 t + r: the row attends to that key.
+template <class C, bool TREE>
+__device__ __forceinline__ unsigned seen_keys(const Mask& mk, int lim, uint64_t seen) {
+    unsigned bits = 0;
+#pragma unroll
+    for (int t = 0; t < C::kPages; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int key = mk.key0 + lane_key<C>(t, r);
+            bool see = key < lim;
+            if constexpr (TREE)
+                if (mk.draft) see = key < mk.len && ((seen >> (key & 63)) & 1u);
+            bits |= see ? 1u << (4 * t + r) : 0u;
+        }
+    return bits;
+}
+
+// Bits of this lane's V values of step p that belong to the row (the rest is cleared: slots
+// past its length and missing pages may hold NaN).
+template <class C>
+__device__ __forceinline__ u32x4 kept_values(const Mask& mk, int p) {
+    u32x4 keep;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (C::kBf16) {
+            const int key = mk.key0 + lane_key<C>(2 * p + (j >> 1), 2 * (j & 1));
+            const bool ok = (mk.ok >> lane_page<C>(2 * p)) & 1u;
+            keep[j] = (ok && key < mk.len ? 0xFFFFu : 0u) | (ok && key + 1 < mk.len ? 0xFFFF0000u : 0u);
+        } else {
+            keep[j] = ((mk.ok >> p) & 1u) && mk.key0 + lane_key<C>(p, j) < mk.len ? 0xFFFFFFFFu : 0u;
+        }
+    }
+    return keep;
+}
+
+// A block whose V holds infinities or NaN that some row must not see: a weight of 0 times
+// such a value would be NaN.  This adds to every row the infinities and NaN of the tokens
+// it attends to (a product of the masks with codes of the values); then clear_nonfinite
+// takes them out of the block, and compute_block adds the rest.
+template <class C, bool TREE>
+__device__ __forceinline__ void add_nonfinite(State<C>& st, const char* stage, const Mask& mk, const int (&lim)[C::kNT],
+                                              const uint64_t (&seen)[C::kNT]) {
+    const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, x = lane & 15;
+    const char* vb = C::kBf16 ? stage + (g >> 1) * C::kPage + C::kTile + (g & 1) * 256 + x * 16
+                              : stage + C::kTile + lane * 16;
+    constexpr int kSteps = C::kBf16 ? C::kPages / 2 : C::kPages;
+    unsigned sees[C::kNT];
+#pragma unroll
+    for (int n = 0; n < C::kNT; ++n) sees[n] = seen_keys<C, TREE>(mk, lim[n], seen[n]);
+#pragma unroll
+    for (int c = 0; c < C::kC; ++c) {
+        f32x4 codes[C::kNT];
+#pragma unroll
+        for (int n = 0; n < C::kNT; ++n) codes[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < kSteps; ++p) {
+            u32x4 v = *reinterpret_cast<const u32x4*>(vb + p * (C::kBf16 ? 2 : 1) * C::kPage + c * 256 * C::kElt);
+            v &= kept_values<C>(mk, p);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v[j] = C::kBf16 ? nonfinite_code(v[j] & 0xFFFFu) | (nonfinite_code(v[j] >> 16) << 16)
+                                : __float_as_uint(nonfinite_code32(v[j]));
+#pragma unroll
+            for (int n = 0; n < C::kNT; ++n) {
+                if constexpr (C::kBf16) {
+                    u32x4 one;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int bit = 4 * (2 * p + (j >> 1)) + 2 * (j & 1);
+                        one[j] = ((sees[n] >> bit) & 1u ? 0x3F80u : 0u) |
+                                 ((sees[n] >> (bit + 1)) & 1u ? 0x3F800000u : 0u);
+                    }
+                    codes[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, one), codes[n], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        codes[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            __uint_as_float(v[j]), (sees[n] >> (4 * p + j)) & 1u ? 1.f : 0.f, codes[n], 0, 0, 0);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < C::kNT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st.o[n][c][r] += nonfinite_value(codes[n][r]);
+    }
+}
+
+// This thread's share of a block's V: the i-th of its 16-byte groups.
+template <class C>
+__device__ __forceinline__ u32x4* value_group(char* stage, int i) {
+    return reinterpret_cast<u32x4*>(stage + i / (C::kTile / 16) * C::kPage + C::kTile + i % (C::kTile / 16) * 16);
+}
+template <class C>
+__device__ __forceinline__ void clear_nonfinite(char* stage) {
+    for (int i = threadIdx.x; i < C::kPages * C::kTile / 16; i += C::kThreads) {
+        u32x4 v = *value_group<C>(stage, i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (C::kBf16)
+                v[j] &= (nonfinite_code(v[j] & 0xFFFFu) ? 0u : 0xFFFFu) | (nonfinite_code(v[j] >> 16) ? 0u : 0xFFFF0000u);
+            else
+                v[j] = nonfinite_code32(v[j]) != 0.f ? 0u : v[j];
+        }
+        *value_group<C>(stage, i) = v;
+    }
+}
+
 // One block for one wave.  MASKED blocks hold keys that some row must not see: their
-// scores are left out, their weights are 0, and values at or past the row's length are
-// cleared.  `poison` (the block's V has infinities or NaN): a weight of 0 times such a
-// value would be NaN, so they are taken out of the product and put into the outputs of
-// the rows that attend to them.
+// scores are left out, their weights are 0, and values that are none of the row's are cleared.
 template <class C, bool TREE, bool MASKED>
 __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, float scale, float slack, const Mask& mk,
-                                              const int (&lim)[C::kNT], const uint64_t (&seen)[C::kNT],
-                                              bool poison) {
+                                              const int (&lim)[C::kNT], const uint64_t (&seen)[C::kNT]) {
     const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, x = lane & 15;
     f32x4 s[C::kPages][C::kNT];
 #pragma unroll
@@ -477,31 +614,19 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
             }
         }
     }
-    // key of (t, r) in this lane, from the block's first
-    const auto key_of = [&](int t, int r) {
-        if constexpr (C::kBf16) return 32 * (t >> 1) + 8 * g + 4 * (t & 1) + r;
-        else return 16 * t + 4 * g + r;
-    };
-    const auto page_of = [&](int t) { return C::kBf16 ? 2 * (t >> 1) + (g >> 1) : t; };
-    unsigned sees[C::kNT];   // bit 4 t + r: this row attends to that key
+    if constexpr (C::kBf16) schedule_reads<C::kPages * C::kQ, C::kNT, QKAHEAD>();
+    unsigned sees[C::kNT];
     if constexpr (MASKED) {
 #pragma unroll
         for (int n = 0; n < C::kNT; ++n) {
-            unsigned bits = 0;
+            sees[n] = seen_keys<C, TREE>(mk, lim[n], seen[n]);
 #pragma unroll
             for (int t = 0; t < C::kPages; ++t) {
-                const bool ok = (mk.ok >> page_of(t)) & 1u;
+                const bool ok = (mk.ok >> lane_page<C>(t)) & 1u;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int key = mk.key0 + key_of(t, r);
-                    bool see = key < lim[n];
-                    if constexpr (TREE)
-                        if (mk.draft) see = key < mk.len && ((seen[n] >> (key & 63)) & 1u);
-                    bits |= see ? 1u << (4 * t + r) : 0u;
-                    s[t][n][r] = see ? (ok ? s[t][n][r] : NAN) : -INFINITY;
-                }
+                for (int r = 0; r < 4; ++r)
+                    s[t][n][r] = (sees[n] >> (4 * t + r)) & 1u ? (ok ? s[t][n][r] : NAN) : -INFINITY;
             }
-            sees[n] = bits;
         }
     }
     // Running maximum.  It is raised only where a score exceeds it by more than 2^8 in the
@@ -523,7 +648,9 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
         for (int n = 0; n < C::kNT; ++n) {
             float v = fmaxf(mx[n], __shfl_xor(mx[n], 16));
             v = fmaxf(v, __shfl_xor(v, 32));
-            const float f = st.m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((st.m[n] - v) * scale);
+            // (l and o of a row without a maximum hold 0, or an infinity or NaN that has to stay;
+            // neither does it become 0 times infinity below)
+            const float f = st.m[n] == -INFINITY ? 1.f : fmaxf(__builtin_amdgcn_exp2f((st.m[n] - v) * scale), 1e-37f);
             st.l[n] *= f;
 #pragma unroll
             for (int c = 0; c < C::kC; ++c) st.o[n][c] *= f;
@@ -562,82 +689,13 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
     else vb = stage + C::kTile + lane * 16;
     constexpr int kSteps = C::kBf16 ? C::kPages / 2 : C::kPages;
     u32x4 keep[MASKED ? kSteps : 1];
-    if constexpr (MASKED) {
+    if constexpr (MASKED)
 #pragma unroll
-        for (int p = 0; p < kSteps; ++p)
+        for (int p = 0; p < kSteps; ++p) keep[p] = kept_values<C>(mk, p);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (C::kBf16) {
-                    const int key = mk.key0 + 32 * p + 8 * g + 2 * j;
-                    const bool ok = (mk.ok >> (2 * p + (g >> 1))) & 1u;
-                    keep[p][j] = (ok && key < mk.len ? 0xFFFFu : 0u) | (ok && key + 1 < mk.len ? 0xFFFF0000u : 0u);
-                } else {
-                    const bool ok = (mk.ok >> p) & 1u;
-                    keep[p][j] = ok && mk.key0 + 16 * p + 4 * g + j < mk.len ? 0xFFFFFFFFu : 0u;
-                }
-            }
-        if (poison) {
+    for (int p = 0; p < kSteps; ++p) {
 #pragma unroll
-            for (int c = 0; c < C::kC; ++c) {
-                f32x4 codes[C::kNT];
-#pragma unroll
-                for (int n = 0; n < C::kNT; ++n) codes[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int p = 0; p < kSteps; ++p) {
-                    u32x4 v, code;
-                    if constexpr (C::kBf16) v = *reinterpret_cast<const u32x4*>(vb + p * 2 * C::kPage + c * 512);
-                    else v = *reinterpret_cast<const u32x4*>(vb + p * C::kPage + c * 1024);
-                    v &= keep[p];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if constexpr (C::kBf16) {
-                            const unsigned lo = nonfinite_code(v[j] & 0xFFFFu), hi = nonfinite_code(v[j] >> 16);
-                            code[j] = lo | (hi << 16);
-                            v[j] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-                        } else {
-                            const float f = nonfinite_code32(v[j]);
-                            code[j] = __float_as_uint(f);
-                            v[j] = f != 0.f ? 0u : v[j];
-                        }
-                    }
-#pragma unroll
-                    for (int n = 0; n < C::kNT; ++n) {
-                        if constexpr (C::kBf16) {
-                            u32x4 one;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const int bit = 4 * (2 * p + (j >> 1)) + 2 * (j & 1);
-                                one[j] = ((sees[n] >> bit) & 1u ? 0x3F80u : 0u) |
-                                         ((sees[n] >> (bit + 1)) & 1u ? 0x3F800000u : 0u);
-                            }
-                            st.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pb[p][n]), st.o[n][c], 0, 0, 0);
-                            codes[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                __builtin_bit_cast(bf16x8, code), __builtin_bit_cast(bf16x8, one), codes[n], 0, 0, 0);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                st.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[j]), s[p][n][j],
-                                                                                  st.o[n][c], 0, 0, 0);
-                                codes[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                                    __uint_as_float(code[j]), (sees[n] >> (4 * p + j)) & 1u ? 1.f : 0.f, codes[n], 0,
-                                    0, 0);
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int n = 0; n < C::kNT; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) st.o[n][c][r] += nonfinite_value(codes[n][r]);
-            }
-            return;
-        }
-    }
-#pragma unroll
-    for (int c = 0; c < C::kC; ++c) {
-#pragma unroll
-        for (int p = 0; p < kSteps; ++p) {
+        for (int c = 0; c < C::kC; ++c) {
             if constexpr (C::kBf16) {
                 u32x4 v = *reinterpret_cast<const u32x4*>(vb + p * 2 * C::kPage + c * 512);
                 if constexpr (MASKED) v &= keep[p];
@@ -657,6 +715,7 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
             }
         }
     }
+    if constexpr (C::kBf16 && !MASKED) schedule_reads<kSteps * C::kC, C::kNT, PVAHEAD>();
 }
 
 __device__ __forceinline__ void store4(const ChunkArgs& a, bool bf16, char* out, const f32x4& v) {
@@ -673,7 +732,8 @@ __device__ __forceinline__ void store4(const ChunkArgs& a, bool bf16, char* out,
 template <class C, bool TREE>
 __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(const ChunkArgs a) {
     extern __shared__ __align__(1024) char s_kv[];
-    __shared__ int s_poison;
+    __shared__ int s_poison;   // 1 + the last block found with infinities or NaN to take out
+    __shared__ int s_bad;      // 1: a page that every row of the tile attends to is missing
     const int lane = threadIdx.x & (kWave - 1), gq = lane >> 4, x = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     // neighbouring ranges to one XCD (blocks go to the XCDs in turn)
@@ -683,6 +743,9 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
     const int workers = worker_range<C, TREE>(a, k, at, end);
     int first_rec = -1, last_rec = -1;   // tiles this worker shares with the one before, the ones after
     const Loader<C> ld;
+#ifdef PRIO
+    if (wave >= C::kWaves / 2) __builtin_amdgcn_s_setprio(PRIO);
+#endif
     const unsigned head_bytes = 2 * C::kTile;
     bool first_piece = true;
     if (k < workers) {
@@ -716,7 +779,8 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
 
             if (!first_piece) wait_loads_and_sync<63>();   // the last piece's reads of the stages are over
             first_piece = false;
-            if (threadIdx.x == 0) s_poison = 0;
+            if (threadIdx.x == 0) s_poison = s_bad = 0;
+            wait_loads_and_sync<63>();
 
             // this wave's rows
             State<C> st;
@@ -726,8 +790,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
             int64_t qrow[C::kNT];
             const int w0 = wave * C::kWaveRows;
             const bool wave_live = w0 < toks * a.group;
-            const int wtok0 = w0 / a.group;                                               // its first token
-            const int wtok1 = min(toks - 1, (w0 + C::kWaveRows - 1) / a.group);           // and last
+            const int wtok1 = min(toks - 1, (w0 + C::kWaveRows - 1) / a.group);   // its last token
 #pragma unroll
             for (int n = 0; n < C::kNT; ++n) {
                 const int r = w0 + n * 16 + x;
@@ -756,92 +819,89 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
             // Order of a tile's blocks: the drafts', then the context's from its end down, so that the
             // blocks that need masks come first (they are the ones at the end of what a row sees).
             const int nc = nb - nd;                              // context blocks
-            const auto page_of_block = [&](int j) { return (nc - 1 - (j - nd)) * C::kPages; };
-            const auto load_ids = [&](int j, int (&pid)[C::kPages]) {
-                const int p0 = j >= nd && j < k1 ? page_of_block(j) : 0;
-#pragma unroll
-                for (int i = 0; i < C::kPages; ++i) {
-                    // a page past the row's last holds no key that a row sees: no page
-                    const int p = p0 + i;
-                    const int e = last_page < 0 ? -1 : pt[p <= last_page ? p : last_page];
-                    pid[i] = p <= last_page ? e : -1;
-                }
-            };
-            unsigned oks = 0;   // page bits of the blocks in flight, the next one lowest
-            static_assert(C::kPages * C::kStages <= 32, "page bits");
-            int ids[C::kPages];   // of the block that is fetched next
-            const auto fetch = [&](int j) {   // block j of [k0, k1) into its stage
-                char* stage = s_kv + ((j - k0) % C::kStages) * C::kStage;
-                unsigned ok = (1u << C::kPages) - 1;
-                if (TREE && j < nd) {
-                    ld.draft_keys(a, at.b, at.g, row.n, j * C::kBlock, stage);
-                    ld.draft_values(a, at.b, at.g, row.n, j * C::kBlock, stage);
-                } else {
-                    ld.pages(a, ids, head_off, stage);
-                    ok = 0;
-#pragma unroll
-                    for (int i = 0; i < C::kPages; ++i) ok |= is_hot(a, ids[i]) || is_cold(a, ids[i]) ? 1u << i : 0u;
-                }
-                load_ids(j + 1, ids);
-                return ok;
-            };
-            load_ids(k0, ids);
-#pragma unroll
-            for (int j = 0; j < C::kStages - 1; ++j)
-                if (k0 + j < k1) oks |= fetch(k0 + j) << (C::kPages * j);
-
-            // blocks that some row of the tile does not see whole; of this wave's rows; that none of them sees
+            // blocks that some row of the tile does not see whole; those and a tail that is not full;
+            // blocks that no row of this wave sees
             int partly, masked, unseen = 0;
             if constexpr (TREE) {
                 partly = nd;
                 masked = nd + (row.ctx % C::kBlock != 0);
             } else {
-                partly = nb - (row.ctx + tok0 + 1) / C::kBlock;
-                masked = nb - (row.ctx + tok0 + wtok0 + 1) / C::kBlock;
+                partly = masked = nb - (row.ctx + tok0 + 1) / C::kBlock;
                 unseen = nb - ((row.ctx + tok0 + wtok1) / C::kBlock + 1);
             }
-            if (!wave_live) masked = unseen = nb;
+            if (!wave_live) unseen = nb;
+            const auto first_page = [&](int j) { return (nc - 1 - (j - nd)) * C::kPages; };
+            // Entry of page i of block j; a page past the row's last holds no key that a row sees: no page.
+            const auto page_id = [&](int j, int i) {
+                const int p = (j >= nd && j < k1 ? first_page(j) : 0) + i;
+                return p <= last_page ? pt[p] : -1;
+            };
+            int id = page_id(k0, ld.page());      // of this wave's page of the block that is fetched next
+            char* into = s_kv;                    // stage of that block
+            const auto next_stage = [&](char* p) { return p == s_kv + (C::kStages - 1) * C::kStage ? s_kv : p + C::kStage; };
+            const auto fetch = [&](int j) {       // block j of [k0, k1)
+                if (TREE && j < nd) {
+                    ld.draft_keys(a, at.b, at.g, row.n, j * C::kBlock, into);
+                    ld.draft_values(a, at.b, at.g, row.n, j * C::kBlock, into);
+                } else if (!ld.load_page(a, id, head_off, into)) {
+                    // a missing page of a block that every row sees whole is NaN for all of them
+                    // (tokens past the row's last, in its last block, are no matter)
+                    if (j >= partly && first_page(j) + ld.page() <= last_page) s_bad = 1;
+                }
+                id = page_id(j + 1, ld.page());
+                into = next_stage(into);
+            };
+#pragma unroll
+            for (int i = 0; i < C::kStages - 1; ++i)
+                if (k0 + i < k1) fetch(k0 + i);
             int j = k0;
-            unsigned ok = 0;
-            char* stage = nullptr;
-            // Block j has arrived for every wave, and the block STAGES - 1 later is on its way.
-            const auto turn = [&]() {
-                stage = s_kv + ((j - k0) % C::kStages) * C::kStage;
-                ok = oks & ((1u << C::kPages) - 1);
-                oks >>= C::kPages;
-                // loads of later blocks may go on: 1 KiB each, kLoads per block and wave
+            char* stage = s_kv;
+            const auto mask_of = [&](int j) {
+                if (TREE && j < nd) return Mask{j * C::kBlock, row.n, ~0u, true};
+                unsigned ok = 0;
+#pragma unroll
+                for (int i = 0; i < C::kPages; ++i) {
+                    const int e = page_id(j, i);
+                    ok |= (TREE || is_hot(a, e) || is_cold(a, e)) ? 1u << i : 0u;   // (trees: s_bad)
+                }
+                return Mask{first_page(j) * kPageTokens, keys, ok, false};
+            };
+            // Block j has arrived for every wave (the loads of later blocks may go on: 1 KiB each,
+            // kLoads per block and wave).
+            const auto arrive = [&]() {
                 if ((TREE && j < nd) || k1 - 1 - j < C::kStages - 2)
                     wait_loads_and_sync<0>();
                 else
                     wait_loads_and_sync<(C::kStages - 2) * C::kLoads>();
+            };
+            for (; j < k1 && j < masked; ++j) {
+                arrive();
                 if (j < partly) {
                     // an infinity or NaN among values that some row must not see?
                     bool hit = false;
-                    constexpr int kVec = C::kPages * C::kTile / 16;
-                    for (int i = threadIdx.x; i < kVec; i += C::kThreads)
-                        hit |= any_nonfinite(*reinterpret_cast<const u32x4*>(stage + (i / (C::kTile / 16)) * C::kPage +
-                                                                            C::kTile + i % (C::kTile / 16) * 16),
-                                             C::kBf16);
-                    if (__builtin_amdgcn_ballot_w64(hit) && lane == 0) s_poison = 1;
+                    for (int i = threadIdx.x; i < C::kPages * C::kTile / 16; i += C::kThreads)
+                        hit |= any_nonfinite(*value_group<C>(stage, i), C::kBf16);
+                    if (__builtin_amdgcn_ballot_w64(hit) && lane == 0) s_poison = j + 1;
                     wait_loads_and_sync<63>();
+                    if (s_poison == j + 1) {
+                        if (j >= unseen) add_nonfinite<C, TREE>(st, stage, mask_of(j), lim, seen);
+                        wait_loads_and_sync<63>();
+                        clear_nonfinite<C>(stage);
+                        wait_loads_and_sync<63>();
+                    }
                 }
-                if (j + C::kStages - 1 < k1) oks |= fetch(j + C::kStages - 1) << (C::kPages * (C::kStages - 2));
-            };
-            for (; j < k1 && j < masked; ++j) {
-                turn();
-                if (j < unseen) continue;
-                const bool draft = TREE && j < nd;
-                const int key0 = draft ? j * C::kBlock : page_of_block(j) * kPageTokens;
-                const Mask mk{key0, draft ? row.n : keys, ok, draft};
-                compute_block<C, TREE, true>(st, stage, a.scale_log2, a.slack, mk, lim, seen, j < partly && s_poison);
+                if (j + C::kStages - 1 < k1) fetch(j + C::kStages - 1);
+                if (j >= unseen) compute_block<C, TREE, true>(st, stage, a.scale_log2, a.slack, mask_of(j), lim, seen);
+                stage = next_stage(stage);
+            }
+            for (; j < k1; ++j) {
+                arrive();
+                if (j + C::kStages - 1 < k1) fetch(j + C::kStages - 1);
+                if (wave_live) compute_block<C, TREE, false>(st, stage, a.scale_log2, a.slack, Mask{}, lim, seen);
+                stage = next_stage(stage);
             }
             bool bad = row.bad;
-            for (; j < k1; ++j) {
-                turn();
-                // every row of this wave attends to every token here: a missing page is NaN for all
-                bad |= ok != (1u << C::kPages) - 1;
-                compute_block<C, TREE, false>(st, stage, a.scale_log2, a.slack, Mask{}, lim, seen, false);
-            }
+            bad |= s_bad != 0;   // set by fetches before the last turn's barrier
 
             // the rows' sums over their four lanes
             float l[C::kNT];
@@ -991,7 +1051,10 @@ hipError_t launch_shape(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s, c
                         const LaunchEvents& ev_merge) {
     constexpr int kPages = BF16 ? 4 : 2;
     if (p.rows == 64) return launch_cfg<Cfg<D, BF16, 4, 1, kPages, 2>, TREE>(a, p.workers, s, ev, ev_merge);
-    return launch_cfg<Cfg<D, BF16, 8, 2, kPages, 3>, TREE>(a, p.workers, s, ev, ev_merge);
+#ifndef BIGCFG
+#define BIGCFG 8, 2, kPages, 3
+#endif
+    return launch_cfg<Cfg<D, BF16, BIGCFG>, TREE>(a, p.workers, s, ev, ev_merge);
 }
 
 }  // namespace
@@ -999,8 +1062,12 @@ hipError_t launch_shape(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s, c
 // Rows of a tile: 64 where a row's queries fit into them, else 256.
 ChunkPlan chunk_plan(int cus, int group, int64_t rows_per_seq) {
     ChunkPlan p;
-    p.rows = rows_per_seq <= 64 ? 64 : 256;
-    p.workers = p.rows == 64 ? 2 * cus : cus;
+  #ifndef BIGROWS
+#define BIGROWS 256
+#define BIGWG 1
+#endif
+    p.rows = rows_per_seq <= 64 ? 64 : BIGROWS;
+    p.workers = p.rows == 64 ? 2 * cus : BIGWG * cus;
     return p;
 }
 
