@@ -48,7 +48,7 @@ __device__ __forceinline__ const_i32 uniform_ptr(const int32_t* p) {
     return (const_i32)(reinterpret_cast<uintptr_t>(p));
 }
 
-template <int D, bool BF16, int WAVES, int NT, int PAGES, int STAGES>
+template <int D, bool BF16, int WAVES, int NT, int PAGES, int STAGES, int GROUPS>
 struct Cfg {
     static constexpr int kD = D, kWaves = WAVES, kNT = NT, kPages = PAGES, kStages = STAGES;
     static constexpr bool kBf16 = BF16;
@@ -59,10 +59,7 @@ struct Cfg {
     static constexpr int kBlock = PAGES * kPageTokens;    // keys per block
     static constexpr int kStage = PAGES * kPage;          // LDS bytes of a block
     static constexpr int kThreads = WAVES * kWave;
-#ifndef PERSIMD
-#define PERSIMD 2
-#endif
-    static constexpr int kPerSimd = NT == 1 ? 2 : PERSIMD;                    // waves per SIMD the registers are made for
+    static constexpr int kPerSimd = WAVES * GROUPS / 4;    // waves per SIMD the registers are made for
     static constexpr int kWaveRows = 16 * NT;
     static constexpr int kRows = WAVES * kWaveRows;
     static constexpr int kTileLoads = kTile / 1024;       // 1 KiB loads of a tile
@@ -80,15 +77,24 @@ struct Row {
     int ctx;       // cached tokens that every query sees
     int bad;       // 1: lengths that do not fit, the row's outputs are NaN
     int tiles;     // tiles per KV head
-    int64_t base;  // cost of tile i < tiles - 1: base + slope (i + 1)
+    int64_t base;  // keys of tile i < tiles - 1: base + slope (i + 1)
     int64_t slope;
-    int64_t last;  // cost of the last tile
-    __device__ int64_t tile_start(int64_t i) const { return i * base + slope * (i * (i + 1) / 2); }
-    __device__ int64_t head_units() const { return tiles ? tile_start(tiles - 1) + last : 0; }
+    int64_t last;  // keys of the last tile
+    // First unit of tile i, and all units of one KV head, where a tile costs its keys and `cost` more.
+    __device__ int64_t tile_start(int64_t i, int cost) const {
+        return i * (base + cost) + slope * (i * (i + 1) / 2);
+    }
+    __device__ int64_t head_units(int cost) const { return tiles ? tile_start(tiles - 1, cost) + last + cost : 0; }
 };
 
-// Fixed cost of a tile in keys: its queries' load, its output and the pipeline's start.
-constexpr int kTileCost = 64;
+// What a tile costs beside its keys, in keys: its queries' load, its output, the pipeline's
+// start and the masked blocks.  kTileCost is what balances calls with work for every worker
+// (twelve packed prompts: 64: 1694 us, 192: 1330, 320: 1144, 448: 1160); calls with less
+// than that are cut finer, with kTileCostFine (8 sessions x 8 drafts: 64: 40 us, 320: 42).
+#ifndef TILECOST
+#define TILECOST 320
+#endif
+constexpr int kTileCost = TILECOST, kTileCostFine = 64;
 
 template <class C, bool TREE>
 __device__ __forceinline__ Row row_info(const ChunkArgs& a, int b) {
@@ -112,13 +118,13 @@ __device__ __forceinline__ Row row_info(const ChunkArgs& a, int b) {
     }
     r.tiles = (r.n + a.tile_tokens - 1) / a.tile_tokens;
     if (r.bad) {
-        r.base = r.last = kTileCost;
+        r.base = r.last = 0;
         r.slope = 0;
     } else if constexpr (TREE) {
-        r.base = r.last = kTileCost + static_cast<int64_t>((r.n + C::kBlock - 1) / C::kBlock) * C::kBlock + r.ctx;
+        r.base = r.last = static_cast<int64_t>((r.n + C::kBlock - 1) / C::kBlock) * C::kBlock + r.ctx;
         r.slope = 0;
     } else {
-        r.base = kTileCost + static_cast<int64_t>(r.ctx);
+        r.base = r.ctx;
         r.slope = a.tile_tokens;
         r.last = r.base + r.n;
     }
@@ -142,44 +148,84 @@ __device__ __forceinline__ int tile_blocks(const ChunkArgs& a, const Row& r, int
     return draft_blocks<C, TREE>(r) + (tile_keys<C, TREE>(a, r, i) + C::kBlock - 1) / C::kBlock;
 }
 
-// A place in the order of blocks: block `blk` of tile `tile` of (row b, KV head g).
+// A place in the order of blocks: block `blk` of tile `tile` of (row b, group hg of `team` KV heads).
 struct Place {
-    int b, g, tile, blk;
+    int b, hg, tile, blk;
 };
+
+// What a worker takes: the blocks from `from` up to `to`.  Where `to` lies inside a tile,
+// `parts` is the number of workers that share that tile from this one on.
+struct Range {
+    Place from, to;
+    int parts;
+};
+
+// How the call's units are cut: `total` units over `workers` equal ranges, a tile costing its
+// keys and `cost` more.
+struct Cuts {
+    int64_t total;
+    int workers, cost;
+    __device__ int64_t at(int k) const {   // floor(k total / workers), in 32 bits where they do
+        if ((total >> 32) == 0) {
+            const unsigned t = static_cast<unsigned>(total), w = static_cast<unsigned>(workers);
+            const unsigned q = t / w, m = t - q * w, n = static_cast<unsigned>(k);
+            return static_cast<int64_t>(n * q + n * m / w);
+        }
+        return k * (total / workers) + k * (total % workers) / workers;
+    }
+};
+
+// Enough units for a block or more in every range (see place_of).
+template <class C>
+__device__ __forceinline__ Cuts cuts_of(const ChunkArgs& a, int64_t keys, int64_t tiles) {
+    const int most = a.workers / a.team;
+    Cuts c;
+    c.cost = kTileCost;
+    if (keys + c.cost * tiles < static_cast<int64_t>(c.cost + 2 * C::kBlock) * most) c.cost = kTileCostFine;
+    c.total = keys + c.cost * tiles;
+    const int64_t n = (c.total >> 32) == 0
+                          ? static_cast<int64_t>(static_cast<unsigned>(c.total) / static_cast<unsigned>(c.cost + 2 * C::kBlock))
+                          : most;
+    c.workers = c.total <= 0 ? 0 : static_cast<int>(n < 1 ? 1 : (n > most ? most : n));
+    return c;
+}
 
 // The place of unit `u` of row b (0 <= u < its units).  Both workers at a cut compute it
 // from the same numbers, so their ranges meet without a gap; a place past a tile's last
 // block is the next tile's first.  A tile without blocks belongs to the worker that has
-// its first unit.  Ranges of at least kTileCost + 2 kBlock units hold one block or more.
+// its first unit.  Ranges of at least cost + 2 kBlock units hold one block or more.
+// `more`: for a place inside a tile, how many units further a cut still lies inside it.
 template <class C, bool TREE>
-__device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int b, int64_t u) {
+__device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int b, int64_t u, int cost, int64_t& more) {
     Place p;
     p.b = b;
-    const int64_t h = r.head_units();
+    const int64_t h = r.head_units(cost);
     if (((u | h) >> 32) == 0) {
-        p.g = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(h));
+        p.hg = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(h));
     } else {
-        p.g = static_cast<int>(u / h);
+        p.hg = static_cast<int>(u / h);
     }
-    int64_t rem = u - p.g * h;
+    int64_t rem = u - p.hg * h;
     int lo = 0, hi = r.tiles - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (r.tile_start(mid) <= rem) lo = mid; else hi = mid - 1;
+        if (r.tile_start(mid, cost) <= rem) lo = mid; else hi = mid - 1;
     }
-    rem -= r.tile_start(lo);
+    rem -= r.tile_start(lo, cost);
     p.tile = lo;
     p.blk = 0;
+    more = 0;
     if (rem > 0) {
-        const int64_t x = rem - kTileCost;
+        const int64_t x = rem - cost;
         const int nb = tile_blocks<C, TREE>(a, r, lo);
         const int64_t k = x <= 0 ? 0 : (x + C::kBlock - 1) / C::kBlock;
         p.blk = k < nb ? static_cast<int>(k) : nb;
+        more = static_cast<int64_t>(nb - 1) * C::kBlock - x;
         if (p.blk == nb) {
             p.blk = 0;
             if (++p.tile == r.tiles) {
                 p.tile = 0;
-                ++p.g;     // may be num_kv_heads: the walk moves on to the next row
+                ++p.hg;    // may be the number of head groups: the walk moves on to the next row
             }
         }
     }
@@ -187,73 +233,118 @@ __device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int 
 }
 
 __device__ __forceinline__ Place uniform_place(const Place& p) {
-    return Place{__builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.g),
+    return Place{__builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.hg),
                  __builtin_amdgcn_readfirstlane(p.tile), __builtin_amdgcn_readfirstlane(p.blk)};
 }
 
 __device__ __forceinline__ bool before(const Place& x, const Place& y) {
     if (x.b != y.b) return x.b < y.b;
-    if (x.g != y.g) return x.g < y.g;
+    if (x.hg != y.hg) return x.hg < y.hg;
     if (x.tile != y.tile) return x.tile < y.tile;
     return x.blk < y.blk;
 }
 
-__device__ __forceinline__ int64_t wave_scan64(int64_t x) {
-    const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    return x;
+// The last worker whose range begins at unit `u` or before.
+__device__ __forceinline__ int worker_at(const Cuts& c, int64_t u) {
+    const int64_t n = (u + 1) * c.workers - 1;
+    const int64_t k = ((n | c.total) >> 32) == 0
+                          ? static_cast<int64_t>(static_cast<unsigned>(n) / static_cast<unsigned>(c.total))
+                          : n / c.total;
+    return k < c.workers ? static_cast<int>(k) : c.workers - 1;
 }
 
-// Worker k's range of places.  Every thread sums a run of rows; the two threads whose
-// runs hold the range's ends walk them.  Returns the number of workers with work.
+// Inclusive sum over the lanes of a wave of numbers below 2^52.
+__device__ __forceinline__ int64_t wave_scan64(int64_t x) {
+    constexpr int kLow = 26;
+    const unsigned lo = static_cast<unsigned>(wave_scan(static_cast<int>(x & ((1 << kLow) - 1))));
+    const unsigned hi = static_cast<unsigned>(wave_scan(static_cast<int>(x >> kLow)));
+    return static_cast<int64_t>(lo) + (static_cast<int64_t>(hi) << kLow);
+}
+__device__ __forceinline__ int64_t lane_value64(int64_t x, int lane) {
+    const unsigned lo = __builtin_amdgcn_readlane(static_cast<int>(x), lane);
+    const unsigned hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), lane);
+    return static_cast<int64_t>(lo) | (static_cast<int64_t>(hi) << 32);
+}
+
+// Worker k's range; false where there is none.
 template <class C, bool TREE>
-__device__ int worker_range(const ChunkArgs& a, int k, Place& from, Place& to) {
-    __shared__ int64_t s_sum[C::kWaves];
-    __shared__ Place s_place[2];
+__device__ bool worker_range(const ChunkArgs& a, int k, Range& out) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    const int per = (a.batch + C::kThreads - 1) / C::kThreads;
-    const int lo = min(a.batch, tid * per), hi = min(a.batch, lo + per);
-    int64_t sum = 0;
-    for (int b = lo; b < hi; ++b) sum += a.num_kv_heads * row_info<C, TREE>(a, b).head_units();
-    const int64_t incl = wave_scan64(sum);
-    if (lane == kWave - 1) s_sum[wave] = incl;
-    if (tid < 2) s_place[tid] = Place{a.batch, 0, 0, 0};
-    __syncthreads();
-    int64_t total = 0, before_wave = 0;
-    for (int w = 0; w < C::kWaves; ++w) {
-        if (w == wave) before_wave = total;
-        total += s_sum[w];
-    }
-    const int64_t first = before_wave + incl - sum;
-    const int64_t least = kTileCost + 2 * C::kBlock;
-    int64_t n = total / least;
-    n = n < 1 ? 1 : (n > a.workers ? a.workers : n);
-    const int workers = total > 0 ? static_cast<int>(n) : 0;
-    if (k < workers) {
-        int64_t u[2];
-        if ((total >> 32) == 0) {   // k total / workers = k (total / workers) + k (total mod workers) / workers
-            const unsigned t = static_cast<unsigned>(total), w = static_cast<unsigned>(workers);
-            const unsigned q = t / w, m = t - q * w, kk = static_cast<unsigned>(k);
-            u[0] = static_cast<int64_t>(kk) * q + kk * m / w;
-            u[1] = static_cast<int64_t>(kk + 1) * q + (kk + 1) * m / w;
-        } else {
-            const int64_t q = total / workers, m = total % workers;
-            u[0] = k * q + k * m / workers;
-            u[1] = (k + 1) * q + (k + 1) * m / workers;
-        }
+    const int heads = a.num_kv_heads / a.team;
+    if (a.batch <= kWave) {
+        // a row per lane; every wave finds the range by itself
+        Row r = {};
+        if (lane < a.batch) r = row_info<C, TREE>(a, lane);
+        const int64_t keys = heads * r.head_units(0), tiles = static_cast<int64_t>(heads) * r.tiles;
+        const int64_t keys_to = wave_scan64(keys), tiles_to = wave_scan64(tiles);
+        const Cuts cuts = cuts_of<C>(a, lane_value64(keys_to, kWave - 1), lane_value64(tiles_to, kWave - 1));
+        if (k >= cuts.workers) return false;
+        const int64_t units = keys + cuts.cost * tiles;
+        const int64_t first = keys_to + cuts.cost * tiles_to - units;
+        out.parts = 0;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            if (u[j] < first || u[j] >= first + sum) continue;
+            const int64_t u = cuts.at(k + j);
+            Place p{a.batch, 0, 0, 0};
+            if (u < cuts.total) {
+                const uint64_t has = __builtin_amdgcn_ballot_w64(units > 0 && first <= u);
+                const int b = kWave - 1 - __builtin_clzll(has);
+                int64_t more;
+                p = uniform_place(place_of<C, TREE>(a, row_info<C, TREE>(a, b), b, u - lane_value64(first, b),
+                                                    cuts.cost, more));
+                if (j == 1 && p.blk > 0) out.parts = worker_at(cuts, u + more) - k + 1;
+            }
+            (j == 0 ? out.from : out.to) = p;
+        }
+        out.parts = __builtin_amdgcn_readfirstlane(out.parts);
+        return true;
+    }
+    // a run of rows per thread; the threads whose runs hold the range's ends walk them
+    __shared__ int64_t s_keys[C::kWaves], s_tiles[C::kWaves];
+    __shared__ Place s_place[2];
+    __shared__ int s_parts;
+    const int per = (a.batch + C::kThreads - 1) / C::kThreads;
+    const int lo = min(a.batch, tid * per), hi = min(a.batch, lo + per);
+    int64_t keys = 0, tiles = 0;
+    for (int b = lo; b < hi; ++b) {
+        const Row r = row_info<C, TREE>(a, b);
+        keys += heads * r.head_units(0);
+        tiles += static_cast<int64_t>(heads) * r.tiles;
+    }
+    const int64_t keys_to = wave_scan64(keys), tiles_to = wave_scan64(tiles);
+    if (lane == kWave - 1) {
+        s_keys[wave] = keys_to;
+        s_tiles[wave] = tiles_to;
+    }
+    if (tid < 2) s_place[tid] = Place{a.batch, 0, 0, 0};
+    if (tid == 0) s_parts = 0;
+    __syncthreads();
+    int64_t all_keys = 0, all_tiles = 0, keys_before = 0, tiles_before = 0;
+    for (int w = 0; w < C::kWaves; ++w) {
+        if (w == wave) {
+            keys_before = all_keys;
+            tiles_before = all_tiles;
+        }
+        all_keys += s_keys[w];
+        all_tiles += s_tiles[w];
+    }
+    const Cuts cuts = cuts_of<C>(a, all_keys, all_tiles);
+    const int64_t sum = keys + cuts.cost * tiles;
+    const int64_t first = keys_before + keys_to - keys + cuts.cost * (tiles_before + tiles_to - tiles);
+    if (k < cuts.workers) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t u = cuts.at(k + j);
+            if (u < first || u >= first + sum) continue;
             int64_t at = first;
             for (int b = lo; b < hi; ++b) {
                 const Row r = row_info<C, TREE>(a, b);
-                const int64_t units = a.num_kv_heads * r.head_units();
-                if (u[j] < at + units) {
-                    s_place[j] = place_of<C, TREE>(a, r, b, u[j] - at);
+                const int64_t units = heads * r.head_units(cuts.cost);
+                if (u < at + units) {
+                    int64_t more;
+                    const Place p = place_of<C, TREE>(a, r, b, u - at, cuts.cost, more);
+                    s_place[j] = p;
+                    if (j == 1 && p.blk > 0) s_parts = worker_at(cuts, u + more) - k + 1;
                     break;
                 }
                 at += units;
@@ -261,9 +352,10 @@ __device__ int worker_range(const ChunkArgs& a, int k, Place& from, Place& to) {
         }
     }
     __syncthreads();
-    from = uniform_place(s_place[0]);
-    to = uniform_place(s_place[1]);
-    return __builtin_amdgcn_readfirstlane(workers);
+    out.from = uniform_place(s_place[0]);
+    out.to = uniform_place(s_place[1]);
+    out.parts = __builtin_amdgcn_readfirstlane(s_parts);
+    return __builtin_amdgcn_readfirstlane(k < cuts.workers);
 }
 
 // Page-table entry `pid`: a hot page, a cold page (num_cold is 0 where the pool reads no
@@ -291,7 +383,6 @@ __device__ __forceinline__ void wait_loads_and_sync() {
 template <class C>
 struct Loader {
     unsigned koff, voff;   // this lane's byte in a tile, first load (an even page's K; V)
-    unsigned koff_page;    // the same for the K of the wave's page
     int wave, lane;
     __device__ explicit Loader() {
         lane = threadIdx.x & (kWave - 1);
@@ -308,16 +399,17 @@ struct Loader {
             koff = lane * 16;
             voff = C::kTile + x * 64 + g * 16;
         }
-        koff_page = C::kBf16 ? koff ^ ((page() & 1) * 64) : koff;
     }
-    // This wave's share of a block is in one page: its tiles (K, V or both), or a part of one.
+    // This wave's share of a block: whole pages, one page's K or V tile, or a part of one.
     static constexpr int kShare = C::kTileLoads > C::kLoads ? C::kTileLoads / C::kLoads : 1;  // waves of a tile
     static constexpr int kTiles = C::kLoads > C::kTileLoads ? C::kLoads / C::kTileLoads : 1;  // tiles of a wave
-    static_assert(kTiles <= 2, "a wave's tiles are one page's");
+    static constexpr int kMyPages = kTiles > 2 ? kTiles / 2 : 1;
+    static_assert(kTiles <= 2 || kTiles % 2 == 0, "a wave's tiles are whole pages'");
     __device__ __forceinline__ int tile() const { return kShare > 1 ? wave / kShare : wave * kTiles; }
-    __device__ __forceinline__ int page() const { return tile() >> 1; }
-    // Its loads, from the page that entry `id` names; an id that names none reads zeros.
-    __device__ __forceinline__ bool load_page(const ChunkArgs& a, int id, unsigned head_off, char* stage) const {
+    __device__ __forceinline__ int page() const { return tile() >> 1; }   // the first of kMyPages
+    // Its loads of its i-th page, which entry `id` names; an id that names none reads zeros.
+    __device__ __forceinline__ bool load_page(const ChunkArgs& a, int id, int i_page, unsigned head_off,
+                                              char* stage) const {
         const bool hot = is_hot(a, id), cold = is_cold(a, id);
         const char* pool = cold ? a.cold : a.hot;
         const int64_t stride = cold ? a.cold_stride : a.hot_stride;
@@ -325,14 +417,17 @@ struct Loader {
         const __amdgpu_buffer_rsrc_t rs =
             __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool + n * stride + head_off), static_cast<short>(0),
                                               hot || cold ? C::kPage : 0, kRsrcWord3);
+        constexpr int kHere = kTiles < 2 ? kTiles : 2;      // tiles of the page
+        constexpr int kEach = C::kLoads / kTiles;           // loads of a tile
 #pragma unroll
-        for (int j = 0; j < kTiles; ++j) {
-            const int t = tile() + j;
+        for (int j = 0; j < kHere; ++j) {
+            const int t = tile() + 2 * i_page + j;
             const int first = kShare > 1 ? (wave % kShare) * C::kLoads : 0;
-            const unsigned off = (t & 1) ? voff : koff_page;
+            const unsigned k = C::kBf16 && ((page() + i_page) & 1) ? koff ^ 64 : koff;
+            const unsigned off = (t & 1) ? voff : k;
             char* dst = stage + t * C::kTile + first * 1024;
 #pragma unroll
-            for (int i = 0; i < C::kLoads / kTiles; ++i) load_lds16(rs, dst + i * 1024, off + (first + i) * 1024);
+            for (int i = 0; i < kEach; ++i) load_lds16(rs, dst + i * 1024, off + (first + i) * 1024);
         }
         return hot || cold;
     }
@@ -364,15 +459,21 @@ struct Loader {
         constexpr int kGroups = C::kPages * C::kD * kQuarters;    // of the block
         const elt* base = static_cast<const elt*>(a.v_new) +
                           (static_cast<int64_t>(b) * a.width * a.num_kv_heads + g) * C::kD;
-        const int64_t row = static_cast<int64_t>(a.num_kv_heads) * C::kD;
-#pragma unroll
-        for (int s = threadIdx.x; s < kGroups; s += C::kThreads) {
+        const int row = a.num_kv_heads * C::kD;       // (at most 64 drafts: 32-bit offsets do)
+        constexpr int kRounds = (kGroups + C::kThreads - 1) / C::kThreads;
+#pragma unroll 2
+        for (int round = 0; round < kRounds; ++round) {
+            const int s = threadIdx.x + round * C::kThreads;
+            if (kGroups % C::kThreads && s >= kGroups) break;
             const int page = s / (C::kD * kQuarters), in = s % (C::kD * kQuarters);
             const int c = in / (16 * kQuarters), q = in / 16 % kQuarters, dim = c * 16 + in % 16;
             const int first = key0 + page * kPageTokens + q * C::kX;
             elt e[C::kX];
+            // (the last draft in place of those past it, so that the loads go out together)
 #pragma unroll
-            for (int j = 0; j < C::kX; ++j) e[j] = first + j < n ? base[(first + j) * row + dim] : elt(0);
+            for (int j = 0; j < C::kX; ++j) e[j] = base[min(first + j, n - 1) * row + dim];
+#pragma unroll
+            for (int j = 0; j < C::kX; ++j) e[j] = first + j < n ? e[j] : elt(0);
             u32x4 w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -430,25 +531,10 @@ __device__ __forceinline__ bool any_nonfinite(const u32x4& v, bool bf16) {
     return hit;
 }
 
-#ifndef QKAHEAD
-#define QKAHEAD 8
-#endif
-#ifndef PVAHEAD
-#define PVAHEAD 8
-#endif
-// Order of a section's LDS reads and matrix instructions: `AHEAD` reads first, then one per
-// MFMAS matrix instructions, so that a read's latency lies under AHEAD * MFMAS of them.
-template <int READS, int MFMAS, int AHEAD>
-__device__ __forceinline__ void schedule_reads() {
-    constexpr int kFirst = AHEAD < READS ? AHEAD : READS;
-    __builtin_amdgcn_sched_group_barrier(0x100, kFirst, 0);
-#pragma unroll
-    for (int i = kFirst; i < READS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, MFMAS, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, MFMAS * kFirst, 0);
-}
+// Fence between a group of LDS reads and a group of matrix instructions: other instructions
+// may cross it.  Without fences the compiler puts each read right before its use and the
+// wave waits out the LDS latency 32 times per block.
+__device__ __forceinline__ void order_fence() { __builtin_amdgcn_sched_barrier(0x0406); }
 
 // Key that this lane's register (t, r) of S^T stands for, from the block's first, and its page.
 template <class C>
@@ -577,44 +663,71 @@ template <class C, bool TREE, bool MASKED>
 __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, float scale, float slack, const Mask& mk,
                                               const int (&lim)[C::kNT], const uint64_t (&seen)[C::kNT]) {
     const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, x = lane & 15;
+    // Fragments of K and then of V, in groups of kG, two groups ahead of the products.
+    constexpr int kG = C::kPages * C::kQ >= 8 && C::kD > 64 && C::kPerSimd <= 2 ? 4 : 2;
+    constexpr int kKF = C::kPages * C::kQ;                           // K fragments: (i, page t)
+    constexpr int kSteps = C::kBf16 ? C::kPages / 2 : C::kPages;     // contraction steps of the output
+    constexpr int kVF = kSteps * C::kC;                              // V fragments: (step p, c)
+    static_assert(kKF % kG == 0 && kKF / kG >= 2 && kVF % kG == 0 && kVF / kG >= 2, "groups");
+    u32x4 kf[2][kG], vf[2][kG];
+    const char *kb, *vb;
+    unsigned flip = 0;
+    if constexpr (C::kBf16) {
+        kb = stage + (x >> 3) * C::kPage + g * 256 + (x & 7) * 16;
+        flip = (x >> 3) * 128;
+        vb = stage + (g >> 1) * C::kPage + C::kTile + (g & 1) * 256 + x * 16;
+    } else {
+        kb = stage + lane * 16;
+        vb = stage + C::kTile + lane * 16;
+    }
+    const auto load_k = [&](int group) {
+#pragma unroll
+        for (int u = 0; u < kG; ++u) {
+            const int i = (group * kG + u) / C::kPages, t = (group * kG + u) % C::kPages;
+            const char* kt = C::kBf16 ? kb + (t >> 1) * 2 * C::kPage + (((t & 1) * 128) ^ flip) : kb + t * C::kPage;
+            kf[group & 1][u] = *reinterpret_cast<const u32x4*>(kt + i * 1024);
+        }
+    };
+    const auto load_v = [&](int group) {
+#pragma unroll
+        for (int u = 0; u < kG; ++u) {
+            const int p = (group * kG + u) / C::kC, c = (group * kG + u) % C::kC;
+            vf[group & 1][u] = *reinterpret_cast<const u32x4*>(vb + p * (C::kBf16 ? 2 : 1) * C::kPage + c * 256 * C::kElt);
+        }
+    };
     f32x4 s[C::kPages][C::kNT];
 #pragma unroll
     for (int t = 0; t < C::kPages; ++t)
 #pragma unroll
         for (int n = 0; n < C::kNT; ++n) s[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // scores
-    if constexpr (C::kBf16) {
-        const char* kb = stage + (x >> 3) * C::kPage + g * 256 + (x & 7) * 16;
-        const unsigned flip = (x >> 3) * 128;
+    load_k(0);
+    load_k(1);
+    order_fence();
 #pragma unroll
-        for (int t = 0; t < C::kPages; ++t) {
-            const char* kt = kb + (t >> 1) * 2 * C::kPage + (((t & 1) * 128) ^ flip);
+    for (int group = 0; group < kKF / kG; ++group) {
 #pragma unroll
-            for (int i = 0; i < C::kQ; ++i) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + i * 1024);
+        for (int u = 0; u < kG; ++u) {
+            const int i = (group * kG + u) / C::kPages, t = (group * kG + u) % C::kPages;
+            const u32x4 k = kf[group & 1][u];
+            if constexpr (C::kBf16) {
 #pragma unroll
                 for (int n = 0; n < C::kNT; ++n)
-                    s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, st.q[n][i]),
-                                                                      s[t][n], 0, 0, 0);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int t = 0; t < C::kPages; ++t) {
-            const char* kt = stage + t * C::kPage + lane * 16;
-#pragma unroll
-            for (int i = 0; i < C::kQ; ++i) {
-                const f32x4 kf = *reinterpret_cast<const f32x4*>(kt + i * 1024);
+                    s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, st.q[n][i]), s[t][n], 0, 0, 0);
+            } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int n = 0; n < C::kNT; ++n)
-                        s[t][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j], __uint_as_float(st.q[n][i][j]),
-                                                                       s[t][n], 0, 0, 0);
+                        s[t][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            __uint_as_float(k[j]), __uint_as_float(st.q[n][i][j]), s[t][n], 0, 0, 0);
             }
         }
+        order_fence();
+        if (group + 2 < kKF / kG) load_k(group + 2);
+        else load_v(group + 2 - kKF / kG);
+        order_fence();
     }
-    if constexpr (C::kBf16) schedule_reads<C::kPages * C::kQ, C::kNT, QKAHEAD>();
     unsigned sees[C::kNT];
     if constexpr (MASKED) {
 #pragma unroll
@@ -684,28 +797,23 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
         }
     }
     // output
-    const char* vb;
-    if constexpr (C::kBf16) vb = stage + (g >> 1) * C::kPage + C::kTile + (g & 1) * 256 + x * 16;
-    else vb = stage + C::kTile + lane * 16;
-    constexpr int kSteps = C::kBf16 ? C::kPages / 2 : C::kPages;
     u32x4 keep[MASKED ? kSteps : 1];
     if constexpr (MASKED)
 #pragma unroll
         for (int p = 0; p < kSteps; ++p) keep[p] = kept_values<C>(mk, p);
 #pragma unroll
-    for (int p = 0; p < kSteps; ++p) {
+    for (int group = 0; group < kVF / kG; ++group) {
 #pragma unroll
-        for (int c = 0; c < C::kC; ++c) {
+        for (int u = 0; u < kG; ++u) {
+            const int p = (group * kG + u) / C::kC, c = (group * kG + u) % C::kC;
+            u32x4 v = vf[group & 1][u];
+            if constexpr (MASKED) v &= keep[p];
             if constexpr (C::kBf16) {
-                u32x4 v = *reinterpret_cast<const u32x4*>(vb + p * 2 * C::kPage + c * 512);
-                if constexpr (MASKED) v &= keep[p];
 #pragma unroll
                 for (int n = 0; n < C::kNT; ++n)
                     st.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                         __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pb[p][n]), st.o[n][c], 0, 0, 0);
             } else {
-                u32x4 v = *reinterpret_cast<const u32x4*>(vb + p * C::kPage + c * 1024);
-                if constexpr (MASKED) v &= keep[p];
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -714,8 +822,10 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
                                                                           0, 0, 0);
             }
         }
+        order_fence();
+        if (group + 2 < kVF / kG) load_v(group + 2);
+        order_fence();
     }
-    if constexpr (C::kBf16 && !MASKED) schedule_reads<kSteps * C::kC, C::kNT, PVAHEAD>();
 }
 
 __device__ __forceinline__ void store4(const ChunkArgs& a, bool bf16, char* out, const f32x4& v) {
@@ -730,29 +840,31 @@ __device__ __forceinline__ void store4(const ChunkArgs& a, bool bf16, char* out,
 }
 
 template <class C, bool TREE>
-__global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(const ChunkArgs a) {
+__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kPerSimd, C::kPerSimd))) void chunk_attend_kernel(const ChunkArgs a) {
     extern __shared__ __align__(1024) char s_kv[];
     __shared__ int s_poison;   // 1 + the last block found with infinities or NaN to take out
     __shared__ int s_bad;      // 1: a page that every row of the tile attends to is missing
     const int lane = threadIdx.x & (kWave - 1), gq = lane >> 4, x = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    // neighbouring ranges to one XCD (blocks go to the XCDs in turn)
+    // neighbouring ranges to one XCD (blocks go to the XCDs in turn); a team takes one range
+    // of head groups, a KV head each
     int k = blockIdx.x;
     if (gridDim.x % kXcds == 0) k = (k % kXcds) * (gridDim.x / kXcds) + k / kXcds;
-    Place at, end;
-    const int workers = worker_range<C, TREE>(a, k, at, end);
-    int first_rec = -1, last_rec = -1;   // tiles this worker shares with the one before, the ones after
+    const int member = k % a.team;
+    const int heads = a.num_kv_heads / a.team;
+    Range range;
+    const bool work = worker_range<C, TREE>(a, k / a.team, range);
+    Place at = range.from;
+    const Place end = range.to;
+    bool recorded = false;   // this worker holds the first part of a cut tile
     const Loader<C> ld;
-#ifdef PRIO
-    if (wave >= C::kWaves / 2) __builtin_amdgcn_s_setprio(PRIO);
-#endif
     const unsigned head_bytes = 2 * C::kTile;
     bool first_piece = true;
-    if (k < workers) {
+    if (work) {
         while (before(at, end)) {
             if (at.b >= a.batch) break;
             const Row row = row_info<C, TREE>(a, at.b);
-            if (at.g >= a.num_kv_heads || row.tiles == 0) {   // on to the next row with queries
+            if (at.hg >= heads || row.tiles == 0) {   // on to the next row with queries
                 int b = at.b + 1;
                 while (b < a.batch) {
                     const uint64_t some = __builtin_amdgcn_ballot_w64(
@@ -767,13 +879,14 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
                 continue;
             }
             const int nb = tile_blocks<C, TREE>(a, row, at.tile);
-            const bool to_end = end.b == at.b && end.g == at.g && end.tile == at.tile;
+            const int kv_head = at.hg * a.team + member;
+            const bool to_end = end.b == at.b && end.hg == at.hg && end.tile == at.tile;
             const int k0 = at.blk, k1 = to_end ? end.blk : nb;
             const int nd = draft_blocks<C, TREE>(row);
             const int keys = tile_keys<C, TREE>(a, row, at.tile);
             const int tok0 = at.tile * a.tile_tokens;
             const int toks = min(a.tile_tokens, row.n - tok0);
-            const unsigned head_off = at.g * head_bytes;
+            const unsigned head_off = kv_head * head_bytes;
             const const_i32 pt = uniform_ptr(a.page_table + static_cast<int64_t>(at.b) * a.pt_stride);
             const int last_page = (keys + kPageTokens - 1) / kPageTokens - 1;
 
@@ -798,7 +911,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
                 live[n] = tok[n] < toks;
                 const int t = live[n] ? tok0 + tok[n] : 0;
                 const int h = live[n] ? r % a.group : 0;
-                qrow[n] = ((static_cast<int64_t>(row.start) + t) * a.num_q_heads + at.g * a.group + h) * C::kD;
+                qrow[n] = ((static_cast<int64_t>(row.start) + t) * a.num_q_heads + kv_head * a.group + h) * C::kD;
                 lim[n] = TREE ? row.ctx : (live[n] ? row.ctx + t + 1 : 0);
                 seen[n] = 0;
                 if constexpr (TREE)
@@ -836,20 +949,34 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
                 const int p = (j >= nd && j < k1 ? first_page(j) : 0) + i;
                 return p <= last_page ? pt[p] : -1;
             };
-            int id = page_id(k0, ld.page());      // of this wave's page of the block that is fetched next
+            constexpr int kMine = Loader<C>::kMyPages;
+            int id[kMine];                        // of this wave's pages of the block that is fetched next
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) id[i] = page_id(k0, ld.page() + i);
             char* into = s_kv;                    // stage of that block
             const auto next_stage = [&](char* p) { return p == s_kv + (C::kStages - 1) * C::kStage ? s_kv : p + C::kStage; };
-            const auto fetch = [&](int j) {       // block j of [k0, k1)
-                if (TREE && j < nd) {
-                    ld.draft_keys(a, at.b, at.g, row.n, j * C::kBlock, into);
-                    ld.draft_values(a, at.b, at.g, row.n, j * C::kBlock, into);
-                } else if (!ld.load_page(a, id, head_off, into)) {
+            const auto next_block = [&](int j) {
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) id[i] = page_id(j, ld.page() + i);
+                into = next_stage(into);
+            };
+            const auto fetch_pages = [&](int j) {   // context block j of [k0, k1)
+#pragma unroll
+                for (int i = 0; i < kMine; ++i)
                     // a missing page of a block that every row sees whole is NaN for all of them
                     // (tokens past the row's last, in its last block, are no matter)
-                    if (j >= partly && first_page(j) + ld.page() <= last_page) s_bad = 1;
+                    if (!ld.load_page(a, id[i], i, head_off, into))
+                        if (j >= partly && first_page(j) + ld.page() + i <= last_page) s_bad = 1;
+                next_block(j + 1);
+            };
+            const auto fetch = [&](int j) {         // block j of [k0, k1)
+                if (TREE && j < nd) {
+                    ld.draft_keys(a, at.b, kv_head, row.n, j * C::kBlock, into);
+                    ld.draft_values(a, at.b, kv_head, row.n, j * C::kBlock, into);
+                    next_block(j + 1);
+                } else {
+                    fetch_pages(j);
                 }
-                id = page_id(j + 1, ld.page());
-                into = next_stage(into);
             };
 #pragma unroll
             for (int i = 0; i < C::kStages - 1; ++i)
@@ -896,7 +1023,7 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
             }
             for (; j < k1; ++j) {
                 arrive();
-                if (j + C::kStages - 1 < k1) fetch(j + C::kStages - 1);
+                if (j + C::kStages - 1 < k1) fetch_pages(j + C::kStages - 1);
                 if (wave_live) compute_block<C, TREE, false>(st, stage, a.scale_log2, a.slack, Mask{}, lim, seen);
                 stage = next_stage(stage);
             }
@@ -938,101 +1065,100 @@ __global__ __launch_bounds__(C::kThreads, C::kPerSimd) void chunk_attend_kernel(
                         pm[C::kRows + r] = l[n];
                     }
                 }
-                if (k0 == 0) last_rec = 1; else first_rec = 1;
+                if (k0 == 0) {
+                    recorded = true;
+                    if (threadIdx.x == 0)
+                        a.recs[k] = ChunkRec{range.parts, toks * a.group,
+                                             (static_cast<int64_t>(row.start) + tok0) * a.num_q_heads + kv_head * a.group};
+                }
             }
-            if (threadIdx.x == 0 && (last_rec == 1 || first_rec == 1)) {
-                ChunkRec* rec = a.recs + 2 * k + (last_rec == 1 ? 1 : 0);
-                *rec = ChunkRec{at.b, at.g, at.tile, 1};
-            }
-            if (last_rec == 1) last_rec = 2;
-            if (first_rec == 1) first_rec = 2;
             if (to_end) break;
             at.blk = 0;
             if (++at.tile == row.tiles) {
                 at.tile = 0;
-                ++at.g;
+                ++at.hg;
             }
         }
     }
-    if (threadIdx.x == 0) {
-        if (first_rec < 0) a.recs[2 * k] = ChunkRec{-1, -1, -1, 0};
-        if (last_rec < 0) a.recs[2 * k + 1] = ChunkRec{-1, -1, -1, 0};
-    }
+    if (!recorded && threadIdx.x == 0) a.recs[k] = ChunkRec{0, 0, 0};
 }
 
 // Joins the partial results of the tiles cut between workers: with M the largest of the
 // parts' maxima, out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Block (k, y) takes
 // rows of the tile whose first part worker k left in slot 2 k + 1; its other parts are
-// slots 2 (k + 1), 2 (k + 2), .. as long as they name the same tile.  A wave per row, a
-// float4 per lane, kWave / (D / 4) parts at a time.
-constexpr int kMergeRows = 16;
+// slots 2 (k + team), 2 (k + 2 team), ..  A wave per row, a float4 per lane, kAtOnce parts
+// at a time, joined as they come; the record holds all that the row's place needs, so that
+// only two loads follow each other.
+constexpr int kMergeRows = 4;
 
-template <class C, bool TREE>
+template <class C>
 __global__ __launch_bounds__(kBlockThreads) void chunk_merge_kernel(const ChunkArgs a) {
     const int k = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    ChunkRec rec = a.recs[2 * k + 1];
-    if (!rec.used) return;
-    rec.b = __builtin_amdgcn_readfirstlane(rec.b);
-    const Row row = row_info<C, TREE>(a, rec.b);
-    const int tok0 = rec.tile * a.tile_tokens;
-    const int rows = min(a.tile_tokens, row.n - tok0) * a.group;
-    if (static_cast<int>(blockIdx.y) * kMergeRows >= rows) return;
-    int parts = 1;   // slots 2 k + 1, 2 (k + 1), ..
-    for (int j = k + 1; j < a.workers; j += kWave) {
-        bool same = false;
-        if (j + lane < a.workers) {
-            const ChunkRec r = a.recs[2 * (j + lane)];
-            same = r.used && r.b == rec.b && r.g == rec.g && r.tile == rec.tile;
-        }
-        const uint64_t m = __builtin_amdgcn_ballot_w64(same);
-        const int run = m == ~0ull ? kWave : __builtin_ctzll(~m);
-        parts += run;
-        if (run < kWave) break;
-    }
+    const ChunkRec rec = a.recs[k];
+    const int parts = __builtin_amdgcn_readfirstlane(rec.parts), rows = __builtin_amdgcn_readfirstlane(rec.rows);
+    if (parts == 0) return;
     constexpr int kLanes = C::kD / 4, kAtOnce = kWave / kLanes;
     const int sub = lane / kLanes, col = lane % kLanes;
-    for (int i = wave; i < kMergeRows; i += kBlockWaves) {
-        const int r = blockIdx.y * kMergeRows + i;
-        if (r >= rows) break;
-        const auto slot_of = [&](int p) { return p == 0 ? 2 * k + 1 : 2 * (k + p); };
-        float top = -INFINITY;
-        for (int p = lane; p < parts; p += kWave)
-            top = fmaxf(top, a.part_ml[static_cast<int64_t>(slot_of(p)) * 2 * C::kRows + r]);
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    for (int r = blockIdx.y * kMergeRows + wave; r < rows; r += gridDim.y * kMergeRows) {
+        const auto slot_of = [&](int p) { return static_cast<int64_t>(p == 0 ? 2 * k + 1 : 2 * (k + p * a.team)); };
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        float den = 0.f;
-#pragma unroll 4
-        for (int p = sub; p < parts; p += kAtOnce) {
-            const int64_t slot = slot_of(p);
-            const float m = a.part_ml[slot * 2 * C::kRows + r], l = a.part_ml[slot * 2 * C::kRows + C::kRows + r];
-            const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + (slot * C::kRows + r) * C::kD + col * 4);
-            const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-            acc += o * w;
-            // a part whose scores were all NaN has no maximum: its sum is NaN
-            den += l * w;
+        float top = -INFINITY, den = 0.f;
+        const auto join = [&](float m, float l, const f32x4& o) {
+            const float t = fmaxf(top, m);
+            // (1 for a part without a maximum, which holds 0 or NaN; never 0 times infinity)
+            const float w0 = top == -INFINITY ? 1.f : fmaxf(__builtin_amdgcn_exp2f(top - t), 1e-37f);
+            const float w1 = m == -INFINITY ? 1.f : fmaxf(__builtin_amdgcn_exp2f(m - t), 1e-37f);
+            acc = acc * w0 + o * w1;
+            den = den * w0 + l * w1;
+            top = t;
+        };
+        constexpr int kBatch = 8;   // parts whose loads are in flight together, per lane group
+        for (int p0 = sub; p0 < parts; p0 += kBatch * kAtOnce) {
+            float m[kBatch], l[kBatch];
+            f32x4 o[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int p = p0 + i * kAtOnce;
+                const int64_t slot = slot_of(p < parts ? p : 0);
+                m[i] = a.part_ml[slot * 2 * C::kRows + r];
+                l[i] = a.part_ml[slot * 2 * C::kRows + C::kRows + r];
+                o[i] = *reinterpret_cast<const f32x4*>(a.part_o + (slot * C::kRows + r) * C::kD + col * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (p0 + i * kAtOnce < parts) join(m[i], l[i], o[i]);
         }
 #pragma unroll
         for (int d = kLanes; d < kWave; d <<= 1) {
+            const float m = __shfl_xor(top, d), l = __shfl_xor(den, d);
+            f32x4 o;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], d);
-            den += __shfl_xor(den, d);
+            for (int j = 0; j < 4; ++j) o[j] = __shfl_xor(acc[j], d);
+            join(m, l, o);
         }
         if (sub == 0) {
-            const int t = tok0 + r / a.group, h = r % a.group;
+            const int64_t q = rec.first + static_cast<int64_t>(r / a.group) * a.num_q_heads + r % a.group;
             const float inv = den == 0.f ? 0.f : 1.f / den;
-            char* out = static_cast<char*>(a.out) +
-                        (((static_cast<int64_t>(row.start) + t) * a.num_q_heads + rec.g * a.group + h) * C::kD + col * 4) *
-                            C::kElt;
-            store4(a, C::kBf16, out, acc * inv);
+            store4(a, C::kBf16, static_cast<char*>(a.out) + (q * C::kD + col * 4) * C::kElt, acc * inv);
         }
     }
 }
 
+#ifndef MERGEITER
+#define MERGEITER 1
+#endif
+#ifndef TEAM
+#define TEAM(TREE, C) (C::kRows < 256)
+#endif
 template <class C, bool TREE>
 hipError_t launch_cfg(ChunkArgs a, int workers, hipStream_t s, const LaunchEvents& ev, const LaunchEvents& ev_merge) {
     a.tile_tokens = C::kRows / a.group;
-    a.workers = workers;
+    // Teams: four workers (two, where the KV heads come in twos) read the tiles of neighbouring
+    // heads of the same pages at the same time, which HBM serves faster than unrelated tiles.
+    // Large tiles are bound by the products and share K and V in the L2 better alone.
+    a.team = TEAM(TREE, C) ? (a.num_kv_heads % 4 == 0 ? 4 : (a.num_kv_heads % 2 == 0 ? 2 : 1)) : 1;
+    a.workers = workers - workers % a.team;
+    workers = a.workers;
     chunk_workspace_layout(a, C::kRows, C::kD);
     const size_t lds = static_cast<size_t>(C::kStages) * C::kStage;
     const void* kern = reinterpret_cast<const void*>(&chunk_attend_kernel<C, TREE>);
@@ -1041,8 +1167,8 @@ hipError_t launch_cfg(ChunkArgs a, int workers, hipStream_t s, const LaunchEvent
     void* args[] = {&a};
     e = launch_kernel(kern, dim3(workers), dim3(C::kThreads), args, lds, s, ev);
     if (e != hipSuccess) return e;
-    const void* merge = reinterpret_cast<const void*>(&chunk_merge_kernel<C, TREE>);
-    return launch_kernel(merge, dim3(workers, (C::kRows + kMergeRows - 1) / kMergeRows), dim3(kBlockThreads), args, 0,
+    const void* merge = reinterpret_cast<const void*>(&chunk_merge_kernel<C>);
+    return launch_kernel(merge, dim3(workers, C::kRows / (kMergeRows * MERGEITER)), dim3(kBlockThreads), args, 0,
                          s, ev_merge);
 }
 
@@ -1050,10 +1176,17 @@ template <int D, bool BF16, bool TREE>
 hipError_t launch_shape(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s, const LaunchEvents& ev,
                         const LaunchEvents& ev_merge) {
     constexpr int kPages = BF16 ? 4 : 2;
-    if (p.rows == 64) return launch_cfg<Cfg<D, BF16, 4, 1, kPages, 2>, TREE>(a, p.workers, s, ev, ev_merge);
-#ifndef BIGCFG
-#define BIGCFG 8, 2, kPages, 3
+#ifndef SMALLCFG
+#define SMALLCFG 4, 1, kPages, 2, 2
 #endif
+#ifndef MIDCFG
+#define MIDCFG 8, 1, kPages, 4, 1
+#endif
+#ifndef BIGCFG
+#define BIGCFG 8, 2, kPages, 3, 1
+#endif
+    if (p.rows == 64) return launch_cfg<Cfg<D, BF16, SMALLCFG>, TREE>(a, p.workers, s, ev, ev_merge);
+    if (p.rows == 128) return launch_cfg<Cfg<D, BF16, MIDCFG>, TREE>(a, p.workers, s, ev, ev_merge);
     return launch_cfg<Cfg<D, BF16, BIGCFG>, TREE>(a, p.workers, s, ev, ev_merge);
 }
 
@@ -1062,12 +1195,14 @@ hipError_t launch_shape(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s, c
 // Rows of a tile: 64 where a row's queries fit into them, else 256.
 ChunkPlan chunk_plan(int cus, int group, int64_t rows_per_seq) {
     ChunkPlan p;
-  #ifndef BIGROWS
-#define BIGROWS 256
-#define BIGWG 1
+  #ifndef SMALLWG
+#define SMALLWG 2
 #endif
-    p.rows = rows_per_seq <= 64 ? 64 : BIGROWS;
-    p.workers = p.rows == 64 ? 2 * cus : BIGWG * cus;
+#ifndef MIDWG
+#define MIDWG 1
+#endif
+    p.rows = rows_per_seq <= 64 ? 64 : (rows_per_seq <= 128 ? 128 : 256);
+    p.workers = (p.rows == 64 ? SMALLWG : p.rows == 128 ? MIDWG : 1) * cus;
     return p;
 }
 

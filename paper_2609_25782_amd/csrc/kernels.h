@@ -277,8 +277,10 @@ struct AppendTableArgs {
 hipError_t launch_append_table(const AppendTableArgs& a, hipStream_t s);
 
 // Attention of several new tokens per row (prompt chunks, draft trees).
-struct ChunkRec {   // a part of a tile left in the workspace
-    int32_t b, g, tile, used;
+struct ChunkRec {      // of a worker that holds the first part of a tile cut between workers
+    int32_t parts;     // parts of the tile, 0: the worker holds no such part
+    int32_t rows;      // rows of the tile
+    int64_t first;     // (token, query head) of the tile's first row in q
 };
 struct ChunkArgs {
     const char* hot;           // slice of hot page 0 for the layer
@@ -308,9 +310,10 @@ struct ChunkArgs {
     void* workspace;
     // set by the launch
     int32_t tile_tokens, workers;
+    int32_t team;              // workers that take the KV heads of one range, a head each
     float* part_o;             // [2 workers][rows of a tile][D]
     float* part_ml;            // [2 workers][2][rows of a tile]
-    ChunkRec* recs;            // [2 workers]
+    ChunkRec* recs;            // [workers]
 };
 struct ChunkPlan {
     int32_t rows;      // rows of a tile
@@ -318,7 +321,7 @@ struct ChunkPlan {
 };
 ChunkPlan chunk_plan(int cus, int group, int64_t rows_per_seq);
 inline size_t chunk_workspace_bytes(const ChunkPlan& p, int head_dim) {
-    const size_t n = static_cast<size_t>(2) * p.workers * (static_cast<size_t>(p.rows) * (head_dim + 2) * 4 + sizeof(ChunkRec));
+    const size_t n = static_cast<size_t>(p.workers) * (static_cast<size_t>(2) * p.rows * (head_dim + 2) * 4 + sizeof(ChunkRec));
     return (n + 255) & ~static_cast<size_t>(255);
 }
 inline void chunk_workspace_layout(ChunkArgs& a, int rows, int head_dim) {

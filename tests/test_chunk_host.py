@@ -30,34 +30,32 @@ def test_metadata_only_pools_are_refused(meta):
 
 
 # -- the work split: tiles laid end to end, cut into equal ranges --------------
-# The same arithmetic as the kernel's (kTileCost, places of units), on plain integers.
-
-COST = 64
+# The same arithmetic as the kernel's (a tile's fixed cost, places of units), on plain integers.
 
 
-def row_units(ctx, n, tok, block, tree):
+def row_units(ctx, n, tok, block, tree, fixed):
     """Costs of a row's tiles of one KV head, and their numbers of blocks."""
     tiles = -(-n // tok)
     cost, blocks = [], []
     for i in range(tiles):
         if tree:
             nd = -(-n // block)
-            cost.append(COST + nd * block + ctx)
+            cost.append(fixed + nd * block + ctx)
             blocks.append(nd + -(-ctx // block))
         else:
             keys = ctx + min((i + 1) * tok, n)
-            cost.append(COST + keys)
+            cost.append(fixed + keys)
             blocks.append(-(-keys // block))
     return cost, blocks
 
 
-def place(tiles, u, block):
+def place(tiles, u, block, fixed):
     """Block that unit u begins with: (tile, block) over the flat list of (cost, blocks)."""
     for i, (cost, nb) in enumerate(tiles):
         if u < cost:
             if u == 0:
                 return i, 0
-            x = u - COST
+            x = u - fixed
             k = min(nb, 0 if x <= 0 else -(-x // block))
             return (i, k) if k < nb else (i + 1, 0)
         u -= cost
@@ -72,15 +70,16 @@ def test_every_block_belongs_to_one_worker(tree):
         group = rng.choice([1, 2, 3, 5, 8, 16])
         tok = rng.choice([64, 256]) // group
         heads = rng.choice([1, 2, 4])
+        fixed = rng.choice([64, 320])
         tiles = []
         for _ in range(rng.randint(1, 6)):
             ctx = rng.choice([0, 1, rng.randint(0, 100), rng.randint(0, 5000)])
             n = rng.choice([0, 1, rng.randint(1, 64)] if tree else [0, 1, rng.randint(1, 3000)])
-            tiles += list(zip(*row_units(ctx, n, tok, block, tree))) * heads
+            tiles += list(zip(*row_units(ctx, n, tok, block, tree, fixed))) * heads
         total = sum(c for c, _ in tiles)
         most = rng.choice([1, 7, 256, 512])
-        workers = max(1, min(most, total // (COST + 2 * block))) if total else 0
-        cuts = [place(tiles, k * total // workers, block) for k in range(workers)] + [(len(tiles), 0)]
+        workers = max(1, min(most, total // (fixed + 2 * block))) if total else 0
+        cuts = [place(tiles, k * total // workers, block, fixed) for k in range(workers)] + [(len(tiles), 0)]
         assert not workers or cuts[0] == (0, 0)
         done = []
         for k in range(workers):
