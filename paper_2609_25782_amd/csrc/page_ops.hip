@@ -488,32 +488,93 @@ __global__ __launch_bounds__(kAppendThreads) void append_table_kernel(const Appe
     }
 }
 
-// Accepted drafts into the pages: block (b * width + j, y) writes accepted draft j of row b
-// for layers y, y + gridDim.y, ..
-__global__ __launch_bounds__(kAppendThreads) void accept_drafts_kernel(const AcceptArgs a) {
-    const int elt = a.dtype == kDtypeBf16 ? 2 : 4;
-    const int x = 16 / elt;
-    const int groups = a.head_dim / x;
-    const int64_t tile = static_cast<int64_t>(kPageTokens) * a.head_dim * elt;
-    const int b = static_cast<int>(blockIdx.x) / a.width, j = static_cast<int>(blockIdx.x) % a.width;
-    if (j >= a.counts[b]) return;
-    const int32_t src = a.path[blockIdx.x], len = a.lens[b];
-    if (src < 0 || src >= a.width || len < 0) return;
-    const int64_t pos = static_cast<int64_t>(len) + j;
-    if (pos / kPageTokens >= a.pt_stride) return;
-    const int32_t pid = a.table[static_cast<int64_t>(b) * a.pt_stride + pos / kPageTokens];
-    const unsigned id = static_cast<unsigned>(pid) & static_cast<unsigned>(kPageIdMask);
-    const unsigned tag = static_cast<unsigned>(pid) >> 29;   // 0 hot, 2 cold; others name no page
-    if (!((tag == 0 && id < static_cast<unsigned>(a.num_hot)) || (tag == 2 && id < static_cast<unsigned>(a.num_cold))))
-        return;
-    const AppendThread w = append_thread(static_cast<int>(threadIdx.x), groups);
-    if (w.head >= a.num_kv_heads) return;
-    for (int li = static_cast<int>(blockIdx.y); li < a.num_layers; li += static_cast<int>(gridDim.y)) {
-        char* lh = entry_slice(a.hot, a.cold, pid, a.layer + li) + static_cast<int64_t>(w.head) * 2 * tile;
-        const int64_t from = ((((static_cast<int64_t>(li) * a.batch + b) * a.width + src) * a.num_kv_heads + w.head) *
-                                  a.head_dim + w.cd * x) * elt;
-        write_token_group(lh, tile, static_cast<int>(pos % kPageTokens), w.cd, x, elt,
-                          static_cast<const char*>(a.k) + from, static_cast<const char*>(a.v) + from, true);
+// W consecutive slots of one V row from the drafts path[0 .. W).
+template <typename T, int W>
+__device__ __forceinline__ void write_run(T* out, const T* v, const int32_t* path, int row) {
+    T e[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) e[i] = v[static_cast<int64_t>(path[i]) * row];
+    if constexpr (W == 1) {
+        *out = e[0];
+    } else {
+        typedef T vec __attribute__((ext_vector_type(W)));
+        vec w;
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = e[i];
+        *reinterpret_cast<vec*>(out) = w;
+    }
+}
+
+// Accepted drafts into the pages.  Block (b, y, z) writes kBlockThreads elements of a token
+// (dims of one head, then of the next) of row b's accepted drafts, for layers y, y +
+// gridDim.y, ..  K goes out in 16-byte groups.  V is dims-major in its tile, so a thread
+// takes one (head, dim) and writes its drafts of a page side by side: the drafts of a row lie
+// in consecutive slots, so a run of 8 is one 16-byte store, where a store per draft and dim
+// would be 2 bytes each (64 rows x 0-16 drafts x 48 layers, 51 MB: 139 us with those).
+// Bound by the bytes: each 32-byte row of a V tile is written in part.
+template <typename T>
+__global__ __launch_bounds__(kBlockThreads) void accept_drafts_kernel(const AcceptArgs a) {
+    constexpr int x = 16 / sizeof(T);
+    const int b = static_cast<int>(blockIdx.x), tid = static_cast<int>(threadIdx.x);
+    const int n = min(a.counts[b], a.width);
+    const int32_t len = a.lens[b];
+    if (n <= 0 || len < 0) return;
+    const int row = a.num_kv_heads * a.head_dim;    // elements of a token
+    const int first = static_cast<int>(blockIdx.z) * kBlockThreads;
+    const int64_t tile = static_cast<int64_t>(kPageTokens) * a.head_dim;
+    const int32_t* path = a.path + static_cast<int64_t>(b) * a.width;
+    // (head, dim) of this thread's V and of its K group
+    const int v_at = first + tid, k_at = first + tid % (kBlockThreads / x) * x;
+    const int v_head = v_at / a.head_dim, v_dim = v_at % a.head_dim;
+    const int k_head = k_at / a.head_dim, k_dim = k_at % a.head_dim;
+    for (int j0 = 0; j0 < n;) {     // the drafts of one page: j0 .. j1
+        const int64_t pos = static_cast<int64_t>(len) + j0;
+        const int slot = static_cast<int>(pos % kPageTokens);
+        const int j1 = min(n, j0 + kPageTokens - slot);
+        const int64_t page = pos / kPageTokens;
+        if (page >= a.pt_stride) return;
+        const int32_t pid = a.table[static_cast<int64_t>(b) * a.pt_stride + page];
+        const unsigned id = static_cast<unsigned>(pid) & static_cast<unsigned>(kPageIdMask);
+        const unsigned tag = static_cast<unsigned>(pid) >> 29;   // 0 hot, 2 cold; others name no page
+        const bool ok = (tag == 0 && id < static_cast<unsigned>(a.num_hot)) ||
+                        (tag == 2 && id < static_cast<unsigned>(a.num_cold));
+        for (int li = static_cast<int>(blockIdx.y); ok && li < a.num_layers; li += static_cast<int>(gridDim.y)) {
+            T* lh = reinterpret_cast<T*>(entry_slice(a.hot, a.cold, pid, a.layer + li));
+            const int64_t from = (static_cast<int64_t>(li) * a.batch + b) * a.width * row;
+            const T* k = static_cast<const T*>(a.k) + from;
+            const T* v = static_cast<const T*>(a.v) + from;
+            for (int j = j0 + tid / (kBlockThreads / x); j < j1; j += x) {
+                const int src = path[j];
+                if (src < 0 || src >= a.width || k_at >= row) continue;
+                *reinterpret_cast<u32x4*>(lh + k_head * 2 * tile + (static_cast<int64_t>(k_dim) * kPageTokens +
+                                          (slot + j - j0) * x)) =
+                    *reinterpret_cast<const u32x4*>(k + static_cast<int64_t>(src) * row + k_at);
+            }
+            if (v_at >= row) continue;
+            T* out = lh + (2 * v_head + 1) * tile + v_dim * kPageTokens + slot - j0;   // slot of draft 0
+            int j = j0;
+            while (j < j1) {
+                // the widest store that this slot's alignment and the run's end allow
+                const int at = slot + j - j0;
+                int w = (at & -at) ? (at & -at) : x;
+                w = w < x ? w : x;
+                while (w > j1 - j) w >>= 1;
+                bool all = true;     // (the same for every thread)
+                for (int i = 0; i < w; ++i) all &= path[j + i] >= 0 && path[j + i] < a.width;
+                if (!all) w = 1;
+                if (w == x) {
+                    write_run<T, x>(out + j, v + v_at, path + j, row);
+                } else if (x > 4 && w == 4) {
+                    write_run<T, 4>(out + j, v + v_at, path + j, row);
+                } else if (w == 2) {
+                    write_run<T, 2>(out + j, v + v_at, path + j, row);
+                } else if (path[j] >= 0 && path[j] < a.width) {
+                    write_run<T, 1>(out + j, v + v_at, path + j, row);
+                }
+                j += w;
+            }
+        }
+        j0 = j1;
     }
 }
 
@@ -713,10 +774,12 @@ hipError_t launch_append_table(const AppendTableArgs& a, hipStream_t s) {
 hipError_t launch_accept_drafts(const AcceptArgs& a, hipStream_t s) {
     if (a.batch <= 0 || a.width <= 0 || a.num_layers <= 0) return hipSuccess;
     const unsigned layers = a.num_layers < 65535 ? static_cast<unsigned>(a.num_layers) : 65535u;
-    const unsigned threads = append_threads(a.num_kv_heads, a.head_dim, a.dtype);
-    if (threads > kAppendThreads) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(accept_drafts_kernel, dim3(static_cast<unsigned>(a.batch * a.width), layers), dim3(threads), 0,
-                       s, a);
+    const unsigned parts = static_cast<unsigned>((a.num_kv_heads * a.head_dim + kBlockThreads - 1) / kBlockThreads);
+    const dim3 grid(static_cast<unsigned>(a.batch), layers, parts);
+    if (a.dtype == kDtypeBf16)
+        hipLaunchKernelGGL(accept_drafts_kernel<uint16_t>, grid, dim3(kBlockThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL(accept_drafts_kernel<uint32_t>, grid, dim3(kBlockThreads), 0, s, a);
     return hipGetLastError();
 }
 
