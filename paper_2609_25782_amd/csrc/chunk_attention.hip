@@ -100,39 +100,45 @@ struct Row {
 #endif
 constexpr int kTileCost = TILECOST, kTileCostFine = 64;
 
+// The units of a row that brings n queries after ctx tokens.
+template <class C, bool TREE>
+__device__ __forceinline__ Row make_row(const ChunkArgs& a, int start, int n, int ctx, int bad) {
+    Row r;
+    r.start = start;
+    r.n = n;
+    r.ctx = ctx;
+    r.bad = bad;
+    r.tiles = (n + a.tile_tokens - 1) / a.tile_tokens;
+    r.slope = 0;
+    if (bad) {
+        r.base = r.last = 0;
+    } else if constexpr (TREE) {
+        r.base = r.last = static_cast<int64_t>((n + C::kBlock - 1) / C::kBlock) * C::kBlock + ctx;
+    } else {
+        r.base = ctx;
+        r.slope = a.tile_tokens;
+        r.last = r.base + n;
+    }
+    return r;
+}
+
 template <class C, bool TREE>
 __device__ __forceinline__ Row row_info(const ChunkArgs& a, int b) {
-    Row r;
     const int64_t most = static_cast<int64_t>(kPageTokens) * a.pt_stride;
     const int32_t len = uniform_ptr(a.lens)[b];
+    int start, n;
     if constexpr (TREE) {
-        int n = a.draft_lens ? uniform_ptr(a.draft_lens)[b] : a.width;
+        n = a.draft_lens ? uniform_ptr(a.draft_lens)[b] : a.width;
         n = n < 0 ? 0 : (n > a.width ? a.width : n);
-        r.n = n;
-        r.start = b * a.width;
-        r.bad = len < 0 || len > most;
-        r.ctx = r.bad ? 0 : len;
+        start = b * a.width;
     } else {
         const int s = uniform_ptr(a.starts)[b], e = uniform_ptr(a.starts)[b + 1];
         const bool in = s >= 0 && e >= s && e <= a.total_q;
-        r.start = in ? s : 0;
-        r.n = in ? e - s : 0;
-        r.bad = len < r.n || len > most;
-        r.ctx = r.bad ? 0 : len - r.n;
+        start = in ? s : 0;
+        n = in ? e - s : 0;
     }
-    r.tiles = (r.n + a.tile_tokens - 1) / a.tile_tokens;
-    if (r.bad) {
-        r.base = r.last = 0;
-        r.slope = 0;
-    } else if constexpr (TREE) {
-        r.base = r.last = static_cast<int64_t>((r.n + C::kBlock - 1) / C::kBlock) * C::kBlock + r.ctx;
-        r.slope = 0;
-    } else {
-        r.base = r.ctx;
-        r.slope = a.tile_tokens;
-        r.last = r.base + r.n;
-    }
-    return r;
+    const int bad = len < (TREE ? 0 : n) || len > most;
+    return make_row<C, TREE>(a, start, n, bad ? 0 : (TREE ? len : len - n), bad);
 }
 
 // Blocks of tile i: the drafts' first (trees), then the context's.
@@ -161,6 +167,7 @@ struct Place {
 // `parts` is the number of workers that share that tile from this one on.
 struct Range {
     Place from, to;
+    Row row;     // of from.b
     int parts;
 };
 
@@ -293,9 +300,11 @@ __device__ bool worker_range(const ChunkArgs& a, int k, Range& out) {
             if (u < cuts.total) {
                 const uint64_t has = __builtin_amdgcn_ballot_w64(units > 0 && first <= u);
                 const int b = kWave - 1 - __builtin_clzll(has);
+                const Row at = make_row<C, TREE>(a, __builtin_amdgcn_readlane(r.start, b), __builtin_amdgcn_readlane(r.n, b),
+                                                 __builtin_amdgcn_readlane(r.ctx, b), __builtin_amdgcn_readlane(r.bad, b));
                 int64_t more;
-                p = uniform_place(place_of<C, TREE>(a, row_info<C, TREE>(a, b), b, u - lane_value64(first, b),
-                                                    cuts.cost, more));
+                p = uniform_place(place_of<C, TREE>(a, at, b, u - lane_value64(first, b), cuts.cost, more));
+                if (j == 0) out.row = at;
                 if (j == 1 && p.blk > 0) out.parts = worker_at(cuts, u + more) - k + 1;
             }
             (j == 0 ? out.from : out.to) = p;
@@ -359,7 +368,9 @@ __device__ bool worker_range(const ChunkArgs& a, int k, Range& out) {
     out.from = uniform_place(s_place[0]);
     out.to = uniform_place(s_place[1]);
     out.parts = __builtin_amdgcn_readfirstlane(s_parts);
-    return __builtin_amdgcn_readfirstlane(k < cuts.workers);
+    if (k >= cuts.workers) return false;
+    out.row = row_info<C, TREE>(a, min(out.from.b, a.batch - 1));
+    return true;
 }
 
 // Page-table entry `pid`: a hot page, a cold page (num_cold is 0 where the pool reads no
@@ -553,20 +564,26 @@ __device__ __forceinline__ int lane_page(int t) {
     return C::kBf16 ? 2 * (t >> 1) + (g >> 1) : t;
 }
 
-// Bit 4 t + r: the row attends to that key.
+// The lowest `n` of kX bits (n below 0: none, above kX: all).
+template <class C>
+__device__ __forceinline__ unsigned low_bits(int n) {
+    n = n < 0 ? 0 : (n > C::kX ? C::kX : n);
+    return (1u << n) - 1u;
+}
+
+// Bit 4 t + r: the row attends to that key.  A lane's keys of a contraction step are kX
+// consecutive ones, so a step's bits are one run of a limit or of a draft's mask.
 template <class C, bool TREE>
 __device__ __forceinline__ unsigned seen_keys(const Mask& mk, int lim, uint64_t seen) {
     unsigned bits = 0;
 #pragma unroll
-    for (int t = 0; t < C::kPages; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int key = mk.key0 + lane_key<C>(t, r);
-            bool see = key < lim;
-            if constexpr (TREE)
-                if (mk.draft) see = key < mk.len && ((seen >> (key & 63)) & 1u);
-            bits |= see ? 1u << (4 * t + r) : 0u;
-        }
+    for (int p = 0; p < C::kPages * 4 / C::kX; ++p) {
+        const int key = mk.key0 + lane_key<C>(p * C::kX / 4, 0);
+        unsigned run = low_bits<C>((TREE && mk.draft ? mk.len : lim) - key);
+        if constexpr (TREE)
+            if (mk.draft) run &= static_cast<unsigned>(seen >> (key & 63));
+        bits |= run << (C::kX * p);
+    }
     return bits;
 }
 
@@ -574,16 +591,15 @@ __device__ __forceinline__ unsigned seen_keys(const Mask& mk, int lim, uint64_t 
 // past its length and missing pages may hold NaN).
 template <class C>
 __device__ __forceinline__ u32x4 kept_values(const Mask& mk, int p) {
+    unsigned run = low_bits<C>(mk.len - (mk.key0 + lane_key<C>(p * C::kX / 4, 0)));
+    if (!((mk.ok >> lane_page<C>(p * C::kX / 4)) & 1u)) run = 0;
     u32x4 keep;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        if constexpr (C::kBf16) {
-            const int key = mk.key0 + lane_key<C>(2 * p + (j >> 1), 2 * (j & 1));
-            const bool ok = (mk.ok >> lane_page<C>(2 * p)) & 1u;
-            keep[j] = (ok && key < mk.len ? 0xFFFFu : 0u) | (ok && key + 1 < mk.len ? 0xFFFF0000u : 0u);
-        } else {
-            keep[j] = ((mk.ok >> p) & 1u) && mk.key0 + lane_key<C>(p, j) < mk.len ? 0xFFFFFFFFu : 0u;
-        }
+        if constexpr (C::kBf16)
+            keep[j] = ((run >> (2 * j)) & 1u) * 0xFFFFu | ((run >> (2 * j + 1)) & 1u) * 0xFFFF0000u;
+        else
+            keep[j] = 0u - ((run >> j) & 1u);
     }
     return keep;
 }
@@ -733,17 +749,20 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
         else load_v(group + 2 - kKF / kG);
         order_fence();
     }
-    unsigned sees[C::kNT];
     if constexpr (MASKED) {
 #pragma unroll
         for (int n = 0; n < C::kNT; ++n) {
-            sees[n] = seen_keys<C, TREE>(mk, lim[n], seen[n]);
+            const unsigned sees = seen_keys<C, TREE>(mk, lim[n], seen[n]);
 #pragma unroll
-            for (int t = 0; t < C::kPages; ++t) {
-                const bool ok = (mk.ok >> lane_page<C>(t)) & 1u;
+            for (int t = 0; t < C::kPages; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    s[t][n][r] = (sees[n] >> (4 * t + r)) & 1u ? (ok ? s[t][n][r] : NAN) : -INFINITY;
+                for (int r = 0; r < 4; ++r) s[t][n][r] = (sees >> (4 * t + r)) & 1u ? s[t][n][r] : -INFINITY;
+            if (!TREE && mk.ok != (1u << C::kPages) - 1) {   // tokens of a missing page: NaN to rows that see them
+#pragma unroll
+                for (int t = 0; t < C::kPages; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!((mk.ok >> lane_page<C>(t)) & 1u) && ((sees >> (4 * t + r)) & 1u)) s[t][n][r] = NAN;
             }
         }
     }
@@ -784,8 +803,7 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
         for (int t = 0; t < C::kPages; ++t) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][r], scale, -ms));
-                if constexpr (MASKED) w = (sees[n] >> (4 * t + r)) & 1u ? w : 0.f;
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][r], scale, -ms));   // left out: 0
                 s[t][n][r] = w;
                 st.l[n] += w;
             }
@@ -861,6 +879,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
     const bool work = worker_range<C, TREE>(a, k / a.team, range);
     Place at = range.from;
     const Place end = range.to;
+    Row row = range.row;     // of at.b
     bool recorded = false;   // this worker holds the first part of a cut tile
     const Loader<C> ld;
     const unsigned head_bytes = 2 * C::kTile;
@@ -868,7 +887,6 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
     if (work) {
         while (before(at, end)) {
             if (at.b >= a.batch) break;
-            const Row row = row_info<C, TREE>(a, at.b);
             if (at.hg >= heads || row.tiles == 0) {   // on to the next row with queries
                 int b = at.b + 1;
                 while (b < a.batch) {
@@ -881,6 +899,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                     b += kWave;
                 }
                 at = Place{b, 0, 0, 0};
+                if (b < a.batch) row = row_info<C, TREE>(a, b);
                 continue;
             }
             const int nb = tile_blocks<C, TREE>(a, row, at.tile);
@@ -926,7 +945,6 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 for (int i = 0; i < C::kQ; ++i) {
                     u32x4 v = {0u, 0u, 0u, 0u};
                     if (live[n]) v = *reinterpret_cast<const u32x4*>(qp + i * 64);
-                    if (a.negate) v ^= C::kBf16 ? 0x80008000u : 0x80000000u;
                     st.q[n][i] = v;
                 }
                 st.m[n] = -INFINITY;
@@ -994,6 +1012,12 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 }
 #pragma unroll
             for (int m = 0; m < kMine; ++m) id[m] = page_id(k0 + C::kStages - 1, ld.page() + m);
+            if (a.negate) {
+#pragma unroll
+                for (int n = 0; n < C::kNT; ++n)
+#pragma unroll
+                    for (int i = 0; i < C::kQ; ++i) st.q[n][i] ^= C::kBf16 ? 0x80008000u : 0x80000000u;
+            }
             int j = k0;
             char* stage = s_kv;
             const auto mask_of = [&](int j) {

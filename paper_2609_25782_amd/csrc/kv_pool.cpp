@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -1619,7 +1620,9 @@ int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_
     a.pt_stride = pt_stride;
     a.lens = seq_lens;
     a.batch = batch;
-    a.scale_log2 = (scale < 0.f ? -scale : scale) * 1.4426950408889634f;
+    // (a scale of 0 stands as the smallest normal number: every weight is 1, and the minus
+    // infinity of a token left out stays one)
+    a.scale_log2 = std::max((scale < 0.f ? -scale : scale) * 1.4426950408889634f, FLT_MIN);
     // 2^8 in the weights; finite, so that a row's first score always raises its maximum
     a.slack = a.scale_log2 > 1e-30f ? 8.f / a.scale_log2 : 8e30f;
     a.negate = scale < 0.f ? 1 : 0;
