@@ -35,6 +35,7 @@
 
 #include <math.h>
 
+#include <atomic>
 #include <type_traits>
 
 namespace hck {
@@ -1211,8 +1212,17 @@ hipError_t launch_cfg(ChunkArgs a, int workers, hipStream_t s, const LaunchEvent
     chunk_workspace_layout(a, C::kRows, C::kD);
     const size_t lds = static_cast<size_t>(C::kStages) * C::kStage;
     const void* kern = reinterpret_cast<const void*>(&chunk_attend_kernel<C, TREE>);
-    hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+    // more LDS than a launch gets unasked, asked for once per kernel and device
+    static std::atomic<uint64_t> asked{0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
+    const uint64_t bit = uint64_t(1) << (dev & 63);
+    if (dev > 63 || !(asked.load(std::memory_order_relaxed) & bit)) {
+        e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+        if (e != hipSuccess) return e;
+        asked.fetch_or(bit, std::memory_order_relaxed);
+    }
     void* args[] = {&a};
     e = launch_kernel(kern, dim3(workers), dim3(C::kThreads), args, lds, s, ev);
     if (e != hipSuccess) return e;

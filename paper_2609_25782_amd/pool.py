@@ -224,27 +224,44 @@ class HotColdPool:
         return out
 
     # -- several new tokens per session --------------------------------------
-    def _on(self, stream):
-        """(raw stream, torch context) of a call: `stream`, or the pool device's current one."""
-        st = stream if stream is not None else torch.cuda.current_stream(self.device)
-        return int(st.cuda_stream), torch.cuda.stream(st)
+    def _raw(self, stream) -> int:
+        """Raw handle of `stream`, or of the pool device's current stream."""
+        if stream is not None:
+            return int(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
-    def _chunk_workspace(self, need: int, key: int) -> torch.Tensor:
-        """Workspace of a prompt or tree call, on the stream made current.  A captured call gets
-        memory of its graph's own pool, so graphs never share it; others keep one per stream."""
+    def _memory(self, need, like: Optional[torch.Tensor], stream):
+        """An output like `like` and, where `need` is not 0, bytes of workspace, both of the call's
+        stream: torch hands out memory that another stream may still be using otherwise."""
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+            return (None if like is None else torch.empty_like(like),
+                    torch.empty(need, dtype=torch.uint8, device=self.device) if need else None)
+
+    def _chunk_buffers(self, need: int, q: torch.Tensor, out: Optional[torch.Tensor], st: int, stream):
+        """(out, workspace) of a prompt or tree call.  A captured call's workspace is memory of its
+        graph's own pool, so that no two graphs share one; other calls keep one per stream."""
+        if out is not None:
+            assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype and out.device == q.device
         if torch.cuda.is_current_stream_capturing():
-            return torch.empty(need, dtype=torch.uint8, device=self.device)
-        ws = self._ws.get(("chunk", key))
-        if ws is None or ws.numel() < need:
-            ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-            self._ws[("chunk", key)] = ws
-        return ws
+            new, ws = self._memory(need, q if out is None else None, stream)
+            return (new if out is None else out), ws
+        ws = self._ws.get(("chunk", st))
+        if out is None or ws is None or ws.numel() < need:
+            new, more = self._memory(0 if ws is not None and ws.numel() >= need else need,
+                                     q if out is None else None, stream)
+            if out is None:
+                out = new
+            if more is not None:
+                ws = self._ws[("chunk", st)] = more
+        return out, ws
 
     def _table(self, page_table, batch: int) -> torch.Tensor:
-        pt = self.page_table if page_table is None else page_table
-        assert pt.dtype == torch.int32 and pt.is_contiguous() and pt.dim() == 2 and pt.device == self.device
-        assert pt.shape[0] >= batch, "the page table has fewer rows than the batch"
-        return pt
+        if page_table is None:
+            page_table = self.page_table
+        assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.dim() == 2
+        assert page_table.device == self.device
+        assert page_table.shape[0] >= batch, "the page table has fewer rows than the batch"
+        return page_table
 
     def _ints(self, t: torch.Tensor, *shape) -> int:
         assert t.dtype == torch.int32 and t.is_contiguous() and t.device == self.device
@@ -256,22 +273,17 @@ class HotColdPool:
                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Causal attention of packed prompt chunks: queries q_starts[b] .. q_starts[b + 1] of q
         ([total][Hq][head_dim]) are the last tokens of row b's seq_lens[b], whose K and V are in
-        its pages.  Queries of no row keep what `out` holds (a new one holds zeros there only if
-        the caller asks for it by passing it)."""
+        its pages.  Queries of no row keep what `out` holds (without `out`: anything)."""
         assert q.is_contiguous() and q.dtype == self.torch_dtype and q.dim() == 3 and q.device == self.device
-        assert q.shape[2] == self.head_dim
         B, (total, Hq, D) = seq_lens.shape[0], q.shape
+        assert D == self.head_dim
         pt = self._table(page_table, B)
         lens, starts = self._ints(seq_lens, B), self._ints(q_starts, B + 1)
-        st, ctx = self._on(stream)
-        with ctx:
-            if out is None:
-                out = torch.empty_like(q)
-            assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype and out.device == q.device
-            ws = self._chunk_workspace(kv.paged_prefill_workspace_bytes(self.handle, B, total, Hq), st)
-            kv.paged_prefill_attention(self.handle, layer, q.data_ptr(), starts, total, pt.data_ptr(), pt.shape[1],
-                                       lens, B, Hq, float(scale if scale is not None else D ** -0.5), out.data_ptr(),
-                                       ws.data_ptr(), ws.numel(), st)
+        st = self._raw(stream)
+        out, ws = self._chunk_buffers(kv.paged_prefill_workspace_bytes(self.handle, B, total, Hq), q, out, st, stream)
+        kv.paged_prefill_attention(self.handle, layer, q.data_ptr(), starts, total, pt.data_ptr(), pt.shape[1],
+                                   lens, B, Hq, float(scale if scale is not None else D ** -0.5), out.data_ptr(),
+                                   ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0, st)
         return out
 
     def tree_decode(self, layer: int, q: torch.Tensor, k_draft: torch.Tensor, v_draft: torch.Tensor,
@@ -281,7 +293,7 @@ class HotColdPool:
         """Attention of drafted tokens: q [B][width][Hq][head_dim], k_draft and v_draft
         [B][width][kv_heads][head_dim]; draft i of row b sees the row's seq_lens[b] cached tokens
         and the drafts whose bits are set in masks[b][i] (int64 or uint64).  Drafts at or past
-        draft_lens[b] keep what `out` holds."""
+        draft_lens[b] keep what `out` holds (without `out`: anything)."""
         assert q.is_contiguous() and q.dtype == self.torch_dtype and q.dim() == 4 and q.device == self.device
         B, T, Hq, D = q.shape
         assert D == self.head_dim
@@ -293,16 +305,12 @@ class HotColdPool:
         pt = self._table(page_table, B)
         lens = self._ints(seq_lens, B)
         drafts = 0 if draft_lens is None else self._ints(draft_lens, B)
-        st, ctx = self._on(stream)
-        with ctx:
-            if out is None:
-                out = torch.empty_like(q)
-            assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype and out.device == q.device
-            ws = self._chunk_workspace(kv.paged_tree_workspace_bytes(self.handle, B, T, Hq), st)
-            kv.paged_tree_attention(self.handle, layer, q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(),
-                                    masks.data_ptr(), drafts, T, pt.data_ptr(), pt.shape[1], lens, B, Hq,
-                                    float(scale if scale is not None else D ** -0.5), out.data_ptr(), ws.data_ptr(),
-                                    ws.numel(), st)
+        st = self._raw(stream)
+        out, ws = self._chunk_buffers(kv.paged_tree_workspace_bytes(self.handle, B, T, Hq), q, out, st, stream)
+        kv.paged_tree_attention(self.handle, layer, q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(),
+                                masks.data_ptr(), drafts, T, pt.data_ptr(), pt.shape[1], lens, B, Hq,
+                                float(scale if scale is not None else D ** -0.5), out.data_ptr(),
+                                ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0, st)
         return out
 
     def accept_drafts(self, layer_begin: int, table: torch.Tensor, seq_lens: torch.Tensor, path: torch.Tensor,
@@ -311,12 +319,12 @@ class HotColdPool:
         ([num_layers][B][width][kv_heads][head_dim]).  Capturable in a HIP graph."""
         assert k.is_contiguous() and v.is_contiguous() and k.shape == v.shape and k.dim() == 5
         assert k.dtype == v.dtype == self.torch_dtype and k.device == v.device == self.device
-        L, B, T = k.shape[:3]
-        assert k.shape[3:] == (self.num_kv_heads, self.head_dim)
+        L, B, T, heads, D = k.shape
+        assert heads == self.num_kv_heads and D == self.head_dim
         pt = self._table(table, B)
-        st, _ = self._on(stream)
         kv.kv_accept_drafts(self.handle, layer_begin, L, pt.data_ptr(), pt.shape[1], self._ints(seq_lens, B),
-                            self._ints(path, B, T), self._ints(counts, B), B, T, k.data_ptr(), v.data_ptr(), st)
+                            self._ints(path, B, T), self._ints(counts, B), B, T, k.data_ptr(), v.data_ptr(),
+                            self._raw(stream))
 
     def gather_table(self, sids: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Page-table rows of the given sessions (device int32 ids), for decoding them as a batch."""
