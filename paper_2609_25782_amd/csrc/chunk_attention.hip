@@ -1130,54 +1130,26 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
 // Joins the partial results of the tiles cut between workers: with M the largest of the
 // parts' maxima, out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Block (k, y) takes
 // rows of the tile whose first part worker k left in slot 2 k + 1; its other parts are
-// slots 2 (k + team), 2 (k + 2 team), ..  A wave per row, a float4 per lane, kAtOnce parts
-// at a time, joined as they come; the record holds all that the row's place needs, so that
-// only two loads follow each other.
-constexpr int kMergeRows = 4;
-
-template <class C, int BATCH, class Join>
-__device__ __forceinline__ void join_parts(const ChunkArgs& a, int k, int r, int sub, int col, int parts, Join join) {
-    constexpr int kAtOnce = kWave / (C::kD / 4);
-    for (int p0 = sub; p0 < parts; p0 += BATCH * kAtOnce) {
-        float m[BATCH], l[BATCH];
-        f32x4 o[BATCH];
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int p = min(p0 + i * kAtOnce, parts - 1);
-            const int64_t slot = p == 0 ? 2 * k + 1 : 2 * (k + p * a.team);
-            m[i] = a.part_ml[slot * 2 * C::kRows + r];
-            l[i] = a.part_ml[slot * 2 * C::kRows + C::kRows + r];
-            o[i] = *reinterpret_cast<const f32x4*>(a.part_o + (slot * C::kRows + r) * C::kD + col * 4);
-        }
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i)
-            if (p0 + i * kAtOnce < parts) join(m[i], l[i], o[i]);
-    }
-}
-
+// slots 2 (k + team), 2 (k + 2 team), ..  A wave takes kIter rows, a float4 per lane and
+// kAtOnce parts at a time.  Most tiles are cut once or twice: then the loads of all of the
+// wave's rows are in flight together.  The record holds all that a row's place needs, so
+// that only two loads follow each other.
 template <class C>
-__global__ __launch_bounds__(kBlockThreads) void chunk_merge_kernel(const ChunkArgs a) {
-    const int k = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const ChunkRec rec = a.recs[k];
-    const int parts = __builtin_amdgcn_readfirstlane(rec.parts), rows = __builtin_amdgcn_readfirstlane(rec.rows);
-    if (parts == 0) return;
-    constexpr int kLanes = C::kD / 4, kAtOnce = kWave / kLanes;
-    const int sub = lane / kLanes, col = lane % kLanes;
-    for (int r = blockIdx.y * kMergeRows + wave; r < rows; r += gridDim.y * kMergeRows) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        float top = -INFINITY, den = 0.f;
-        const auto join = [&](float m, float l, const f32x4& o) {
-            const float t = fmaxf(top, m);
-            // (1 for a part without a maximum, which holds 0 or NaN; never 0 times infinity)
-            const float w0 = top == -INFINITY ? 1.f : fmaxf(__builtin_amdgcn_exp2f(top - t), 1e-37f);
-            const float w1 = m == -INFINITY ? 1.f : fmaxf(__builtin_amdgcn_exp2f(m - t), 1e-37f);
-            acc = acc * w0 + o * w1;
-            den = den * w0 + l * w1;
-            top = t;
-        };
-        // parts whose loads are in flight together: most tiles are cut once or twice
-        if (parts <= 2 * kAtOnce) join_parts<C, 2>(a, k, r, sub, col, parts, join);
-        else join_parts<C, 8>(a, k, r, sub, col, parts, join);
+struct Merge {
+    static constexpr int kLanes = C::kD / 4, kAtOnce = kWave / kLanes;
+    static constexpr int kIter = C::kRows / 64;     // rows of a wave
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, den = 0.f;
+    __device__ __forceinline__ void join(float m, float l, const f32x4& o) {
+        const float t = fmaxf(top, m);
+        // (1 for a part without a maximum, which holds 0 or NaN; never 0 times infinity)
+        const float w0 = top == -INFINITY ? 1.f : fmaxf(__builtin_amdgcn_exp2f(top - t), 1e-37f);
+        const float w1 = m == -INFINITY ? 1.f : fmaxf(__builtin_amdgcn_exp2f(m - t), 1e-37f);
+        acc = acc * w0 + o * w1;
+        den = den * w0 + l * w1;
+        top = t;
+    }
+    __device__ __forceinline__ void finish(const ChunkArgs& a, const ChunkRec& rec, int r, int sub, int col) {
 #pragma unroll
         for (int d = kLanes; d < kWave; d <<= 1) {
             const float m = __shfl_xor(top, d), l = __shfl_xor(den, d);
@@ -1186,17 +1158,66 @@ __global__ __launch_bounds__(kBlockThreads) void chunk_merge_kernel(const ChunkA
             for (int j = 0; j < 4; ++j) o[j] = __shfl_xor(acc[j], d);
             join(m, l, o);
         }
-        if (sub == 0) {
+        if (sub == 0 && r < rec.rows) {
             const int64_t q = rec.first + static_cast<int64_t>(r / a.group) * a.num_q_heads + r % a.group;
             const float inv = den == 0.f ? 0.f : 1.f / den;
             store4(a, C::kBf16, static_cast<char*>(a.out) + (q * C::kD + col * 4) * C::kElt, acc * inv);
         }
     }
+};
+
+template <class C>
+__global__ __launch_bounds__(kBlockThreads) void chunk_merge_kernel(const ChunkArgs a) {
+    using M = Merge<C>;
+    const int k = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    ChunkRec rec = a.recs[k];
+    rec.parts = __builtin_amdgcn_readfirstlane(rec.parts);
+    rec.rows = __builtin_amdgcn_readfirstlane(rec.rows);
+    const int r0 = blockIdx.y * kBlockWaves + wave, step = gridDim.y * kBlockWaves;
+    if (rec.parts == 0 || r0 >= rec.rows) return;
+    const int sub = lane / M::kLanes, col = lane % M::kLanes;
+    const auto part_of = [&](int p, int r, float& m, float& l, f32x4& o) {
+        const int64_t slot = p == 0 ? 2 * k + 1 : 2 * (k + p * a.team);
+        m = a.part_ml[slot * 2 * C::kRows + r];
+        l = a.part_ml[slot * 2 * C::kRows + C::kRows + r];
+        o = *reinterpret_cast<const f32x4*>(a.part_o + (slot * C::kRows + r) * C::kD + col * 4);
+    };
+    constexpr int kFew = 2;     // rounds of kAtOnce parts
+    if (rec.parts <= kFew * M::kAtOnce) {
+        float m[M::kIter][kFew], l[M::kIter][kFew];
+        f32x4 o[M::kIter][kFew];
+#pragma unroll
+        for (int i = 0; i < M::kIter; ++i)
+#pragma unroll
+            for (int f = 0; f < kFew; ++f)   // (a row or part past the last: the last)
+                part_of(min(sub + f * M::kAtOnce, rec.parts - 1), min(r0 + i * step, rec.rows - 1), m[i][f], l[i][f],
+                        o[i][f]);
+#pragma unroll
+        for (int i = 0; i < M::kIter; ++i) {
+            M row;
+#pragma unroll
+            for (int f = 0; f < kFew; ++f)
+                if (sub + f * M::kAtOnce < rec.parts) row.join(m[i][f], l[i][f], o[i][f]);
+            row.finish(a, rec, r0 + i * step, sub, col);
+        }
+        return;
+    }
+    for (int r = r0; r < rec.rows; r += step) {
+        M row;
+        constexpr int kMany = 8;
+        for (int p0 = sub; p0 < rec.parts; p0 += kMany * M::kAtOnce) {
+            float m[kMany], l[kMany];
+            f32x4 o[kMany];
+#pragma unroll
+            for (int f = 0; f < kMany; ++f) part_of(min(p0 + f * M::kAtOnce, rec.parts - 1), r, m[f], l[f], o[f]);
+#pragma unroll
+            for (int f = 0; f < kMany; ++f)
+                if (p0 + f * M::kAtOnce < rec.parts) row.join(m[f], l[f], o[f]);
+        }
+        row.finish(a, rec, r, sub, col);
+    }
 }
 
-#ifndef MERGEITER
-#define MERGEITER 1
-#endif
 #ifndef TEAM
 #define TEAM(TREE, C) (C::kRows < 256)
 #endif
@@ -1227,7 +1248,7 @@ hipError_t launch_cfg(ChunkArgs a, int workers, hipStream_t s, const LaunchEvent
     e = launch_kernel(kern, dim3(workers), dim3(C::kThreads), args, lds, s, ev);
     if (e != hipSuccess) return e;
     const void* merge = reinterpret_cast<const void*>(&chunk_merge_kernel<C>);
-    return launch_kernel(merge, dim3(workers, C::kRows / (kMergeRows * MERGEITER)), dim3(kBlockThreads), args, 0,
+    return launch_kernel(merge, dim3(workers, C::kRows / (kBlockWaves * Merge<C>::kIter)), dim3(kBlockThreads), args, 0,
                          s, ev_merge);
 }
 
