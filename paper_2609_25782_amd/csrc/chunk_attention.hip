@@ -517,6 +517,7 @@ struct Mask {
     int len;                  // keys at or past it hold nothing of the row
     unsigned ok;              // bit i: page i of the block exists
     bool draft;
+    bool some;                // some row of the wave does not see the block whole
 };
 
 __device__ __forceinline__ unsigned nonfinite_code(unsigned h) {
@@ -750,7 +751,7 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
         else load_v(group + 2 - kKF / kG);
         order_fence();
     }
-    if constexpr (MASKED) {
+    if (MASKED && mk.some) {
 #pragma unroll
         for (int n = 0; n < C::kNT; ++n) {
             const unsigned sees = seen_keys<C, TREE>(mk, lim[n], seen[n]);
@@ -822,9 +823,14 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
     }
     // output
     u32x4 keep[MASKED ? kSteps : 1];
-    if constexpr (MASKED)
+    if constexpr (MASKED) {
 #pragma unroll
-        for (int p = 0; p < kSteps; ++p) keep[p] = kept_values<C>(mk, p);
+        for (int p = 0; p < kSteps; ++p) keep[p] = ~u32x4{0u, 0u, 0u, 0u};
+        // (past the last draft there are zeros)
+        if (!mk.draft && (mk.key0 + C::kBlock > mk.len || mk.ok != (1u << C::kPages) - 1))
+#pragma unroll
+            for (int p = 0; p < kSteps; ++p) keep[p] = kept_values<C>(mk, p);
+    }
 #pragma unroll
     for (int group = 0; group < kVF / kG; ++group) {
 #pragma unroll
@@ -959,12 +965,14 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
             // blocks that some row of the tile does not see whole; those and a tail that is not full;
             // blocks that no row of this wave sees
             int partly, masked, unseen = 0;
+            int sure = keys;   // what the wave's first row sees
             if constexpr (TREE) {
                 partly = nd;
                 masked = nd + (row.ctx % C::kBlock != 0);
             } else {
                 partly = masked = nb - (row.ctx + tok0 + 1) / C::kBlock;
                 unseen = nb - ((row.ctx + tok0 + wtok1) / C::kBlock + 1);
+                sure = row.ctx + tok0 + w0 / a.group + 1;
             }
             if (!wave_live) unseen = nb;
             const auto first_page = [&](int j) { return (nc - 1 - (j - nd)) * C::kPages; };
@@ -1022,14 +1030,15 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
             int j = k0;
             char* stage = s_kv;
             const auto mask_of = [&](int j) {
-                if (TREE && j < nd) return Mask{j * C::kBlock, row.n, ~0u, true};
+                if (TREE && j < nd) return Mask{j * C::kBlock, row.n, ~0u, true, true};
                 unsigned ok = 0;
 #pragma unroll
                 for (int i = 0; i < C::kPages; ++i) {
                     const int e = page_id(j, i);
                     ok |= (TREE || is_hot(a, e) || is_cold(a, e)) ? 1u << i : 0u;   // (trees: s_bad)
                 }
-                return Mask{first_page(j) * kPageTokens, keys, ok, false};
+                const int key0 = first_page(j) * kPageTokens;
+                return Mask{key0, keys, ok, false, key0 + C::kBlock > sure || ok != (1u << C::kPages) - 1};
             };
             // Block j has arrived for every wave (the loads of later blocks may go on: 1 KiB each,
             // kLoads per block and wave).
@@ -1260,7 +1269,7 @@ hipError_t launch_shape(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s, c
 #define SMALLCFG 4, 1, kPages, 4, 1
 #endif
 #ifndef MIDCFG
-#define MIDCFG 8, 1, kPages, 4, 1
+#define MIDCFG 8, 1, kPages, 3, 1
 #endif
 #ifndef BIGCFG
 #define BIGCFG 8, 2, kPages, 3, 1
