@@ -410,7 +410,8 @@ int kv_append_tokens_table(kv_pool* pool, int32_t layer_begin, int32_t num_layer
  * A count above `width` counts as `width`, one below 0 as 0.  An entry that names
  * no draft (outside [0, width)), whose position lies outside the table row or whose
  * table entry names no page of either pool writes nothing.  The same draft may be
- * named twice.  Rejected drafts are never written.
+ * named twice; two rows whose tables name the same page race where their tokens
+ * meet.  Rejected drafts are never written.
  * As with kv_append_tokens_table the pool's bookkeeping is not read or changed:
  * call kv_session_extend first, to the most tokens that may be accepted.
  * Errors: KV_ERR_INVALID (layer range, batch, width, NULL or misaligned buffers,
@@ -755,8 +756,8 @@ size_t paged_prefill_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t
  *   q_starts   device int32 [batch + 1], ascending from 0 on to at most total_q;
  *              a row without queries is fine.  A row whose range does not lie in
  *              [0, total_q] or descends writes nothing
- *   seq_lens   device int32 [batch], the new tokens included.  L < n or
- *              L > 16 * pt_stride: the row's outputs are NaN and nothing is read
+ *   seq_lens   device int32 [batch], the new tokens included.  L < n, L > 16 *
+ *              pt_stride or L > 2^30: the row's outputs are NaN and nothing is read
  *   out        device, like q.  Only the rows' queries are written: queries before
  *              q_starts[0] or from q_starts[batch] on are left as they were
  *   workspace  device, >= paged_prefill_workspace_bytes(), 256-byte aligned
@@ -804,8 +805,8 @@ size_t paged_tree_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t wi
  *   draft_lens        device int32 [batch] or NULL; outside [0, width] it counts as the
  *                     nearer end.  Drafts at or past n are neither read nor written
  *   width             1 .. KV_MAX_DRAFTS
- *   seq_lens          device int32 [batch]; C < 0 or C > 16 * pt_stride: NaN for the
- *                     row's drafts, nothing is read
+ *   seq_lens          device int32 [batch]; C < 0, C > 16 * pt_stride or C > 2^30: NaN for
+ *                     the row's drafts, nothing is read
  *   out               device, like q
  *   workspace         device, >= paged_tree_workspace_bytes(), 256-byte aligned
  *

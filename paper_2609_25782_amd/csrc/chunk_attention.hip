@@ -125,7 +125,8 @@ __device__ __forceinline__ Row make_row(const ChunkArgs& a, int start, int n, in
 
 template <class C, bool TREE>
 __device__ __forceinline__ Row row_info(const ChunkArgs& a, int b) {
-    const int64_t most = static_cast<int64_t>(kPageTokens) * a.pt_stride;
+    // (2^30 tokens at most, so that places of keys stay in 32 bits)
+    const int64_t most = min(static_cast<int64_t>(kPageTokens) * a.pt_stride, int64_t(1) << 30);
     const int32_t len = uniform_ptr(a.lens)[b];
     int start, n;
     if constexpr (TREE) {
