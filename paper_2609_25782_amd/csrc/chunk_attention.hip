@@ -49,30 +49,33 @@ __device__ __forceinline__ const_i32 uniform_ptr(const int32_t* p) {
     return (const_i32)(reinterpret_cast<uintptr_t>(p));
 }
 
-template <int D, bool BF16, int WAVES, int NT, int PAGES, int STAGES, int GROUPS>
+// Tiles of 128 NT rows: 8 waves of 16 NT rows; one workgroup per CU, two waves per SIMD with 256
+// registers each.  Blocks of 64 keys (f32: 32), 32 KiB at a head size of 128, in three stages
+// (four measure the same within 3 %).
+template <int D, bool BF16, int NT>
 struct Cfg {
-    static constexpr int kD = D, kWaves = WAVES, kNT = NT, kPages = PAGES, kStages = STAGES;
+    static constexpr int kD = D, kWaves = 8, kNT = NT, kPages = BF16 ? 4 : 2, kStages = 3;
     static constexpr bool kBf16 = BF16;
     static constexpr int kElt = BF16 ? 2 : 4;
     static constexpr int kX = 16 / kElt;                  // elements of a 16-byte group
     static constexpr int kTile = kPageTokens * D * kElt;  // bytes of a K or V tile
     static constexpr int kPage = 2 * kTile;               // a page's K and V tiles of one KV head
-    static constexpr int kBlock = PAGES * kPageTokens;    // keys per block
-    static constexpr int kStage = PAGES * kPage;          // LDS bytes of a block
-    static constexpr int kThreads = WAVES * kWave;
-    // Cache policy of the page loads: nontemporal (2) where one tile holds all of a row's queries
-    // of a KV head, so that its K and V are read once (32 sessions x 4-16 drafts: 278 -> 263 us);
+    static constexpr int kBlock = kPages * kPageTokens;    // keys per block
+    static constexpr int kStage = kPages * kPage;         // LDS bytes of a block
+    static constexpr int kThreads = kWaves * kWave;
+    // Cache policy of the page loads: nontemporal (2) where one tile holds most rows' queries
+    // of a KV head, so that its K and V are read once (32 sessions x 4-16 drafts over 8K-32K tokens: 272 -> 259 us);
     // tiles of 256 rows read them again and again.
-    static constexpr int kAux = WAVES * NT * 16 < 256 ? 2 : 0;
-    static constexpr int kPerSimd = WAVES * GROUPS / 4;    // waves per SIMD the registers are made for
+    static constexpr int kAux = NT == 1 ? 2 : 0;
+    static constexpr int kPerSimd = kWaves / 4;           // waves per SIMD the registers are made for
     static constexpr int kWaveRows = 16 * NT;
-    static constexpr int kRows = WAVES * kWaveRows;
+    static constexpr int kRows = kWaves * kWaveRows;
     static constexpr int kTileLoads = kTile / 1024;       // 1 KiB loads of a tile
-    static constexpr int kLoads = PAGES * 2 * kTileLoads / WAVES;  // a wave's loads per block
+    static constexpr int kLoads = kPages * 2 * kTileLoads / kWaves;  // a wave's loads per block
     static constexpr int kQ = D / (4 * kX);               // 16-byte Q fragments of a row per lane
     static constexpr int kC = D / 16;                     // 16-dim output chunks
-    static_assert(kLoads >= 1 && (kLoads % kTileLoads == 0 || kTileLoads % kLoads == 0), "load split");
-    static_assert(!BF16 || PAGES % 2 == 0, "bf16 fragments take pages in pairs");
+    static_assert(kLoads >= 1 && kTileLoads % kLoads == 0, "a wave loads one tile or a part of one");
+    static_assert(!BF16 || kPages % 2 == 0, "bf16 fragments take pages in pairs");
 };
 
 // What one row b brings: n tokens (or drafts), `ctx` tokens before them, the row's units.
@@ -94,12 +97,10 @@ struct Row {
 
 // What a tile costs beside its keys, in keys: its queries' load, its output, the pipeline's
 // start and the masked blocks.  kTileCost is what balances calls with work for every worker
-// (twelve packed prompts: 64: 1694 us, 192: 1330, 320: 1144, 448: 1160); calls with less
-// than that are cut finer, with kTileCostFine (8 sessions x 8 drafts: 64: 40 us, 320: 42).
-#ifndef TILECOST
-#define TILECOST 320
-#endif
-constexpr int kTileCost = TILECOST, kTileCostFine = 64;
+// (twelve packed prompts, on one build: 64: 1879 us, 192: 1453, 320: 1220, 448: 1241, 640:
+// 1282); calls with less than that are cut finer, with kTileCostFine (8 sessions x 8 drafts
+// over 2K tokens: 64: 39.8 us, 320: 41.7).
+constexpr int kTileCost = 320, kTileCostFine = 64;
 
 // The units of a row that brings n queries after ctx tokens.
 template <class C, bool TREE>
@@ -160,9 +161,9 @@ __device__ __forceinline__ int tile_blocks(const ChunkArgs& a, const Row& r, int
     return draft_blocks<C, TREE>(r) + (tile_keys<C, TREE>(a, r, i) + C::kBlock - 1) / C::kBlock;
 }
 
-// A place in the order of blocks: block `blk` of tile `tile` of (row b, group hg of `team` KV heads).
+// A place in the order of blocks: block `blk` of tile `tile` of (row b, KV head g).
 struct Place {
-    int b, hg, tile, blk;
+    int b, g, tile, blk;
 };
 
 // What a worker takes: the blocks from `from` up to `to`.  Where `to` lies inside a tile,
@@ -191,7 +192,7 @@ struct Cuts {
 // Enough units for a block or more in every range (see place_of).
 template <class C>
 __device__ __forceinline__ Cuts cuts_of(const ChunkArgs& a, int64_t keys, int64_t tiles) {
-    const int most = a.workers / a.team;
+    const int most = a.workers;
     Cuts c;
     c.cost = kTileCost;
     if (keys + c.cost * tiles < static_cast<int64_t>(c.cost + 2 * C::kBlock) * most) c.cost = kTileCostFine;
@@ -214,11 +215,11 @@ __device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int 
     p.b = b;
     const int64_t h = r.head_units(cost);
     if (((u | h) >> 32) == 0) {
-        p.hg = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(h));
+        p.g = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(h));
     } else {
-        p.hg = static_cast<int>(u / h);
+        p.g = static_cast<int>(u / h);
     }
-    int64_t rem = u - p.hg * h;
+    int64_t rem = u - p.g * h;
     int lo = 0, hi = r.tiles - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -238,7 +239,7 @@ __device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int 
             p.blk = 0;
             if (++p.tile == r.tiles) {
                 p.tile = 0;
-                ++p.hg;    // may be the number of head groups: the walk moves on to the next row
+                ++p.g;    // may be the number of KV heads: the walk moves on to the next row
             }
         }
     }
@@ -246,13 +247,13 @@ __device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int 
 }
 
 __device__ __forceinline__ Place uniform_place(const Place& p) {
-    return Place{__builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.hg),
+    return Place{__builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.g),
                  __builtin_amdgcn_readfirstlane(p.tile), __builtin_amdgcn_readfirstlane(p.blk)};
 }
 
 __device__ __forceinline__ bool before(const Place& x, const Place& y) {
     if (x.b != y.b) return x.b < y.b;
-    if (x.hg != y.hg) return x.hg < y.hg;
+    if (x.g != y.g) return x.g < y.g;
     if (x.tile != y.tile) return x.tile < y.tile;
     return x.blk < y.blk;
 }
@@ -279,15 +280,68 @@ __device__ __forceinline__ int64_t lane_value64(int64_t x, int lane) {
     return static_cast<int64_t>(lo) | (static_cast<int64_t>(hi) << 32);
 }
 
+// Where no more than `workers` tiles have about the same cost in each row (drafts, short
+// chunks over long contexts) and equal parts of them differ little, every tile is cut into
+// whole parts, as many as its share of the workers: no worker then has parts of two tiles,
+// whose starts and ends follow each other.  8 sessions x 8 drafts over 2K tokens: 26.5 us with
+// the ranges below, 22.7 so; 2 x 5 drafts in float32: 16.6 and 14.2.  Taken without looking at
+// the longest part, 32 sessions of 8K to 32K tokens lose (248 us with ranges, 311 so).
+// A row per lane.  True where the call is cut so; out.parts is then the number of parts of
+// the worker's tile, 0 for a worker without one.
+template <class C, bool TREE>
+__device__ bool whole_parts(const ChunkArgs& a, int k, const Row& r, Range& out) {
+    const int heads = a.num_kv_heads;
+    const int most = a.workers;
+    const bool even = r.tiles <= 1 || r.slope == 0 || static_cast<int64_t>(r.n) * 4 <= r.ctx;
+    if (__builtin_amdgcn_ballot_w64(!even)) return false;
+    if (__builtin_amdgcn_ballot_w64(static_cast<int64_t>(heads) * r.tiles > most)) return false;
+    const int count = heads * r.tiles;       // tiles of the row (rows without queries: none)
+    const float cost = r.tiles ? static_cast<float>(r.last) : 0.f;
+    float total = cost * count;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) total += __shfl_xor(total, d);
+    int w = static_cast<int>(most * cost / fmaxf(total, 1.f));
+    const int nb = r.tiles ? tile_blocks<C, TREE>(a, r, 0) : 0;      // of its shortest tile
+    w = max(1, min(w, nb / 2));
+    const int mine = count * w;
+    const int upto = wave_scan(mine);
+    const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
+    float longest = cost / w;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) longest = fmaxf(longest, __shfl_xor(longest, d));
+    if (all > most || longest > total / most + kTileCost) return false;
+    out.parts = 0;
+    if (k >= all) return true;
+    const uint64_t has = __builtin_amdgcn_ballot_w64(mine > 0 && upto - mine <= k);
+    const int b = kWave - 1 - __builtin_clzll(has);
+    out.row = make_row<C, TREE>(a, __builtin_amdgcn_readlane(r.start, b), __builtin_amdgcn_readlane(r.n, b),
+                                __builtin_amdgcn_readlane(r.ctx, b), __builtin_amdgcn_readlane(r.bad, b));
+    out.parts = __builtin_amdgcn_readlane(w, b);
+    const int rem = k - (__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(mine, b));
+    const unsigned at = static_cast<unsigned>(rem) / static_cast<unsigned>(out.parts);
+    const int part = rem - at * out.parts;
+    const int g = at / static_cast<unsigned>(out.row.tiles), tile = at - g * out.row.tiles;
+    const int blocks = tile_blocks<C, TREE>(a, out.row, tile);
+    const auto cut = [&](int p) {      // p blocks / parts
+        return static_cast<int>(static_cast<unsigned>(p * (blocks % out.parts)) / static_cast<unsigned>(out.parts)) +
+               p * (blocks / out.parts);
+    };
+    const int to = cut(part + 1);
+    out.from = uniform_place(Place{b, g, tile, cut(part)});
+    out.to = uniform_place(to == blocks ? Place{b, g, tile + 1, 0} : Place{b, g, tile, to});
+    return true;
+}
+
 // Worker k's range; false where there is none.
 template <class C, bool TREE>
 __device__ bool worker_range(const ChunkArgs& a, int k, Range& out) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    const int heads = a.num_kv_heads / a.team;
+    const int heads = a.num_kv_heads;
     if (a.batch <= kWave) {
         // a row per lane; every wave finds the range by itself
         Row r = {};
         if (lane < a.batch) r = row_info<C, TREE>(a, lane);
+        if (whole_parts<C, TREE>(a, k, r, out)) return out.parts > 0;
         const int64_t keys = heads * r.head_units(0), tiles = static_cast<int64_t>(heads) * r.tiles;
         const int64_t keys_to = wave_scan64(keys), tiles_to = wave_scan64(tiles);
         const Cuts cuts = cuts_of<C>(a, lane_value64(keys_to, kWave - 1), lane_value64(tiles_to, kWave - 1));
@@ -418,16 +472,12 @@ struct Loader {
             voff = C::kTile + x * 64 + g * 16;
         }
     }
-    // This wave's share of a block: whole pages, one page's K or V tile, or a part of one.
-    static constexpr int kShare = C::kTileLoads > C::kLoads ? C::kTileLoads / C::kLoads : 1;  // waves of a tile
-    static constexpr int kTiles = C::kLoads > C::kTileLoads ? C::kLoads / C::kTileLoads : 1;  // tiles of a wave
-    static constexpr int kMyPages = kTiles > 2 ? kTiles / 2 : 1;
-    static_assert(kTiles <= 2 || kTiles % 2 == 0, "a wave's tiles are whole pages'");
-    __device__ __forceinline__ int tile() const { return kShare > 1 ? wave / kShare : wave * kTiles; }
-    __device__ __forceinline__ int page() const { return tile() >> 1; }   // the first of kMyPages
-    // Its loads of its i-th page, which entry `id` names; an id that names none reads zeros.
-    __device__ __forceinline__ bool load_page(const ChunkArgs& a, int id, int i_page, unsigned head_off,
-                                              char* stage) const {
+    // This wave's share of a block: one page's K or V tile, or a part of one.
+    static constexpr int kShare = C::kTileLoads / C::kLoads;     // waves of a tile
+    __device__ __forceinline__ int tile() const { return wave / kShare; }
+    __device__ __forceinline__ int page() const { return tile() >> 1; }
+    // Its loads of the page that entry `id` names; an id that names none reads zeros.
+    __device__ __forceinline__ bool load_page(const ChunkArgs& a, int id, unsigned head_off, char* stage) const {
         const bool hot = is_hot(a, id), cold = is_cold(a, id);
         const char* pool = cold ? a.cold : a.hot;
         const int64_t stride = cold ? a.cold_stride : a.hot_stride;
@@ -435,18 +485,12 @@ struct Loader {
         const __amdgpu_buffer_rsrc_t rs =
             __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool + n * stride + head_off), static_cast<short>(0),
                                               hot || cold ? C::kPage : 0, kRsrcWord3);
-        constexpr int kHere = kTiles < 2 ? kTiles : 2;      // tiles of the page
-        constexpr int kEach = C::kLoads / kTiles;           // loads of a tile
+        const int t = tile(), first = (wave % kShare) * C::kLoads;
+        const unsigned k = C::kBf16 && (page() & 1) ? koff ^ 64 : koff;
+        const unsigned off = (t & 1) ? voff : k;
+        char* dst = stage + t * C::kTile + first * 1024;
 #pragma unroll
-        for (int j = 0; j < kHere; ++j) {
-            const int t = tile() + 2 * i_page + j;
-            const int first = kShare > 1 ? (wave % kShare) * C::kLoads : 0;
-            const unsigned k = C::kBf16 && ((page() + i_page) & 1) ? koff ^ 64 : koff;
-            const unsigned off = (t & 1) ? voff : k;
-            char* dst = stage + t * C::kTile + first * 1024;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) load_lds16<C::kAux>(rs, dst + i * 1024, off + (first + i) * 1024);
-        }
+        for (int i = 0; i < C::kLoads; ++i) load_lds16<C::kAux>(rs, dst + i * 1024, off + (first + i) * 1024);
         return hot || cold;
     }
     // The K of drafts [key0, key0 + kBlock) of a row, by the same kind of loads; drafts past n read zeros.
@@ -688,7 +732,7 @@ __device__ __forceinline__ void compute_block(State<C>& st, const char* stage, f
                                               const int (&lim)[C::kNT], const uint64_t (&seen)[C::kNT]) {
     const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, x = lane & 15;
     // Fragments of K and then of V, in groups of kG, two groups ahead of the products.
-    constexpr int kG = C::kPages * C::kQ >= 8 && C::kD > 64 && C::kPerSimd <= 2 ? 4 : 2;
+    constexpr int kG = C::kPages * C::kQ >= 8 && C::kD > 64 ? 4 : 2;
     constexpr int kKF = C::kPages * C::kQ;                           // K fragments: (i, page t)
     constexpr int kSteps = C::kBf16 ? C::kPages / 2 : C::kPages;     // contraction steps of the output
     constexpr int kVF = kSteps * C::kC;                              // V fragments: (step p, c)
@@ -877,17 +921,19 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
     __shared__ int s_bad;      // 1: a page that every row of the tile attends to is missing
     const int lane = threadIdx.x & (kWave - 1), gq = lane >> 4, x = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    // neighbouring ranges to one XCD (blocks go to the XCDs in turn); a team takes one range
-    // of head groups, a KV head each
+    // neighbouring ranges to one XCD (blocks go to the XCDs in turn)
     int k = blockIdx.x;
     if (gridDim.x % kXcds == 0) k = (k % kXcds) * (gridDim.x / kXcds) + k / kXcds;
-    const int member = k % a.team;
-    const int heads = a.num_kv_heads / a.team;
-    Range range;
-    const bool work = worker_range<C, TREE>(a, k / a.team, range);
-    Place at = range.from;
-    const Place end = range.to;
-    Row row = range.row;     // of at.b
+    Range range = {};
+    const bool work = worker_range<C, TREE>(a, k, range);
+    // the range is one for the workgroup: in scalar registers, whichever way it was found
+    Place at = uniform_place(range.from);
+    const Place end = uniform_place(range.to);
+    const int parts = __builtin_amdgcn_readfirstlane(range.parts);
+    Row row = make_row<C, TREE>(a, __builtin_amdgcn_readfirstlane(range.row.start),
+                                __builtin_amdgcn_readfirstlane(range.row.n),
+                                __builtin_amdgcn_readfirstlane(range.row.ctx),
+                                __builtin_amdgcn_readfirstlane(range.row.bad));     // of at.b
     bool recorded = false;   // this worker holds the first part of a cut tile
     const Loader<C> ld;
     const unsigned head_bytes = 2 * C::kTile;
@@ -895,7 +941,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
     if (work) {
         while (before(at, end)) {
             if (at.b >= a.batch) break;
-            if (at.hg >= heads || row.tiles == 0) {   // on to the next row with queries
+            if (at.g >= a.num_kv_heads || row.tiles == 0) {   // on to the next row with queries
                 int b = at.b + 1;
                 while (b < a.batch) {
                     const uint64_t some = __builtin_amdgcn_ballot_w64(
@@ -911,8 +957,8 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 continue;
             }
             const int nb = tile_blocks<C, TREE>(a, row, at.tile);
-            const int kv_head = at.hg * a.team + member;
-            const bool to_end = end.b == at.b && end.hg == at.hg && end.tile == at.tile;
+            const int kv_head = at.g;
+            const bool to_end = end.b == at.b && end.g == at.g && end.tile == at.tile;
             const int k0 = at.blk, k1 = to_end ? end.blk : nb;
             const int nd = draft_blocks<C, TREE>(row);
             const int keys = tile_keys<C, TREE>(a, row, at.tile);
@@ -982,26 +1028,18 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 const int p = (j >= nd && j < k1 ? first_page(j) : 0) + i;
                 return p <= last_page ? pt[p] : -1;
             };
-            constexpr int kMine = Loader<C>::kMyPages;
-            int id[kMine];                        // of this wave's pages of the block that is fetched next
-            int first_ids[C::kStages - 1][kMine]; // of the first blocks, loaded together
+            int id;                        // of this wave's page of the block that is fetched next
+            int first_ids[C::kStages - 1]; // of the first blocks, loaded together
 #pragma unroll
-            for (int i = 0; i < C::kStages - 1; ++i)
-#pragma unroll
-                for (int m = 0; m < kMine; ++m) first_ids[i][m] = page_id(k0 + i, ld.page() + m);
+            for (int i = 0; i < C::kStages - 1; ++i) first_ids[i] = page_id(k0 + i, ld.page());
             char* into = s_kv;                    // stage of that block
             const auto next_stage = [&](char* p) { return p == s_kv + (C::kStages - 1) * C::kStage ? s_kv : p + C::kStage; };
-            const auto next_ids = [&](int j) {
-#pragma unroll
-                for (int i = 0; i < kMine; ++i) id[i] = page_id(j, ld.page() + i);
-            };
+            const auto next_id = [&](int j) { id = page_id(j, ld.page()); };
             const auto fetch_pages = [&](int j) {   // context block j of [k0, k1)
-#pragma unroll
-                for (int i = 0; i < kMine; ++i)
-                    // a missing page of a block that every row sees whole is NaN for all of them
-                    // (tokens past the row's last, in its last block, are no matter)
-                    if (!ld.load_page(a, id[i], i, head_off, into))
-                        if (j >= partly && first_page(j) + ld.page() + i <= last_page) s_bad = 1;
+                // a missing page of a block that every row sees whole is NaN for all of them
+                // (tokens past the row's last, in its last block, are no matter)
+                if (!ld.load_page(a, id, head_off, into))
+                    if (j >= partly && first_page(j) + ld.page() <= last_page) s_bad = 1;
                 into = next_stage(into);
             };
             const auto fetch = [&](int j) {         // block j of [k0, k1)
@@ -1016,12 +1054,10 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
 #pragma unroll
             for (int i = 0; i < C::kStages - 1; ++i)
                 if (k0 + i < k1) {
-#pragma unroll
-                    for (int m = 0; m < kMine; ++m) id[m] = first_ids[i][m];
+                    id = first_ids[i];
                     fetch(k0 + i);
                 }
-#pragma unroll
-            for (int m = 0; m < kMine; ++m) id[m] = page_id(k0 + C::kStages - 1, ld.page() + m);
+            next_id(k0 + C::kStages - 1);
             if (a.negate) {
 #pragma unroll
                 for (int n = 0; n < C::kNT; ++n)
@@ -1067,7 +1103,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 }
                 if (j + C::kStages - 1 < k1) {
                     fetch(j + C::kStages - 1);
-                    next_ids(j + C::kStages);
+                    next_id(j + C::kStages);
                 }
                 if (j >= unseen) compute_block<C, TREE, true>(st, stage, a.scale_log2, a.slack, mask_of(j), lim, seen);
                 stage = next_stage(stage);
@@ -1076,7 +1112,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 arrive();
                 if (j + C::kStages - 1 < k1) {
                     fetch_pages(j + C::kStages - 1);
-                    next_ids(j + C::kStages);
+                    next_id(j + C::kStages);
                 }
                 if (wave_live) compute_block<C, TREE, false>(st, stage, a.scale_log2, a.slack, Mask{}, lim, seen);
                 stage = next_stage(stage);
@@ -1122,7 +1158,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 if (k0 == 0) {
                     recorded = true;
                     if (threadIdx.x == 0)
-                        a.recs[k] = ChunkRec{range.parts, toks * a.group,
+                        a.recs[k] = ChunkRec{parts, toks * a.group,
                                              (static_cast<int64_t>(row.start) + tok0) * a.num_q_heads + kv_head * a.group};
                 }
             }
@@ -1130,7 +1166,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
             at.blk = 0;
             if (++at.tile == row.tiles) {
                 at.tile = 0;
-                ++at.hg;
+                ++at.g;
             }
         }
     }
@@ -1138,12 +1174,15 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
 }
 
 // Joins the partial results of the tiles cut between workers: with M the largest of the
-// parts' maxima, out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  Block (k, y) takes
-// rows of the tile whose first part worker k left in slot 2 k + 1; its other parts are
-// slots 2 (k + team), 2 (k + 2 team), ..  A wave takes kIter rows, a float4 per lane and
-// kAtOnce parts at a time.  Most tiles are cut once or twice: then the loads of all of the
+// parts' maxima, out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  A block takes rows of the
+// tile whose first part worker k left in slot 2 k + 1; its other parts are
+// in the slots 2 (k + 1), 2 (k + 2), ... of the workers after it.  A wave takes kIter
+// rows, kAtOnce parts at a time.  Most tiles are cut once or twice: then the loads of all of the
 // wave's rows are in flight together.  The record holds all that a row's place needs, so
-// that only two loads follow each other.
+// that only two loads follow each other.  Where few tiles are cut into equal parts, the k that
+// hold a record are multiples of 8 and more, which plain block numbers all send to one XCD:
+// the blocks of one k differ in blockIdx.x (4 sessions x 32 drafts, 16 parts each: 38 us with
+// plain numbers, 10 so).
 template <class C>
 struct Merge {
     static constexpr int kLanes = C::kD / 4, kAtOnce = kWave / kLanes;
@@ -1179,7 +1218,7 @@ struct Merge {
 template <class C>
 __global__ __launch_bounds__(kBlockThreads) void chunk_merge_kernel(const ChunkArgs a) {
     using M = Merge<C>;
-    const int k = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int k = (blockIdx.x + blockIdx.y) % gridDim.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     ChunkRec rec = a.recs[k];
     rec.parts = __builtin_amdgcn_readfirstlane(rec.parts);
     rec.rows = __builtin_amdgcn_readfirstlane(rec.rows);
@@ -1187,7 +1226,7 @@ __global__ __launch_bounds__(kBlockThreads) void chunk_merge_kernel(const ChunkA
     if (rec.parts == 0 || r0 >= rec.rows) return;
     const int sub = lane / M::kLanes, col = lane % M::kLanes;
     const auto part_of = [&](int p, int r, float& m, float& l, f32x4& o) {
-        const int64_t slot = p == 0 ? 2 * k + 1 : 2 * (k + p * a.team);
+        const int64_t slot = p == 0 ? 2 * k + 1 : 2 * (k + p);
         m = a.part_ml[slot * 2 * C::kRows + r];
         l = a.part_ml[slot * 2 * C::kRows + C::kRows + r];
         o = *reinterpret_cast<const f32x4*>(a.part_o + (slot * C::kRows + r) * C::kD + col * 4);
@@ -1228,18 +1267,10 @@ __global__ __launch_bounds__(kBlockThreads) void chunk_merge_kernel(const ChunkA
     }
 }
 
-#ifndef TEAM
-#define TEAM(TREE, C) (C::kRows < 256)
-#endif
 template <class C, bool TREE>
 hipError_t launch_cfg(ChunkArgs a, int workers, hipStream_t s, const LaunchEvents& ev, const LaunchEvents& ev_merge) {
     a.tile_tokens = C::kRows / a.group;
-    // Teams: four workers (two, where the KV heads come in twos) read the tiles of neighbouring
-    // heads of the same pages at the same time, which HBM serves faster than unrelated tiles.
-    // Large tiles are bound by the products and share K and V in the L2 better alone.
-    a.team = TEAM(TREE, C) ? (a.num_kv_heads % 4 == 0 ? 4 : (a.num_kv_heads % 2 == 0 ? 2 : 1)) : 1;
-    a.workers = workers - workers % a.team;
-    workers = a.workers;
+    a.workers = workers;
     chunk_workspace_layout(a, C::kRows, C::kD);
     const size_t lds = static_cast<size_t>(C::kStages) * C::kStage;
     const void* kern = reinterpret_cast<const void*>(&chunk_attend_kernel<C, TREE>);
@@ -1265,34 +1296,24 @@ hipError_t launch_cfg(ChunkArgs a, int workers, hipStream_t s, const LaunchEvent
 template <int D, bool BF16, bool TREE>
 hipError_t launch_shape(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s, const LaunchEvents& ev,
                         const LaunchEvents& ev_merge) {
-    constexpr int kPages = BF16 ? 4 : 2;
-#ifndef SMALLCFG
-#define SMALLCFG 4, 1, kPages, 4, 1
-#endif
-#ifndef MIDCFG
-#define MIDCFG 8, 1, kPages, 3, 1
-#endif
-#ifndef BIGCFG
-#define BIGCFG 8, 2, kPages, 3, 1
-#endif
-    if (p.rows == 64) return launch_cfg<Cfg<D, BF16, SMALLCFG>, TREE>(a, p.workers, s, ev, ev_merge);
-    if (p.rows == 128) return launch_cfg<Cfg<D, BF16, MIDCFG>, TREE>(a, p.workers, s, ev, ev_merge);
-    return launch_cfg<Cfg<D, BF16, BIGCFG>, TREE>(a, p.workers, s, ev, ev_merge);
+    if (p.rows == 128) return launch_cfg<Cfg<D, BF16, 1>, TREE>(a, p.workers, s, ev, ev_merge);
+    return launch_cfg<Cfg<D, BF16, 2>, TREE>(a, p.workers, s, ev, ev_merge);
 }
 
 }  // namespace
 
-// Rows of a tile: 64 where a row's queries fit into them, else 256.
-ChunkPlan chunk_plan(int cus, int group, int64_t rows_per_seq) {
+// Rows of a tile, by the rows that a session brings to a KV head (the average of prompt
+// chunks, the most of trees).  256: a wave has 32 rows, and each K and V fragment that it reads
+// from LDS serves two products, else the reads bound the call; 128, where a tile of 256 would
+// compute rows that are not there or wait for K and V all the same.  16 sessions of 8K-32K
+// tokens, 128 rows each: 147 us with tiles of 128 rows, 156 with 256; 136 rows: 240 and 191;
+// 256 rows: 278 and 225; 64 sessions of 8 rows: 92 and 111.  64 decode steps of 8 rows and a
+// chunk of 4096 rows in one call (71 rows on average): 138 and 162.  (Tiles of 64 rows were
+// never faster by more than 2 %: 8 sessions x 8 drafts 22.4 us, with 128 rows 20.9.)
+ChunkPlan chunk_plan(int cus, int64_t rows_per_seq) {
     ChunkPlan p;
-  #ifndef SMALLWG
-#define SMALLWG 1
-#endif
-#ifndef MIDWG
-#define MIDWG 1
-#endif
-    p.rows = rows_per_seq <= 64 ? 64 : (rows_per_seq <= 128 ? 128 : 256);
-    p.workers = (p.rows == 64 ? SMALLWG : p.rows == 128 ? MIDWG : 1) * cus;
+    p.rows = rows_per_seq <= 128 ? 128 : 256;
+    p.workers = cus;
     return p;
 }
 

@@ -310,7 +310,6 @@ struct ChunkArgs {
     void* workspace;
     // set by the launch
     int32_t tile_tokens, workers;
-    int32_t team;              // workers that take the KV heads of one range, a head each
     float* part_o;             // [2 workers][rows of a tile][D]
     float* part_ml;            // [2 workers][2][rows of a tile]
     ChunkRec* recs;            // [workers]
@@ -319,7 +318,7 @@ struct ChunkPlan {
     int32_t rows;      // rows of a tile
     int32_t workers;   // workgroups
 };
-ChunkPlan chunk_plan(int cus, int group, int64_t rows_per_seq);
+ChunkPlan chunk_plan(int cus, int64_t rows_per_seq);
 inline size_t chunk_workspace_bytes(const ChunkPlan& p, int head_dim) {
     const size_t n = static_cast<size_t>(p.workers) * (static_cast<size_t>(2) * p.rows * (head_dim + 2) * 4 + sizeof(ChunkRec));
     return (n + 255) & ~static_cast<size_t>(255);

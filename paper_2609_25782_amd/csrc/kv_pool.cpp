@@ -1589,8 +1589,7 @@ int paged_decode_attention_append(kv_pool* pool, int32_t layer, const void* q, c
 
 namespace {
 
-// Checks and arguments that prompt chunks and draft trees share.  rows_per_seq: queries of
-// a row times the query heads of a KV head, the average (prompt chunks) or the most (trees).
+// Checks and arguments that prompt chunks and draft trees share.
 int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
                const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, float scale, void* out, hck::ChunkArgs& a) {
     if (pool->meta) return fail(KV_ERR_INVALID, "metadata-only pool has no pages");
@@ -1629,6 +1628,7 @@ int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_
     return KV_OK;
 }
 
+// Queries of a row times the query heads of a KV head, on average.
 int64_t prefill_rows(const kv_pool* pool, int32_t batch, int32_t total_q, int32_t num_q_heads) {
     const int64_t group = num_q_heads / pool->d.num_kv_heads;
     return (static_cast<int64_t>(total_q) * group + batch - 1) / batch;
@@ -1636,7 +1636,7 @@ int64_t prefill_rows(const kv_pool* pool, int32_t batch, int32_t total_q, int32_
 
 int chunk_launch(kv_pool* pool, hck::ChunkArgs& a, int64_t rows_per_seq, bool tree, void* workspace, size_t ws_bytes,
                  kv_stream_t stream) {
-    const hck::ChunkPlan plan = hck::chunk_plan(pool->cus, a.group, rows_per_seq);
+    const hck::ChunkPlan plan = hck::chunk_plan(pool->cus, rows_per_seq);
     const size_t need = hck::chunk_workspace_bytes(plan, pool->d.head_dim);
     if (!workspace) return fail(KV_ERR_INVALID, "NULL workspace");
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KV_ERR_INVALID, "workspace must be 256-byte aligned");
@@ -1667,8 +1667,7 @@ size_t paged_prefill_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t
     if (!pool || pool->meta || batch < 0 || total_q < 0 || num_q_heads <= 0 || num_q_heads % pool->d.num_kv_heads)
         return 0;
     if (batch == 0) return 256;
-    const hck::ChunkPlan plan = hck::chunk_plan(pool->cus, num_q_heads / pool->d.num_kv_heads,
-                                                prefill_rows(pool, batch, total_q, num_q_heads));
+    const hck::ChunkPlan plan = hck::chunk_plan(pool->cus, prefill_rows(pool, batch, total_q, num_q_heads));
     return hck::chunk_workspace_bytes(plan, pool->d.head_dim);
 }
 
@@ -1696,7 +1695,7 @@ size_t paged_tree_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t wi
         num_q_heads % pool->d.num_kv_heads)
         return 0;
     const int32_t group = num_q_heads / pool->d.num_kv_heads;
-    return hck::chunk_workspace_bytes(hck::chunk_plan(pool->cus, group, static_cast<int64_t>(width) * group),
+    return hck::chunk_workspace_bytes(hck::chunk_plan(pool->cus, static_cast<int64_t>(width) * group),
                                       pool->d.head_dim);
 }
 

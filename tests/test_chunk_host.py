@@ -113,3 +113,74 @@ def test_every_block_belongs_to_one_worker(tree):
                     break
             want += 1
         assert next(flat, None) is None
+
+
+# -- the other split: every tile in whole parts ---------------------------------
+
+
+def whole_parts(rows, heads, tok, block, tree, most, tile_cost=320):
+    """Kernel's rule on float32 numbers: [(row, head, tile, first block, end)] per worker, or None."""
+    import numpy as np
+    f = np.float32
+    infos = []
+    for ctx, n in rows:
+        tiles = -(-n // tok)
+        slope = 0 if tree else tok
+        last = -(-n // block) * block + ctx if tree else ctx + n
+        if not (tiles <= 1 or slope == 0 or n * 4 <= ctx) or heads * tiles > most:
+            return None
+        infos.append((ctx, n, tiles, f(last) if tiles else f(0)))
+    total = f(sum(c * f(heads * t) for _, _, t, c in infos))
+    split, longest = [], f(0)
+    for ctx, n, tiles, cost in infos:
+        blocks = row_units(ctx, n, tok, block, tree, 0)[1]
+        w = max(1, min(int(f(most) * cost / max(total, f(1))), blocks[0] // 2 if tiles else 0))
+        split.append((tiles, w, blocks))
+        longest = max(longest, cost / f(w))
+    if sum(heads * t * w for t, w, _ in split) > most or longest > total / f(most) + f(tile_cost):
+        return None
+    out = []
+    for b, (tiles, w, blocks) in enumerate(split):
+        for g in range(heads):
+            for t in range(tiles):
+                nb = blocks[t]
+                cut = [p * (nb % w) // w + p * (nb // w) for p in range(w + 1)]
+                out += [(b, g, t, cut[p], cut[p + 1]) for p in range(w)]
+    return out
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_equal_parts_cover_every_tile_once(tree):
+    rng = random.Random(8)
+    taken = 0
+    for trial in range(600):
+        block = rng.choice([32, 64])
+        group = rng.choice([1, 2, 3, 5, 8, 16])
+        tok = rng.choice([128, 256]) // group
+        heads = rng.choice([1, 2, 4, 8])
+        most = rng.choice([8, 256, 304])
+        base = rng.choice([0, 5, 300, 5000, 100000])
+        rows = [(base + rng.randint(0, 1 + base // rng.choice([2, 50])),
+                 rng.choice([0, 1, rng.randint(1, 64), rng.randint(1, 64 if tree else 300)]))
+                for _ in range(rng.randint(1, 12))]
+        parts = whole_parts(rows, heads, tok, block, tree, most)
+        if parts is None:
+            continue
+        taken += 1
+        assert len(parts) <= most
+        want = []
+        for b, (ctx, n) in enumerate(rows):
+            blocks = row_units(ctx, n, tok, block, tree, 0)[1]
+            want += [(b, g, t, nb) for g in range(heads) for t, nb in enumerate(blocks)]
+        got = iter(parts)
+        for b, g, t, nb in want:
+            upto = 0
+            while True:
+                part = next(got)
+                assert part[:4] == (b, g, t, upto)
+                assert part[4] >= upto + 2 or part[3:] == (0, nb)     # a whole tile, or two blocks or more
+                upto = part[4]
+                if upto == nb:
+                    break
+        assert next(got, None) is None
+    assert taken > 100

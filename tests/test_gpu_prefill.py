@@ -297,6 +297,23 @@ def test_profiling_counts_both_kernels():
         assert n == 1 and ms > 0
 
 
+def test_a_length_past_2_30_is_nan():
+    """Lengths of more than 2^30 tokens fit no row, however long its table claims to be: NaN, and
+    nothing of the table or the pages is read (2^30 tokens of a table that is there would not fit
+    into memory)."""
+    s = Sessions([40], 4, 2, 64, "bf16", seed=30)
+    q = s.normal(16, 4, 64).cuda()
+    out = torch.zeros_like(q)
+    ws = torch.empty(kv.paged_prefill_workspace_bytes(s.pool.handle, 1, 16, 4), dtype=torch.uint8, device="cuda")
+    for length in ((1 << 30) + 1, 2**31 - 1):
+        out.zero_()
+        starts, lens = i32([0, 16]), i32([length])
+        kv.paged_prefill_attention(s.pool.handle, 0, q.data_ptr(), starts.data_ptr(), 16, s.pool.page_table.data_ptr(),
+                                   1 << 28, lens.data_ptr(), 1, 4, 0.1, out.data_ptr(), ws.data_ptr(), ws.numel())
+        torch.cuda.synchronize()
+        assert out.isnan().all()
+
+
 def test_refusals():
     s = Sessions([40], 4, 2, 64, "bf16", seed=18, layers=2)
     q = s.normal(16, 4, 64).cuda()
