@@ -29,6 +29,20 @@
 // queries all fill the GPU.  A tile cut between workers leaves partial results
 // (o, m, l) in the workspace, which chunk_merge_kernel joins.  Workgroups of one XCD
 // take neighbouring ranges: they read the same K/V through the same L2.
+//
+// Bounds and figures (bf16, d = 128, 8 query heads per KV head, 4 KV heads, unless said).
+// Prompt chunks are bound by the products and by power: one prompt of 24,576 tokens takes
+// 4.2-4.5 ms = 1.10-1.18 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches
+// 1.19 and of two 16384 x 16384 ones 1.37, both at clocks of about 2 GHz.  Per block
+// of 64 keys and 32 rows a wave issues 64 matrix instructions (1024 cycles) and 144 others, of
+// them 32 exponentials (960 cycles); the matrix cores are busy 52 % of the time.  What was
+// measured and left out: half a block's offset between the two waves of a SIMD by barriers (4.25
+// -> 4.64 ms), the next block's scores between this one's weights (registers spill: 6.0 ms), 64
+// rows per wave (spills as well), wave priorities (no change).  With K and V always in the L2 the
+// long prompt would take 8 % less.  Trees of 4-16 drafts over 8K-32K tokens (32 sessions, 1.39
+// GB) are bound by the reads: 242 us = 5.75 TB/s, the attention kernel alone 5.9.  Small calls
+// are bound by the chain of dependent loads and the two launches: 13.5 us for 2 x 5 drafts in
+// float32, 10 of them in this kernel and 2.5-4 in the merge.  No LDS bank conflicts are counted.
 
 #include "device_common.h"
 #include "kernels.h"
@@ -1175,10 +1189,11 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
 
 // Joins the partial results of the tiles cut between workers: with M the largest of the
 // parts' maxima, out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.  A block takes rows of the
-// tile whose first part worker k left in slot 2 k + 1; its other parts are
-// in the slots 2 (k + 1), 2 (k + 2), ... of the workers after it.  A wave takes kIter
-// rows, kAtOnce parts at a time.  Most tiles are cut once or twice: then the loads of all of the
-// wave's rows are in flight together.  The record holds all that a row's place needs, so
+// tile whose first part worker k left in slot 2 k + 1; its other parts are in the slots 2 (k + 1),
+// 2 (k + 2), ... of the workers after it.  A wave takes kIter rows, kAtOnce parts at a time.
+// Most tiles are cut once or twice: then the loads of all of the wave's rows are in flight
+// together.  (2 x 5 drafts in float32: 14.3 us; with half as many rows per wave 15.9, the
+// blocks without work cost; with twice as many 15.7, 64 rows over 32K tokens 28.3 -> 34.4.)  The record holds all that a row's place needs, so
 // that only two loads follow each other.  Where few tiles are cut into equal parts, the k that
 // hold a record are multiples of 8 and more, which plain block numbers all send to one XCD:
 // the blocks of one k differ in blockIdx.x (4 sessions x 32 drafts, 16 parts each: 38 us with

@@ -510,8 +510,11 @@ __device__ __forceinline__ void write_run(T* out, const T* v, const int32_t* pat
 // gridDim.y, ..  K goes out in 16-byte groups.  V is dims-major in its tile, so a thread
 // takes one (head, dim) and writes its drafts of a page side by side: the drafts of a row lie
 // in consecutive slots, so a run of 8 is one 16-byte store, where a store per draft and dim
-// would be 2 bytes each (64 rows x 0-16 drafts x 48 layers, 51 MB: 139 us with those).
-// Bound by the bytes: each 32-byte row of a V tile is written in part.
+// would be 2 bytes each (64 rows x 0-16 drafts x 48 layers, 51 MB read and 51 MB written: 139 us
+// with those, 46 so where the same pages were just written, 80 where they were not, 2.3 and 1.3
+// TB/s).  Bound by the pages' lines: a token has 16 bytes in every 256 of its K tile and 2 in
+// every 32 of its V tile, so the call touches every line of the tiles it writes to, in part:
+// WRITE_SIZE counts 117 MB, 2.3 times the accepted bytes.
 template <typename T>
 __global__ __launch_bounds__(kBlockThreads) void accept_drafts_kernel(const AcceptArgs a) {
     constexpr int x = 16 / sizeof(T);
