@@ -299,7 +299,10 @@ __device__ __forceinline__ int64_t lane_value64(int64_t x, int lane) {
 // whole parts, as many as its share of the workers: no worker then has parts of two tiles,
 // whose starts and ends follow each other.  8 sessions x 8 drafts over 2K tokens: 26.5 us with
 // the ranges below, 22.7 so; 2 x 5 drafts in float32: 16.6 and 14.2.  Taken without looking at
-// the longest part, 32 sessions of 8K to 32K tokens lose (248 us with ranges, 311 so).
+// the longest part, 32 sessions of 8K to 32K tokens lose (248 us with ranges, 311 so).  Parts
+// up to an eighth longer than even ones are taken: tiles of one row, cut alike, read the same
+// keys at the same time, from one L2 (4 sessions x 49-64 drafts, two tiles a row: 219 us with
+// ranges, 207 so); with one tile a row they measure the same.
 // A row per lane.  True where the call is cut so; out.parts is then the number of parts of
 // the worker's tile, 0 for a worker without one.
 template <class C, bool TREE>
@@ -323,7 +326,7 @@ __device__ bool whole_parts(const ChunkArgs& a, int k, const Row& r, Range& out)
     float longest = cost / w;
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) longest = fmaxf(longest, __shfl_xor(longest, d));
-    if (all > most || longest > total / most + kTileCost) return false;
+    if (all > most || longest > 1.125f * (total / most) + kTileCost) return false;
     out.parts = 0;
     if (k >= all) return true;
     const uint64_t has = __builtin_amdgcn_ballot_w64(mine > 0 && upto - mine <= k);

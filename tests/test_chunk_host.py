@@ -137,7 +137,7 @@ def whole_parts(rows, heads, tok, block, tree, most, tile_cost=320):
         w = max(1, min(int(f(most) * cost / max(total, f(1))), blocks[0] // 2 if tiles else 0))
         split.append((tiles, w, blocks))
         longest = max(longest, cost / f(w))
-    if sum(heads * t * w for t, w, _ in split) > most or longest > total / f(most) + f(tile_cost):
+    if sum(heads * t * w for t, w, _ in split) > most or longest > f(1.125) * (total / f(most)) + f(tile_cost):
         return None
     out = []
     for b, (tiles, w, blocks) in enumerate(split):
