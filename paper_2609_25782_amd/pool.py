@@ -230,6 +230,13 @@ class HotColdPool:
             return int(stream.cuda_stream)
         return torch._C._cuda_getCurrentRawStream(self.device.index)
 
+    def _capturing(self, stream) -> bool:
+        """Whether the call's stream, which need not be the current one, is being captured."""
+        if stream is None and torch.cuda.current_device() == self.device.index:
+            return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+            return torch.cuda.is_current_stream_capturing()
+
     def _memory(self, need, like: Optional[torch.Tensor], stream):
         """An output like `like` and, where `need` is not 0, bytes of workspace, both of the call's
         stream: torch hands out memory that another stream may still be using otherwise."""
@@ -242,7 +249,7 @@ class HotColdPool:
         graph's own pool, so that no two graphs share one; other calls keep one per stream."""
         if out is not None:
             assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype and out.device == q.device
-        if torch.cuda.is_current_stream_capturing():
+        if self._capturing(stream):
             new, ws = self._memory(need, q if out is None else None, stream)
             return (new if out is None else out), ws
         ws = self._ws.get(("chunk", st))

@@ -297,6 +297,34 @@ def test_profiling_counts_both_kernels():
         assert n == 1 and ms > 0
 
 
+def test_a_captured_stream_that_is_not_current():
+    """A call on a stream under capture, made while another stream is current, takes its workspace
+    from its graph as well: the graph and eager calls on that stream do not share one."""
+    rows = [(0, 40), (77, 9)]
+    starts, lens = packed(rows)
+    s = Sessions(lens, 8, 2, 64, "bf16", seed=31)
+    q = s.normal(starts[-1], 8, 64)
+    side, dq, dstarts, dlens = torch.cuda.Stream(), q.cuda(), i32(starts), i32(lens)
+    out = torch.empty_like(dq)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    main = torch.cuda.current_stream()
+    with torch.cuda.graph(graph, stream=side):
+        with torch.cuda.stream(main):
+            s.pool.prefill(0, dq, dstarts, dlens, out=out, stream=side)
+    assert not s.pool._ws
+    ref = prefill_reference(s, q, starts, lens)
+    for _ in range(3):
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        got = s.pool.prefill(0, dq, dstarts, dlens, stream=side)
+        torch.cuda.synchronize()
+        check(out, *ref)
+        check(got, *ref)
+    assert s.pool._ws
+
+
 def test_a_length_past_2_30_is_nan():
     """Lengths of more than 2^30 tokens fit no row, however long its table claims to be: NaN, and
     nothing of the table or the pages is read (2^30 tokens of a table that is there would not fit
