@@ -31,14 +31,16 @@
 // take neighbouring ranges: they read the same K/V through the same L2.
 //
 // Bounds and figures (bf16, d = 128, 8 query heads per KV head, 4 KV heads, unless said).
-// Prompt chunks are bound by the products and by power: one prompt of 24,576 tokens takes
+// Prompt chunks are bound by the products and the weights between them: one prompt of 24,576 tokens takes
 // 4.2-4.5 ms = 1.10-1.18 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches
 // 1.19 and of two 16384 x 16384 ones 1.37, both at clocks of about 2 GHz.  Per block
 // of 64 keys and 32 rows a wave issues 64 matrix instructions (1024 cycles) and 144 others, of
-// them 32 exponentials (960 cycles); the matrix cores are busy 52 % of the time.  What was
-// measured and left out: half a block's offset between the two waves of a SIMD by barriers (4.25
-// -> 4.64 ms), the next block's scores between this one's weights (registers spill: 6.0 ms), 64
-// rows per wave (spills as well), wave priorities (no change).  With K and V always in the L2 the
+// them 32 exponentials (960 cycles); the matrix cores are busy 52 % of the time, waves wait for
+// their turn to issue 38 % and for data or the others 24 % of theirs.  What was measured and left
+// out: half a block's offset between the two waves of a SIMD, by two barriers a block (4.25 ->
+// 4.64 ms) or by one that half of the waves pass before their outputs (4.56 -> 4.85 ms, 9.1 -> 10.5
+// M cycles: not the clock), the next block's scores between this one's weights (registers spill:
+// 6.0 ms), 64 rows per wave (spills as well), wave priorities (no change).  With K and V always in the L2 the
 // long prompt would take 8 % less.  Trees of 4-16 drafts over 8K-32K tokens (32 sessions, 1.39
 // GB) are bound by the reads: 242 us = 5.75 TB/s, the attention kernel alone 5.9.  Small calls
 // are bound by the chain of dependent loads and the two launches: 13.5 us for 2 x 5 drafts in
