@@ -297,6 +297,20 @@ def test_profiling_counts_both_kernels():
         assert n == 1 and ms > 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", ["64", "65", "even", "uneven", "several tiles"])
+def test_splits(rows, dtype):
+    """Batches on both sides of a wave's lanes; tiles in equal parts, and where those would be
+    uneven, in ranges; several tiles a row."""
+    r = {"64": [(40 * b % 700, b % 4) for b in range(64)], "65": [(40 * b % 700, b % 4) for b in range(65)],
+         "even": [(3000, 8), (3010, 7), (2900, 8), (2990, 1)], "uneven": [(5000, 8), (3, 7), (90, 8), (2500, 1)],
+         "several tiles": [(3000, 120), (2900, 70), (3100, 33)]}[rows]
+    starts, lens = packed(r)
+    s = Sessions(lens, 8, 1, 128, dtype, seed=32)
+    q = s.normal(starts[-1], 8, 128)
+    check(call(s, q, starts, lens), *prefill_reference(s, q, starts, lens))
+
+
 def test_a_captured_stream_that_is_not_current():
     """A call on a stream under capture, made while another stream is current, takes its workspace
     from its graph as well: the graph and eager calls on that stream do not share one."""

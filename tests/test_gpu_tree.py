@@ -129,6 +129,20 @@ def test_long_context_split_over_the_gpu(width):
     check(call(s, q, kd, vd, masks, lens, drafts), *tree_reference(s, q, kd, vd, masks, lens, drafts))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", ["64", "65", "even", "uneven", "two tiles"])
+def test_splits(rows, dtype):
+    """Batches on both sides of a wave's lanes; tiles in equal parts, and where those would be
+    uneven, in ranges; two tiles a row cut alike."""
+    width, r = {"64": (3, [(40 * b % 700, b % 4) for b in range(64)]),
+                "65": (3, [(40 * b % 700, b % 4) for b in range(65)]),
+                "even": (8, [(3000, 8), (3010, 7), (2900, 8), (2990, 1)]),
+                "uneven": (8, [(5000, 8), (3, 7), (90, 8), (2500, 1)]),
+                "two tiles": (64, [(3000, 64), (2900, 40), (3100, 50)])}[rows]
+    s, lens, drafts, masks, q, kd, vd = setup(r, width, 8, 1, 128, dtype, seed=21)
+    check(call(s, q, kd, vd, masks, lens, drafts), *tree_reference(s, q, kd, vd, masks, lens, drafts))
+
+
 def test_one_draft_is_a_decode_step():
     """A draft that sees itself, accepted, then decoded: decode over C + 1 tokens."""
     rows = [(100, 1), (31, 1), (640, 1)]
