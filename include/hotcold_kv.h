@@ -68,10 +68,10 @@
  *  - A failing call changes nothing: no bookkeeping, no page table, no pages.
  *  - A pool is externally synchronised: one thread at a time.  Work on one
  *    stream is ordered; across streams the caller orders it with events, with
- *    one exception the pool handles itself: hot pages freed by an eviction or
- *    a destroy are not handed out to a call on another stream before the
- *    freeing call's device work has finished, on whichever streams the
- *    freeing calls ran.  Other readers of a session's pages (a decode, a
+ *    one exception the pool handles itself: hot pages freed by an eviction, a
+ *    destroy or a shortening kv_session_reserve are not handed out to a call on
+ *    another stream before the freeing call's device work has finished, on
+ *    whichever streams the freeing calls ran.  Other readers of a session's pages (a decode, a
  *    resume still copying, on another stream) are the caller's to order
  *    before the call that frees those pages, hot or cold.
  */
@@ -235,6 +235,27 @@ int kv_session_create(kv_pool* pool, int32_t seq_len, const int32_t* hot_pages,
 int kv_session_extend(kv_pool* pool, int32_t sid, int32_t new_seq_len, kv_stream_t stream);
 
 /*
+ * Make tokens [kept, new_seq_len) the last ones of an ACTIVE session, to be written by
+ * calls that are resolved on the device and do no bookkeeping (kv_accept_drafts,
+ * kv_append_tokens_table, paged_decode_attention_append).  `kept` is how many tokens the
+ * session really holds: after a step that rejected drafts that is less than its length,
+ * which counts the room made for all of them.  Where only the device knows, any lower
+ * bound will do.  Every page that holds a token of the range counts as written: its cold
+ * copy is dropped and the next eviction writes it again (Sec. III, write-on-evict).  An
+ * eviction gives all pages of a session cold copies, so this call stands between a
+ * session's last eviction or resume and the calls that write to it.  The session's
+ * length becomes new_seq_len, longer or shorter than it was: missing pages are allocated
+ * like kv_session_create's, pages past the new length are released like
+ * kv_session_destroy's and their row entries become -1.  Tokens before `kept` and those
+ * that were written at or past it on pages that stay keep their values.
+ * kv_session_extend is this call with the session's length as `kept`.
+ * Errors: KV_ERR_INVALID (`kept` outside [0, length], new_seq_len below it, row stride),
+ * KV_ERR_STATE (not ACTIVE, or a page that holds a token of the range is spilled to a
+ * cold page shared with another session), KV_ERR_NO_HOT_PAGES, KV_ERR_NO_COLD_PAGES.
+ */
+int kv_session_reserve(kv_pool* pool, int32_t sid, int32_t kept, int32_t new_seq_len, kv_stream_t stream);
+
+/*
  * Pause an ACTIVE session (the agent waits for a tool or a user, Sec. II): no
  * data moves.  Its pages stay in the hot tier but become evictable, least
  * recently used first: the paper evicts LRU blocks, and since active blocks are
@@ -383,9 +404,11 @@ int kv_append_tokens(kv_pool* pool, int32_t layer, const int32_t* sids, const in
  * nothing.  Two entries naming the same token race.
  * The pool's bookkeeping is not read or changed.  Write-on-evict stays exact
  * for tokens that extend a session (positions at or past its length before its
- * last kv_session_extend): the extension already dropped the cold copy of the
- * page the new tokens go into.  Rewriting older tokens this way would leave
- * that page's cold copy stale; use kv_write_tokens for those.
+ * last kv_session_extend, or the `kept` of its last kv_session_reserve, with no
+ * eviction since): that call already dropped the cold copies of the pages the
+ * new tokens go into.  Rewriting older tokens this way, or writing into room made
+ * before an eviction, would leave a cold copy stale; use kv_write_tokens for
+ * those, or call kv_session_reserve again.
  * Errors: KV_ERR_INVALID (layer range, n, NULL or misaligned buffers, table
  * shape, metadata-only pool), KV_ERR_HIP.
  */
@@ -412,8 +435,11 @@ int kv_append_tokens_table(kv_pool* pool, int32_t layer_begin, int32_t num_layer
  * table entry names no page of either pool writes nothing.  The same draft may be
  * named twice; two rows whose tables name the same page race where their tokens
  * meet.  Rejected drafts are never written.
- * As with kv_append_tokens_table the pool's bookkeeping is not read or changed:
- * call kv_session_extend first, to the most tokens that may be accepted.
+ * As with kv_append_tokens_table the pool's bookkeeping is not read or changed.  Before
+ * each step's drafts call kv_session_reserve with the tokens that the session really
+ * holds and, as its length, those and the most that may be accepted, and gather the batch's table
+ * after it.  Without it, tokens accepted into a page whose cold copy still counts as
+ * valid are lost at the session's next eviction, and those past its pages at once.
  * Errors: KV_ERR_INVALID (layer range, batch, width, NULL or misaligned buffers,
  * table shape, metadata-only pool), KV_ERR_HIP.
  */
@@ -698,8 +724,8 @@ int paged_decode_attention(kv_pool* pool, int32_t layer, const void* q, const in
  * whole decode step's attention and KV append, and a serving step captured in
  * a HIP graph holds no append nodes.  A tail entry naming no page writes
  * nothing (and that row decodes to NaN, as in paged_decode_attention).  The
- * pool's bookkeeping is untouched: call kv_session_extend first, which drops
- * the cold copy of the page receiving the token.  A layer with staged entries
+ * pool's bookkeeping is untouched: call kv_session_extend or kv_session_reserve
+ * first, as for kv_append_tokens_table.  A layer with staged entries
  * (paged_decode_prefetch) is refused: the token must go to the page itself.
  * Other arguments and errors as paged_decode_attention.
  */

@@ -34,6 +34,11 @@ Readings where the paper is silent:
   drops that page's cold copy (and, for a spilled tail page shared with another
   session, is refused), so appends whose page is resolved on the device need no
   bookkeeping of their own.
+* A session may be longer than what it really holds: room for drafts of which
+  some were rejected.  Reserving tokens [kept, new length) says how many it
+  holds; every page with a token of that range counts as written (refused if
+  one is spilled to a shared cold page), and pages past the new length are
+  freed.  Extending is reserving from the session's length on.
 * Cold pages may be shared by several paused sessions (a virtualised cold
   pool); they are reference counted and freed when the last user lets go.
 * Every failing call leaves the whole state unchanged.
@@ -401,6 +406,37 @@ class PoolModel:
             if c >= 0:
                 self._release_cold(c)
         self.sessions[sid] = _Session()
+
+    def reserve(self, sid: int, kept: int, new_len: int) -> None:
+        """Tokens [kept, new_len) become the last ones and count as written."""
+        s = self._session(sid)
+        if s.state != ACTIVE:
+            raise ModelError(ERR_STATE, "not active")
+        if not 0 <= kept <= s.seq_len or new_len < kept or _pages(new_len) > self.stride:
+            raise ModelError(ERR_INVALID, "bad length")
+        have, want = len(s.hot), _pages(new_len)
+        written = [i for i in sorted({t // PAGE_TOKENS for t in range(kept, new_len)}) if i < have]
+        if any(s.hot[i] < 0 and self.cold_ref[s.cold[i]] > 1 for i in written):
+            raise ModelError(ERR_STATE, "spilled page shared with another session")
+        victims, cold, pages, spill = self._plan(max(want - have, 0))
+        self.last_victim_copies = self._evict_victims(victims, cold)
+        self._take_hot(pages)
+        self._take_cold(spill)
+        for i in written:
+            if s.hot[i] >= 0 and s.cold[i] >= 0:
+                self._release_cold(s.cold[i])
+                s.cold[i] = -1
+        while len(s.hot) > want:              # pages past the new length are let go
+            h, c = s.hot.pop(), s.cold.pop()
+            s.spilled.pop()
+            if h >= 0:
+                self.hot_free.add(h)
+            if c >= 0:
+                self._release_cold(c)
+        s.hot += list(pages) + [-1] * len(spill)
+        s.cold += [-1] * len(pages) + list(spill)
+        s.spilled += [False] * len(pages) + [True] * len(spill)
+        s.seq_len = new_len
 
     def promote(self, n: int):
         """Move up to n spilled pages of active sessions to the hot tier.

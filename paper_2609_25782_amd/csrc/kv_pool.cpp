@@ -670,6 +670,62 @@ struct kv_pool {
         }
     }
 
+    // Make tokens [kept, new_seq_len) of an ACTIVE session its last ones, to be
+    // written by calls that are resolved on the device and so do no bookkeeping:
+    // every page that holds one of them counts as written (its cold copy goes
+    // stale), and a spilled one shared with another session cannot be.  Pages
+    // that are missing are allocated, pages past the new length are released.
+    int reserve(int32_t sid, int32_t kept, int32_t new_seq_len, kv_stream_t stream) {
+        Session& s = sessions[sid];
+        const int32_t n_old = static_cast<int32_t>(s.hot.size());
+        const int32_t n_new = pages_of(new_seq_len);
+        if (n_new > d.max_pages_per_session)
+            return fail(KV_ERR_INVALID, "%d pages exceed the row stride %d", n_new, d.max_pages_per_session);
+        // pages that are there already and hold such tokens
+        const int32_t first = kept / KV_PAGE_TOKENS;
+        const int32_t end = new_seq_len > kept ? std::min(n_old, n_new) : first;
+        for (int32_t i = first; i < end; ++i)
+            if (s.hot[i] < 0 && cold_ref[s.cold[i]] > 1)
+                return fail(KV_ERR_STATE, "page %d is spilled to a cold page shared with another session", i);
+        Alloc a;
+        int rc = plan_alloc(std::max(n_new - n_old, 0), {}, a);
+        if (rc) return rc;
+        const std::vector<int32_t> entries = n_new < n_old ? std::vector<int32_t>(n_old - n_new, -1) : new_entries(a);
+        if (!meta && n_new != n_old) {
+            DeviceGuard g(d.device);
+            hipStream_t st = strm(stream);
+            rc = order_after_frees(st);
+            if (!rc) rc = submit_victims(a, st);
+            if (!rc) rc = submit_row_at(sid, std::min(n_old, n_new), entries.data(), static_cast<int32_t>(entries.size()), st);
+            if (!rc && n_new < n_old) rc = note_frees(st);
+            if (rc) return rc;
+        }
+        commit_victims(a);
+        commit_spill(a);
+        for (int32_t p : a.pages) hot_free.take(p);
+        for (int32_t i = first; i < end; ++i)
+            if (s.hot[i] >= 0 && s.cold[i] >= 0) {   // a spilled page is written in place
+                release_cold(s.cold[i]);
+                s.cold[i] = -1;
+            }
+        for (int32_t i = n_new; i < n_old; ++i) {
+            if (s.hot[i] >= 0) hot_free.give(s.hot[i]);
+            if (s.cold[i] >= 0) release_cold(s.cold[i]);
+        }
+        const int32_t stay = std::min(n_old, n_new), hot_end = stay + static_cast<int32_t>(a.pages.size());
+        s.hot.resize(stay);
+        s.hot.insert(s.hot.end(), a.pages.begin(), a.pages.end());
+        s.hot.resize(n_new, -1);
+        s.cold.resize(stay);
+        s.cold.resize(hot_end, -1);
+        s.cold.insert(s.cold.end(), a.spill_cold.begin(), a.spill_cold.end());
+        s.spilled.resize(stay);
+        s.spilled.resize(hot_end, 0);
+        s.spilled.resize(n_new, 1);
+        s.seq_len = new_seq_len;
+        return KV_OK;
+    }
+
     int32_t new_sid() const {
         for (int32_t i = 0; i < d.max_sessions; ++i)
             if (sessions[i].state == KV_SESSION_FREE) return i;
@@ -870,45 +926,17 @@ int kv_session_extend(kv_pool* pool, int32_t sid, int32_t new_seq_len, kv_stream
     if (!s) return fail(KV_ERR_INVALID, "bad session id %d", sid);
     if (s->state != KV_SESSION_ACTIVE) return fail(KV_ERR_STATE, "session %d is not active", sid);
     if (new_seq_len < s->seq_len) return fail(KV_ERR_INVALID, "a session only grows");
-    const int32_t n_old = static_cast<int32_t>(s->hot.size());
-    const int32_t n_new = pages_of(new_seq_len);
-    if (n_new > pool->d.max_pages_per_session)
-        return fail(KV_ERR_INVALID, "%d pages exceed the row stride %d", n_new,
-                    pool->d.max_pages_per_session);
-    // The new tokens go into the partially filled tail page, if any: extending
-    // counts as writing it (so appends resolved on the device need no
-    // bookkeeping), and a spilled tail page shared with another session cannot
-    // be written.
-    const int32_t tail = (new_seq_len > s->seq_len && s->seq_len % KV_PAGE_TOKENS) ? s->seq_len / KV_PAGE_TOKENS : -1;
-    if (tail >= 0 && s->hot[tail] < 0 && pool->cold_ref[s->cold[tail]] > 1)
-        return fail(KV_ERR_STATE, "tail page %d is spilled to a cold page shared with another session", tail);
-    Alloc a;
-    int rc = pool->plan_alloc(std::max(n_new - n_old, 0), {}, a);
-    if (rc) return rc;
-    const std::vector<int32_t> entries = kv_pool::new_entries(a);
-    if (!pool->meta && n_new > n_old) {
-        DeviceGuard g(pool->d.device);
-        hipStream_t st = pool->strm(stream);
-        rc = pool->order_after_frees(st);
-        if (!rc) rc = pool->submit_victims(a, st);
-        if (!rc) rc = pool->submit_row_at(sid, n_old, entries.data(), n_new - n_old, st);
-        if (rc) return rc;
-    }
-    pool->commit_victims(a);
-    pool->commit_spill(a);
-    for (int32_t p : a.pages) pool->hot_free.take(p);
-    if (tail >= 0 && s->hot[tail] >= 0 && s->cold[tail] >= 0) {  // its cold copy goes stale
-        pool->release_cold(s->cold[tail]);
-        s->cold[tail] = -1;
-    }
-    s->hot.insert(s->hot.end(), a.pages.begin(), a.pages.end());
-    s->hot.resize(n_new, -1);
-    s->cold.resize(n_old + a.pages.size(), -1);
-    s->cold.insert(s->cold.end(), a.spill_cold.begin(), a.spill_cold.end());
-    s->spilled.resize(n_old + a.pages.size(), 0);
-    s->spilled.resize(n_new, 1);
-    s->seq_len = new_seq_len;
-    return KV_OK;
+    return pool->reserve(sid, s->seq_len, new_seq_len, stream);
+}
+
+int kv_session_reserve(kv_pool* pool, int32_t sid, int32_t kept, int32_t new_seq_len, kv_stream_t stream) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    Session* s = pool->session(sid);
+    if (!s) return fail(KV_ERR_INVALID, "bad session id %d", sid);
+    if (s->state != KV_SESSION_ACTIVE) return fail(KV_ERR_STATE, "session %d is not active", sid);
+    if (kept < 0 || kept > s->seq_len) return fail(KV_ERR_INVALID, "kept %d outside [0, %d]", kept, s->seq_len);
+    if (new_seq_len < kept) return fail(KV_ERR_INVALID, "length %d below the %d kept tokens", new_seq_len, kept);
+    return pool->reserve(sid, kept, new_seq_len, stream);
 }
 
 int kv_session_pause(kv_pool* pool, int32_t sid) {

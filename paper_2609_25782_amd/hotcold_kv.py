@@ -79,6 +79,7 @@ _SIGS = {
     "kv_session_create": (ctypes.c_int, [_P, _I32, _PI32, _P, _PI32]),
     "kv_session_import_cold": (ctypes.c_int, [_P, _I32, _PI32, _PI32]),
     "kv_session_extend": (ctypes.c_int, [_P, _I32, _I32, _P]),
+    "kv_session_reserve": (ctypes.c_int, [_P, _I32, _I32, _I32, _P]),
     "kv_session_pause": (ctypes.c_int, [_P, _I32]),
     "kv_evict_pages": (ctypes.c_int, [_P, _I32, _P, _PI32]),
     "kv_session_destroy": (ctypes.c_int, [_P, _I32, _P]),
@@ -206,6 +207,10 @@ def kv_session_import_cold(pool: int, seq_len: int, cold_pages: Sequence[int]) -
 
 def kv_session_extend(pool: int, sid: int, new_seq_len: int, stream: int = 0) -> None:
     _check(_lib.kv_session_extend(pool, sid, new_seq_len, stream or None), "kv_session_extend")
+
+
+def kv_session_reserve(pool: int, sid: int, kept: int, new_seq_len: int, stream: int = 0) -> None:
+    _check(_lib.kv_session_reserve(pool, sid, kept, new_seq_len, stream or None), "kv_session_reserve")
 
 
 def kv_session_pause(pool: int, sid: int) -> None:

@@ -100,6 +100,11 @@ class HotColdPool:
     def extend(self, sid: int, new_seq_len: int, stream=None) -> None:
         kv.kv_session_extend(self.handle, sid, int(new_seq_len), _stream(stream))
 
+    def reserve(self, sid: int, kept: int, new_seq_len: int, stream=None) -> None:
+        """Tokens [kept, new_seq_len) become the session's last ones, to be written by accept_drafts or
+        append_tokens_table; `kept` is how many it really holds (rejected drafts forgotten), or fewer."""
+        kv.kv_session_reserve(self.handle, sid, int(kept), int(new_seq_len), _stream(stream))
+
     def pause(self, sid: int) -> None:
         kv.kv_session_pause(self.handle, sid)
 
