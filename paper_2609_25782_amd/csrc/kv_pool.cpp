@@ -1617,6 +1617,14 @@ int paged_decode_attention_append(kv_pool* pool, int32_t layer, const void* q, c
 
 namespace {
 
+constexpr int32_t kMaxGroup = 16;   // query heads per KV head of prompt chunks and draft trees
+
+// Whether prompt chunks and draft trees take this batch and these heads: else they need no workspace.
+bool chunk_shape_ok(const kv_pool* pool, int32_t batch, int32_t num_q_heads) {
+    return pool && !pool->meta && batch >= 0 && batch <= kMaxDecodeBatch && num_q_heads > 0 &&
+           num_q_heads % pool->d.num_kv_heads == 0 && num_q_heads / pool->d.num_kv_heads <= kMaxGroup;
+}
+
 // Checks and arguments that prompt chunks and draft trees share.
 int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
                const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, float scale, void* out, hck::ChunkArgs& a) {
@@ -1626,7 +1634,8 @@ int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_
     if (num_q_heads <= 0 || num_q_heads % pool->d.num_kv_heads)
         return fail(KV_ERR_INVALID, "query heads %d not a multiple of KV heads %d", num_q_heads,
                     pool->d.num_kv_heads);
-    if (num_q_heads / pool->d.num_kv_heads > 16) return fail(KV_ERR_INVALID, "more than 16 query heads per KV head");
+    if (num_q_heads / pool->d.num_kv_heads > kMaxGroup)
+        return fail(KV_ERR_INVALID, "more than %d query heads per KV head", kMaxGroup);
     if (pt_stride < 1 || static_cast<int64_t>(batch) * pt_stride >= (int64_t(1) << 31))
         return fail(KV_ERR_INVALID, "bad page-table stride");
     if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15)
@@ -1692,8 +1701,7 @@ int chunk_launch(kv_pool* pool, hck::ChunkArgs& a, int64_t rows_per_seq, bool tr
 extern "C" {
 
 size_t paged_prefill_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t total_q, int32_t num_q_heads) {
-    if (!pool || pool->meta || batch < 0 || total_q < 0 || num_q_heads <= 0 || num_q_heads % pool->d.num_kv_heads)
-        return 0;
+    if (!chunk_shape_ok(pool, batch, num_q_heads) || total_q < 0) return 0;
     if (batch == 0) return 256;
     const hck::ChunkPlan plan = hck::chunk_plan(pool->cus, prefill_rows(pool, batch, total_q, num_q_heads));
     return hck::chunk_workspace_bytes(plan, pool->d.head_dim);
@@ -1719,9 +1727,7 @@ int paged_prefill_attention(kv_pool* pool, int32_t layer, const void* q, const i
 }
 
 size_t paged_tree_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t width, int32_t num_q_heads) {
-    if (!pool || pool->meta || batch < 0 || width < 1 || width > KV_MAX_DRAFTS || num_q_heads <= 0 ||
-        num_q_heads % pool->d.num_kv_heads)
-        return 0;
+    if (!chunk_shape_ok(pool, batch, num_q_heads) || width < 1 || width > KV_MAX_DRAFTS) return 0;
     const int32_t group = num_q_heads / pool->d.num_kv_heads;
     return hck::chunk_workspace_bytes(hck::chunk_plan(pool->cus, static_cast<int64_t>(width) * group),
                                       pool->d.head_dim);

@@ -391,3 +391,21 @@ def test_refusals():
         args.update(wrong)
         with pytest.raises(AssertionError):
             s.pool.prefill(**args)
+
+
+@pytest.mark.parametrize("hkv", [1, 2])
+def test_workspace_sizes_know_what_is_refused(hkv):
+    """0 for the batches and heads that the calls refuse, and for no others."""
+    pool = Sessions([40], 4 * hkv, hkv, 64, "bf16", seed=19).pool
+    sizes = {"prefill": lambda batch, heads: kv.paged_prefill_workspace_bytes(pool.handle, batch, 16, heads),
+             "tree": lambda batch, heads: kv.paged_tree_workspace_bytes(pool.handle, batch, 4, heads)}
+    for name, size in sizes.items():
+        for batch in (0, 1, 8192):
+            for heads in (hkv, 3 * hkv, 16 * hkv):
+                assert size(batch, heads) > 0, (name, batch, heads)
+        for batch, heads in ((8193, hkv), (1 << 30, hkv), (-1, hkv), (1, 17 * hkv), (1, 32 * hkv), (1, 0), (1, -hkv),
+                             (0, 17 * hkv)):
+            assert size(batch, heads) == 0, (name, batch, heads)
+    assert kv.paged_prefill_workspace_bytes(pool.handle, 1, -1, hkv) == 0
+    for width in (0, -1, 65):
+        assert kv.paged_tree_workspace_bytes(pool.handle, 1, width, hkv) == 0
