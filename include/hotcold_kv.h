@@ -796,7 +796,9 @@ size_t paged_prefill_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t
  * into a HIP graph (two kernels, nothing else) may be replayed after they change, for
  * the same batch and total_q.  Concurrent calls need workspaces of their own.
  * Numerics: float32 scores, maximum, sum and output; bf16 pools round the softmax
- * weights to bf16 for the weighted sum of V, and the output once.  The result does not
+ * weights to bf16 for the weighted sum of V, and the output once.  A weight below 2^-126 of
+ * the query's largest counts as 0.  Weights, the largest between 1 and 2^8, are summed with V
+ * before the division by their sum, so values of V past 2^120 / L may overflow.  The result does not
  * depend on where pages sit; it does depend, in float32 rounding, on the lengths of the
  * batch's other rows, which move the cuts of the work split.
  * num_q_heads / num_kv_heads must be an integer in 1 .. 16.
