@@ -791,7 +791,8 @@ size_t paged_prefill_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t
  * A query sees its own tokens only: whatever later tokens of its row, other slots of the
  * tail page and pages past it hold, NaN and infinities included, does not change it.
  * A query that attends to a token on a page outside the pools (or on a staged copy,
- * which only the decode reads) gets NaN.  Spilled pages (KV_PAGE_COLD) are read in place.
+ * which only the decode reads) gets NaN, and so does one all of whose scores are minus
+ * infinity.  Spilled pages (KV_PAGE_COLD) are read in place.
  * q_starts, seq_lens and the page table are read when the kernels run: a call captured
  * into a HIP graph (two kernels, nothing else) may be replayed after they change, for
  * the same batch and total_q.  Concurrent calls need workspaces of their own.
@@ -838,7 +839,7 @@ size_t paged_tree_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t wi
  *   out               device, like q
  *   workspace         device, >= paged_tree_workspace_bytes(), 256-byte aligned
  *
- * A draft that attends to nothing (C = 0 and an empty mask) gets zeros.  What a draft
+ * A draft that attends to nothing (C = 0 and no bit below n) gets zeros.  What a draft
  * does not attend to does not change it, NaN and infinities included.  Page ids, spilled
  * pages, capture, concurrent calls, numerics and errors as paged_prefill_attention.
  */

@@ -49,6 +49,7 @@
 #include "device_common.h"
 #include "kernels.h"
 
+#include <float.h>
 #include <math.h>
 
 #include <atomic>
@@ -1155,6 +1156,11 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
             bool bad = row.bad;
             bad |= s_bad != 0;   // set by fetches before the last turn's barrier
 
+            // Whether a row attends to anything at all: to tokens whose scores are all minus infinity the
+            // weights are 0 / 0, to nothing the output is zero.
+            const auto attends = [&](int n) {
+                return !TREE || row.ctx > 0 || (seen[n] & (~0ull >> (64 - row.n))) != 0;
+            };
             // the rows' sums over their four lanes
             float l[C::kNT];
 #pragma unroll
@@ -1166,8 +1172,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
             if (k0 == 0 && k1 == nb) {
 #pragma unroll
                 for (int n = 0; n < C::kNT; ++n) {
-                    // l = 0: nothing to attend to, the output is zero; NaN stays NaN
-                    const float inv = l[n] == 0.f ? 0.f : 1.f / l[n];
+                    const float inv = l[n] == 0.f ? (attends(n) ? NAN : 0.f) : 1.f / l[n];
                     char* out = static_cast<char*>(a.out) + (qrow[n] + 4 * gq) * C::kElt;
                     if (live[n]) {
 #pragma unroll
@@ -1186,7 +1191,8 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                     for (int c = 0; c < C::kC; ++c)
                         *reinterpret_cast<f32x4*>(po + r * C::kD + c * 16 + 4 * gq) = st.o[n][c];
                     if (gq == 0) {
-                        pm[r] = st.m[n] == -INFINITY ? -INFINITY : st.m[n] * a.scale_log2;
+                        // (finite wherever the row attends to anything, in this part or another)
+                        pm[r] = attends(n) ? fmaxf(st.m[n] * a.scale_log2, -FLT_MAX) : -INFINITY;
                         pm[C::kRows + r] = l[n];
                     }
                 }
@@ -1227,7 +1233,7 @@ struct Merge {
     float top = -INFINITY, den = 0.f;
     __device__ __forceinline__ void join(float m, float l, const f32x4& o) {
         const float t = fmaxf(top, m);
-        // (1 for a part without a maximum, which holds 0, or an infinity or NaN that has to stay)
+        // (1 for a lane without a part, or parts of a row that attends to nothing: they hold 0)
         const Factor w0(top == -INFINITY ? 0.f : top - t), w1(m == -INFINITY ? 0.f : m - t);
         acc = acc * w0.f * w0.g + o * w1.f * w1.g;
         den = den * w0.f + l * w1.f;
@@ -1244,7 +1250,7 @@ struct Merge {
         }
         if (sub == 0 && r < rec.rows) {
             const int64_t q = rec.first + static_cast<int64_t>(r / a.group) * a.num_q_heads + r % a.group;
-            const float inv = den == 0.f ? 0.f : 1.f / den;
+            const float inv = den == 0.f ? (top == -INFINITY ? 0.f : NAN) : 1.f / den;
             store4(a, C::kBf16, static_cast<char*>(a.out) + (q * C::kD + col * 4) * C::kElt, acc * inv);
         }
     }

@@ -1,5 +1,5 @@
 """Prompt and tree attention where numbers reach the ends of their range: weights that underflow
-beside values near the largest."""
+beside values near the largest, and scores of minus infinity."""
 
 import numpy as np
 import pytest
@@ -47,3 +47,61 @@ def test_underflowing_weights_add_nothing(tokens, high, dtype, d):
                              i32([tokens]), scale=1.0)
     for i in range(2):
         check(got[0, i:i + 1], ref, bound, what="draft %d" % i)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+def test_scores_of_minus_infinity_in_prompts(dtype, d):
+    """A query all of whose scores are minus infinity has no softmax: NaN, as from decode; beside any
+    other score such a token has no weight."""
+    first, n = 70, 150
+    s = Sessions([n, 9000, 9000], 4, 1, d, dtype, seed=51)
+    qs, refs, bounds = [], [], []
+    for b, (tokens, new, low) in enumerate(((n, n, range(first)), (9000, 2, range(9000)), (9000, 2, range(16, 9000)))):
+        scores = s.normal(tokens).float().tolist()
+        for t in low:
+            scores[t] = float("-inf")
+        q = scored(s, b, scores, 4, new)
+        q[:, :, 1:] = 0.5          # against zeros
+        seen = np.arange(tokens)[None, :] <= (tokens - new + np.arange(new))[:, None]
+        seen[:, list(low)] = False
+        ref, bound = attend(q, s.k[b][0], s.v[b][0], seen, 1.0, dtype)
+        ref[~seen.any(axis=1)] = np.nan
+        qs.append(q), refs.append(ref), bounds.append(bound)
+    q, ref, bound = torch.cat(qs), np.concatenate(refs), np.concatenate(bounds)
+    assert np.isnan(ref).any(axis=(1, 2)).tolist() == [True] * first + [False] * (n - first) + [True] * 2 + [False] * 2
+    starts = [0, n, n + 2, n + 4]
+    got = s.pool.prefill(0, q.cuda(), i32(starts), i32([n, 9000, 9000]), scale=1.0)
+    check(got, ref, bound)
+    alone = s.pool.prefill(0, q[n:n + 2].contiguous().cuda(), i32([0, 2]), i32([9000]),
+                           page_table=s.pool.page_table[1:2].contiguous(), scale=1.0)
+    assert alone.isnan().all()
+    dec = s.pool.decode(0, q[[0, n + 1]].contiguous().cuda(), i32([1, 9000]),
+                        page_table=s.pool.page_table[:2].contiguous(), scale=1.0)
+    assert dec.isnan().all()
+
+
+@pytest.mark.parametrize("width", [6, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ctx", [0, 30, 9000])
+def test_scores_of_minus_infinity_in_trees(ctx, dtype, width):
+    """The same for drafts: NaN where everything that a draft sees scores minus infinity, zeros
+    where it sees nothing, and no weight beside other scores."""
+    d, hq = 64, 4
+    s = Sessions([ctx], hq, 1, d, dtype, seed=52)
+    q = torch.zeros((1, width, hq, d), dtype=s.k[0].dtype)
+    q[..., 0] = 1
+    if ctx:
+        scored(s, 0, [float("-inf")] * ctx, hq, 1)
+    kd, vd = torch.zeros((1, width, 1, d), dtype=q.dtype), s.normal(1, width, 1, d)
+    kd[0, :, 0, 0] = float("-inf")
+    kd[0, 1, 0, 0] = 2.0
+    last = 1 << (width - 1)
+    masks = [1, 2, 3, 0, last, last | 2] + [last | 1] * (width - 6)
+    got = s.pool.tree_decode(0, q.cuda(), kd.cuda(), vd.cuda(), mask_tensor([masks]), i32([ctx]), scale=1.0)
+    ref, bound = np.zeros(tuple(q.shape)), np.zeros(tuple(q.shape))
+    for i, m in enumerate(masks):
+        if m & 2:                        # draft 1 alone counts
+            ref[0, i], bound[0, i] = (x[0] for x in attend(q[0, i:i + 1], kd[0, 1:2], vd[0, 1:2], np.ones((1, 1), bool), 1.0, dtype))
+        elif m or ctx:
+            ref[0, i] = np.nan
+    check(got, ref, bound)
