@@ -46,6 +46,7 @@
 // are bound by the chain of dependent loads and the two launches: 13.5 us for 2 x 5 drafts in
 // float32, 10 of them in this kernel and 2.5-4 in the merge.  No LDS bank conflicts are counted.
 
+#include "chunk_split.h"
 #include "device_common.h"
 #include "kernels.h"
 
@@ -95,52 +96,6 @@ struct Cfg {
     static_assert(!BF16 || kPages % 2 == 0, "bf16 fragments take pages in pairs");
 };
 
-// What one row b brings: n tokens (or drafts), `ctx` tokens before them, the row's units.
-struct Row {
-    int start;     // first query of the row in q (tokens)
-    int n;         // queries
-    int ctx;       // cached tokens that every query sees
-    int bad;       // 1: lengths that do not fit, the row's outputs are NaN
-    int tiles;     // tiles per KV head
-    int64_t base;  // keys of tile i < tiles - 1: base + slope (i + 1)
-    int64_t slope;
-    int64_t last;  // keys of the last tile
-    // First unit of tile i, and all units of one KV head, where a tile costs its keys and `cost` more.
-    __device__ int64_t tile_start(int64_t i, int cost) const {
-        return i * (base + cost) + slope * (i * (i + 1) / 2);
-    }
-    __device__ int64_t head_units(int cost) const { return tiles ? tile_start(tiles - 1, cost) + last + cost : 0; }
-};
-
-// What a tile costs beside its keys, in keys: its queries' load, its output, the pipeline's
-// start and the masked blocks.  kTileCost is what balances calls with work for every worker
-// (twelve packed prompts, on one build: 64: 1879 us, 192: 1453, 320: 1220, 448: 1241, 640:
-// 1282); calls with less than that are cut finer, with kTileCostFine (8 sessions x 8 drafts
-// over 2K tokens: 64: 39.8 us, 320: 41.7).
-constexpr int kTileCost = 320, kTileCostFine = 64;
-
-// The units of a row that brings n queries after ctx tokens.
-template <class C, bool TREE>
-__device__ __forceinline__ Row make_row(const ChunkArgs& a, int start, int n, int ctx, int bad) {
-    Row r;
-    r.start = start;
-    r.n = n;
-    r.ctx = ctx;
-    r.bad = bad;
-    r.tiles = (n + a.tile_tokens - 1) / a.tile_tokens;
-    r.slope = 0;
-    if (bad) {
-        r.base = r.last = 0;
-    } else if constexpr (TREE) {
-        r.base = r.last = static_cast<int64_t>((n + C::kBlock - 1) / C::kBlock) * C::kBlock + ctx;
-    } else {
-        r.base = ctx;
-        r.slope = a.tile_tokens;
-        r.last = r.base + n;
-    }
-    return r;
-}
-
 template <class C, bool TREE>
 __device__ __forceinline__ Row row_info(const ChunkArgs& a, int b) {
     // (2^30 tokens at most, so that places of keys stay in 32 bits)
@@ -158,30 +113,8 @@ __device__ __forceinline__ Row row_info(const ChunkArgs& a, int b) {
         n = in ? e - s : 0;
     }
     const int bad = len < (TREE ? 0 : n) || len > most;
-    return make_row<C, TREE>(a, start, n, bad ? 0 : (TREE ? len : len - n), bad);
+    return make_row<C, TREE>(a.tile_tokens, start, n, bad ? 0 : (TREE ? len : len - n), bad);
 }
-
-// Blocks of tile i: the drafts' first (trees), then the context's.
-template <class C, bool TREE>
-__device__ __forceinline__ int draft_blocks(const Row& r) {
-    return TREE && !r.bad ? (r.n + C::kBlock - 1) / C::kBlock : 0;
-}
-template <class C, bool TREE>
-__device__ __forceinline__ int tile_keys(const ChunkArgs& a, const Row& r, int i) {
-    if (r.bad) return 0;
-    if (TREE) return r.ctx;
-    const int64_t hi = static_cast<int64_t>(i + 1) * a.tile_tokens;
-    return r.ctx + (hi < r.n ? static_cast<int>(hi) : r.n);
-}
-template <class C, bool TREE>
-__device__ __forceinline__ int tile_blocks(const ChunkArgs& a, const Row& r, int i) {
-    return draft_blocks<C, TREE>(r) + (tile_keys<C, TREE>(a, r, i) + C::kBlock - 1) / C::kBlock;
-}
-
-// A place in the order of blocks: block `blk` of tile `tile` of (row b, KV head g).
-struct Place {
-    int b, g, tile, blk;
-};
 
 // What a worker takes: the blocks from `from` up to `to`.  Where `to` lies inside a tile,
 // `parts` is the number of workers that share that tile from this one on.
@@ -191,97 +124,9 @@ struct Range {
     int parts;
 };
 
-// How the call's units are cut: `total` units over `workers` equal ranges, a tile costing its
-// keys and `cost` more.
-struct Cuts {
-    int64_t total;
-    int workers, cost;
-    __device__ int64_t at(int k) const {   // floor(k total / workers), in 32 bits where they do
-        if ((total >> 32) == 0) {
-            const unsigned t = static_cast<unsigned>(total), w = static_cast<unsigned>(workers);
-            const unsigned q = t / w, m = t - q * w, n = static_cast<unsigned>(k);
-            return static_cast<int64_t>(n * q + n * m / w);
-        }
-        return k * (total / workers) + k * (total % workers) / workers;
-    }
-};
-
-// Enough units for a block or more in every range (see place_of).
-template <class C>
-__device__ __forceinline__ Cuts cuts_of(const ChunkArgs& a, int64_t keys, int64_t tiles) {
-    const int most = a.workers;
-    Cuts c;
-    c.cost = kTileCost;
-    if (keys + c.cost * tiles < static_cast<int64_t>(c.cost + 2 * C::kBlock) * most) c.cost = kTileCostFine;
-    c.total = keys + c.cost * tiles;
-    const int64_t n = (c.total >> 32) == 0
-                          ? static_cast<int64_t>(static_cast<unsigned>(c.total) / static_cast<unsigned>(c.cost + 2 * C::kBlock))
-                          : most;
-    c.workers = c.total <= 0 ? 0 : static_cast<int>(n < 1 ? 1 : (n > most ? most : n));
-    return c;
-}
-
-// The place of unit `u` of row b (0 <= u < its units).  Both workers at a cut compute it
-// from the same numbers, so their ranges meet without a gap; a place past a tile's last
-// block is the next tile's first.  A tile without blocks belongs to the worker that has
-// its first unit.  Ranges of at least cost + 2 kBlock units hold one block or more.
-// `more`: for a place inside a tile, how many units further a cut still lies inside it.
-template <class C, bool TREE>
-__device__ __forceinline__ Place place_of(const ChunkArgs& a, const Row& r, int b, int64_t u, int cost, int64_t& more) {
-    Place p;
-    p.b = b;
-    const int64_t h = r.head_units(cost);
-    if (((u | h) >> 32) == 0) {
-        p.g = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(h));
-    } else {
-        p.g = static_cast<int>(u / h);
-    }
-    int64_t rem = u - p.g * h;
-    int lo = 0, hi = r.tiles - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (r.tile_start(mid, cost) <= rem) lo = mid; else hi = mid - 1;
-    }
-    rem -= r.tile_start(lo, cost);
-    p.tile = lo;
-    p.blk = 0;
-    more = 0;
-    if (rem > 0) {
-        const int64_t x = rem - cost;
-        const int nb = tile_blocks<C, TREE>(a, r, lo);
-        const int64_t k = x <= 0 ? 0 : (x + C::kBlock - 1) / C::kBlock;
-        p.blk = k < nb ? static_cast<int>(k) : nb;
-        more = static_cast<int64_t>(nb - 1) * C::kBlock - x;
-        if (p.blk == nb) {
-            p.blk = 0;
-            if (++p.tile == r.tiles) {
-                p.tile = 0;
-                ++p.g;    // may be the number of KV heads: the walk moves on to the next row
-            }
-        }
-    }
-    return p;
-}
-
 __device__ __forceinline__ Place uniform_place(const Place& p) {
     return Place{__builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.g),
                  __builtin_amdgcn_readfirstlane(p.tile), __builtin_amdgcn_readfirstlane(p.blk)};
-}
-
-__device__ __forceinline__ bool before(const Place& x, const Place& y) {
-    if (x.b != y.b) return x.b < y.b;
-    if (x.g != y.g) return x.g < y.g;
-    if (x.tile != y.tile) return x.tile < y.tile;
-    return x.blk < y.blk;
-}
-
-// The last worker whose range begins at unit `u` or before.
-__device__ __forceinline__ int worker_at(const Cuts& c, int64_t u) {
-    const int64_t n = (u + 1) * c.workers - 1;
-    const int64_t k = ((n | c.total) >> 32) == 0
-                          ? static_cast<int64_t>(static_cast<unsigned>(n) / static_cast<unsigned>(c.total))
-                          : n / c.total;
-    return k < c.workers ? static_cast<int>(k) : c.workers - 1;
 }
 
 // Inclusive sum over the lanes of a wave of numbers below 2^52.
@@ -297,58 +142,39 @@ __device__ __forceinline__ int64_t lane_value64(int64_t x, int lane) {
     return static_cast<int64_t>(lo) | (static_cast<int64_t>(hi) << 32);
 }
 
-// Where no more than `workers` tiles have about the same cost in each row (drafts, short
-// chunks over long contexts) and equal parts of them differ little, every tile is cut into
-// whole parts, as many as its share of the workers: no worker then has parts of two tiles,
-// whose starts and ends follow each other.  8 sessions x 8 drafts over 2K tokens: 26.5 us with
-// the ranges below, 22.7 so; 2 x 5 drafts in float32: 16.6 and 14.2.  Taken without looking at
-// the longest part, 32 sessions of 8K to 32K tokens lose (248 us with ranges, 311 so).  Parts
-// up to an eighth longer than even ones are taken: tiles of one row, cut alike, read the same
-// keys at the same time, from one L2 (4 sessions x 49-64 drafts, two tiles a row: 219 us with
-// ranges, 207 so); with one tile a row they measure the same.
-// A row per lane.  True where the call is cut so; out.parts is then the number of parts of
-// the worker's tile, 0 for a worker without one.
+// The split into whole parts, a row per lane.  True where the call is cut so; out.parts is then the
+// number of parts of the worker's tile, 0 for a worker without one.
 template <class C, bool TREE>
 __device__ bool whole_parts(const ChunkArgs& a, int k, const Row& r, Range& out) {
     const int heads = a.num_kv_heads;
     const int most = a.workers;
-    const bool even = r.tiles <= 1 || r.slope == 0 || static_cast<int64_t>(r.n) * 4 <= r.ctx;
-    if (__builtin_amdgcn_ballot_w64(!even)) return false;
+    if (__builtin_amdgcn_ballot_w64(!even_tiles(r))) return false;
     if (__builtin_amdgcn_ballot_w64(static_cast<int64_t>(heads) * r.tiles > most)) return false;
     const int count = heads * r.tiles;       // tiles of the row (rows without queries: none)
-    const float cost = r.tiles ? static_cast<float>(r.last) : 0.f;
+    const float cost = tile_cost(r);
     float total = cost * count;
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) total += __shfl_xor(total, d);
-    int w = static_cast<int>(most * cost / fmaxf(total, 1.f));
-    const int nb = r.tiles ? tile_blocks<C, TREE>(a, r, 0) : 0;      // of its shortest tile
-    w = max(1, min(w, nb / 2));
+    const int w = tile_parts<C, TREE>(a.tile_tokens, r, most, total);
     const int mine = count * w;
     const int upto = wave_scan(mine);
     const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
     float longest = cost / w;
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) longest = fmaxf(longest, __shfl_xor(longest, d));
-    if (all > most || longest > 1.125f * (total / most) + kTileCost) return false;
+    if (all > most || parts_too_long(longest, total, most)) return false;
     out.parts = 0;
     if (k >= all) return true;
     const uint64_t has = __builtin_amdgcn_ballot_w64(mine > 0 && upto - mine <= k);
     const int b = kWave - 1 - __builtin_clzll(has);
-    out.row = make_row<C, TREE>(a, __builtin_amdgcn_readlane(r.start, b), __builtin_amdgcn_readlane(r.n, b),
+    out.row = make_row<C, TREE>(a.tile_tokens, __builtin_amdgcn_readlane(r.start, b), __builtin_amdgcn_readlane(r.n, b),
                                 __builtin_amdgcn_readlane(r.ctx, b), __builtin_amdgcn_readlane(r.bad, b));
     out.parts = __builtin_amdgcn_readlane(w, b);
     const int rem = k - (__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(mine, b));
-    const unsigned at = static_cast<unsigned>(rem) / static_cast<unsigned>(out.parts);
-    const int part = rem - at * out.parts;
-    const int g = at / static_cast<unsigned>(out.row.tiles), tile = at - g * out.row.tiles;
-    const int blocks = tile_blocks<C, TREE>(a, out.row, tile);
-    const auto cut = [&](int p) {      // p blocks / parts
-        return static_cast<int>(static_cast<unsigned>(p * (blocks % out.parts)) / static_cast<unsigned>(out.parts)) +
-               p * (blocks / out.parts);
-    };
-    const int to = cut(part + 1);
-    out.from = uniform_place(Place{b, g, tile, cut(part)});
-    out.to = uniform_place(to == blocks ? Place{b, g, tile + 1, 0} : Place{b, g, tile, to});
+    Place from, to;
+    part_place<C, TREE>(a.tile_tokens, out.row, b, rem, out.parts, from, to);
+    out.from = uniform_place(from);
+    out.to = uniform_place(to);
     return true;
 }
 
@@ -364,7 +190,7 @@ __device__ bool worker_range(const ChunkArgs& a, int k, Range& out) {
         if (whole_parts<C, TREE>(a, k, r, out)) return out.parts > 0;
         const int64_t keys = heads * r.head_units(0), tiles = static_cast<int64_t>(heads) * r.tiles;
         const int64_t keys_to = wave_scan64(keys), tiles_to = wave_scan64(tiles);
-        const Cuts cuts = cuts_of<C>(a, lane_value64(keys_to, kWave - 1), lane_value64(tiles_to, kWave - 1));
+        const Cuts cuts = cuts_of<C>(a.workers, lane_value64(keys_to, kWave - 1), lane_value64(tiles_to, kWave - 1));
         if (k >= cuts.workers) return false;
         const int64_t units = keys + cuts.cost * tiles;
         const int64_t first = keys_to + cuts.cost * tiles_to - units;
@@ -376,10 +202,10 @@ __device__ bool worker_range(const ChunkArgs& a, int k, Range& out) {
             if (u < cuts.total) {
                 const uint64_t has = __builtin_amdgcn_ballot_w64(units > 0 && first <= u);
                 const int b = kWave - 1 - __builtin_clzll(has);
-                const Row at = make_row<C, TREE>(a, __builtin_amdgcn_readlane(r.start, b), __builtin_amdgcn_readlane(r.n, b),
+                const Row at = make_row<C, TREE>(a.tile_tokens, __builtin_amdgcn_readlane(r.start, b), __builtin_amdgcn_readlane(r.n, b),
                                                  __builtin_amdgcn_readlane(r.ctx, b), __builtin_amdgcn_readlane(r.bad, b));
                 int64_t more;
-                p = uniform_place(place_of<C, TREE>(a, at, b, u - lane_value64(first, b), cuts.cost, more));
+                p = uniform_place(place_of<C, TREE>(a.tile_tokens, at, b, u - lane_value64(first, b), cuts.cost, more));
                 if (j == 0) out.row = at;
                 if (j == 1 && p.blk > 0) out.parts = worker_at(cuts, u + more) - k + 1;
             }
@@ -417,7 +243,7 @@ __device__ bool worker_range(const ChunkArgs& a, int k, Range& out) {
         all_keys += s_keys[w];
         all_tiles += s_tiles[w];
     }
-    const Cuts cuts = cuts_of<C>(a, all_keys, all_tiles);
+    const Cuts cuts = cuts_of<C>(a.workers, all_keys, all_tiles);
     const int64_t sum = keys + cuts.cost * tiles;
     const int64_t first = keys_before + keys_to - keys + cuts.cost * (tiles_before + tiles_to - tiles);
     if (k < cuts.workers) {
@@ -431,7 +257,7 @@ __device__ bool worker_range(const ChunkArgs& a, int k, Range& out) {
                 const int64_t units = heads * r.head_units(cuts.cost);
                 if (u < at + units) {
                     int64_t more;
-                    const Place p = place_of<C, TREE>(a, r, b, u - at, cuts.cost, more);
+                    const Place p = place_of<C, TREE>(a.tile_tokens, r, b, u - at, cuts.cost, more);
                     s_place[j] = p;
                     if (j == 1 && p.blk > 0) s_parts = worker_at(cuts, u + more) - k + 1;
                     break;
@@ -966,7 +792,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
     Place at = uniform_place(range.from);
     const Place end = uniform_place(range.to);
     const int parts = __builtin_amdgcn_readfirstlane(range.parts);
-    Row row = make_row<C, TREE>(a, __builtin_amdgcn_readfirstlane(range.row.start),
+    Row row = make_row<C, TREE>(a.tile_tokens, __builtin_amdgcn_readfirstlane(range.row.start),
                                 __builtin_amdgcn_readfirstlane(range.row.n),
                                 __builtin_amdgcn_readfirstlane(range.row.ctx),
                                 __builtin_amdgcn_readfirstlane(range.row.bad));     // of at.b
@@ -992,12 +818,12 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 if (b < a.batch) row = row_info<C, TREE>(a, b);
                 continue;
             }
-            const int nb = tile_blocks<C, TREE>(a, row, at.tile);
+            const int nb = tile_blocks<C, TREE>(a.tile_tokens, row, at.tile);
             const int kv_head = at.g;
             const bool to_end = end.b == at.b && end.g == at.g && end.tile == at.tile;
             const int k0 = at.blk, k1 = to_end ? end.blk : nb;
             const int nd = draft_blocks<C, TREE>(row);
-            const int keys = tile_keys<C, TREE>(a, row, at.tile);
+            const int keys = tile_keys<C, TREE>(a.tile_tokens, row, at.tile);
             const int tok0 = at.tile * a.tile_tokens;
             const int toks = min(a.tile_tokens, row.n - tok0);
             const unsigned head_off = kv_head * head_bytes;
