@@ -242,8 +242,9 @@ int kv_session_extend(kv_pool* pool, int32_t sid, int32_t new_seq_len, kv_stream
  * which counts the room made for all of them.  Where only the device knows, any lower
  * bound will do.  Every page that holds a token of the range counts as written: its cold
  * copy is dropped and the next eviction writes it again (Sec. III, write-on-evict).  An
- * eviction gives all pages of a session cold copies, so this call stands between a
- * session's last eviction or resume and the calls that write to it.  The session's
+ * eviction gives all pages of a session cold copies, and a spilled page that is promoted
+ * keeps its cold page as one, so this call stands between a session's last resume or
+ * promotion (kv_promote_pages) and the calls that write to it.  The session's
  * length becomes new_seq_len, longer or shorter than it was: missing pages are allocated
  * like kv_session_create's, pages past the new length are released like
  * kv_session_destroy's and their row entries become -1.  Tokens before `kept` and those
@@ -306,7 +307,10 @@ int kv_pool_set_spill(kv_pool* pool, int32_t enable);
  * does not read.  Writes to those sessions on another stream
  * (kv_append_tokens, kv_write_tokens) are another matter: the caller orders
  * them around this call's work, since the copy could miss a write enqueued
- * before it and overwrite one enqueued after it.
+ * before it and overwrite one enqueued after it.  A step that promotes and whose
+ * tokens the device writes (kv_append_tokens_table, kv_accept_drafts) promotes
+ * first and calls kv_session_extend or kv_session_reserve after it: those drop
+ * the cold copies of the resident pages that will be written.
  * Errors: KV_ERR_INVALID, KV_ERR_NO_COLD_PAGES (evicted pages need cold copies;
  * nothing changes).
  */
@@ -405,10 +409,10 @@ int kv_append_tokens(kv_pool* pool, int32_t layer, const int32_t* sids, const in
  * The pool's bookkeeping is not read or changed.  Write-on-evict stays exact
  * for tokens that extend a session (positions at or past its length before its
  * last kv_session_extend, or the `kept` of its last kv_session_reserve, with no
- * eviction since): that call already dropped the cold copies of the pages the
- * new tokens go into.  Rewriting older tokens this way, or writing into room made
- * before an eviction, would leave a cold copy stale; use kv_write_tokens for
- * those, or call kv_session_reserve again.
+ * eviction and no promotion since): that call already dropped the cold copies of
+ * the pages the new tokens go into.  Rewriting older tokens this way, or writing
+ * into room made before an eviction or a promotion, would leave a cold copy
+ * stale; use kv_write_tokens for those, or call kv_session_reserve again.
  * Errors: KV_ERR_INVALID (layer range, n, NULL or misaligned buffers, table
  * shape, metadata-only pool), KV_ERR_HIP.
  */

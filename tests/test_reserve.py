@@ -68,6 +68,14 @@ class Step:
             if h >= 0:
                 self.hot_data[h] = self.cold_data.get(cold[i])
 
+    def promote(self, n):
+        before, _ = self.pages()
+        self.kv.kv_promote_pages(self.pool, n)
+        new, cold = self.pages()
+        for h, old, c in zip(new, before, cold):
+            if h >= 0 and old < 0:
+                self.hot_data[h] = self.cold_data.get(c)
+
     def check(self):
         hot, _ = self.pages()
         for i, want in self.want.items():
@@ -195,3 +203,26 @@ def test_refusals_change_nothing():
     kv.kv_session_reserve(pool, 0, 30, 30)            # and let go; page 1, shared, takes no tokens
     assert kv.kv_session_info(pool, 0)[3] == [5, 6]
     kv.kv_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("width", [1, 8, 64])
+def test_promotions_between_steps_lose_nothing(width):
+    """Spilled pages are promoted before a step's room is made: the resident pages that the step
+    writes have no cold copies that count as valid."""
+    rng = np.random.default_rng(80 + width)
+    promoted = 0
+    for trial in range(12):
+        s = Step(int(rng.integers(0, 120)), spill=True)
+        for turn in range(30):
+            if s.length + width > 16 * 64:
+                break
+            s.promote(int(rng.integers(0, 8)))
+            s.check()
+            s.reserve(width)
+            s.accept(int(rng.integers(0, width, endpoint=True)))
+            s.check()
+            if rng.random() < 0.5:
+                s.evict_and_resume(lazy=rng.random() < 0.8)
+                s.check()
+        promoted += s.kv.kv_pool_stats(s.pool)["promoted_pages"]
+    assert promoted > 50
