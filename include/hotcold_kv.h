@@ -806,7 +806,9 @@ size_t paged_prefill_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t
  * before the division by their sum, so values of V past 2^120 / L may overflow.  The result does not
  * depend on where pages sit; it does depend, in float32 rounding, on the lengths of the
  * batch's other rows, which move the cuts of the work split.
- * num_q_heads / num_kv_heads must be an integer in 1 .. 16.
+ * num_q_heads / num_kv_heads must be an integer in 1 .. 16.  The call has as many workgroups
+ * as the device has CUs, each filling one: on a stream of fewer CUs
+ * (kv_stream_create_cu_slots) some wait for others, up to twice the time.
  * Errors: KV_ERR_INVALID (shapes, sizes, layer, alignment to 16 bytes of q and out,
  * workspace, metadata-only pool), KV_ERR_HIP.
  */

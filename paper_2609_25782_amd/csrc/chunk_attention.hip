@@ -32,7 +32,7 @@
 //
 // Bounds and figures (bf16, d = 128, 8 query heads per KV head, 4 KV heads, unless said).
 // Prompt chunks are bound by the products and the weights between them: one prompt of 24,576 tokens takes
-// 4.2-4.5 ms = 1.10-1.18 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches
+// 4.2-4.5 ms = 1.09-1.19 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches
 // 1.19 and of two 16384 x 16384 ones 1.37, both at clocks of about 2 GHz.  Per block
 // of 64 keys and 32 rows a wave issues 64 matrix instructions (1024 cycles) and 144 others, of
 // them 32 exponentials (960 cycles); the matrix cores are busy 52 % of the time, waves wait for
@@ -82,7 +82,7 @@ struct Cfg {
     static constexpr int kStage = kPages * kPage;         // LDS bytes of a block
     static constexpr int kThreads = kWaves * kWave;
     // Cache policy of the page loads: nontemporal (2) where one tile holds most rows' queries
-    // of a KV head, so that its K and V are read once (32 sessions x 4-16 drafts over 8K-32K tokens: 272 -> 259 us);
+    // of a KV head, so that its K and V are read once (32 sessions x 4-16 drafts over 8K-32K tokens: 267 -> 241 us);
     // tiles of 256 rows read them again and again.
     static constexpr int kAux = NT == 1 ? 2 : 0;
     static constexpr int kPerSimd = kWaves / 4;           // waves per SIMD the registers are made for
@@ -1045,12 +1045,13 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
 // tile whose first part worker k left in slot 2 k + 1; its other parts are in the slots 2 (k + 1),
 // 2 (k + 2), ... of the workers after it.  A wave takes kIter rows, kAtOnce parts at a time.
 // Most tiles are cut once or twice: then the loads of all of the wave's rows are in flight
-// together.  (2 x 5 drafts in float32: 14.3 us; with half as many rows per wave 15.9, the
-// blocks without work cost; with twice as many 15.7, 64 rows over 32K tokens 28.3 -> 34.4.)  The record holds all that a row's place needs, so
+// together.  (2 x 5 drafts in float32: 13.6 us; with half as many rows per wave 14.4, the
+// blocks without work cost, though 16 sessions with one KV head gain, 70.5 -> 65.4; with twice as many
+// 14.4, and 64 rows over 32K tokens 27.3 -> 34.0.)  The record holds all that a row's place needs, so
 // that only two loads follow each other.  Where few tiles are cut into equal parts, the k that
 // hold a record are multiples of 8 and more, which plain block numbers all send to one XCD:
-// the blocks of one k differ in blockIdx.x (4 sessions x 32 drafts, 16 parts each: 38 us with
-// plain numbers, 10 so).
+// the blocks of one k differ in blockIdx.x (4 sessions x 32 drafts over 8K tokens, 16 parts each: the
+// call takes 77.9 us with plain numbers, 45.1 so).
 template <class C>
 struct Merge {
     static constexpr int kLanes = C::kD / 4, kAtOnce = kWave / kLanes;
@@ -1173,10 +1174,12 @@ hipError_t launch_shape(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s, c
 // chunks, the most of trees).  256: a wave has 32 rows, and each K and V fragment that it reads
 // from LDS serves two products, else the reads bound the call; 128, where a tile of 256 would
 // compute rows that are not there or wait for K and V all the same.  16 sessions of 8K-32K
-// tokens, 128 rows each: 147 us with tiles of 128 rows, 156 with 256; 136 rows: 240 and 191;
-// 256 rows: 278 and 225; 64 sessions of 8 rows: 92 and 111.  64 decode steps of 8 rows and a
-// chunk of 4096 rows in one call (71 rows on average): 138 and 162.  (Tiles of 64 rows were
-// never faster by more than 2 %: 8 sessions x 8 drafts 22.4 us, with 128 rows 20.9.)
+// tokens, 128 rows each: 131 us with tiles of 128 rows, 158 with 256; 136 rows: 231 and 166;
+// 256 rows: 247 and 201; 64 sessions of 8 rows: 93 and 111.  64 decode steps of 8 rows and a
+// chunk of 4096 rows in one call (71 rows on average): 127 and 158.  Calls whose few tiles do not
+// fill the workers would do better with 128 rows, which the rule does not see: 4 x 256 rows over 8K
+// tokens 35.6 and 45.1, 7 chunks of 1-701 tokens with 3 heads 28.8 and 32.7.  (Tiles of 64 rows were
+// never faster by more than 2 %.)
 ChunkPlan chunk_plan(int cus, int64_t rows_per_seq) {
     ChunkPlan p;
     p.rows = rows_per_seq <= 128 ? 128 : 256;

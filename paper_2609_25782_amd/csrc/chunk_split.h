@@ -33,9 +33,11 @@ struct Row {
 
 // What a tile costs beside its keys, in keys: its queries' load, its output, the pipeline's
 // start and the masked blocks.  kTileCost is what balances calls with work for every worker
-// (twelve packed prompts, on one build: 64: 1879 us, 192: 1453, 320: 1220, 448: 1241, 640:
-// 1282); calls with less than that are cut finer, with kTileCostFine (8 sessions x 8 drafts
-// over 2K tokens: 64: 39.8 us, 320: 41.7).
+// (twelve packed prompts: 64: 1510 us, 192: 1195, 320: 1037, 448: 1041, 640: 1060; with 64 dims
+// 985, 778, 711, 740 and 768; in float32, where a key costs more, 6 prompts of 100-2000 tokens over
+// up to 2000: 507, 537, 528, 550 and 559).  Calls with less than that are cut finer, with
+// kTileCostFine (2 x 5 float32 drafts: 64: 13.5 us, 320: 13.9; 12 chunks of 20-300 tokens 56.3 and
+// 56.0; 7 chunks of 1-701 tokens, 3 heads of 64 dims: 32.7 and 31.1).
 constexpr int kTileCost = 320, kTileCostFine = 64;
 
 // The units of a row that brings n queries after ctx tokens.
@@ -172,12 +174,12 @@ HCK_HD int worker_at(const Cuts& c, int64_t u) {
 // Where no more than `workers` tiles have about the same cost in each row (drafts, short
 // chunks over long contexts) and equal parts of them differ little, every tile is cut into
 // whole parts, as many as its share of the workers: no worker then has parts of two tiles,
-// whose starts and ends follow each other.  8 sessions x 8 drafts over 2K tokens: 26.5 us with
-// ranges, 22.7 so; 2 x 5 drafts in float32: 16.6 and 14.2.  Taken without looking at
-// the longest part, 32 sessions of 8K to 32K tokens lose (248 us with ranges, 311 so).  Parts
+// whose starts and ends follow each other.  8 sessions x 8 drafts over 2K tokens: 23.9 us with
+// ranges, 19.3 so; 2 x 5 drafts in float32: 17.0 and 13.5.  Taken without looking at
+// the longest part, 32 sessions of 8K to 32K tokens lose (240 us with ranges, 305 so).  Parts
 // up to an eighth longer than even ones are taken: tiles of one row, cut alike, read the same
-// keys at the same time, from one L2 (4 sessions x 49-64 drafts, two tiles a row: 219 us with
-// ranges, 207 so); with one tile a row they measure the same.
+// keys at the same time, from one L2 (4 sessions x 49-64 drafts, two tiles a row: 192 us with
+// ranges, 180 so); with one tile a row the difference is small (4 x 32 drafts over 8K: 43.7 and 44.9).
 HCK_HD bool even_tiles(const Row& r) {
     return r.tiles <= 1 || r.slope == 0 || static_cast<int64_t>(r.n) * 4 <= r.ctx;
 }

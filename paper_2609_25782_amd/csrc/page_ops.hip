@@ -512,9 +512,11 @@ __device__ __forceinline__ void write_run(T* out, const T* v, const int32_t* pat
 // in consecutive slots, so a run of 8 is one 16-byte store, where a store per draft and dim
 // would be 2 bytes each (64 rows x 0-16 drafts x 48 layers, 51 MB read and 51 MB written: 139 us
 // with those, 46 so where the same pages were just written, 80 where they were not, 2.3 and 1.3
-// TB/s).  Bound by the pages' lines: a token has 16 bytes in every 256 of its K tile and 2 in
-// every 32 of its V tile, so the call touches every line of the tiles it writes to, in part:
-// WRITE_SIZE counts 117 MB, 2.3 times the accepted bytes.
+// TB/s).  A token has 16 bytes in every 256 of its K tile and 2 in every 32 of its V tile, so
+// the call touches every line of the tiles it writes to, in part: WRITE_SIZE counts 117 MB, 2.3
+// times the accepted bytes, which takes 34 us with the reads at a copy's rate.  The rest is in how they are
+// moved: a wave's K store is 32 places 256 bytes apart, its V load 2 bytes a lane, and a block waits for
+// count, entry, path and data in turn, for one layer.
 template <typename T>
 __global__ __launch_bounds__(kBlockThreads) void accept_drafts_kernel(const AcceptArgs a) {
     constexpr int x = 16 / sizeof(T);
