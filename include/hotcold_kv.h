@@ -239,8 +239,9 @@ int kv_session_extend(kv_pool* pool, int32_t sid, int32_t new_seq_len, kv_stream
  * calls that are resolved on the device and do no bookkeeping (kv_accept_drafts,
  * kv_append_tokens_table, paged_decode_attention_append).  `kept` is how many tokens the
  * session really holds: after a step that rejected drafts that is less than its length,
- * which counts the room made for all of them.  Where only the device knows, any lower
- * bound will do.  Every page that holds a token of the range counts as written: its cold
+ * which counts the room made for all of them.  Where only the device knows, a lower
+ * bound stands for `kept`, and new_seq_len counts from an upper one (the last length).
+ * Every page that holds a token of the range counts as written: its cold
  * copy is dropped and the next eviction writes it again (Sec. III, write-on-evict).  An
  * eviction gives all pages of a session cold copies, and a spilled page that is promoted
  * keeps its cold page as one, so this call stands between a session's last resume or

@@ -27,11 +27,13 @@ class Step:
         _, _, hot, cold = self.kv.kv_session_info(self.pool, self.sid)
         return hot, cold
 
-    def reserve(self, room):
+    def reserve(self, room, low=None, high=None):
+        """Room behind the tokens held, of which the host may know bounds only."""
         before = self.pages()[0]
-        self.kv.kv_session_reserve(self.pool, self.sid, self.length, self.length + room)
+        end = (self.length if high is None else high) + room
+        self.kv.kv_session_reserve(self.pool, self.sid, self.length if low is None else low, end)
         hot, _ = self.pages()
-        assert len(hot) == -(-(self.length + room) // 16)
+        assert len(hot) == -(-end // 16)
         for i in range(len(hot)):       # a new page holds nothing yet
             if i >= len(before):
                 self.want[i] = self.now = self.now + 1
@@ -203,6 +205,28 @@ def test_refusals_change_nothing():
     kv.kv_session_reserve(pool, 0, 30, 30)            # and let go; page 1, shared, takes no tokens
     assert kv.kv_session_info(pool, 0)[3] == [5, 6]
     kv.kv_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("spill", [False, True])
+@pytest.mark.parametrize("width", [1, 8, 40])
+def test_lengths_that_only_the_device_knows(width, spill):
+    """The accepted counts reach the host every few steps: bounds of the length do between them."""
+    rng = np.random.default_rng(90 + width)
+    for trial in range(12):
+        s = Step(int(rng.integers(0, 120)), spill)
+        low = high = s.length
+        for turn in range(30):
+            if high + width > 16 * 64:
+                break
+            s.reserve(width, low, high)
+            s.accept(int(rng.integers(0, width, endpoint=True)))
+            high += width
+            s.check()
+            if rng.random() < 0.3:
+                s.evict_and_resume(lazy=spill and rng.random() < 0.5)
+                s.check()
+            if rng.random() < 0.3:
+                low = high = s.length
 
 
 @pytest.mark.parametrize("width", [1, 8, 64])
