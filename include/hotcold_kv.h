@@ -129,7 +129,13 @@ enum kv_kernel_id {
     KV_KERNEL_PREFETCH_COPY = 4,  /* one layer's slices of spilled pages -> staging */
     KV_KERNEL_CHUNK = 5,          /* attention of prompt chunks and draft trees */
     KV_KERNEL_CHUNK_MERGE = 6,    /* join of its partial results */
-    KV_KERNEL_COUNT = 7
+    KV_KERNEL_BOUNDS = 7,         /* key bounds of pages */
+    KV_KERNEL_PAGE_SCORES = 8,    /* pages scored by their bounds */
+    KV_KERNEL_PAGE_PICK = 9,      /* the choice among them */
+    KV_KERNEL_SPARSE = 10,        /* decode attention over picked pages */
+    KV_KERNEL_SPARSE_MERGE = 11,  /* join of its partial results */
+    KV_KERNEL_FORK_COPY = 12,     /* pages of a session to its branches */
+    KV_KERNEL_COUNT = 13
 };
 
 typedef void* kv_stream_t;
@@ -337,6 +343,27 @@ int kv_resume_sessions_lazy(kv_pool* pool, const int32_t* sids, int32_t n, kv_st
  */
 int kv_session_import_cold(kv_pool* pool, int32_t seq_len, const int32_t* cold_pages,
                            int32_t* sid_out);
+
+/*
+ * Branches: n new ACTIVE sessions, the i-th with the first kept[i] tokens of ACTIVE session
+ * sids[i] (host arrays; the same session may stand several times), in pages of its own: an
+ * agent tries several continuations of one context and drops those that lead nowhere.
+ * Pages are allocated like kv_session_create's, in argument and logical order (evicting
+ * resident pages of paused sessions where too few are free; spill does not apply: the
+ * call fails rather than place a branch in the cold tier), and the parents' pages are
+ * copied to them on `stream`, every page read once for all branches of its session and
+ * call (up to 14); a spilled page is fetched from the cold tier.  Whole pages are copied,
+ * slots past kept[i] included.  Pages whose 16 tokens are all kept are never written again:
+ * the branch shares the parent's valid cold copies of them (an eviction then writes nothing;
+ * a spilled page of the parent becomes shared).  Key bounds (kv_pool_set_bounds) go along.
+ * The new ids (lowest free rows) go to sids_out[0 .. n), host.  The parents stay as they
+ * are; their tokens must have been written on `stream` or be ordered before it.
+ * Errors: KV_ERR_INVALID (ids, kept outside [0, length], too few free session slots),
+ * KV_ERR_STATE (a session not ACTIVE), KV_ERR_NO_HOT_PAGES, KV_ERR_NO_COLD_PAGES,
+ * KV_ERR_OOM.
+ */
+int kv_fork_sessions(kv_pool* pool, const int32_t* sids, const int32_t* kept, int32_t n, kv_stream_t stream,
+                     int32_t* sids_out);
 
 /* Release a session: its hot pages return to the free set (see the cross-stream
  * rule above), its cold references are dropped and its row is reset to -1. */
@@ -854,6 +881,127 @@ int paged_tree_attention(kv_pool* pool, int32_t layer, const void* q, const void
                          const uint64_t* masks, const int32_t* draft_lens, int32_t width, const int32_t* page_table,
                          int64_t pt_stride, const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, float scale,
                          void* out, void* workspace, size_t ws_bytes, kv_stream_t stream);
+
+/* ----------------------------------------------------------------------- */
+/* Decode attention over picked pages                                       */
+/* ----------------------------------------------------------------------- */
+
+/*
+ * A long session's decode step need not read all its pages: most hold no token that the new
+ * token's queries give weight to.  Each page's keys have bounds (kv_update_bounds), a cheap
+ * score from them picks pages for every session and KV head (paged_select_pages), and the
+ * attention reads those alone (paged_sparse_attention).  That leaves tokens out, so its
+ * result is not that of paged_decode_attention unless every page is picked.  Pages in the
+ * cold tier (spill) are read where they are picked only.
+ *
+ * kv_bounds_bytes: device bytes of a pool's bounds, about 1/31 of its pages in bfloat16 (0 if
+ *   the descriptor is invalid).
+ * kv_pool_set_bounds: keep bounds in `bounds` (device, caller-owned, 256-byte aligned, of at
+ *   least kv_bounds_bytes; NULL: keep none).  What the buffer holds are the bounds: zeros, or
+ *   anything else, until kv_update_bounds has set them.  From then on every copy of a page
+ *   between the pools and to a branch (resume, eviction, promotion, kv_fork_sessions) takes
+ *   the page's bounds along.  No work of the pool may be running.
+ *   KV_ERR_INVALID (alignment, size, metadata-only pool).
+ */
+size_t kv_bounds_bytes(const kv_pool_desc* desc);
+int kv_pool_set_bounds(kv_pool* pool, void* bounds, size_t bytes);
+
+/*
+ * Bounds of the pages that hold tokens [starts[b], seq_lens[b]) of row b of `page_table`
+ * (device int32 [batch][pt_stride]), b < batch, for layers [layer_begin, layer_begin +
+ * num_layers): for KV head g and dim d of a page, over its tokens t < seq_lens[b],
+ *
+ *     lo = floor(min_t k[t][g][d] / 2^e),  hi = ceil(max_t k[t][g][d] / 2^e),
+ *
+ * whole numbers of [-127, 127], with e the least of [-50, 50] such that no |k| of the
+ * page and head is above 127 * 2^e (larger ones count as 127 * 2^50; NaN as the infinity of
+ * its sign).  The pool's writes do not do this: call it after writing tokens (one call
+ * serves all layers; a page's earlier tokens are taken in again) and before picking pages by
+ * them.  A page that was written since is picked by its old bounds.
+ *   starts    device int32 [batch] or NULL (0); below 0 it counts as 0
+ *   seq_lens  device int32 [batch]; at or below starts[b], below 0 or above 16 * pt_stride:
+ *             nothing is done for the row
+ * An entry that names no page of either pool is skipped (KV_PAGE_COLD entries count with spill
+ * on or staging set).  Rows that name the same page race.  All arrays are read when the
+ * kernel runs; a captured call takes their current values.
+ * Errors: KV_ERR_INVALID (no bounds, layer range, batch, NULL, stride), KV_ERR_HIP.
+ */
+int kv_update_bounds(kv_pool* pool, int32_t layer_begin, int32_t num_layers, const int32_t* page_table,
+                     int64_t pt_stride, const int32_t* starts, const int32_t* seq_lens, int32_t batch,
+                     kv_stream_t stream);
+
+/*
+ * Bounds as values, for a rule of choice of the caller's own: out (device float32
+ * [num_layers][n][num_kv_heads][2][head_dim], 16-byte aligned) gets lo * 2^e and hi * 2^e of
+ * the pages named by pages[0 .. n) (device int32, as page-table entries: hot ids or KV_PAGE_COLD
+ * | id), NaN for an entry that names no page of either pool.
+ * Errors: KV_ERR_INVALID (no bounds, layer range, n, NULL, alignment), KV_ERR_HIP.
+ */
+int kv_read_bounds(kv_pool* pool, int32_t layer_begin, int32_t num_layers, const int32_t* pages, int32_t n,
+                   float* out, kv_stream_t stream);
+
+/* Device workspace bytes paged_select_pages needs (0: invalid arguments). */
+size_t paged_select_workspace_bytes(const kv_pool* pool, int32_t batch, int64_t pt_stride, int32_t width);
+
+/*
+ * The pages that each row's new token reads, for one layer.  Row b has P = ceil(seq_lens[b] /
+ * 16) pages.  If P <= width all are picked for every KV head; else the first `first`, the last
+ * `recent` and, of those between, the width - first - recent of the largest score, ties to the
+ * lower page.  The score of page p for KV head g is the largest, over the query heads h of g, of
+ *
+ *     2^(e_h + e_p) * sum_d (max(n_hd, 0) * hi_d + min(n_hd, 0) * lo_d)
+ *
+ * with the page's bounds and the queries as whole numbers n_hd = round(q[b][h][d] / 2^e_h) (ties
+ * to even) of [-127, 127], e_h chosen like a page's e: an upper bound, but for the rounding of
+ * q, of q . k over the page's tokens.  It is computed exactly.  The attention's scale is
+ * taken as positive: for a negative one pass -q.
+ *   q          device [batch][num_q_heads][head_dim], pool dtype, 16-byte aligned
+ *   page_table, pt_stride, seq_lens   as paged_decode_attention; seq_lens[b] <= 0 or above 16 *
+ *              pt_stride picks nothing
+ *   width      1 .. ; first, recent >= 0, together at most width
+ *   picks      device int32 [batch][num_kv_heads][width]: page numbers of the row (not ids),
+ *              ascending, then -1
+ *   counts     device int32 [batch][num_kv_heads]: how many
+ *   workspace  device, >= paged_select_workspace_bytes(), 256-byte aligned
+ * A page that no pool holds is picked before all others, so that the attention shows it (NaN).
+ * Capture and concurrent calls as paged_prefill_attention.
+ * Errors: KV_ERR_INVALID (no bounds, shapes, sizes, layer, alignment), KV_ERR_HIP.
+ */
+int paged_select_pages(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
+                       const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, int32_t width, int32_t first,
+                       int32_t recent, int32_t* picks, int32_t* counts, void* workspace, size_t ws_bytes,
+                       kv_stream_t stream);
+
+/* Device workspace bytes paged_sparse_attention needs (0: invalid arguments). */
+size_t paged_sparse_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t width);
+
+/*
+ * Decode attention of one new token per row over listed pages, for one layer: for query head h
+ * of KV head g,
+ *
+ *     out[b][h] = sum_t softmax_t(scale * q[b][h] . k_t) v_t
+ *
+ * over the tokens t < seq_lens[b] of pages picks[b][g][0 .. counts[b][g]) of row b.  A page that
+ * is listed twice counts twice; an entry outside the row's pages [0, ceil(seq_lens[b] / 16)) is
+ * passed over.  The lists may come from paged_select_pages or from any other rule.
+ *   counts     device int32 [batch][num_kv_heads] or NULL (width each); outside [0, width] it
+ *              counts as the nearer end
+ *   out        device [batch][num_q_heads][head_dim], written in full: zeros where a list holds
+ *              no token, NaN for a row whose length is below 0 or above 16 * pt_stride, for a list
+ *              with a page outside the pools (or a staged copy), and where every score is
+ *              minus infinity
+ *   workspace  device, >= paged_sparse_workspace_bytes(), 256-byte aligned
+ * Slots past seq_lens[b] of a listed tail page may hold anything.  The order of a list changes
+ * the result in float32 rounding only.  No pool bounds are needed.  q, page_table, numerics: as
+ * paged_decode_attention; any sign of scale.  Capture (one or two kernels, nothing else) and
+ * concurrent calls as paged_prefill_attention.
+ * num_q_heads / num_kv_heads must be an integer in 1 .. 16.
+ * Errors: KV_ERR_INVALID (shapes, sizes, layer, alignment, workspace), KV_ERR_HIP.
+ */
+int paged_sparse_attention(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
+                           const int32_t* seq_lens, const int32_t* picks, const int32_t* counts, int32_t width,
+                           int32_t batch, int32_t num_q_heads, float scale, void* out, void* workspace,
+                           size_t ws_bytes, kv_stream_t stream);
 
 /*
  * The work split of paged_decode_attention, written out (device int32

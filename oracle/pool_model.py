@@ -39,6 +39,8 @@ Readings where the paper is silent:
   holds; every page with a token of that range counts as written (refused if
   one is spilled to a shared cold page), and pages past the new length are
   freed.  Extending is reserving from the session's length on.
+* A branch gets hot pages of its own (never spilled ones) with the parent's tokens, and
+  shares the parent's cold copies of pages that are full: those are never written again.
 * Cold pages may be shared by several paused sessions (a virtualised cold
   pool); they are reference counted and freed when the last user lets go.
 * Every failing call leaves the whole state unchanged.
@@ -250,6 +252,33 @@ class PoolModel:
         s.cold += [-1] * len(pages) + list(spill)
         s.spilled += [False] * len(pages) + [True] * len(spill)
         s.seq_len = new_len
+
+    def fork(self, sids: Sequence[int], kept: Sequence[int]) -> List[int]:
+        """Branches: new sessions, the i-th with the first kept[i] tokens of sids[i]; the (source session,
+        logical page, hot page) copies are in `last_fork`."""
+        parents = [self._session(int(x)) for x in sids]
+        for s, k in zip(parents, kept):
+            if s.state != ACTIVE:
+                raise ModelError(ERR_STATE, "not active")
+            if not 0 <= k <= s.seq_len:
+                raise ModelError(ERR_INVALID, "bad length")
+        free = [sid for sid, s in enumerate(self.sessions) if s.state == FREE]
+        if len(free) < len(parents):
+            raise ModelError(ERR_INVALID, "no free session slots")
+        victims, cold, pages, _ = self._plan(sum(_pages(k) for k in kept), spill=False)
+        self.last_victim_copies = self._evict_victims(victims, cold)
+        self._take_hot(pages)
+        self.last_fork, it = [], iter(pages)
+        for sid, s, src, k in zip(free, parents, sids, kept):
+            hot = [next(it) for _ in range(_pages(k))]
+            whole = k // PAGE_TOKENS         # pages all of whose slots are kept tokens
+            shared = s.cold[:whole]
+            for c in shared:
+                if c >= 0:
+                    self.cold_ref[c] += 1
+            self.sessions[sid] = _Session(ACTIVE, k, 0, hot, shared + [-1] * (len(hot) - whole), [False] * len(hot))
+            self.last_fork += [(src, i, h) for i, h in enumerate(hot)]
+        return free[:len(parents)]
 
     def pause(self, sid: int) -> None:
         s = self._session(sid)

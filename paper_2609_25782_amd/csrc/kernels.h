@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "hotcold_kv.h"
 
 namespace hck {
@@ -348,5 +350,103 @@ struct AcceptArgs {
     const void* v;
 };
 hipError_t launch_accept_drafts(const AcceptArgs& a, hipStream_t s);
+
+// One hot page copied to several others, all layers: read once, written n times.
+constexpr int kForkDests = 14;
+struct ForkEntry {
+    int32_t src;
+    int32_t n;                 // destinations in use, 1 .. kForkDests
+    int32_t dst[kForkDests];
+};
+constexpr int kForkInline = 48;  // entries that travel in the kernel arguments
+hipError_t launch_fork_copy(const PoolGeom& pool, int64_t slice_bytes, int32_t layers, const ForkEntry* entries,
+                            bool on_host, int32_t n, int32_t max_blocks, hipStream_t s, const LaunchEvents& ev = {});
+
+// Key bounds of pages.  A record (one page of one layer) is [KV head][lo, hi][head_dim] bytes,
+// then the heads' powers of two in 16 bytes; those of the hot pages come first, then the cold ones.
+inline int32_t bounds_record_bytes(int num_kv_heads, int head_dim) { return num_kv_heads * 2 * head_dim + 16; }
+struct BoundsUpdateArgs {
+    PoolGeom hot, cold;
+    int32_t num_hot, num_cold;   // num_cold 0: tagged entries name no page
+    char* bounds;
+    int32_t record;
+    int64_t layer_stride;
+    const int32_t* table;
+    int64_t pt_stride;
+    const int32_t* starts;       // [batch] or null: from 0 on
+    const int32_t* lens;         // [batch]
+    int32_t batch, num_kv_heads, layer;
+};
+hipError_t launch_bounds_update(const BoundsUpdateArgs& a, int head_dim, int dtype, int32_t num_layers, hipStream_t s,
+                                const LaunchEvents& ev = {});
+struct BoundsReadArgs {
+    const char* bounds;
+    int32_t record;
+    int64_t layer_stride;
+    int32_t num_hot, num_cold;
+    const int32_t* pages;        // [n] as page-table entries
+    int32_t n, num_kv_heads, head_dim, layer;
+    float* out;
+};
+hipError_t launch_bounds_read(const BoundsReadArgs& a, int32_t num_layers, hipStream_t s);
+// Records that follow copied pages (n entries on the device; page-table fields are not used).
+hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t record, int32_t layers,
+                              const CopyEntry* entries, int32_t n, hipStream_t s);
+
+// The choice of pages for decode attention.
+struct SelectArgs {
+    const char* bounds;
+    int32_t record;
+    int64_t layer_stride;
+    int32_t num_hot, num_cold;
+    const void* q;               // [batch][num_q_heads][D]
+    const int32_t* table;
+    int64_t pt_stride;
+    const int32_t* lens;
+    int32_t batch, num_kv_heads, group, num_q_heads, layer;
+    int32_t width, first, recent;
+    unsigned* keys;              // [batch][num_kv_heads][pt_stride]
+    int32_t* picks;              // [batch][num_kv_heads][width]
+    int32_t* counts;             // [batch][num_kv_heads]
+};
+// Bytes of the keys: none where no row can have more pages than are picked.
+inline size_t select_workspace_bytes(int64_t lists, int64_t pt_stride, int32_t width) {
+    const size_t n = pt_stride > width ? static_cast<size_t>(lists) * static_cast<size_t>(pt_stride) * 4 : 0;
+    return std::max<size_t>((n + 255) & ~static_cast<size_t>(255), 256);
+}
+hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hipStream_t s, const LaunchEvents& ev = {},
+                               const LaunchEvents& ev_pick = {});
+
+// Decode attention over listed pages.
+struct SparseArgs {
+    const char* hot;             // slice of hot page 0 for the layer
+    int64_t hot_stride;
+    const char* cold;
+    int64_t cold_stride;
+    int32_t num_hot, num_cold;
+    const void* q;
+    void* out;
+    const int32_t* table;
+    int64_t pt_stride;
+    const int32_t* lens;
+    const int32_t* picks;        // [batch][num_kv_heads][width]
+    const int32_t* counts;       // [batch][num_kv_heads] or null: width
+    int32_t batch, num_kv_heads, group, width;
+    float scale_log2;
+    int32_t parts;               // workgroups of a list
+    float* part_o;               // [lists][parts][group][D]
+    float* part_ml;              // [lists][parts][2][group]
+};
+struct SparsePlan {
+    int32_t waves;   // of a workgroup
+    int32_t parts;
+};
+SparsePlan sparse_plan(int cus, int batch, int num_kv_heads, int group, int width);
+inline size_t sparse_workspace_bytes(const SparsePlan& p, int64_t lists, int group, int head_dim) {
+    const size_t n = p.parts > 1 ? static_cast<size_t>(lists) * p.parts * group * (head_dim + 2) * 4 : 0;
+    return std::max<size_t>((n + 255) & ~static_cast<size_t>(255), 256);
+}
+hipError_t launch_sparse_attention(const SparseArgs& a, const SparsePlan& p, int head_dim, int dtype, hipStream_t s,
+                                   const LaunchEvents& ev = {}, const LaunchEvents& ev_merge = {});
 
 }  // namespace hck

@@ -212,6 +212,10 @@ struct kv_pool {
     // pages together: a decode reads within 1 / num_layers of it), the cold
     // pool page-major (each 16-token block contiguous).
     hck::PoolGeom hot_geom, cold_geom;
+    // Key bounds of the pages (kv_pool_set_bounds): records of the hot pages, then of the cold
+    // ones, layer after layer.
+    char* bounds = nullptr;
+    hck::PoolGeom bounds_hot, bounds_cold;
     int32_t host_copy = KV_HOST_COPY_DMA;
     int32_t compute_mode = KV_DECODE_MATRIX;
     int32_t* counters = nullptr;  // decode arrival counters, zero between calls
@@ -380,13 +384,76 @@ struct kv_pool {
         }
     }
 
+    int32_t bounds_record() const { return hck::bounds_record_bytes(d.num_kv_heads, d.head_dim); }
+
+    // Cold pages that page-table entries may name.
+    int32_t named_cold() const { return cold && tiered() ? d.num_cold_pages : 0; }
+
+    // The records of copied pages, after the copies.
+    int submit_bounds_copies(const hck::PoolGeom& src, const hck::PoolGeom& dst,
+                             const std::vector<hck::CopyEntry>& copies, hipStream_t s) {
+        for (size_t off = 0; off < copies.size(); off += kStagingEntries) {
+            const int32_t n = static_cast<int32_t>(std::min<size_t>(kStagingEntries, copies.size() - off));
+            StagingSlot* slot;
+            int rc = acquire_slot(&slot);
+            if (rc) return rc;
+            std::memcpy(slot->host, copies.data() + off, n * sizeof(hck::CopyEntry));
+            hipError_t e = hck::launch_upload(slot->mapped, slot->dev, n * sizeof(hck::CopyEntry), s);
+            if (e == hipSuccess)
+                e = hck::launch_bounds_copy(src, dst, bounds_record(), d.num_layers,
+                                            static_cast<const hck::CopyEntry*>(slot->dev), n, s);
+            if (e != hipSuccess) return hip_fail(e, "bounds copy launch");
+            rc = release_slot(slot, s);
+            if (rc) return rc;
+        }
+        return KV_OK;
+    }
+
+    // Hot pages to the branches' pages (read once for up to kForkDests of them).
+    int submit_fork(const std::vector<hck::ForkEntry>& entries, hipStream_t s) {
+        if (!entries.empty() && entries.size() <= static_cast<size_t>(hck::kForkInline)) {
+            const hck::LaunchEvents ev = prof_events();
+            hipError_t e = hck::launch_fork_copy(hot_geom, slice_bytes, d.num_layers, entries.data(), /*on_host=*/true,
+                                                 static_cast<int32_t>(entries.size()), copy_blocks, s, ev);
+            prof_done(KV_KERNEL_FORK_COPY, ev, e);
+            return e == hipSuccess ? KV_OK : hip_fail(e, "fork copy launch");
+        }
+        constexpr size_t kEntries = kStagingBytes / sizeof(hck::ForkEntry);
+        for (size_t off = 0; off < entries.size(); off += kEntries) {
+            const size_t n = std::min(kEntries, entries.size() - off);
+            StagingSlot* slot;
+            int rc = acquire_slot(&slot);
+            if (rc) return rc;
+            std::memcpy(slot->host, entries.data() + off, n * sizeof(hck::ForkEntry));
+            hipError_t e = hck::launch_upload(slot->mapped, slot->dev, n * sizeof(hck::ForkEntry), s);
+            if (e != hipSuccess) return hip_fail(e, "fork list upload");
+            const hck::LaunchEvents ev = prof_events();
+            e = hck::launch_fork_copy(hot_geom, slice_bytes, d.num_layers, static_cast<const hck::ForkEntry*>(slot->dev),
+                                      /*on_host=*/false, static_cast<int32_t>(n), copy_blocks, s, ev);
+            prof_done(KV_KERNEL_FORK_COPY, ev, e);
+            if (e != hipSuccess) return hip_fail(e, "fork copy launch");
+            rc = release_slot(slot, s);
+            if (rc) return rc;
+        }
+        return KV_OK;
+    }
+
+    // Whole-page copies between the pools, and their records where the pool keeps bounds.
+    int submit_copies(bool to_hot, const std::vector<hck::CopyEntry>& copies,
+                      const std::vector<hck::CopyEntry>& writes, hipStream_t s, int kernel_id) {
+        const int rc = submit_page_copies(to_hot, copies, writes, s, kernel_id);
+        if (rc || !bounds || copies.empty()) return rc;
+        return to_hot ? submit_bounds_copies(bounds_cold, bounds_hot, copies, s)
+                      : submit_bounds_copies(bounds_hot, bounds_cold, copies, s);
+    }
+
     // Enqueue whole-page copies between the pools (in chunks that fit a
     // staging slot): cold -> hot when to_hot, else hot -> cold.  `writes` are
     // page-table entries without a copy (rows cleared on eviction, resident
     // pages remapped on resume): they go to the table-write kernel, so the copy
     // grid only walks pages that move.
-    int submit_copies(bool to_hot, const std::vector<hck::CopyEntry>& copies,
-                      const std::vector<hck::CopyEntry>& writes, hipStream_t s, int kernel_id) {
+    int submit_page_copies(bool to_hot, const std::vector<hck::CopyEntry>& copies,
+                           const std::vector<hck::CopyEntry>& writes, hipStream_t s, int kernel_id) {
         if (!writes.empty()) {
             int rc = submit_table_writes(writes, s);
             if (rc) return rc;
@@ -589,9 +656,9 @@ struct kv_pool {
     // `exclude`) when too few hot pages are free.  Without spill all k are hot
     // or the call fails; with spill (the pool's, or `allow_spill`) the pages
     // that find no hot page spill: fresh cold pages if `fresh_spill`, else they
-    // stay where they are.  Changes nothing.
+    // stay where they are; never with `all_hot`.  Changes nothing.
     int plan_alloc(int64_t k, const std::vector<int32_t>& exclude, Alloc& a, bool fresh_spill = true,
-                   bool allow_spill = false) {
+                   bool allow_spill = false, bool all_hot = false) {
         a = Alloc();
         const int64_t have = hot_free.free_count();
         if (k <= have) {
@@ -600,7 +667,7 @@ struct kv_pool {
         }
         plan_lru(k - have, exclude, a.victims);
         const int64_t short_by = k - have - static_cast<int64_t>(a.victims.size());
-        if (short_by > 0 && !(spill || allow_spill))
+        if (short_by > 0 && (all_hot || !(spill || allow_spill)))
             return fail(KV_ERR_NO_HOT_PAGES, "need %lld hot pages: %lld free, %zu evictable",
                         static_cast<long long>(k), static_cast<long long>(have), a.victims.size());
         const int64_t n_hot = k - std::max<int64_t>(short_by, 0);
@@ -994,6 +1061,105 @@ int kv_session_import_cold(kv_pool* pool, int32_t seq_len, const int32_t* cold_p
     ss.spilled.assign(n, 0);
     *sid_out = sid;
     return KV_OK;
+}
+
+int kv_fork_sessions(kv_pool* pool, const int32_t* sids, const int32_t* kept, int32_t n, kv_stream_t stream,
+                     int32_t* sids_out) {
+    if (!pool || n < 0 || (n > 0 && (!sids || !kept || !sids_out))) return fail(KV_ERR_INVALID, "bad arguments");
+    if (n == 0) return KV_OK;
+    try {
+        int64_t need = 0;
+        for (int32_t i = 0; i < n; ++i) {
+            const Session* s = pool->session(sids[i]);
+            if (!s) return fail(KV_ERR_INVALID, "bad session id %d", sids[i]);
+            if (s->state != KV_SESSION_ACTIVE) return fail(KV_ERR_STATE, "session %d is not active", sids[i]);
+            if (kept[i] < 0 || kept[i] > s->seq_len)
+                return fail(KV_ERR_INVALID, "%d tokens kept of session %d's %d", kept[i], sids[i], s->seq_len);
+            need += pages_of(kept[i]);
+        }
+        std::vector<int32_t> ids;
+        for (int32_t i = 0; i < pool->d.max_sessions && static_cast<int32_t>(ids.size()) < n; ++i)
+            if (pool->sessions[i].state == KV_SESSION_FREE) ids.push_back(i);
+        if (static_cast<int32_t>(ids.size()) < n) return fail(KV_ERR_INVALID, "fewer than %d free session slots", n);
+        Alloc a;
+        int rc = pool->plan_alloc(need, {}, a, /*fresh_spill=*/false, /*allow_spill=*/false, /*all_hot=*/true);
+        if (rc) return rc;
+        // The branches, their pages in argument and logical order.  Pages whose slots are all
+        // tokens are never written again, so their cold copies (a spilled page is its own) serve
+        // both sessions; a partly filled one will be, by either.
+        std::vector<Session> made(static_cast<size_t>(n));
+        int64_t at = 0;
+        for (int32_t i = 0; i < n; ++i) {
+            const Session& s = pool->sessions[sids[i]];
+            Session& f = made[i];
+            const int32_t pages = pages_of(kept[i]);
+            f.state = KV_SESSION_ACTIVE;
+            f.seq_len = kept[i];
+            f.hot.assign(a.pages.begin() + at, a.pages.begin() + at + pages);
+            f.cold.assign(s.cold.begin(), s.cold.begin() + pages);
+            if (kept[i] % KV_PAGE_TOKENS) f.cold[pages - 1] = -1;
+            f.spilled.assign(pages, 0);
+            at += pages;
+        }
+        if (!pool->meta && need > 0) {
+            DeviceGuard g(pool->d.device);
+            hipStream_t st = pool->strm(stream);
+            // every page of a parent with the branches' pages that it goes to
+            std::vector<hck::ForkEntry> forks;
+            std::vector<hck::CopyEntry> fetched, records;
+            std::vector<uint8_t> done(static_cast<size_t>(n), 0);
+            std::vector<int32_t> mine;
+            for (int32_t i = 0; i < n; ++i) {
+                if (done[i]) continue;
+                mine.clear();
+                size_t most = 0;
+                for (int32_t j = i; j < n; ++j)
+                    if (sids[j] == sids[i]) {
+                        mine.push_back(j);
+                        done[j] = 1;
+                        most = std::max(most, made[j].hot.size());
+                    }
+                const Session& s = pool->sessions[sids[i]];
+                for (size_t p = 0; p < most; ++p) {
+                    bool fresh = true;   // the next destination opens an entry
+                    for (int32_t j : mine) {
+                        if (p >= made[j].hot.size()) continue;
+                        const int32_t dst = made[j].hot[p];
+                        if (s.hot[p] < 0) {
+                            fetched.push_back(hck::CopyEntry{s.cold[p], dst, -1, 0});
+                            continue;
+                        }
+                        if (pool->bounds) records.push_back(hck::CopyEntry{s.hot[p], dst, -1, 0});
+                        if (fresh || forks.back().n == hck::kForkDests) {
+                            forks.push_back(hck::ForkEntry{});
+                            forks.back().src = s.hot[p];
+                            fresh = false;
+                        }
+                        forks.back().dst[forks.back().n++] = dst;
+                    }
+                }
+            }
+            rc = pool->order_after_frees(st);
+            if (!rc) rc = pool->submit_victims(a, st);
+            if (!rc) rc = pool->submit_copies(true, fetched, {}, st, KV_KERNEL_PAGE_COPY);
+            if (!rc) rc = pool->submit_fork(forks, st);
+            if (!rc) rc = pool->submit_bounds_copies(pool->bounds_hot, pool->bounds_hot, records, st);
+            for (int32_t i = 0; i < n && !rc; ++i)
+                rc = pool->submit_row_at(ids[i], 0, made[i].hot.data(), static_cast<int32_t>(made[i].hot.size()), st);
+            if (rc) return rc;
+        }
+        pool->commit_victims(a);
+        for (int32_t p : a.pages) pool->hot_free.take(p);
+        for (int32_t i = 0; i < n; ++i) {
+            for (int32_t c : made[i].cold)
+                if (c >= 0) ++pool->cold_ref[c];
+            pool->sessions[ids[i]] = std::move(made[i]);
+            sids_out[i] = ids[i];
+        }
+        return KV_OK;
+    } catch (const std::bad_alloc&) {
+        return fail(KV_ERR_OOM, "out of host memory");
+    }
 }
 
 int kv_session_destroy(kv_pool* pool, int32_t sid, kv_stream_t stream) {
@@ -1665,6 +1831,44 @@ int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_
     return KV_OK;
 }
 
+// Checks and arguments that the choice of pages and the attention over them share.
+int sparse_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
+                const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, hck::SparseArgs& a) {
+    if (pool->meta) return fail(KV_ERR_INVALID, "metadata-only pool has no pages");
+    if (layer < 0 || layer >= pool->d.num_layers) return fail(KV_ERR_INVALID, "bad layer %d", layer);
+    if (!q || !page_table || !seq_lens) return fail(KV_ERR_INVALID, "NULL buffer");
+    if (num_q_heads <= 0 || num_q_heads % pool->d.num_kv_heads)
+        return fail(KV_ERR_INVALID, "query heads %d not a multiple of KV heads %d", num_q_heads,
+                    pool->d.num_kv_heads);
+    if (num_q_heads / pool->d.num_kv_heads > kMaxGroup)
+        return fail(KV_ERR_INVALID, "more than %d query heads per KV head", kMaxGroup);
+    if (pt_stride < 1 || static_cast<int64_t>(batch) * pt_stride >= (int64_t(1) << 31))
+        return fail(KV_ERR_INVALID, "bad page-table stride");
+    if (reinterpret_cast<uintptr_t>(q) & 15) return fail(KV_ERR_INVALID, "q must be 16-byte aligned");
+    a = hck::SparseArgs{};
+    a.hot = hck::slice_at(pool->hot_geom, 0, layer);
+    a.hot_stride = pool->hot_geom.page_stride;
+    a.num_hot = pool->d.num_hot_pages;
+    a.cold = pool->cold ? hck::slice_at(pool->cold_geom, 0, layer) : nullptr;
+    a.cold_stride = pool->cold_geom.page_stride;
+    a.num_cold = pool->named_cold();
+    a.q = q;
+    a.table = page_table;
+    a.pt_stride = pt_stride;
+    a.lens = seq_lens;
+    a.batch = batch;
+    a.num_kv_heads = pool->d.num_kv_heads;
+    a.group = num_q_heads / pool->d.num_kv_heads;
+    return KV_OK;
+}
+
+int workspace_ok(const void* workspace, size_t bytes, size_t need) {
+    if (!workspace) return fail(KV_ERR_INVALID, "NULL workspace");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KV_ERR_INVALID, "workspace must be 256-byte aligned");
+    if (bytes < need) return fail(KV_ERR_INVALID, "workspace %zu bytes, need %zu", bytes, need);
+    return KV_OK;
+}
+
 // Queries of a row times the query heads of a KV head, on average.
 int64_t prefill_rows(const kv_pool* pool, int32_t batch, int32_t total_q, int32_t num_q_heads) {
     const int64_t group = num_q_heads / pool->d.num_kv_heads;
@@ -1756,6 +1960,204 @@ int paged_tree_attention(kv_pool* pool, int32_t layer, const void* q, const void
     a.draft_lens = draft_lens;
     a.width = width;
     return chunk_launch(pool, a, static_cast<int64_t>(width) * a.group, /*tree=*/true, workspace, ws_bytes, stream);
+}
+
+}  // extern "C"
+
+extern "C" {
+
+size_t kv_bounds_bytes(const kv_pool_desc* desc) {
+    if (!desc_valid(desc)) return 0;
+    const size_t pages = static_cast<size_t>(desc->num_hot_pages) + static_cast<size_t>(desc->num_cold_pages);
+    const size_t n = std::max<size_t>(pages, 1) * static_cast<size_t>(desc->num_layers) *
+                     static_cast<size_t>(hck::bounds_record_bytes(desc->num_kv_heads, desc->head_dim));
+    return (n + 255) & ~static_cast<size_t>(255);
+}
+
+int kv_pool_set_bounds(kv_pool* pool, void* bounds, size_t bytes) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (pool->meta) return fail(KV_ERR_INVALID, "metadata-only pool has no pages");
+    if (!bounds) {
+        pool->bounds = nullptr;
+        return KV_OK;
+    }
+    if (reinterpret_cast<uintptr_t>(bounds) & 255) return fail(KV_ERR_INVALID, "bounds must be 256-byte aligned");
+    if (static_cast<int64_t>(pool->d.num_hot_pages) + pool->d.num_cold_pages >= (int64_t(1) << 31))
+        return fail(KV_ERR_INVALID, "more than 2^31 - 1 pages");
+    const size_t need = kv_bounds_bytes(&pool->d);
+    if (bytes < need) return fail(KV_ERR_INVALID, "bounds %zu bytes, need %zu", bytes, need);
+    const int64_t record = pool->bounds_record();
+    const int64_t layer = record * std::max<int64_t>(static_cast<int64_t>(pool->d.num_hot_pages) + pool->d.num_cold_pages, 1);
+    pool->bounds = static_cast<char*>(bounds);
+    pool->bounds_hot = hck::PoolGeom{pool->bounds, record, layer};
+    pool->bounds_cold = hck::PoolGeom{pool->bounds + record * pool->d.num_hot_pages, record, layer};
+    return KV_OK;
+}
+
+int kv_update_bounds(kv_pool* pool, int32_t layer_begin, int32_t num_layers, const int32_t* page_table,
+                     int64_t pt_stride, const int32_t* starts, const int32_t* seq_lens, int32_t batch,
+                     kv_stream_t stream) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (!pool->bounds) return fail(KV_ERR_INVALID, "the pool keeps no bounds (kv_pool_set_bounds)");
+    if (layer_begin < 0 || num_layers < 1 || layer_begin + static_cast<int64_t>(num_layers) > pool->d.num_layers)
+        return fail(KV_ERR_INVALID, "layers from %d, %d of them, outside the pool's %d", layer_begin, num_layers,
+                    pool->d.num_layers);
+    if (batch < 0 || batch > kMaxDecodeBatch)
+        return fail(KV_ERR_INVALID, "batch %d outside [0, %d]", batch, kMaxDecodeBatch);
+    if (batch == 0) return KV_OK;
+    if (!page_table || !seq_lens) return fail(KV_ERR_INVALID, "NULL buffer");
+    if (pt_stride < 1 || static_cast<int64_t>(batch) * pt_stride >= (int64_t(1) << 31))
+        return fail(KV_ERR_INVALID, "bad page-table stride");
+    DeviceGuard g(pool->d.device);
+    hipStream_t st = pool->strm(stream);
+    hck::BoundsUpdateArgs a;
+    a.hot = pool->hot_geom;
+    a.cold = pool->cold_geom;
+    a.num_hot = pool->d.num_hot_pages;
+    a.num_cold = pool->named_cold();
+    a.bounds = pool->bounds;
+    a.record = pool->bounds_record();
+    a.layer_stride = pool->bounds_hot.layer_stride;
+    a.table = page_table;
+    a.pt_stride = pt_stride;
+    a.starts = starts;
+    a.lens = seq_lens;
+    a.batch = batch;
+    a.num_kv_heads = pool->d.num_kv_heads;
+    a.layer = layer_begin;
+    const hck::LaunchEvents ev = kv_pool::plain_stream(st) ? pool->prof_events() : hck::LaunchEvents{};
+    const hipError_t e = hck::launch_bounds_update(a, pool->d.head_dim, pool->d.dtype, num_layers, st, ev);
+    pool->prof_done(KV_KERNEL_BOUNDS, ev, e);
+    return e == hipSuccess ? KV_OK : hip_fail(e, "bounds update launch");
+}
+
+int kv_read_bounds(kv_pool* pool, int32_t layer_begin, int32_t num_layers, const int32_t* pages, int32_t n,
+                   float* out, kv_stream_t stream) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (!pool->bounds) return fail(KV_ERR_INVALID, "the pool keeps no bounds (kv_pool_set_bounds)");
+    if (layer_begin < 0 || num_layers < 1 || layer_begin + static_cast<int64_t>(num_layers) > pool->d.num_layers)
+        return fail(KV_ERR_INVALID, "layers from %d, %d of them, outside the pool's %d", layer_begin, num_layers,
+                    pool->d.num_layers);
+    if (n < 0) return fail(KV_ERR_INVALID, "n %d is negative", n);
+    if (n == 0) return KV_OK;
+    if (!pages || !out) return fail(KV_ERR_INVALID, "NULL buffer");
+    if (reinterpret_cast<uintptr_t>(out) & 15) return fail(KV_ERR_INVALID, "out must be 16-byte aligned");
+    DeviceGuard g(pool->d.device);
+    hck::BoundsReadArgs a;
+    a.bounds = pool->bounds;
+    a.record = pool->bounds_record();
+    a.layer_stride = pool->bounds_hot.layer_stride;
+    a.num_hot = pool->d.num_hot_pages;
+    a.num_cold = pool->cold ? pool->d.num_cold_pages : 0;
+    a.pages = pages;
+    a.n = n;
+    a.num_kv_heads = pool->d.num_kv_heads;
+    a.head_dim = pool->d.head_dim;
+    a.layer = layer_begin;
+    a.out = out;
+    const hipError_t e = hck::launch_bounds_read(a, num_layers, pool->strm(stream));
+    return e == hipSuccess ? KV_OK : hip_fail(e, "bounds read launch");
+}
+
+size_t paged_select_workspace_bytes(const kv_pool* pool, int32_t batch, int64_t pt_stride, int32_t width) {
+    if (!pool || pool->meta || batch < 0 || batch > kMaxDecodeBatch || width < 1 || pt_stride < 1 ||
+        static_cast<int64_t>(batch) * pt_stride >= (int64_t(1) << 31))
+        return 0;
+    return hck::select_workspace_bytes(static_cast<int64_t>(batch) * pool->d.num_kv_heads, pt_stride, width);
+}
+
+int paged_select_pages(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
+                       const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, int32_t width, int32_t first,
+                       int32_t recent, int32_t* picks, int32_t* counts, void* workspace, size_t ws_bytes,
+                       kv_stream_t stream) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (!pool->bounds) return fail(KV_ERR_INVALID, "the pool keeps no bounds (kv_pool_set_bounds)");
+    if (width < 1 || first < 0 || recent < 0 || static_cast<int64_t>(first) + recent > width)
+        return fail(KV_ERR_INVALID, "width %d below 1 or below %d first and %d recent pages", width, first, recent);
+    if (batch < 0 || batch > kMaxDecodeBatch)
+        return fail(KV_ERR_INVALID, "batch %d outside [0, %d]", batch, kMaxDecodeBatch);
+    if (batch == 0) return KV_OK;
+    hck::SparseArgs shared;
+    int rc = sparse_args(pool, layer, q, page_table, pt_stride, seq_lens, batch, num_q_heads, shared);
+    if (rc != KV_OK) return rc;
+    if (!picks || !counts) return fail(KV_ERR_INVALID, "NULL picks or counts");
+    const size_t need = hck::select_workspace_bytes(static_cast<int64_t>(batch) * pool->d.num_kv_heads, pt_stride, width);
+    rc = workspace_ok(workspace, ws_bytes, need);
+    if (rc != KV_OK) return rc;
+    DeviceGuard g(pool->d.device);
+    hipStream_t st = pool->strm(stream);
+    hck::SelectArgs a;
+    a.bounds = pool->bounds;
+    a.record = pool->bounds_record();
+    a.layer_stride = pool->bounds_hot.layer_stride;
+    a.num_hot = shared.num_hot;
+    a.num_cold = shared.num_cold;
+    a.q = q;
+    a.table = page_table;
+    a.pt_stride = pt_stride;
+    a.lens = seq_lens;
+    a.batch = batch;
+    a.num_kv_heads = pool->d.num_kv_heads;
+    a.group = shared.group;
+    a.num_q_heads = num_q_heads;
+    a.layer = layer;
+    a.width = width;
+    a.first = first;
+    a.recent = recent;
+    a.keys = static_cast<unsigned*>(workspace);
+    a.picks = picks;
+    a.counts = counts;
+    const bool prof = kv_pool::plain_stream(st);
+    const hck::LaunchEvents ev = prof && pt_stride > width ? pool->prof_events() : hck::LaunchEvents{};
+    const hck::LaunchEvents evp = prof ? pool->prof_events() : hck::LaunchEvents{};
+    const hipError_t e = hck::launch_select_pages(a, pool->d.head_dim, pool->d.dtype, st, ev, evp);
+    pool->prof_done(KV_KERNEL_PAGE_SCORES, ev, e);
+    pool->prof_done(KV_KERNEL_PAGE_PICK, evp, e);
+    return e == hipSuccess ? KV_OK : hip_fail(e, "page choice launch");
+}
+
+size_t paged_sparse_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t width) {
+    if (!chunk_shape_ok(pool, batch, num_q_heads) || width < 1) return 0;
+    const int32_t group = num_q_heads / pool->d.num_kv_heads;
+    return hck::sparse_workspace_bytes(hck::sparse_plan(pool->cus, batch, pool->d.num_kv_heads, group, width),
+                                       static_cast<int64_t>(batch) * pool->d.num_kv_heads, group, pool->d.head_dim);
+}
+
+int paged_sparse_attention(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
+                           const int32_t* seq_lens, const int32_t* picks, const int32_t* counts, int32_t width,
+                           int32_t batch, int32_t num_q_heads, float scale, void* out, void* workspace,
+                           size_t ws_bytes, kv_stream_t stream) {
+    if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (width < 1) return fail(KV_ERR_INVALID, "width %d below 1", width);
+    if (batch < 0 || batch > kMaxDecodeBatch)
+        return fail(KV_ERR_INVALID, "batch %d outside [0, %d]", batch, kMaxDecodeBatch);
+    if (batch == 0) return KV_OK;
+    hck::SparseArgs a;
+    int rc = sparse_args(pool, layer, q, page_table, pt_stride, seq_lens, batch, num_q_heads, a);
+    if (rc != KV_OK) return rc;
+    if (!picks || !out) return fail(KV_ERR_INVALID, "NULL picks or out");
+    if (reinterpret_cast<uintptr_t>(out) & 15) return fail(KV_ERR_INVALID, "out must be 16-byte aligned");
+    const hck::SparsePlan plan = hck::sparse_plan(pool->cus, batch, a.num_kv_heads, a.group, width);
+    const int64_t lists = static_cast<int64_t>(batch) * a.num_kv_heads;
+    rc = workspace_ok(workspace, ws_bytes, hck::sparse_workspace_bytes(plan, lists, a.group, pool->d.head_dim));
+    if (rc != KV_OK) return rc;
+    DeviceGuard g(pool->d.device);
+    hipStream_t st = pool->strm(stream);
+    a.out = out;
+    a.picks = picks;
+    a.counts = counts;
+    a.width = width;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.parts = plan.parts;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = a.part_o + lists * plan.parts * a.group * pool->d.head_dim;
+    const bool prof = kv_pool::plain_stream(st);
+    const hck::LaunchEvents ev = prof ? pool->prof_events() : hck::LaunchEvents{};
+    const hck::LaunchEvents evm = prof && plan.parts > 1 ? pool->prof_events() : hck::LaunchEvents{};
+    const hipError_t e = hck::launch_sparse_attention(a, plan, pool->d.head_dim, pool->d.dtype, st, ev, evm);
+    pool->prof_done(KV_KERNEL_SPARSE, ev, e);
+    pool->prof_done(KV_KERNEL_SPARSE_MERGE, evm, e);
+    return e == hipSuccess ? KV_OK : hip_fail(e, "sparse attention launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,858 @@
+// Decode attention over the pages that a cheap score picks, for gfx950: bounds of each
+// page's keys, the choice of pages by those bounds, and the attention over the chosen ones.
+//
+// Mathematics.  For a page, a KV head and a dim d let lo_d and hi_d be the smallest and the
+// largest key value over the page's tokens.  Then for any query q and any token t of it
+//     q . k_t = sum_d q_d k_td <= sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d =: u,
+// so pages with a small u hold no token that matters to q.  lo and hi are kept as whole
+// numbers of 8 bits times a power of two of the page and head (floor and ceil: the bounds
+// stay bounds), q is rounded to whole numbers times a power of two of its own, and u becomes
+// a product of 8-bit matrices: [min(q, 0) | max(q, 0)] . [lo | hi], exact in 32 bits (at most
+// 128 * 127^2 < 2^21 in magnitude), and so is its product with the two powers of two in
+// float32.  Which pages are picked therefore does not depend on the order of any sum.
+//
+// Records.  A page's record of one layer is [KV head][lo: D bytes, hi: D bytes], then 16
+// bytes of which byte h is the power of head h: 1/31 of the page's K and V in bfloat16.
+
+#include "device_common.h"
+#include "kernels.h"
+#include "page_tiles.h"
+
+#include <float.h>
+#include <math.h>
+
+#include <algorithm>
+
+namespace hck {
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kPowerLimit = 50;  // |e| at most: products of two powers and a sum stay normal numbers
+
+// 2^e for |e| < 127.
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float(static_cast<unsigned>(e + 127) << 23); }
+
+// The least e of [-50, 50] with top <= 127 * 2^e (-7 for 0; 50 for what no e suits).
+__device__ __forceinline__ int power_for(float top) {
+    int e = __builtin_amdgcn_frexp_expf(fminf(top, FLT_MAX)) - 7;
+    e = e < -kPowerLimit ? -kPowerLimit : e > kPowerLimit ? kPowerLimit : e;
+    if (top * two_to(-e) > 127.f && e < kPowerLimit) ++e;
+    return e;
+}
+
+__device__ __forceinline__ int clamp_power(int e) {
+    return e < -kPowerLimit ? -kPowerLimit : e > kPowerLimit ? kPowerLimit : e;
+}
+
+// A value that is no number counts as the infinity of its sign.
+__device__ __forceinline__ float no_nan(float x) { return x != x ? copysignf(INFINITY, x) : x; }
+
+__device__ __forceinline__ float clamp_127(float x) { return fminf(fmaxf(x, -127.f), 127.f); }
+
+// The page that a table entry names: its number among the records (hot pages, then cold
+// ones), or -1 where it names no page of either pool.
+__device__ __forceinline__ int page_index(int entry, int num_hot, int num_cold) {
+    const unsigned u = static_cast<unsigned>(entry);
+    const unsigned id = u & static_cast<unsigned>(kPageIdMask), tag = u >> 29;
+    if (tag == 0 && id < static_cast<unsigned>(num_hot)) return static_cast<int>(id);
+    if (tag == 2 && id < static_cast<unsigned>(num_cold)) return num_hot + static_cast<int>(id);
+    return -1;
+}
+
+template <int CTRL>
+__device__ __forceinline__ int dpp(int x) {
+    return __builtin_amdgcn_update_dpp(x, x, CTRL, 0xF, 0xF, false);
+}
+// Lane i's value from lane i ^ 1, i ^ 2, 7 - i of its 8 and 15 - i of its 16.
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppMirror8 = 0x141, kDppMirror16 = 0x140;
+
+// Maximum of non-negative floats over the wave, in every lane.
+__device__ __forceinline__ float wave_max(float x) {
+    int v = __float_as_int(x);  // ordered like the floats
+    v = max(v, dpp<kDppXor1>(v));
+    v = max(v, dpp<kDppXor2>(v));
+    v = max(v, dpp<kDppMirror8>(v));
+    v = max(v, dpp<kDppMirror16>(v));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x142, 0xA, 0xF, false));  // row_bcast:15 into rows 1 and 3
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x143, 0xC, 0xF, false));  // row_bcast:31 into rows 2 and 3
+    return __int_as_float(__builtin_amdgcn_readlane(v, 63));
+}
+
+// ---------------------------------------------------------------------------
+// Bounds of pages.
+
+// Bit patterns in an order that signed comparisons of whole words (bfloat16: of halves) follow;
+// the map is its own inverse.
+template <bool BF16>
+__device__ __forceinline__ unsigned ordered(unsigned w) {
+    if constexpr (BF16) {
+        const s16x2 x = __builtin_bit_cast(s16x2, w);
+        return w ^ (__builtin_bit_cast(unsigned, static_cast<s16x2>(x >> 15)) & 0x7FFF7FFFu);
+    } else {
+        return w ^ (static_cast<unsigned>(static_cast<int>(w) >> 31) & 0x7FFFFFFFu);
+    }
+}
+template <bool BF16, bool MAX>
+__device__ __forceinline__ unsigned pick(unsigned a, unsigned b) {
+    if constexpr (BF16) {
+        const s16x2 x = __builtin_bit_cast(s16x2, a), y = __builtin_bit_cast(s16x2, b);
+        return __builtin_bit_cast(unsigned, MAX ? __builtin_elementwise_max(x, y) : __builtin_elementwise_min(x, y));
+    } else {
+        const int x = static_cast<int>(a), y = static_cast<int>(b);
+        return static_cast<unsigned>(MAX ? max(x, y) : min(x, y));
+    }
+}
+
+// One wave takes a (page, KV head) at a time.  A 16-byte group of dims of all 16 tokens is
+// 256 consecutive bytes of the K tile and belongs to kLanes lanes, each with every kLanes-th
+// token of it, so most of the reduction over tokens stays in a lane's registers.
+template <int D, bool BF16>
+__global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const BoundsUpdateArgs a) {
+    constexpr int kElt = BF16 ? 2 : 4;
+    constexpr int kX = 16 / kElt;                     // dims of a group
+    constexpr int kGroups = D / kX;                   // groups of a tile: 8, 16 or 32
+    constexpr int kLanes = kWave / kGroups;           // lanes of a group: 8, 4 or 2
+    constexpr int kLoads = kPageTokens / kLanes;
+    constexpr int kDims = kX / kLanes;                // dims that a lane writes: 1 or 2
+    constexpr int64_t kTile = static_cast<int64_t>(kPageTokens) * D * kElt;
+    const int b = blockIdx.y;
+    const int layer = a.layer + static_cast<int>(blockIdx.z);
+    const int len = a.lens[b];
+    if (len <= 0 || len > kPageTokens * a.pt_stride) return;
+    int first = a.starts ? a.starts[b] : 0;
+    first = first < 0 ? 0 : first;
+    if (first >= len) return;
+    const int p0 = first / kPageTokens, pages = (len - 1) / kPageTokens + 1 - p0;
+    const unsigned heads = static_cast<unsigned>(a.num_kv_heads);
+    const unsigned units = static_cast<unsigned>(pages) * heads;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int dg = lane / kLanes, sub = lane % kLanes;
+    const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
+    for (unsigned u = blockIdx.x * kBlockWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); u < units;
+         u += gridDim.x * kBlockWaves) {
+        const int page = p0 + static_cast<int>(u / heads), head = static_cast<int>(u % heads);
+        const int at = page_index(__builtin_amdgcn_readfirstlane(row[page]), a.num_hot, a.num_cold);
+        if (at < 0) continue;
+        const char* slice = at < a.num_hot ? slice_at(a.hot, at, layer) : slice_at(a.cold, at - a.num_hot, layer);
+        const char* tile = slice + head * 2 * kTile + dg * 256 + sub * 16;
+        const int valid = len - page * kPageTokens;   // tokens of the page, or more than 16
+        u32x4 w[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tile + i * kLanes * 16));
+        unsigned lo[4], hi[4];
+        constexpr unsigned kLeast = BF16 ? 0x80008000u : 0x80000000u, kMost = BF16 ? 0x7FFF7FFFu : 0x7FFFFFFFu;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            lo[j] = kMost;
+            hi[j] = kLeast;
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const bool in = sub + i * kLanes < valid;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned o = ordered<BF16>(w[i][j]);
+                lo[j] = pick<BF16, false>(lo[j], in ? o : kMost);
+                hi[j] = pick<BF16, true>(hi[j], in ? o : kLeast);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            lo[j] = pick<BF16, false>(lo[j], dpp<kDppXor1>(lo[j]));
+            hi[j] = pick<BF16, true>(hi[j], dpp<kDppXor1>(hi[j]));
+            if constexpr (kLanes >= 4) {
+                lo[j] = pick<BF16, false>(lo[j], dpp<kDppXor2>(lo[j]));
+                hi[j] = pick<BF16, true>(hi[j], dpp<kDppXor2>(hi[j]));
+            }
+            if constexpr (kLanes >= 8) {
+                lo[j] = pick<BF16, false>(lo[j], dpp<kDppMirror8>(lo[j]));
+                hi[j] = pick<BF16, true>(hi[j], dpp<kDppMirror8>(hi[j]));
+            }
+        }
+        // this lane's dims: kDims of its group, from the sub-th on
+        float l[kDims], h[kDims];
+        if constexpr (BF16) {
+            unsigned wl = lo[0], wh = hi[0];
+#pragma unroll
+            for (int j = 1; j < 4; ++j) {
+                wl = sub * kDims / 2 == j ? lo[j] : wl;
+                wh = sub * kDims / 2 == j ? hi[j] : wh;
+            }
+            wl = ordered<true>(wl);
+            wh = ordered<true>(wh);
+            if constexpr (kDims == 2) {
+                l[0] = __uint_as_float(wl << 16);
+                l[1] = __uint_as_float(wl & 0xFFFF0000u);
+                h[0] = __uint_as_float(wh << 16);
+                h[1] = __uint_as_float(wh & 0xFFFF0000u);
+            } else {
+                l[0] = __uint_as_float(sub & 1 ? wl & 0xFFFF0000u : wl << 16);
+                h[0] = __uint_as_float(sub & 1 ? wh & 0xFFFF0000u : wh << 16);
+            }
+        } else {
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) {
+                unsigned wl = lo[d], wh = hi[d];
+#pragma unroll
+                for (int j = 1; j < 4 / kDims; ++j) {
+                    wl = sub == j ? lo[j * kDims + d] : wl;
+                    wh = sub == j ? hi[j * kDims + d] : wh;
+                }
+                l[d] = __uint_as_float(ordered<false>(wl));
+                h[d] = __uint_as_float(ordered<false>(wh));
+            }
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            l[d] = no_nan(l[d]);
+            h[d] = no_nan(h[d]);
+            top = fmaxf(top, fmaxf(fabsf(l[d]), fabsf(h[d])));
+        }
+        const int e = power_for(wave_max(top));
+        const float down = two_to(-e);
+        unsigned ql = 0, qh = 0;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            ql |= (static_cast<unsigned>(static_cast<int>(clamp_127(floorf(l[d] * down)))) & 0xFFu) << (8 * d);
+            qh |= (static_cast<unsigned>(static_cast<int>(clamp_127(ceilf(h[d] * down)))) & 0xFFu) << (8 * d);
+        }
+        char* rec = a.bounds + layer * a.layer_stride + static_cast<int64_t>(at) * a.record;
+        char* out = rec + head * 2 * D + dg * kX + sub * kDims;
+        if constexpr (kDims == 2) {
+            *reinterpret_cast<unsigned short*>(out) = static_cast<unsigned short>(ql);
+            *reinterpret_cast<unsigned short*>(out + D) = static_cast<unsigned short>(qh);
+        } else {
+            *out = static_cast<char>(ql);
+            out[D] = static_cast<char>(qh);
+        }
+        if (lane == 0) rec[a.num_kv_heads * 2 * D + head] = static_cast<char>(e);
+    }
+}
+
+// Records as values: out [layers][n][KV heads][lo, hi][D] float32, NaN where an entry names no page.
+__global__ __launch_bounds__(kBlockThreads) void bounds_read_kernel(const BoundsReadArgs a) {
+    const int per = a.num_kv_heads * 2 * a.head_dim / 4;  // 4-byte words of a record's values
+    const int64_t total = static_cast<int64_t>(a.n) * per;
+    const int layer = a.layer + static_cast<int>(blockIdx.y);
+    f32x4* out = reinterpret_cast<f32x4*>(a.out) + static_cast<int64_t>(blockIdx.y) * total;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlockThreads + threadIdx.x; i < total;
+         i += static_cast<int64_t>(gridDim.x) * kBlockThreads) {
+        const int64_t p = i / per;
+        const int word = static_cast<int>(i - p * per);
+        const int at = page_index(a.pages[p], a.num_hot, a.num_cold);
+        const float nan = __builtin_nanf("");
+        f32x4 v = {nan, nan, nan, nan};
+        if (at >= 0) {
+            const char* rec = a.bounds + layer * a.layer_stride + static_cast<int64_t>(at) * a.record;
+            const unsigned w = reinterpret_cast<const unsigned*>(rec)[word];
+            const int e = static_cast<signed char>(rec[4 * per + word * 2 / a.head_dim]);
+            const float unit = two_to(clamp_power(e));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = static_cast<float>(static_cast<signed char>(w >> (8 * j))) * unit;
+        }
+        out[i] = v;
+    }
+}
+
+// Records of copied pages: entry e's from page e.src of one pool to page e.dst of the other.
+__global__ __launch_bounds__(kBlockThreads) void bounds_copy_kernel(const PoolGeom src, const PoolGeom dst,
+                                                                    const CopyEntry* __restrict__ entries, int32_t n,
+                                                                    int words) {
+    const int layer = static_cast<int>(blockIdx.y);
+    const int64_t total = static_cast<int64_t>(n) * words;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlockThreads + threadIdx.x; i < total;
+         i += static_cast<int64_t>(gridDim.x) * kBlockThreads) {
+        const int64_t k = i / words;
+        const int word = static_cast<int>(i - k * words);
+        const CopyEntry e = entries[k];
+        if (e.src < 0) continue;
+        reinterpret_cast<u32x4*>(slice_at(dst, e.dst, layer))[word] =
+            reinterpret_cast<const u32x4*>(slice_at(src, e.src, layer))[word];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Scores of pages.
+
+constexpr unsigned kKeyBad = 0xFFFFFFFEu;  // above every score: a page that no pool holds
+
+// Scores in an order that unsigned comparisons follow; none maps to 0.
+__device__ __forceinline__ unsigned score_key(float s) {
+    const unsigned u = __float_as_uint(s);
+    return u ^ (u & 0x80000000u ? 0xFFFFFFFFu : 0x80000000u);
+}
+
+// One wave's queries of a KV head as the rows of the product: lane l holds head l % 16 of the
+// group, 16 dims of every 64 from 16 (l / 16) on.
+template <int D>
+struct QueryRows {
+    i32x4 neg[D / 64], pos[D / 64];
+    float unit[4];   // 2^e of heads 4 (l / 16) + r, 0 past the group
+};
+
+template <int D, bool BF16>
+__device__ __forceinline__ void load_query_rows(QueryRows<D>& q, const SelectArgs& a, int b, int g, int lane) {
+    constexpr int kElt = BF16 ? 2 : 4;
+    constexpr int kWords = 16 * kElt / 16;  // 16-byte words of 16 dims
+    const int h = lane & 15, part = lane >> 4;
+    const bool in = h < a.group;
+    const char* src = static_cast<const char*>(a.q) +
+                      ((static_cast<int64_t>(b) * a.num_q_heads + g * a.group + (in ? h : 0)) * D + 16 * part) * kElt;
+    u32x4 w[D / 64][kWords];
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[c][i] = *reinterpret_cast<const u32x4*>(src + 64 * c * kElt + 16 * i);
+    float v[D / 64][16];
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if constexpr (BF16) {
+                const unsigned x = w[c][j / 8][(j % 8) / 2];
+                v[c][j] = __uint_as_float(j & 1 ? x & 0xFFFF0000u : x << 16);
+            } else {
+                v[c][j] = __uint_as_float(w[c][j / 4][j % 4]);
+            }
+            v[c][j] = no_nan(v[c][j]);
+            top = fmaxf(top, fabsf(v[c][j]));
+        }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const int e = power_for(top);
+    const float down = two_to(-e);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            unsigned n = 0, p = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int x = static_cast<int>(clamp_127(rintf(v[c][4 * j + k] * down)));
+                n |= (static_cast<unsigned>(min(x, 0)) & 0xFFu) << (8 * k);
+                p |= (static_cast<unsigned>(max(x, 0)) & 0xFFu) << (8 * k);
+            }
+            q.neg[c][j] = static_cast<int>(n);
+            q.pos[c][j] = static_cast<int>(p);
+        }
+    const float unit = in ? two_to(e) : 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) q.unit[r] = __shfl(unit, 4 * part + r);
+}
+
+// Keys of the scores of all pages of the rows that have more pages than are picked.  A block
+// takes chunks of 64 pages of a row, its waves a KV head each where the heads come in twos or
+// fours: the records of a page are then read side by side.
+template <int D, bool BF16>
+__global__ __launch_bounds__(kBlockThreads) void page_scores_kernel(const SelectArgs a) {
+    const int b = blockIdx.y;
+    const int len = a.lens[b];
+    if (len <= 0 || len > kPageTokens * a.pt_stride) return;
+    const int n = (len - 1) / kPageTokens + 1;
+    if (n <= a.width) return;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int head_waves = a.num_kv_heads % 4 == 0 ? 4 : a.num_kv_heads % 2 == 0 ? 2 : 1;
+    const int slices = kBlockWaves / head_waves;   // waves of a head, 64 pages each in turn
+    const int step = kWave * slices * static_cast<int>(gridDim.x);
+    const int begin = kWave * (slices * static_cast<int>(blockIdx.x) + wave / head_waves);
+    if (begin >= n) return;
+    const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
+    const char* bounds = a.bounds + a.layer * a.layer_stride;
+    const int part = lane >> 4;
+    for (int g = wave % head_waves; g < a.num_kv_heads; g += head_waves) {
+        QueryRows<D> q;
+        load_query_rows<D, BF16>(q, a, b, g, lane);
+        unsigned* keys = a.keys + (static_cast<int64_t>(b) * a.num_kv_heads + g) * a.pt_stride;
+        for (int p0 = begin; p0 < n; p0 += step) {
+            const int at = p0 + lane < n ? page_index(row[p0 + lane], a.num_hot, a.num_cold) : -1;
+            const char* rec = bounds + static_cast<int64_t>(at < 0 ? 0 : at) * a.record;
+            const int e = static_cast<signed char>(rec[a.num_kv_heads * 2 * D + g]);
+            u32x4 w[4][2 * D / 64];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int src = __shfl(at < 0 ? 0 : at, 16 * t + (lane & 15));
+                const char* p = bounds + static_cast<int64_t>(src) * a.record + g * 2 * D + 16 * part;
+#pragma unroll
+                for (int c = 0; c < 2 * D / 64; ++c) w[t][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
+            }
+            float best = 0.f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                i32x4 s = {0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) {
+                    s = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.neg[c], __builtin_bit_cast(i32x4, w[t][c]), s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.pos[c], __builtin_bit_cast(i32x4, w[t][c + D / 64]), s,
+                                                              0, 0, 0);
+                }
+                float x = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (q.unit[r] != 0.f) x = fmaxf(x, static_cast<float>(s[r]) * q.unit[r]);
+                x = fmaxf(x, __shfl_xor(x, 16));
+                x = fmaxf(x, __shfl_xor(x, 32));
+                best = part == t ? x : best;
+            }
+            if (p0 + lane < n) keys[p0 + lane] = at < 0 ? kKeyBad : score_key(best * two_to(clamp_power(e)));
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The choice.
+
+// Block (g, b) writes row b's picks for KV head g: all its pages where they are no more than
+// `width`, else the first `first`, the last `recent` and the best of those between, whose
+// threshold is found bit by bit: of all keys the largest T that at least k of them reach.
+// Ties at T go to the lowest pages.
+template <int THREADS, int KEYS>
+__global__ __launch_bounds__(THREADS) void page_pick_kernel(const SelectArgs a) {
+    constexpr int kWaves = THREADS / kWave;
+    const int g = blockIdx.x, b = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
+    int32_t* picks = a.picks + seg * a.width;
+    const int len = a.lens[b];
+    const int n = len <= 0 || len > kPageTokens * a.pt_stride ? 0 : (len - 1) / kPageTokens + 1;
+    if (n <= a.width) {
+        for (int i = tid; i < a.width; i += THREADS) picks[i] = i < n ? i : -1;
+        if (tid == 0) a.counts[seg] = n;
+        return;
+    }
+    const unsigned* keys = a.keys + seg * a.pt_stride;
+    const int lo = a.first, hi = n - a.recent;
+    const int want = a.width - a.first - a.recent;   // at least 0, less than hi - lo
+    __shared__ int s_count[2][kWaves];
+    // keys that are no candidates count as 0, which no threshold is
+    auto key = [&](int i) { return i >= lo && i < hi ? keys[i] : 0u; };
+    unsigned held[KEYS > 0 ? KEYS : 1];
+    if constexpr (KEYS > 0) {
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j) held[j] = key(j * THREADS + tid);
+    }
+    auto count = [&](unsigned t, int parity) {
+        int c = 0;
+        if constexpr (KEYS > 0) {
+#pragma unroll
+            for (int j = 0; j < KEYS; ++j) c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(held[j] >= t));
+        } else {
+            for (int i0 = 0; i0 < n; i0 += THREADS)
+                c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i0 + tid < n && key(i0 + tid) >= t));
+        }
+        if (lane == 0) s_count[parity][wave] = c;
+        __syncthreads();
+        int total = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) total += s_count[parity][w];
+        return total;
+    };
+    unsigned threshold = 0;
+    int above = hi - lo;   // candidates at or above the threshold
+    if (want == 0) {
+        threshold = 0xFFFFFFFFu;
+    } else {
+        int parity = 0;
+        for (unsigned bit = 0x80000000u; bit != 0 && above != want; bit >>= 1) {
+            const int c = count(threshold | bit, parity);
+            parity ^= 1;
+            if (c >= want) {
+                threshold |= bit;
+                above = c;
+            }
+        }
+    }
+    // In order of the pages: pages kept anyway and keys above the threshold, and of those at it
+    // as many as are left (all of them where the candidates at or above it are just enough).
+    __shared__ int s_more[kWaves], s_tie[kWaves];
+    int base = 0, ties = 0;
+    int spare = want;   // places for ties
+    if (want > 0) {
+        __syncthreads();
+        spare = above == want ? 0x7FFFFFFF : want - count(threshold + 1, 0);
+        __syncthreads();
+    }
+    auto emit = [&](int i, unsigned k) __attribute__((always_inline)) {
+        const bool keep = i < n && (i < lo || i >= hi);
+        const bool more = keep || (want > 0 && k > threshold);
+        const bool tie = want > 0 && !keep && i < n && k == threshold && k != 0;
+        const uint64_t bm = __builtin_amdgcn_ballot_w64(more), bt = __builtin_amdgcn_ballot_w64(tie);
+        if (lane == 0) {
+            s_more[wave] = __builtin_popcountll(bm);
+            s_tie[wave] = __builtin_popcountll(bt);
+        }
+        __syncthreads();
+        int m0 = base, t0 = ties, m1 = 0, t1 = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            m0 += w < wave ? s_more[w] : 0;
+            t0 += w < wave ? s_tie[w] : 0;
+            m1 += s_more[w];
+            t1 += s_tie[w];
+        }
+        const uint64_t below = (1ull << lane) - 1;
+        const int m = m0 + __builtin_popcountll(bm & below), t = t0 + __builtin_popcountll(bt & below);
+        if (more || (tie && t < spare)) picks[m + (t < spare ? t : spare)] = i;
+        base += m1;
+        ties += t1;
+        __syncthreads();
+    };
+    if constexpr (KEYS > 0) {
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j)
+            if (j * THREADS < n) emit(j * THREADS + tid, held[j]);
+    } else {
+        for (int i0 = 0; i0 < n; i0 += THREADS) emit(i0 + tid, key(i0 + tid));
+    }
+    if (tid == 0) a.counts[seg] = a.width;
+}
+
+// ---------------------------------------------------------------------------
+// Attention over picked pages.
+
+template <int D, bool BF16>
+struct SparseState {
+    u32x4 q[Shape<D, BF16>::kKLoads];
+    f32x4 o[Shape<D, BF16>::kChunks];
+    float m;       // running maximum, -inf before the first page
+    float shift;   // what the exponents are taken against: m, or 0 while that is -inf
+    float l;
+};
+
+// One page with `valid` tokens (1..16): online softmax and weighted V.
+template <int D, bool BF16>
+__device__ __forceinline__ void sparse_page(SparseState<D, BF16>& st, PageRegs<D, BF16>& pg, int valid,
+                                            float scale_log2, int qg) {
+    using S = Shape<D, BF16>;
+    f32x4 s = page_scores<D, BF16>(pg, st.q);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[r] *= scale_log2;
+    if (valid < kPageTokens) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = 4 * qg + r < valid ? s[r] : -INFINITY;
+        mask_v<D, BF16>(pg, valid, qg);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[r]);
+    // The maximum is the same on the four lanes of a head; it is reduced over them, and the
+    // sums rescaled, only where some lane sees a score above it.
+    if (__builtin_amdgcn_ballot_w64(mx > st.m)) {
+        const float m_new = fmaxf(st.m, wave_max_4(mx));
+        const float shift = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(st.m - shift);
+        st.l *= alpha;
+#pragma unroll
+        for (int c = 0; c < S::kChunks; ++c) st.o[c] *= alpha;
+        st.m = m_new;
+        st.shift = shift;
+    }
+    float p[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - st.shift);
+    if constexpr (BF16) {
+        // weights rounded to bf16 for the product, the same rounded ones in the sum
+        __bf16 pb[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            pb[r] = static_cast<__bf16>(p[r]);
+            st.l += static_cast<float>(pb[r]);
+        }
+        const s16x4 pv = {__builtin_bit_cast(short, pb[0]), __builtin_bit_cast(short, pb[1]),
+                          __builtin_bit_cast(short, pb[2]), __builtin_bit_cast(short, pb[3])};
+#pragma unroll
+        for (int c = 0; c < S::kChunks; ++c)
+            st.o[c] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, pg.v[c]), pv, st.o[c], 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) st.l += p[r];
+#pragma unroll
+        for (int c = 0; c < S::kChunks; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                st.o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(pg.v[c][j]), p[j], st.o[c], 0, 0, 0);
+    }
+}
+
+// Where a list has tokens but every score was minus infinity its maximum counts as this, so that
+// it ends in 0 / 0; a list without tokens keeps minus infinity and ends in zeros.
+constexpr float kNoScore = -FLT_MAX;
+
+template <int D, bool BF16>
+__device__ __forceinline__ void store_result(const SparseArgs& a, int64_t head_row, int quad, float M, float den,
+                                             const f32x4& acc, bool invalid) {
+    f32x4 v;
+    const float nan = __builtin_nanf("");
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = invalid ? nan : M == -INFINITY && !(den != den) ? 0.f : acc[j] / den;
+    const int64_t at = head_row * D + 4 * quad;
+    if constexpr (BF16) {
+        __bf16 w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = static_cast<__bf16>(v[j]);
+        *reinterpret_cast<u32x2*>(static_cast<__bf16*>(a.out) + at) = __builtin_bit_cast(u32x2, w);
+    } else {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v;
+    }
+}
+
+// Block (s, g, b): part s of row b's list for KV head g, shared by the block's waves in
+// consecutive ranges, joined in LDS.  With one part the block writes the output, else a
+// partial result.
+template <int D, bool BF16, int WAVES, int R>
+__global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const SparseArgs a) {
+    using S = Shape<D, BF16>;
+    const int part = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int qg = lane >> 4;
+    const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
+    const int len = a.lens[b];
+    const bool invalid = len < 0 || len > kPageTokens * a.pt_stride;
+    const int n = invalid || len == 0 ? 0 : (len - 1) / kPageTokens + 1;
+    int count = a.counts ? a.counts[seg] : a.width;
+    count = count < 0 || n == 0 ? 0 : count > a.width ? a.width : count;
+    const int parts = a.parts * WAVES, k = part * WAVES + wave;
+    const int e0 = static_cast<int>(static_cast<int64_t>(count) * k / parts);
+    const int e1 = static_cast<int>(static_cast<int64_t>(count) * (k + 1) / parts);
+    const int32_t* list = a.picks + seg * a.width;
+    const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
+    const unsigned head_off = static_cast<unsigned>(g) * 2u * S::kTile;
+    const unsigned koff = 16u * lane;
+    const unsigned voff = BF16 ? (32u * (lane & 15) + 8u * qg) : (64u * (lane & 15) + 16u * qg);
+
+    SparseState<D, BF16> st;
+    {
+        const __amdgpu_buffer_rsrc_t qr = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char*>(static_cast<const char*>(a.q) + seg * a.group * (D * S::kElt)), static_cast<short>(0),
+            a.group * D * S::kElt, kRsrcWord3);   // head slots past the group read zeros
+        const unsigned off = static_cast<unsigned>((lane & 15) * D * S::kElt + 16 * (lane >> 4));
+#pragma unroll
+        for (int i = 0; i < S::kKLoads; ++i) st.q[i] = __builtin_amdgcn_raw_buffer_load_b128(qr, off + 64u * i, 0, 0);
+    }
+#pragma unroll
+    for (int c = 0; c < S::kChunks; ++c) st.o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st.m = -INFINITY;
+    st.shift = 0.f;
+    st.l = 0.f;
+    bool bad = false, seen = false;
+
+    for (int base = e0; base < e1; base += kWave) {
+        const int cnt = e1 - base < kWave ? e1 - base : kWave;
+        // lane j: entry base + j, its page and how many tokens of it count (0: not of this row)
+        const int p = lane < cnt ? list[base + lane] : -1;
+        const bool in = p >= 0 && p < n;
+        const int entry = in ? row[p] : -1;
+        const int at = page_index(entry, a.num_hot, a.num_cold);
+        const int left = len - p * kPageTokens;
+        const int valid = !in ? 0 : left < kPageTokens ? left : kPageTokens;
+        if (__builtin_amdgcn_ballot_w64(in && at < 0)) bad = true;
+        if (__builtin_amdgcn_ballot_w64(in)) seen = true;
+        PageRegs<D, BF16> ring[R];
+        auto issue = [&](int r, int j) __attribute__((always_inline)) {
+            // every step issues one page's loads, past the end from a resource without records
+            const int page = j < cnt ? __builtin_amdgcn_readlane(at, j) : -1;
+            const int tokens = j < cnt ? __builtin_amdgcn_readlane(valid, j) : 0;
+            PageAddr pa;
+            pa.ok = page >= 0 && tokens > 0;
+            const int id = pa.ok ? page : 0;
+            pa.base = (id < a.num_hot ? a.hot + static_cast<int64_t>(id) * a.hot_stride
+                                      : a.cold + static_cast<int64_t>(id - a.num_hot) * a.cold_stride) + head_off;
+            const __amdgpu_buffer_rsrc_t rs = page_rsrc<D, BF16>(pa);
+            load_page_k<D, BF16>(ring[r], rs, koff);
+            load_page_v<D, BF16>(ring[r], rs, voff);
+        };
+        auto compute = [&](int r, int j) __attribute__((always_inline)) {
+            if (j < 0 || j >= cnt) return;
+            const int tokens = __builtin_amdgcn_readlane(valid, j);
+            if (tokens <= 0) return;
+            sparse_page<D, BF16>(st, ring[r], tokens, a.scale_log2, qg);
+        };
+#pragma unroll
+        for (int r = 0; r < R - 1; ++r) issue(r, r);
+        for (int j = 0; j < cnt; j += R) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                issue((r + R - 1) % R, j + r + R - 1);
+                compute(r, j + r);
+            }
+        }
+    }
+
+    float l = wave_sum_4(st.l);
+    if (bad) l = __builtin_nanf("");
+    float m = st.m == -INFINITY && seen ? kNoScore : st.m;
+
+    // the waves' results meet in LDS: [wave][head][D], then [wave][max, sum][head]
+    extern __shared__ __align__(16) char s_mem[];
+    float* s_o = reinterpret_cast<float*>(s_mem);
+    float* s_ml = s_o + WAVES * a.group * D;
+    const int h = lane & 15;
+    if (h < a.group) {
+        float* o = s_o + (wave * a.group + h) * D + 4 * qg;
+#pragma unroll
+        for (int c = 0; c < S::kChunks; ++c) *reinterpret_cast<f32x4*>(o + 16 * c) = st.o[c];
+        if (qg == 0) {
+            s_ml[wave * 2 * a.group + h] = m;
+            s_ml[wave * 2 * a.group + a.group + h] = l;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.group * (D / 4); i += WAVES * kWave) {
+        const int hh = i / (D / 4), quad = i % (D / 4);
+        float M = -INFINITY, den = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w)
+            lse_merge(M, den, acc, s_ml[w * 2 * a.group + hh], s_ml[w * 2 * a.group + a.group + hh],
+                      *reinterpret_cast<const f32x4*>(s_o + (w * a.group + hh) * D + 4 * quad));
+        if (a.parts == 1) {
+            store_result<D, BF16>(a, seg * a.group + hh, quad, M, den, acc, invalid);
+        } else {
+            const int64_t slot = seg * a.parts + part;
+            *reinterpret_cast<f32x4*>(a.part_o + (slot * a.group + hh) * D + 4 * quad) = acc;
+            if (quad == 0) {
+                a.part_ml[slot * 2 * a.group + hh] = M;
+                a.part_ml[slot * 2 * a.group + a.group + hh] = den;
+            }
+        }
+    }
+}
+
+// The parts of a list joined: one thread per (head, 4 dims).
+template <int D, bool BF16>
+__global__ __launch_bounds__(kBlockThreads) void sparse_merge_kernel(const SparseArgs a) {
+    const int g = blockIdx.y, b = blockIdx.z;
+    const int i = blockIdx.x * kBlockThreads + threadIdx.x;
+    if (i >= a.group * (D / 4)) return;
+    const int h = i / (D / 4), quad = i % (D / 4);
+    const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
+    const int len = a.lens[b];
+    const bool invalid = len < 0 || len > kPageTokens * a.pt_stride;
+    float M = -INFINITY, den = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p) {
+        const int64_t slot = seg * a.parts + p;
+        lse_merge(M, den, acc, a.part_ml[slot * 2 * a.group + h], a.part_ml[slot * 2 * a.group + a.group + h],
+                  *reinterpret_cast<const f32x4*>(a.part_o + (slot * a.group + h) * D + 4 * quad));
+    }
+    store_result<D, BF16>(a, seg * a.group + h, quad, M, den, acc, invalid);
+}
+
+template <int D, bool BF16>
+hipError_t launch_sparse_for(const SparseArgs& a, const SparsePlan& p, hipStream_t s, const LaunchEvents& ev,
+                             const LaunchEvents& ev_merge) {
+    constexpr int R = BF16 ? 3 : 2;
+    const void* k = p.waves == 8 ? reinterpret_cast<const void*>(&sparse_split_kernel<D, BF16, 8, R>)
+                                 : reinterpret_cast<const void*>(&sparse_split_kernel<D, BF16, 4, R>);
+    const size_t lds = static_cast<size_t>(p.waves) * a.group * (D + 2) * sizeof(float);
+    void* args[] = {const_cast<SparseArgs*>(&a)};
+    const dim3 grid(static_cast<unsigned>(a.parts), static_cast<unsigned>(a.num_kv_heads), static_cast<unsigned>(a.batch));
+    hipError_t e = launch_kernel(k, grid, dim3(static_cast<unsigned>(p.waves * kWave)), args, lds, s, ev);
+    if (e != hipSuccess || a.parts == 1) return e;
+    const unsigned blocks = static_cast<unsigned>((a.group * (D / 4) + kBlockThreads - 1) / kBlockThreads);
+    return launch_kernel(reinterpret_cast<const void*>(&sparse_merge_kernel<D, BF16>),
+                         dim3(blocks, static_cast<unsigned>(a.num_kv_heads), static_cast<unsigned>(a.batch)),
+                         dim3(kBlockThreads), args, 0, s, ev_merge);
+}
+
+}  // namespace
+
+hipError_t launch_bounds_update(const BoundsUpdateArgs& a, int head_dim, int dtype, int32_t num_layers, hipStream_t s,
+                                const LaunchEvents& ev) {
+    // enough blocks for the GPU however few rows there are, no more than the longest row has units
+    const int64_t units = a.pt_stride * a.num_kv_heads;
+    const int64_t rows = static_cast<int64_t>(a.batch) * num_layers;
+    int64_t gx = (16384 + rows - 1) / rows;
+    gx = std::min<int64_t>(gx, (units + kBlockWaves - 1) / kBlockWaves);
+    const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>(a.batch), static_cast<unsigned>(num_layers));
+    const void* k = dtype == kDtypeBf16
+                        ? (head_dim == 128 ? reinterpret_cast<const void*>(&bounds_update_kernel<128, true>)
+                                           : reinterpret_cast<const void*>(&bounds_update_kernel<64, true>))
+                        : (head_dim == 128 ? reinterpret_cast<const void*>(&bounds_update_kernel<128, false>)
+                                           : reinterpret_cast<const void*>(&bounds_update_kernel<64, false>));
+    void* args[] = {const_cast<BoundsUpdateArgs*>(&a)};
+    return launch_kernel(k, grid, dim3(kBlockThreads), args, 0, s, ev);
+}
+
+hipError_t launch_bounds_read(const BoundsReadArgs& a, int32_t num_layers, hipStream_t s) {
+    const int64_t total = static_cast<int64_t>(a.n) * (a.num_kv_heads * 2 * a.head_dim / 4);
+    const int64_t blocks = std::min<int64_t>((total + kBlockThreads - 1) / kBlockThreads, 65536);
+    if (blocks <= 0) return hipSuccess;
+    hipLaunchKernelGGL(bounds_read_kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(num_layers)),
+                       dim3(kBlockThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t record, int32_t layers,
+                              const CopyEntry* entries, int32_t n, hipStream_t s) {
+    if (n <= 0) return hipSuccess;
+    const int words = record / 16;
+    const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(n) * words + kBlockThreads - 1) / kBlockThreads, 65536);
+    hipLaunchKernelGGL(bounds_copy_kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(layers)),
+                       dim3(kBlockThreads), 0, s, src, dst, entries, n, words);
+    return hipGetLastError();
+}
+
+hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hipStream_t s, const LaunchEvents& ev,
+                               const LaunchEvents& ev_pick) {
+    void* args[] = {const_cast<SelectArgs*>(&a)};
+    if (a.pt_stride > a.width) {   // else no row has pages to choose from
+        const int head_waves = a.num_kv_heads % 4 == 0 ? 4 : a.num_kv_heads % 2 == 0 ? 2 : 1;
+        const int pages = kWave * (kBlockWaves / head_waves);   // of a block and turn
+        int64_t gx = (4096 + a.batch - 1) / a.batch;
+        gx = std::min<int64_t>(gx, (a.pt_stride + pages - 1) / pages);
+        const void* k = dtype == kDtypeBf16
+                            ? (head_dim == 128 ? reinterpret_cast<const void*>(&page_scores_kernel<128, true>)
+                                               : reinterpret_cast<const void*>(&page_scores_kernel<64, true>))
+                            : (head_dim == 128 ? reinterpret_cast<const void*>(&page_scores_kernel<128, false>)
+                                               : reinterpret_cast<const void*>(&page_scores_kernel<64, false>));
+        const hipError_t e = launch_kernel(k, dim3(static_cast<unsigned>(gx), static_cast<unsigned>(a.batch)),
+                                           dim3(kBlockThreads), args, 0, s, ev);
+        if (e != hipSuccess) return e;
+    }
+    const void* k;
+    unsigned threads;
+    if (a.pt_stride <= 1024) {
+        k = reinterpret_cast<const void*>(&page_pick_kernel<256, 4>);
+        threads = 256;
+    } else if (a.pt_stride <= 4096) {
+        k = reinterpret_cast<const void*>(&page_pick_kernel<512, 8>);
+        threads = 512;
+    } else if (a.pt_stride <= 16384) {
+        k = reinterpret_cast<const void*>(&page_pick_kernel<1024, 16>);
+        threads = 1024;
+    } else {
+        k = reinterpret_cast<const void*>(&page_pick_kernel<1024, 0>);
+        threads = 1024;
+    }
+    return launch_kernel(k, dim3(static_cast<unsigned>(a.num_kv_heads), static_cast<unsigned>(a.batch)), dim3(threads),
+                         args, 0, s, ev_pick);
+}
+
+SparsePlan sparse_plan(int cus, int batch, int num_kv_heads, int group, int width) {
+    SparsePlan p;
+    p.waves = group > 8 ? 4 : 8;
+    const int64_t lists = static_cast<int64_t>(batch) * num_kv_heads;
+    const int64_t fill = (cus + lists - 1) / std::max<int64_t>(lists, 1);
+    const int64_t most = (width + 4 * p.waves - 1) / (4 * p.waves);
+    p.parts = static_cast<int>(std::max<int64_t>(1, std::min(fill, most)));
+    return p;
+}
+
+hipError_t launch_sparse_attention(const SparseArgs& a, const SparsePlan& p, int head_dim, int dtype, hipStream_t s,
+                                   const LaunchEvents& ev, const LaunchEvents& ev_merge) {
+    if (dtype == kDtypeBf16)
+        return head_dim == 128 ? launch_sparse_for<128, true>(a, p, s, ev, ev_merge)
+                               : launch_sparse_for<64, true>(a, p, s, ev, ev_merge);
+    return head_dim == 128 ? launch_sparse_for<128, false>(a, p, s, ev, ev_merge)
+                           : launch_sparse_for<64, false>(a, p, s, ev, ev_merge);
+}
+
+}  // namespace hck

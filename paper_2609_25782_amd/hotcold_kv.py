@@ -26,7 +26,9 @@ KV_COLD_DEVICE, KV_COLD_PINNED_HOST = 0, 1
 KV_SESSION_FREE, KV_SESSION_ACTIVE, KV_SESSION_PAUSED = 0, 1, 2
 KV_POOL_METADATA_ONLY = 1
 KV_KERNEL_DECODE_SPLIT, KV_KERNEL_DECODE_COMBINE, KV_KERNEL_PAGE_COPY, KV_KERNEL_EVICT_COPY = 0, 1, 2, 3
-KV_KERNEL_PREFETCH_COPY, KV_KERNEL_CHUNK, KV_KERNEL_CHUNK_MERGE, KV_KERNEL_COUNT = 4, 5, 6, 7
+KV_KERNEL_PREFETCH_COPY, KV_KERNEL_CHUNK, KV_KERNEL_CHUNK_MERGE = 4, 5, 6
+KV_KERNEL_BOUNDS, KV_KERNEL_PAGE_SCORES, KV_KERNEL_PAGE_PICK = 7, 8, 9
+KV_KERNEL_SPARSE, KV_KERNEL_SPARSE_MERGE, KV_KERNEL_FORK_COPY, KV_KERNEL_COUNT = 10, 11, 12, 13
 KV_MAX_DRAFTS = 64
 KV_PAGE_COLD, KV_PAGE_STAGED = 1 << 30, 1 << 29
 KV_COMBINE_SEPARATE, KV_COMBINE_FUSED = 0, 1
@@ -92,6 +94,17 @@ _SIGS = {
     "kv_fill_synthetic": (ctypes.c_int, [_P, _I32, _I32, _U64, ctypes.c_float, _P]),
     "kv_fill_synthetic_pages": (ctypes.c_int, [_P, _I32, _I32, _U64, ctypes.c_float, _I32, _I32, _P]),
     "kv_evict_session": (ctypes.c_int, [_P, _I32, _P]),
+    "kv_fork_sessions": (ctypes.c_int, [_P, _PI32, _PI32, _I32, _P, _PI32]),
+    "kv_bounds_bytes": (_SZ, [ctypes.POINTER(kv_pool_desc)]),
+    "kv_pool_set_bounds": (ctypes.c_int, [_P, _P, _SZ]),
+    "kv_update_bounds": (ctypes.c_int, [_P, _I32, _I32, _P, _I64, _P, _P, _I32, _P]),
+    "kv_read_bounds": (ctypes.c_int, [_P, _I32, _I32, _P, _I32, _P, _P]),
+    "paged_select_workspace_bytes": (_SZ, [_P, _I32, _I64, _I32]),
+    "paged_select_pages": (ctypes.c_int, [_P, _I32, _P, _P, _I64, _P, _I32, _I32, _I32, _I32, _I32, _P, _P, _P, _SZ,
+                                          _P]),
+    "paged_sparse_workspace_bytes": (_SZ, [_P, _I32, _I32, _I32]),
+    "paged_sparse_attention": (ctypes.c_int, [_P, _I32, _P, _P, _I64, _P, _P, _P, _I32, _I32, _I32, ctypes.c_float,
+                                              _P, _P, _SZ, _P]),
     "kv_pool_set_spill": (ctypes.c_int, [_P, _I32]),
     "kv_promote_pages": (ctypes.c_int, [_P, _I32, _P, _PI32]),
     "kv_resume_sessions_lazy": (ctypes.c_int, [_P, _PI32, _I32, _P]),
@@ -221,6 +234,17 @@ def kv_evict_pages(pool: int, n: int, stream: int = 0) -> int:
     got = ctypes.c_int32()
     _check(_lib.kv_evict_pages(pool, n, stream or None, ctypes.byref(got)), "kv_evict_pages")
     return got.value
+
+
+def kv_fork_sessions(pool: int, sids: Sequence[int], kept: Sequence[int], stream: int = 0):
+    """Ids of new sessions, the i-th with the first kept[i] tokens of session sids[i]."""
+    n = len(sids)
+    if len(kept) != n:
+        raise ValueError("sids and kept differ in length")
+    out = (ctypes.c_int32 * max(n, 1))()
+    _check(_lib.kv_fork_sessions(pool, _i32_array(sids), _i32_array(kept), n, stream or None, out),
+           "kv_fork_sessions")
+    return list(out[:n])
 
 
 def kv_session_destroy(pool: int, sid: int, stream: int = 0) -> None:
@@ -452,6 +476,51 @@ def paged_tree_attention(pool: int, layer: int, q_ptr: int, k_draft_ptr: int, v_
                                      masks_ptr or None, draft_lens_ptr or None, width, page_table_ptr or None,
                                      pt_stride, seq_lens_ptr or None, batch, num_q_heads, scale, out_ptr or None,
                                      workspace_ptr or None, ws_bytes, stream or None), "paged_tree_attention")
+
+
+def kv_bounds_bytes(desc: kv_pool_desc) -> int:
+    return int(_lib.kv_bounds_bytes(ctypes.byref(desc)))
+
+
+def kv_pool_set_bounds(pool: int, bounds_ptr: int, nbytes: int) -> None:
+    _check(_lib.kv_pool_set_bounds(pool, bounds_ptr or None, nbytes), "kv_pool_set_bounds")
+
+
+def kv_update_bounds(pool: int, layer_begin: int, num_layers: int, page_table_ptr: int, pt_stride: int,
+                     starts_ptr: int, seq_lens_ptr: int, batch: int, stream: int = 0) -> None:
+    _check(_lib.kv_update_bounds(pool, layer_begin, num_layers, page_table_ptr or None, pt_stride, starts_ptr or None,
+                                 seq_lens_ptr or None, batch, stream or None), "kv_update_bounds")
+
+
+def kv_read_bounds(pool: int, layer_begin: int, num_layers: int, pages_ptr: int, n: int, out_ptr: int,
+                   stream: int = 0) -> None:
+    _check(_lib.kv_read_bounds(pool, layer_begin, num_layers, pages_ptr or None, n, out_ptr or None, stream or None),
+           "kv_read_bounds")
+
+
+def paged_select_workspace_bytes(pool: int, batch: int, pt_stride: int, width: int) -> int:
+    return int(_lib.paged_select_workspace_bytes(pool, batch, pt_stride, width))
+
+
+def paged_select_pages(pool: int, layer: int, q_ptr: int, page_table_ptr: int, pt_stride: int, seq_lens_ptr: int,
+                       batch: int, num_q_heads: int, width: int, first: int, recent: int, picks_ptr: int,
+                       counts_ptr: int, workspace_ptr: int, ws_bytes: int, stream: int = 0) -> None:
+    _check(_lib.paged_select_pages(pool, layer, q_ptr or None, page_table_ptr or None, pt_stride, seq_lens_ptr or None,
+                                   batch, num_q_heads, width, first, recent, picks_ptr or None, counts_ptr or None,
+                                   workspace_ptr or None, ws_bytes, stream or None), "paged_select_pages")
+
+
+def paged_sparse_workspace_bytes(pool: int, batch: int, num_q_heads: int, width: int) -> int:
+    return int(_lib.paged_sparse_workspace_bytes(pool, batch, num_q_heads, width))
+
+
+def paged_sparse_attention(pool: int, layer: int, q_ptr: int, page_table_ptr: int, pt_stride: int, seq_lens_ptr: int,
+                           picks_ptr: int, counts_ptr: int, width: int, batch: int, num_q_heads: int, scale: float,
+                           out_ptr: int, workspace_ptr: int, ws_bytes: int, stream: int = 0) -> None:
+    _check(_lib.paged_sparse_attention(pool, layer, q_ptr or None, page_table_ptr or None, pt_stride,
+                                       seq_lens_ptr or None, picks_ptr or None, counts_ptr or None, width, batch,
+                                       num_q_heads, scale, out_ptr or None, workspace_ptr or None, ws_bytes,
+                                       stream or None), "paged_sparse_attention")
 
 
 def paged_decode_gather_table(pool: int, sids_ptr: int, n: int, table_ptr: int, stream: int = 0) -> None:

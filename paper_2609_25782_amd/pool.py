@@ -55,6 +55,7 @@ class HotColdPool:
                                         self.cold.data_ptr(), self.cold.numel(),
                                         self.page_table.data_ptr(), _stream(stream))
         self._ws = {}   # decode workspace per stream: decodes on different streams may overlap
+        self.bounds = None   # key bounds of the pages (set_bounds)
 
     # -- layout ------------------------------------------------------------
     @property
@@ -110,6 +111,17 @@ class HotColdPool:
 
     def evict_pages(self, n: int, stream=None) -> int:
         return kv.kv_evict_pages(self.handle, int(n), _stream(stream))
+
+    def fork(self, sids, kept=None, stream=None):
+        """Branches: the id of a new session with the first kept[i] tokens of session sids[i] (the same
+        may stand several times) for each i, or of one for plain numbers; `kept` None: all tokens."""
+        one = isinstance(sids, int)
+        sids = [sids] if one else [int(x) for x in sids]
+        if kept is None:
+            kept = [kv.kv_session_info(self.handle, sid)[1] for sid in sids]
+        kept = [int(kept)] * len(sids) if isinstance(kept, int) else [int(x) for x in kept]
+        made = kv.kv_fork_sessions(self.handle, sids, kept, self._raw(stream))
+        return made[0] if one else made
 
     def destroy_session(self, sid: int, stream=None) -> None:
         kv.kv_session_destroy(self.handle, sid, _stream(stream))
@@ -337,6 +349,90 @@ class HotColdPool:
         kv.kv_accept_drafts(self.handle, layer_begin, L, pt.data_ptr(), pt.shape[1], self._ints(seq_lens, B),
                             self._ints(path, B, T), self._ints(counts, B), B, T, k.data_ptr(), v.data_ptr(),
                             self._raw(stream))
+
+    # -- decode over picked pages ---------------------------------------------
+    def set_bounds(self, enable: bool) -> None:
+        """Keep key bounds of every page (kv_bounds_bytes of device memory, zeros at first), or none."""
+        torch.cuda.synchronize(self.device)
+        bounds = None
+        if enable:
+            bounds = torch.zeros(kv.kv_bounds_bytes(self.desc), dtype=torch.uint8, device=self.device)
+            torch.cuda.synchronize(self.device)
+        kv.kv_pool_set_bounds(self.handle, bounds.data_ptr() if enable else 0, bounds.numel() if enable else 0)
+        self.bounds = bounds
+
+    def update_bounds(self, layer_begin: int, num_layers: int, seq_lens: torch.Tensor,
+                      starts: Optional[torch.Tensor] = None, page_table: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+        """Bounds of the pages that hold tokens starts[b] (default 0) .. seq_lens[b] of table row b: after
+        writing those tokens, before picking pages.  Capturable in a HIP graph."""
+        B = seq_lens.shape[0]
+        pt = self._table(page_table, B)
+        kv.kv_update_bounds(self.handle, layer_begin, num_layers, pt.data_ptr(), pt.shape[1],
+                            0 if starts is None else self._ints(starts, B), self._ints(seq_lens, B), B,
+                            self._raw(stream))
+
+    def key_bounds(self, layer_begin: int, num_layers: int, pages: torch.Tensor, stream=None) -> torch.Tensor:
+        """Bounds of the pages (int32 page-table entries [n]) as float32 [num_layers][n][kv_heads][2][head_dim]:
+        the lowest and the highest value of each dim, rounded outwards to 8 bits."""
+        n = pages.shape[0]
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+            out = torch.empty((num_layers, n, self.num_kv_heads, 2, self.head_dim), dtype=torch.float32,
+                              device=self.device)
+        kv.kv_read_bounds(self.handle, layer_begin, num_layers, self._ints(pages, n), n, out.data_ptr(),
+                          self._raw(stream))
+        return out
+
+    def _scratch(self, kind: str, need: int, st: int, stream) -> torch.Tensor:
+        """Workspace of a call: its graph's own memory under capture, else one per kind and stream."""
+        if self._capturing(stream):
+            return self._memory(need, None, stream)[1]
+        ws = self._ws.get((kind, st))
+        if ws is None or ws.numel() < need:
+            ws = self._ws[(kind, st)] = self._memory(need, None, stream)[1]
+        return ws
+
+    def select_pages(self, layer: int, q: torch.Tensor, seq_lens: torch.Tensor, width: int, first: int = 1,
+                     recent: int = 2, page_table: Optional[torch.Tensor] = None, stream=None):
+        """(picks int32 [B][kv_heads][width], counts int32 [B][kv_heads]): for each row and KV head its first
+        and last pages and those whose bounds allow the largest scores with q [B][Hq][head_dim]."""
+        assert q.is_contiguous() and q.dtype == self.torch_dtype and q.dim() == 3 and q.device == self.device
+        B, Hq, D = q.shape
+        assert D == self.head_dim
+        pt = self._table(page_table, B)
+        lens = self._ints(seq_lens, B)
+        st = self._raw(stream)
+        ws = self._scratch("select", kv.paged_select_workspace_bytes(self.handle, B, pt.shape[1], width), st, stream)
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+            picks = torch.empty((B, self.num_kv_heads, width), dtype=torch.int32, device=self.device)
+            counts = torch.empty((B, self.num_kv_heads), dtype=torch.int32, device=self.device)
+        kv.paged_select_pages(self.handle, layer, q.data_ptr(), pt.data_ptr(), pt.shape[1], lens, B, Hq, width, first,
+                              recent, picks.data_ptr(), counts.data_ptr(), ws.data_ptr() if ws is not None else 0,
+                              ws.numel() if ws is not None else 0, st)
+        return picks, counts
+
+    def sparse_decode(self, layer: int, q: torch.Tensor, seq_lens: torch.Tensor, picks: torch.Tensor,
+                      counts: Optional[torch.Tensor] = None, page_table: Optional[torch.Tensor] = None,
+                      scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Decode attention of one layer over the listed pages of every row and KV head alone (picks
+        [B][kv_heads][width] of select_pages or of any other rule, counts None: width each)."""
+        assert q.is_contiguous() and q.dtype == self.torch_dtype and q.dim() == 3 and q.device == self.device
+        B, Hq, D = q.shape
+        assert D == self.head_dim and picks.dim() == 3
+        width = picks.shape[2]
+        listed = self._ints(picks, B, self.num_kv_heads, width)
+        pt = self._table(page_table, B)
+        lens = self._ints(seq_lens, B)
+        st = self._raw(stream)
+        if out is None:
+            out = self._memory(0, q, stream)[0]
+        assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype and out.device == q.device
+        ws = self._scratch("sparse", kv.paged_sparse_workspace_bytes(self.handle, B, Hq, width), st, stream)
+        kv.paged_sparse_attention(self.handle, layer, q.data_ptr(), pt.data_ptr(), pt.shape[1], lens, listed,
+                                  0 if counts is None else self._ints(counts, B, self.num_kv_heads), width, B, Hq,
+                                  float(scale if scale is not None else D ** -0.5), out.data_ptr(),
+                                  ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0, st)
+        return out
 
     def gather_table(self, sids: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Page-table rows of the given sessions (device int32 ids), for decoding them as a batch."""

@@ -1,0 +1,155 @@
+"""Branches of sessions (kv_fork_sessions): pages, bounds and cold copies, byte for byte."""
+
+import pytest
+import torch
+
+from chunk_reference import Sessions, i32, pages_for
+from paper_2609_25782_amd import hotcold_kv as kv
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(2, 64, "bf16"), (4, 128, "bf16"), (1, 64, "f32"), (3, 128, "f32"), (1, 64, "bf16")]
+
+
+def page_rows(pool, sid, n):
+    """The bytes of a session's first n pages, from where its row says they are."""
+    row = pool.page_table[sid, :n].tolist()
+    assert all(0 <= x < pool.num_hot_pages for x in row)
+    assert row == pool.info(sid)[2][:n]
+    return pool.hot_page_bytes(row)
+
+
+@pytest.mark.parametrize("hkv,d,dtype", SHAPES)
+def test_branches_hold_the_parents_tokens(hkv, d, dtype):
+    lens = [500, 16, 77]
+    s = Sessions(lens, hkv, hkv, d, dtype, seed=1, layers=3, spare=400, stride=40, max_sessions=24)
+    p = s.pool
+    before = p.hot.clone()
+    parents, kept = [0, 2, 0, 0, 1, 2, 0], [500, 77, 333, 0, 16, 33, 16]
+    made = p.fork(parents, kept)
+    assert made == list(range(3, 10))
+    used = set()
+    for sid, parent, n in zip(made, parents, kept):
+        state, length, hot, _ = p.info(sid)
+        assert (state, length) == (kv.KV_SESSION_ACTIVE, n)
+        assert not used & set(hot)
+        used |= set(hot)
+        assert (p.page_table[sid, pages_for(n):] == -1).all()
+        assert torch.equal(page_rows(p, sid, pages_for(n)), p.hot_page_bytes(s.pages[parent][:pages_for(n)]))
+    rest = [x for x in range(p.num_hot_pages) if x not in used]
+    assert torch.equal(p.hot_page_bytes(rest), before.view_as(p.hot).view(p.num_layers, -1, p.slice_bytes)
+                       .transpose(0, 1)[torch.tensor(rest, device="cuda")].reshape(len(rest), -1))
+
+
+@pytest.mark.parametrize("branches", [1, 13, 14, 15, 29])
+def test_many_branches_of_one_session(branches):
+    """Both sides of how many pages one read serves, and of what fits the kernel's arguments."""
+    for n in (40, 16 * 30):
+        s = Sessions([n], 2, 2, 64, "bf16", seed=2, layers=2, spare=30 * 30, stride=30, max_sessions=40)
+        made = s.pool.fork([0] * branches)
+        want = s.pool.hot_page_bytes(s.pages[0])
+        for sid in made:
+            assert torch.equal(page_rows(s.pool, sid, pages_for(n)), want)
+
+
+def test_a_branch_lives_on_its_own():
+    """Writes to a branch or its parent do not reach the other; decode sees each one's tokens."""
+    s = Sessions([100], 8, 2, 128, "bf16", seed=3, spare=40, stride=20, max_sessions=4)
+    p = s.pool
+    child = p.fork(0, 90)
+    q = s.normal(1, 8, 128).cuda()
+    want = p.decode(0, q, i32([90]), page_table=p.page_table[:1].contiguous())
+    k, v = s.normal(5, 2, 128).cuda(), s.normal(5, 2, 128).cuda()
+    p.write_tokens(0, 0, 85, k, v)
+    row = p.page_table[child:child + 1].contiguous()
+    assert torch.equal(p.decode(0, q, i32([90]), page_table=row), want)
+    p.extend(child, 95)
+    p.write_tokens(child, 0, 90, k, v)
+    assert torch.equal(p.hot_page_bytes(s.pages[0])[6], p.hot_page_bytes(s.pages[0])[6])
+    p.destroy_session(0)
+    assert torch.equal(p.decode(0, q, i32([90]), page_table=row), want)
+
+
+def test_evicted_branches_come_back():
+    """A branch's eviction writes only what has no valid cold copy; it and its parent resume whole."""
+    s = Sessions([16 * 6 + 5], 2, 2, 64, "bf16", seed=4, layers=2, spare=40, cold=30, stride=10, max_sessions=6)
+    p = s.pool
+    p.evict(0)
+    p.resume(0)
+    want = p.hot_page_bytes(p.info(0)[2])
+    child = p.fork(0)
+    written = p.stats()["pages_to_cold"]
+    p.evict([child, 0])
+    assert p.stats()["pages_to_cold"] == written + 1
+    filler = p.create_session(64)
+    p.resume([0, child])
+    assert torch.equal(p.hot_page_bytes(p.info(0)[2]), want) and torch.equal(p.hot_page_bytes(p.info(child)[2]), want)
+    p.destroy_session(filler)
+
+
+@pytest.mark.parametrize("where", ["device", "host"])
+def test_spilled_parents(where):
+    from paper_2609_25782_amd.pool import HotColdPool
+    p = HotColdPool(2, 2, 64, "bf16", 24, 40, 6, 12, cold_location=where)
+    p.set_spill(True)
+    sid = p.create_session(100)
+    p.fill_synthetic(sid, 3, 5, 1e-5)
+    want = p.hot_page_bytes(p.info(sid)[2])
+    p.set_bounds(True)
+    p.update_bounds(0, 2, i32([100]))
+    bounds = p.key_bounds(0, 2, i32(p.info(sid)[2]))
+    p.evict(sid)
+    p.resume_lazy(sid)
+    p.promote(3)
+    made = p.fork([sid, sid], [100, 60])
+    for child, n in zip(made, (7, 4)):
+        assert torch.equal(page_rows(p, child, n), want[:n])
+        assert torch.equal(p.key_bounds(0, 2, i32(p.info(child)[2])), bounds[:, :n])
+
+
+def test_branches_make_room():
+    """Pages of paused sessions are evicted for a branch, and come back with their content."""
+    s = Sessions([64, 64], 2, 2, 64, "bf16", seed=5, spare=1, cold=8, stride=8, max_sessions=4)
+    p = s.pool
+    kept = p.hot_page_bytes(s.pages[1])
+    p.pause(1)
+    child = p.fork(0)
+    assert torch.equal(page_rows(p, child, 4), p.hot_page_bytes(s.pages[0]))
+    assert p.stats()["lru_evicted_pages"] == 3
+    p.destroy_session(0)
+    p.resume(1)
+    assert torch.equal(p.hot_page_bytes(p.info(1)[2]), kept)
+
+
+def test_branches_wait_for_freed_pages():
+    """Pages freed behind another stream's work are not written before that work is done."""
+    s = Sessions([16 * 20], 4, 4, 128, "bf16", seed=6, layers=4, spare=20, stride=30, max_sessions=4)
+    p = s.pool
+    want = p.hot_page_bytes(s.pages[0])
+    other = p.create_session(16 * 20)
+    side = torch.cuda.Stream()
+    pages = p.info(other)[2]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        p.fill_synthetic(other, 1, 1, 1e-5, stream=side)      # a late write to pages that are then freed
+        p.destroy_session(other, stream=side)
+    child = p.fork(0)
+    torch.cuda.synchronize()
+    assert set(p.info(child)[2]) == set(pages)
+    assert torch.equal(page_rows(p, child, 20), want)
+
+
+def test_refusals():
+    s = Sessions([40], 2, 2, 64, "bf16", seed=7, spare=2, stride=4, max_sessions=2)
+    p = s.pool
+    before = p.hot.clone(), p.page_table.clone(), p.stats()
+    for sids, kept, status in (([0], [41], kv.KV_ERR_INVALID), ([0], [40], kv.KV_ERR_NO_HOT_PAGES),
+                               ([1], [0], kv.KV_ERR_STATE), ([0, 0], [0, 0], kv.KV_ERR_INVALID)):
+        with pytest.raises(kv.KVError) as e:
+            p.fork(sids, kept)
+        assert e.value.status == status
+    torch.cuda.synchronize()
+    assert p.stats() == before[2] and torch.equal(p.page_table, before[1])
+    assert torch.equal(p.hot.view(torch.int32), before[0].view(torch.int32))
+    assert p.fork([], []) == []

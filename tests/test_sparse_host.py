@@ -1,0 +1,198 @@
+"""Key bounds, page choice, sparse decode and branches on the host: calls that must be refused before
+any device is touched, and the branches' bookkeeping against the model (CPU only)."""
+
+import copy
+import random
+
+import pytest
+
+from oracle.pool_model import ERR_INVALID, ModelError, PoolModel
+
+
+@pytest.fixture
+def kv():
+    import torch  # noqa: F401  (its HIP runtime has to be the one that the library finds)
+    from paper_2609_25782_amd import hotcold_kv
+    return hotcold_kv
+
+
+def meta_pool(kv, hot=8, cold=8, sessions=4, stride=4):
+    d = kv.kv_pool_desc(2, 2, 64, 16, kv.KV_DTYPE_BF16, hot, cold, 0, sessions, stride, 0, kv.KV_POOL_METADATA_ONLY)
+    return kv.kv_pool_create(d, 0, 0, 0, 0, 0)
+
+
+def test_metadata_only_pools_are_refused(kv):
+    meta = meta_pool(kv)
+    for pool in (meta, 0):
+        for call in (lambda: kv.kv_pool_set_bounds(pool, 256, 1 << 30),
+                     lambda: kv.kv_update_bounds(pool, 0, 1, 16, 4, 0, 16, 1),
+                     lambda: kv.kv_read_bounds(pool, 0, 1, 16, 1, 16),
+                     lambda: kv.paged_select_pages(pool, 0, 16, 16, 4, 16, 1, 4, 2, 0, 1, 16, 16, 256, 1 << 30),
+                     lambda: kv.paged_sparse_attention(pool, 0, 16, 16, 4, 16, 16, 16, 2, 1, 4, 0.1, 16, 256, 1 << 30)):
+            with pytest.raises(kv.KVError) as e:
+                call()
+            assert e.value.status == kv.KV_ERR_INVALID
+        assert kv.paged_select_workspace_bytes(pool, 1, 4, 2) == 0
+        assert kv.paged_sparse_workspace_bytes(pool, 1, 4, 2) == 0
+    with pytest.raises(kv.KVError):
+        kv.kv_fork_sessions(0, [0], [0])
+    kv.kv_pool_destroy(meta)
+
+
+@pytest.mark.parametrize("heads,d", [(1, 64), (4, 128), (16, 128), (3, 64)])
+def test_bounds_bytes(kv, heads, d):
+    desc = kv.kv_pool_desc(3, heads, d, 16, kv.KV_DTYPE_BF16, 5, 7, 0, 1, 1, 0, 0)
+    need = 3 * 12 * (heads * 2 * d + 16)
+    assert kv.kv_bounds_bytes(desc) == -(-need // 256) * 256
+    desc.num_hot_pages = desc.num_cold_pages = 0
+    assert kv.kv_bounds_bytes(desc) >= 256
+    desc.page_size = 8
+    assert kv.kv_bounds_bytes(desc) == 0
+
+
+# -- branches ------------------------------------------------------------------
+
+
+def same(kv, pool, m):
+    """The library's sessions and counters are the model's."""
+    for sid, s in enumerate(m.sessions):
+        state, length, hot, cold = kv.kv_session_info(pool, sid)
+        assert (state, length) == (s.state, s.seq_len)
+        assert (hot, cold) == (s.hot, s.cold)
+    st = kv.kv_pool_stats(pool)
+    assert st["free_hot_pages"] == m.free_hot() and st["free_cold_pages"] == m.free_cold()
+    assert st["lru_evicted_pages"] == m.lru_evicted and st["pages_to_cold"] == m.cold_writes
+    assert st["cold_active_pages"] == m.cold_active()
+
+
+def test_branches_share_cold_copies_of_whole_pages(kv):
+    pool, m = meta_pool(kv, hot=16, cold=8, sessions=6), PoolModel(16, 8, 6, 4)
+    a = kv.kv_session_create(pool, 56)
+    assert m.create(56) == a
+    kv.kv_evict_session(pool, a), kv.kv_resume_session(pool, a)
+    m.evict(a), m.resume([a])
+    made = kv.kv_fork_sessions(pool, [a, a], [40, 56])
+    assert made == m.fork([a, a], [40, 56]) == [1, 2]
+    same(kv, pool, m)
+    assert m.sessions[1].cold[:2] == m.sessions[a].cold[:2] and m.sessions[1].cold[2] == -1
+    before = m.cold_writes
+    kv.kv_evict_session(pool, 2), m.evict(2)
+    assert m.cold_writes == before + 1          # the partly filled page alone
+    same(kv, pool, m)
+    for sid in (a, 1, 2):
+        kv.kv_session_destroy(pool, sid), m.destroy(sid)
+    same(kv, pool, m)
+    assert m.free_cold() == 8 and m.free_hot() == 16
+    kv.kv_pool_destroy(pool)
+
+
+def test_refusals_change_nothing(kv):
+    pool = meta_pool(kv, hot=8, cold=2, sessions=4)
+    a = kv.kv_session_create(pool, 40)
+    b = kv.kv_session_create(pool, 16)
+    kv.kv_evict_session(pool, b)
+    before = [kv.kv_session_info(pool, i) for i in range(4)], kv.kv_pool_stats(pool)
+    for sids, kept, status in (([a], [41], kv.KV_ERR_INVALID), ([a], [-1], kv.KV_ERR_INVALID),
+                               ([9], [0], kv.KV_ERR_INVALID), ([-1], [0], kv.KV_ERR_INVALID),
+                               ([3], [0], kv.KV_ERR_STATE), ([b], [16], kv.KV_ERR_STATE),
+                               ([a] * 3, [0] * 3, kv.KV_ERR_INVALID), ([a, a], [40, 40], kv.KV_ERR_NO_HOT_PAGES),
+                               ([a, b], [16, 16], kv.KV_ERR_STATE)):
+        with pytest.raises(kv.KVError) as e:
+            kv.kv_fork_sessions(pool, sids, kept)
+        assert e.value.status == status, (sids, kept)
+        assert ([kv.kv_session_info(pool, i) for i in range(4)], kv.kv_pool_stats(pool)) == before
+    assert kv.kv_fork_sessions(pool, [], []) == []
+    assert kv.kv_fork_sessions(pool, [a, a], [0, 16]) == [2, 3]
+    kv.kv_pool_destroy(pool)
+
+
+def test_branches_never_spill(kv):
+    """A pool with spill on still refuses a branch that finds no hot pages."""
+    pool, m = meta_pool(kv, hot=4, cold=8), PoolModel(4, 8, 4, 4, spill=True)
+    kv.kv_pool_set_spill(pool, True)
+    a = kv.kv_session_create(pool, 56)
+    m.create(56)
+    with pytest.raises(kv.KVError) as e:
+        kv.kv_fork_sessions(pool, [a], [16])
+    assert e.value.status == kv.KV_ERR_NO_HOT_PAGES
+    same(kv, pool, m)
+    kv.kv_pool_destroy(pool)
+
+
+def test_spilled_pages_of_a_parent(kv):
+    """A branch of a lazily resumed session gets hot pages; whole cold pages become shared, and a
+    write to a shared spilled page is refused until it is promoted."""
+    pool, m = meta_pool(kv, hot=8, cold=8), PoolModel(8, 8, 4, 4, spill=True)
+    kv.kv_pool_set_spill(pool, True)
+    a = kv.kv_session_create(pool, 40)
+    m.create(40)
+    kv.kv_evict_session(pool, a), m.evict(a)
+    kv.kv_resume_sessions_lazy(pool, [a]), m.resume_lazy([a])
+    assert kv.kv_fork_sessions(pool, [a], [40]) == m.fork([a], [40])
+    same(kv, pool, m)
+    with pytest.raises(kv.KVError) as e:
+        kv.kv_write_tokens(pool, a, 0, 3, 1, 0, 0)
+    assert e.value.status == kv.KV_ERR_STATE
+    kv.kv_session_extend(pool, a, 44), m.extend(a, 44)      # the tail page is not shared
+    same(kv, pool, m)
+    kv.kv_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("spill", [False, True])
+def test_random_calls_against_the_model(kv, spill):
+    rng = random.Random(11 + spill)
+    for trial in range(40):
+        hot, cold, sessions, stride = rng.randint(4, 24), rng.randint(4, 24), 8, 5
+        pool, m = meta_pool(kv, hot, cold, sessions, stride), PoolModel(hot, cold, sessions, stride, spill=spill)
+        if spill:
+            kv.kv_pool_set_spill(pool, True)
+        for step in range(60):
+            sid = rng.randrange(sessions)
+            length = m.sessions[sid].seq_len
+            op = rng.choice(["create", "fork", "fork", "evict", "resume", "pause", "destroy", "extend", "write",
+                             "reserve", "promote", "evict_pages"])
+            n = rng.randint(1, 3)
+            parents = [rng.choice([sid, rng.randrange(sessions)]) for _ in range(n)]
+            kept = [rng.randint(0, m.sessions[p].seq_len) for p in parents]
+            to = rng.randint(0, 16 * stride)
+            lib, model = {
+                "create": (lambda: kv.kv_session_create(pool, to), lambda: m.create(to)),
+                "fork": (lambda: kv.kv_fork_sessions(pool, parents, kept), lambda: m.fork(parents, kept)),
+                "evict": (lambda: kv.kv_evict_session(pool, sid), lambda: m.evict(sid) and None),
+                "resume": (lambda: kv.kv_resume_session(pool, sid), lambda: m.resume([sid]) and None),
+                "pause": (lambda: kv.kv_session_pause(pool, sid), lambda: m.pause(sid)),
+                "destroy": (lambda: kv.kv_session_destroy(pool, sid), lambda: m.destroy(sid)),
+                "extend": (lambda: kv.kv_session_extend(pool, sid, to), lambda: m.extend(sid, to)),
+                "write": (lambda: kv.kv_write_tokens(pool, sid, 0, length // 2, (length + 1) // 2, 0, 0),
+                          lambda: m.write_tokens(sid, length // 2, (length + 1) // 2)),
+                "reserve": (lambda: kv.kv_session_reserve(pool, sid, length // 2, to),
+                            lambda: m.reserve(sid, length // 2, to)),
+                "promote": (lambda: kv.kv_promote_pages(pool, n), lambda: len(m.promote(n))),
+                "evict_pages": (lambda: kv.kv_evict_pages(pool, n), lambda: m.evict_pages(n)[0]),
+            }[op]
+            got = want = code = status = None
+            try:
+                got = lib()
+            except kv.KVError as e:
+                status = e.status
+            before = copy.deepcopy(m.__dict__)
+            try:
+                want = model()
+            except ModelError as e:
+                code = e.code
+                assert {k: v for k, v in m.__dict__.items() if k != "last_victim_copies"} == \
+                    {k: v for k, v in before.items() if k != "last_victim_copies"}
+            assert status == code, (trial, step, op)
+            assert not isinstance(got, (int, list)) or got == want, (trial, step, op)
+            same(kv, pool, m)
+        kv.kv_pool_destroy(pool)
+
+
+def test_the_model_refuses_too():
+    m = PoolModel(8, 0, 2, 4)
+    a = m.create(20)
+    for parents, kept in (([a], [21]), ([a, a], [0, 0]), ([5], [0])):
+        before = copy.deepcopy(m.__dict__)
+        with pytest.raises(ModelError) as e:
+            m.fork(parents, kept)
+        assert e.value.code == ERR_INVALID and m.__dict__ == before
