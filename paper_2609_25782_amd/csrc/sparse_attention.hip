@@ -80,6 +80,17 @@ __device__ __forceinline__ float wave_max(float x) {
     return __int_as_float(__builtin_amdgcn_readlane(v, 63));
 }
 
+// How the waves of a block share (page, KV head) pairs: `heads` waves stand side by side on the
+// heads of a page, which HBM serves faster than as many unrelated pages, `slices` such groups
+// on different pages.
+struct WaveSplit {
+    int heads, slices;
+};
+__host__ __device__ __forceinline__ WaveSplit wave_split(int num_kv_heads) {
+    const int h = num_kv_heads % 4 == 0 ? 4 : num_kv_heads % 2 == 0 ? 2 : 1;
+    return WaveSplit{h, kBlockWaves / h};
+}
+
 // ---------------------------------------------------------------------------
 // Bounds of pages.
 
@@ -105,6 +116,10 @@ __device__ __forceinline__ unsigned pick(unsigned a, unsigned b) {
     }
 }
 
+#ifndef HCK_BOUNDS_BLOCKS
+#define HCK_BOUNDS_BLOCKS 4096
+#endif
+
 // One wave takes a (page, KV head) at a time.  A 16-byte group of dims of all 16 tokens is
 // 256 consecutive bytes of the K tile and belongs to kLanes lanes, each with every kLanes-th
 // token of it, so most of the reduction over tokens stays in a lane's registers.
@@ -124,24 +139,46 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const Boun
     int first = a.starts ? a.starts[b] : 0;
     first = first < 0 ? 0 : first;
     if (first >= len) return;
-    const int p0 = first / kPageTokens, pages = (len - 1) / kPageTokens + 1 - p0;
-    const unsigned heads = static_cast<unsigned>(a.num_kv_heads);
-    const unsigned units = static_cast<unsigned>(pages) * heads;
+    const int p0 = first / kPageTokens, p1 = (len - 1) / kPageTokens + 1;
     const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const WaveSplit ws = wave_split(a.num_kv_heads);
     const int dg = lane / kLanes, sub = lane % kLanes;
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
-    for (unsigned u = blockIdx.x * kBlockWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); u < units;
-         u += gridDim.x * kBlockWaves) {
-        const int page = p0 + static_cast<int>(u / heads), head = static_cast<int>(u % heads);
-        const int at = page_index(__builtin_amdgcn_readfirstlane(row[page]), a.num_hot, a.num_cold);
-        if (at < 0) continue;
-        const char* slice = at < a.num_hot ? slice_at(a.hot, at, layer) : slice_at(a.cold, at - a.num_hot, layer);
-        const char* tile = slice + head * 2 * kTile + dg * 256 + sub * 16;
-        const int valid = len - page * kPageTokens;   // tokens of the page, or more than 16
-        u32x4 w[kLoads];
+    const int step = ws.slices * static_cast<int>(gridDim.x);
+    // this wave's (page, head) pairs, one after the other; the next one's keys are in flight
+    // while the current one's are reduced
+    struct Unit {
+        int page, head, at;
+    };
+    auto fetch = [&](Unit& u, u32x4 (&w)[kLoads]) __attribute__((always_inline)) {
+        u.at = -1;
+        if (u.page >= p1) return;
+        u.at = page_index(__builtin_amdgcn_readfirstlane(row[u.page]), a.num_hot, a.num_cold);
+        if (u.at < 0) return;
+        const char* slice = u.at < a.num_hot ? slice_at(a.hot, u.at, layer) : slice_at(a.cold, u.at - a.num_hot, layer);
+        const char* tile = slice + u.head * 2 * kTile + dg * 256 + sub * 16;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
             w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tile + i * kLanes * 16));
+    };
+    Unit next = {p0 + ws.slices * static_cast<int>(blockIdx.x) + wave / ws.heads, wave % ws.heads, -1};
+    u32x4 w_next[kLoads];
+    fetch(next, w_next);
+    while (next.page < p1) {
+        const Unit cur = next;
+        u32x4 w[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) w[i] = w_next[i];
+        next.head += ws.heads;
+        if (next.head >= a.num_kv_heads) {
+            next.head = wave % ws.heads;
+            next.page = next.page + step < p1 ? next.page + step : p1;
+        }
+        fetch(next, w_next);
+        if (cur.at < 0) continue;
+        const int at = cur.at, head = cur.head;
+        const int valid = len - cur.page * kPageTokens;   // tokens of the page, or more than 16
         unsigned lo[4], hi[4];
         constexpr unsigned kLeast = BF16 ? 0x80008000u : 0x80000000u, kMost = BF16 ? 0x7FFF7FFFu : 0x7FFFFFFFu;
 #pragma unroll
@@ -236,25 +273,25 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const Boun
 // Records as values: out [layers][n][KV heads][lo, hi][D] float32, NaN where an entry names no page.
 __global__ __launch_bounds__(kBlockThreads) void bounds_read_kernel(const BoundsReadArgs a) {
     const int per = a.num_kv_heads * 2 * a.head_dim / 4;  // 4-byte words of a record's values
-    const int64_t total = static_cast<int64_t>(a.n) * per;
+    const int side = per < kBlockThreads ? kBlockThreads / per : 1;   // pages of a block and turn
     const int layer = a.layer + static_cast<int>(blockIdx.y);
-    f32x4* out = reinterpret_cast<f32x4*>(a.out) + static_cast<int64_t>(blockIdx.y) * total;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlockThreads + threadIdx.x; i < total;
-         i += static_cast<int64_t>(gridDim.x) * kBlockThreads) {
-        const int64_t p = i / per;
-        const int word = static_cast<int>(i - p * per);
+    const int slot = per < kBlockThreads ? static_cast<int>(threadIdx.x) / per : 0;
+    const int first = static_cast<int>(threadIdx.x) - slot * per;
+    if (slot >= side) return;
+    f32x4* out = reinterpret_cast<f32x4*>(a.out) + static_cast<int64_t>(blockIdx.y) * a.n * per;
+    for (int64_t p = static_cast<int64_t>(blockIdx.x) * side + slot; p < a.n;
+         p += static_cast<int64_t>(gridDim.x) * side) {
         const int at = page_index(a.pages[p], a.num_hot, a.num_cold);
-        const float nan = __builtin_nanf("");
-        f32x4 v = {nan, nan, nan, nan};
-        if (at >= 0) {
-            const char* rec = a.bounds + layer * a.layer_stride + static_cast<int64_t>(at) * a.record;
+        const char* rec = a.bounds + layer * a.layer_stride + static_cast<int64_t>(at < 0 ? 0 : at) * a.record;
+        for (int word = first; word < per; word += kBlockThreads) {
             const unsigned w = reinterpret_cast<const unsigned*>(rec)[word];
             const int e = static_cast<signed char>(rec[4 * per + word * 2 / a.head_dim]);
-            const float unit = two_to(clamp_power(e));
+            const float unit = at < 0 ? __builtin_nanf("") : two_to(clamp_power(e));
+            f32x4 v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = static_cast<float>(static_cast<signed char>(w >> (8 * j))) * unit;
+            __builtin_nontemporal_store(v, out + p * per + word);
         }
-        out[i] = v;
     }
 }
 
@@ -294,19 +331,29 @@ struct QueryRows {
     float unit[4];   // 2^e of heads 4 (l / 16) + r, 0 past the group
 };
 
+// Their bits as they lie in memory.
 template <int D, bool BF16>
-__device__ __forceinline__ void load_query_rows(QueryRows<D>& q, const SelectArgs& a, int b, int g, int lane) {
+struct QueryBits {
+    static constexpr int kElt = BF16 ? 2 : 4;
+    u32x4 w[D / 64][kElt];   // 16 dims are kElt words of 16 bytes
+};
+
+template <int D, bool BF16>
+__device__ __forceinline__ void load_query_bits(QueryBits<D, BF16>& q, const SelectArgs& a, int b, int g, int lane) {
     constexpr int kElt = BF16 ? 2 : 4;
-    constexpr int kWords = 16 * kElt / 16;  // 16-byte words of 16 dims
     const int h = lane & 15, part = lane >> 4;
-    const bool in = h < a.group;
-    const char* src = static_cast<const char*>(a.q) +
-                      ((static_cast<int64_t>(b) * a.num_q_heads + g * a.group + (in ? h : 0)) * D + 16 * part) * kElt;
-    u32x4 w[D / 64][kWords];
+    const char* src = static_cast<const char*>(a.q) + ((static_cast<int64_t>(b) * a.num_q_heads + g * a.group +
+                                                        (h < a.group ? h : 0)) * D + 16 * part) * kElt;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) w[c][i] = *reinterpret_cast<const u32x4*>(src + 64 * c * kElt + 16 * i);
+        for (int i = 0; i < kElt; ++i) q.w[c][i] = *reinterpret_cast<const u32x4*>(src + 64 * c * kElt + 16 * i);
+}
+
+template <int D, bool BF16>
+__device__ __forceinline__ void round_queries(QueryRows<D>& q, const QueryBits<D, BF16>& bits, int group, int lane) {
+    const int part = lane >> 4;
+    const bool in = (lane & 15) < group;
     float v[D / 64][16];
     float top = 0.f;
 #pragma unroll
@@ -314,10 +361,10 @@ __device__ __forceinline__ void load_query_rows(QueryRows<D>& q, const SelectArg
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             if constexpr (BF16) {
-                const unsigned x = w[c][j / 8][(j % 8) / 2];
+                const unsigned x = bits.w[c][j / 8][(j % 8) / 2];
                 v[c][j] = __uint_as_float(j & 1 ? x & 0xFFFF0000u : x << 16);
             } else {
-                v[c][j] = __uint_as_float(w[c][j / 4][j % 4]);
+                v[c][j] = __uint_as_float(bits.w[c][j / 4][j % 4]);
             }
             v[c][j] = no_nan(v[c][j]);
             top = fmaxf(top, fabsf(v[c][j]));
@@ -357,17 +404,17 @@ __global__ __launch_bounds__(kBlockThreads) void page_scores_kernel(const Select
     if (n <= a.width) return;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int head_waves = a.num_kv_heads % 4 == 0 ? 4 : a.num_kv_heads % 2 == 0 ? 2 : 1;
-    const int slices = kBlockWaves / head_waves;   // waves of a head, 64 pages each in turn
-    const int step = kWave * slices * static_cast<int>(gridDim.x);
-    const int begin = kWave * (slices * static_cast<int>(blockIdx.x) + wave / head_waves);
+    const WaveSplit ws = wave_split(a.num_kv_heads);
+    const int step = kWave * ws.slices * static_cast<int>(gridDim.x);
+    const int begin = kWave * (ws.slices * static_cast<int>(blockIdx.x) + wave / ws.heads);
     if (begin >= n) return;
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
     const char* bounds = a.bounds + a.layer * a.layer_stride;
     const int part = lane >> 4;
-    for (int g = wave % head_waves; g < a.num_kv_heads; g += head_waves) {
+    for (int g = wave % ws.heads; g < a.num_kv_heads; g += ws.heads) {
+        QueryBits<D, BF16> bits;
+        load_query_bits<D, BF16>(bits, a, b, g, lane);
         QueryRows<D> q;
-        load_query_rows<D, BF16>(q, a, b, g, lane);
         unsigned* keys = a.keys + (static_cast<int64_t>(b) * a.num_kv_heads + g) * a.pt_stride;
         for (int p0 = begin; p0 < n; p0 += step) {
             const int at = p0 + lane < n ? page_index(row[p0 + lane], a.num_hot, a.num_cold) : -1;
@@ -381,6 +428,7 @@ __global__ __launch_bounds__(kBlockThreads) void page_scores_kernel(const Select
 #pragma unroll
                 for (int c = 0; c < 2 * D / 64; ++c) w[t][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
             }
+            if (p0 == begin) round_queries<D, BF16>(q, bits, a.group, lane);   // while the records come
             float best = 0.f;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -407,13 +455,27 @@ __global__ __launch_bounds__(kBlockThreads) void page_scores_kernel(const Select
 // ---------------------------------------------------------------------------
 // The choice.
 
+__device__ __forceinline__ unsigned wave_max_u32(unsigned x) {
+    x = max(x, static_cast<unsigned>(dpp<kDppXor1>(static_cast<int>(x))));
+    x = max(x, static_cast<unsigned>(dpp<kDppXor2>(static_cast<int>(x))));
+    x = max(x, static_cast<unsigned>(dpp<kDppMirror8>(static_cast<int>(x))));
+    x = max(x, static_cast<unsigned>(dpp<kDppMirror16>(static_cast<int>(x))));
+    x = max(x, static_cast<unsigned>(__builtin_amdgcn_update_dpp(x, x, 0x142, 0xA, 0xF, false)));
+    x = max(x, static_cast<unsigned>(__builtin_amdgcn_update_dpp(x, x, 0x143, 0xC, 0xF, false)));
+    return static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(x), 63));
+}
+
 // Block (g, b) writes row b's picks for KV head g: all its pages where they are no more than
-// `width`, else the first `first`, the last `recent` and the best of those between, whose
-// threshold is found bit by bit: of all keys the largest T that at least k of them reach.
-// Ties at T go to the lowest pages.
+// `width`, else the first `first`, the last `recent` and the best of those between.  The keys'
+// range is cut into bins, the bin that the last place falls into into finer ones, and so on until
+// a bin is wanted whole or is one value, whose places go to the lowest pages.  Bins stand in
+// descending order of their keys.
 template <int THREADS, int KEYS>
 __global__ __launch_bounds__(THREADS) void page_pick_kernel(const SelectArgs a) {
     constexpr int kWaves = THREADS / kWave;
+    constexpr int kBinBits = THREADS == 256 ? 10 : THREADS == 512 ? 11 : 12;
+    constexpr int kBins = 1 << kBinBits;
+    static_assert(kBins == 4 * THREADS, "four bins a thread");
     const int g = blockIdx.x, b = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
@@ -425,89 +487,165 @@ __global__ __launch_bounds__(THREADS) void page_pick_kernel(const SelectArgs a) 
         if (tid == 0) a.counts[seg] = n;
         return;
     }
+    __shared__ __align__(16) int s_bins[kBins];
+    __shared__ unsigned s_least[kWaves], s_most[kWaves];
+    __shared__ int s_sum[kWaves], s_bin, s_above, s_in;
     const unsigned* keys = a.keys + seg * a.pt_stride;
     const int lo = a.first, hi = n - a.recent;
     const int want = a.width - a.first - a.recent;   // at least 0, less than hi - lo
-    __shared__ int s_count[2][kWaves];
-    // keys that are no candidates count as 0, which no threshold is
+    // keys that are no candidates count as 0, which no candidate's is
     auto key = [&](int i) { return i >= lo && i < hi ? keys[i] : 0u; };
     unsigned held[KEYS > 0 ? KEYS : 1];
     if constexpr (KEYS > 0) {
 #pragma unroll
         for (int j = 0; j < KEYS; ++j) held[j] = key(j * THREADS + tid);
     }
-    auto count = [&](unsigned t, int parity) {
-        int c = 0;
+    auto each = [&](auto&& f) __attribute__((always_inline)) {
         if constexpr (KEYS > 0) {
 #pragma unroll
-            for (int j = 0; j < KEYS; ++j) c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(held[j] >= t));
+            for (int j = 0; j < KEYS; ++j)
+                if (j * THREADS < n) f(held[j]);
         } else {
-            for (int i0 = 0; i0 < n; i0 += THREADS)
-                c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i0 + tid < n && key(i0 + tid) >= t));
+            for (int i0 = 0; i0 < n; i0 += THREADS) f(key(i0 + tid));
         }
-        if (lane == 0) s_count[parity][wave] = c;
-        __syncthreads();
-        int total = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) total += s_count[parity][w];
-        return total;
     };
-    unsigned threshold = 0;
-    int above = hi - lo;   // candidates at or above the threshold
-    if (want == 0) {
-        threshold = 0xFFFFFFFFu;
-    } else {
-        int parity = 0;
-        for (unsigned bit = 0x80000000u; bit != 0 && above != want; bit >>= 1) {
-            const int c = count(threshold | bit, parity);
-            parity ^= 1;
-            if (c >= want) {
-                threshold |= bit;
-                above = c;
+    reinterpret_cast<i32x4*>(s_bins)[tid] = i32x4{0, 0, 0, 0};
+    unsigned cut = 0xFFFFFFFFu;    // keys from here on are picked,
+    unsigned tie = 0;              // and of those equal to this one
+    int spare = 0;                 // as many
+    if (want > 0) {
+        unsigned least = 0xFFFFFFFFu, most = 0;
+        each([&](unsigned k) {
+            least = k != 0 && k < least ? k : least;
+            most = k > most ? k : most;
+        });
+        least = ~wave_max_u32(~least);
+        most = wave_max_u32(most);
+        if (lane == 0) {
+            s_least[wave] = least;
+            s_most[wave] = most;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            least = min(least, s_least[w]);
+            most = max(most, s_most[w]);
+        }
+        int left = want;   // places for keys of [least, most]
+        while (true) {
+            const int bits = 32 - __clz(static_cast<int>((most - least) | 1u));
+            const int shift = bits > kBinBits ? bits - kBinBits : 0;
+            each([&](unsigned k) {
+                if (k >= least && k <= most) atomicAdd(&s_bins[(most - k) >> shift], 1);
+            });
+            __syncthreads();
+            const i32x4 mine = reinterpret_cast<const i32x4*>(s_bins)[tid];
+            reinterpret_cast<i32x4*>(s_bins)[tid] = i32x4{0, 0, 0, 0};
+            const int sum = mine[0] + mine[1] + mine[2] + mine[3];
+            const int upto = wave_scan(sum);
+            if (lane == kWave - 1) s_sum[wave] = upto;
+            __syncthreads();
+            int above = upto - sum;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) above += w < wave ? s_sum[w] : 0;
+            if (above < left && left <= above + sum) {   // one thread
+                int j = 0;
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (j == i && above + mine[i] < left) {
+                        above += mine[i];
+                        ++j;
+                    }
+                s_bin = 4 * tid + j;
+                s_above = above;
+                s_in = j == 0 ? mine[0] : j == 1 ? mine[1] : j == 2 ? mine[2] : mine[3];
+            }
+            __syncthreads();
+            left -= s_above;
+            most -= static_cast<unsigned>(s_bin) << shift;
+            const unsigned width = (1u << shift) - 1;
+            least = most - least > width ? most - width : least;
+            if (s_in == left) {
+                cut = least;
+                break;
+            }
+            if (shift == 0) {
+                cut = least + 1;
+                tie = least;
+                spare = left;
+                break;
             }
         }
     }
-    // In order of the pages: pages kept anyway and keys above the threshold, and of those at it
-    // as many as are left (all of them where the candidates at or above it are just enough).
-    __shared__ int s_more[kWaves], s_tie[kWaves];
-    int base = 0, ties = 0;
-    int spare = want;   // places for ties
-    if (want > 0) {
-        __syncthreads();
-        spare = above == want ? 0x7FFFFFFF : want - count(threshold + 1, 0);
-        __syncthreads();
-    }
-    auto emit = [&](int i, unsigned k) __attribute__((always_inline)) {
-        const bool keep = i < n && (i < lo || i >= hi);
-        const bool more = keep || (want > 0 && k > threshold);
-        const bool tie = want > 0 && !keep && i < n && k == threshold && k != 0;
-        const uint64_t bm = __builtin_amdgcn_ballot_w64(more), bt = __builtin_amdgcn_ballot_w64(tie);
-        if (lane == 0) {
-            s_more[wave] = __builtin_popcountll(bm);
-            s_tie[wave] = __builtin_popcountll(bt);
-        }
-        __syncthreads();
-        int m0 = base, t0 = ties, m1 = 0, t1 = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            m0 += w < wave ? s_more[w] : 0;
-            t0 += w < wave ? s_tie[w] : 0;
-            m1 += s_more[w];
-            t1 += s_tie[w];
-        }
-        const uint64_t below = (1ull << lane) - 1;
-        const int m = m0 + __builtin_popcountll(bm & below), t = t0 + __builtin_popcountll(bt & below);
-        if (more || (tie && t < spare)) picks[m + (t < spare ? t : spare)] = i;
-        base += m1;
-        ties += t1;
-        __syncthreads();
+    // In order of the pages: those kept anyway, the keys from the cut on, and the first of the ties.
+    auto kinds = [&](int i, unsigned k, bool& more, bool& tied) {
+        more = i < n && (i < lo || i >= hi || k >= cut);
+        tied = k == tie && k != 0;
+    };
+    auto put = [&](int i, bool more, bool tied, uint64_t bm, uint64_t bt, int before) {
+        const uint64_t below = (1ull << lane) - 1;   // `before`: picks in the low half, ties in the high one
+        const int m = (before & 0xFFFF) + __builtin_popcountll(bm & below);
+        const int t = (before >> 16) + __builtin_popcountll(bt & below);
+        if (more || (tied && t < spare)) picks[m + (t < spare ? t : spare)] = i;
     };
     if constexpr (KEYS > 0) {
+        // counts of all (turn, wave) groups of 64 pages, at most 2^14 of each kind
+        constexpr int kGroups = KEYS * kWaves;
+        __shared__ int s_kinds[kGroups];
+        uint64_t bm[KEYS], bt[KEYS];
 #pragma unroll
-        for (int j = 0; j < KEYS; ++j)
-            if (j * THREADS < n) emit(j * THREADS + tid, held[j]);
+        for (int j = 0; j < KEYS; ++j) {
+            bool more, tied;
+            kinds(j * THREADS + tid, held[j], more, tied);
+            bm[j] = __builtin_amdgcn_ballot_w64(more);
+            bt[j] = __builtin_amdgcn_ballot_w64(tied);
+            if (lane == 0)
+                s_kinds[j * kWaves + wave] = __builtin_popcountll(bm[j]) | __builtin_popcountll(bt[j]) << 16;
+        }
+        __syncthreads();
+        int carry = 0;
+        int before[(kGroups + kWave - 1) / kWave];
+#pragma unroll
+        for (int c = 0; c < kGroups; c += kWave) {
+            const int x = c + lane < kGroups ? s_kinds[c + lane] : 0;
+            const int upto = wave_scan(x);
+            before[c / kWave] = carry + upto - x;
+            carry += __builtin_amdgcn_readlane(upto, kWave - 1);
+        }
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j) {
+            const int at = j * kWaves + wave;
+            const int base = __builtin_amdgcn_readlane(before[j * kWaves / kWave],
+                                                       __builtin_amdgcn_readfirstlane(at) % kWave);
+            put(j * THREADS + tid, (bm[j] >> lane) & 1, (bt[j] >> lane) & 1, bm[j], bt[j], base);
+        }
     } else {
-        for (int i0 = 0; i0 < n; i0 += THREADS) emit(i0 + tid, key(i0 + tid));
+        __shared__ int s_more[kWaves], s_tie[kWaves];
+        int base = 0, ties = 0;
+        for (int i0 = 0; i0 < n; i0 += THREADS) {
+            const int i = i0 + tid;
+            bool more, tied;
+            kinds(i, key(i), more, tied);
+            const uint64_t bm = __builtin_amdgcn_ballot_w64(more), bt = __builtin_amdgcn_ballot_w64(tied);
+            if (lane == 0) {
+                s_more[wave] = __builtin_popcountll(bm);
+                s_tie[wave] = __builtin_popcountll(bt);
+            }
+            __syncthreads();
+            int m = base, t = ties;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                m += w < wave ? s_more[w] : 0;
+                t += w < wave ? s_tie[w] : 0;
+                base += s_more[w];
+                ties += s_tie[w];
+            }
+            const uint64_t below = (1ull << lane) - 1;
+            m += __builtin_popcountll(bm & below);
+            t += __builtin_popcountll(bt & below);
+            if (more || (tied && t < spare)) picks[m + (t < spare ? t : spare)] = i;
+            __syncthreads();
+        }
     }
     if (tid == 0) a.counts[seg] = a.width;
 }
@@ -601,8 +739,8 @@ __device__ __forceinline__ void store_result(const SparseArgs& a, int64_t head_r
     }
 }
 
-// Block (s, g, b): part s of row b's list for KV head g, shared by the block's waves in
-// consecutive ranges, joined in LDS.  With one part the block writes the output, else a
+// Block (s, g, b): part s of row b's list for KV head g, shared by the block's waves and joined
+// in LDS.  With one part the block writes the output, else a
 // partial result.
 template <int D, bool BF16, int WAVES, int R>
 __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const SparseArgs a) {
@@ -617,10 +755,13 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
     const int n = invalid || len == 0 ? 0 : (len - 1) / kPageTokens + 1;
     int count = a.counts ? a.counts[seg] : a.width;
     count = count < 0 || n == 0 ? 0 : count > a.width ? a.width : count;
-    const int parts = a.parts * WAVES, k = part * WAVES + wave;
-    const int e0 = static_cast<int>(static_cast<int64_t>(count) * k / parts);
-    const int e1 = static_cast<int>(static_cast<int64_t>(count) * (k + 1) / parts);
+    // This wave takes entries k, k + stride, ..: which they are does not wait for the count, and
+    // the waves of a block read neighbours at a time.
+    const int stride = a.parts * WAVES, k = part * WAVES + wave;
+    const int entries = count > k ? (count - k - 1) / stride + 1 : 0;
     const int32_t* list = a.picks + seg * a.width;
+    const int64_t e_first = k + static_cast<int64_t>(stride) * lane;
+    const int p_first = e_first < a.width ? list[e_first] : -1;
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
     const unsigned head_off = static_cast<unsigned>(g) * 2u * S::kTile;
     const unsigned koff = 16u * lane;
@@ -642,11 +783,12 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
     st.l = 0.f;
     bool bad = false, seen = false;
 
-    for (int base = e0; base < e1; base += kWave) {
-        const int cnt = e1 - base < kWave ? e1 - base : kWave;
-        // lane j: entry base + j, its page and how many tokens of it count (0: not of this row)
-        const int p = lane < cnt ? list[base + lane] : -1;
-        const bool in = p >= 0 && p < n;
+    for (int base = 0; base < entries; base += kWave) {
+        const int cnt = entries - base < kWave ? entries - base : kWave;
+        // lane j: the wave's entry base + j, its page and how many tokens of it count (0: not of
+        // this row)
+        const int p = base == 0 ? p_first : lane < cnt ? list[k + static_cast<int64_t>(stride) * (base + lane)] : -1;
+        const bool in = lane < cnt && p >= 0 && p < n;
         const int entry = in ? row[p] : -1;
         const int at = page_index(entry, a.num_hot, a.num_cold);
         const int left = len - p * kPageTokens;
@@ -767,10 +909,10 @@ hipError_t launch_sparse_for(const SparseArgs& a, const SparsePlan& p, hipStream
 hipError_t launch_bounds_update(const BoundsUpdateArgs& a, int head_dim, int dtype, int32_t num_layers, hipStream_t s,
                                 const LaunchEvents& ev) {
     // enough blocks for the GPU however few rows there are, no more than the longest row has units
-    const int64_t units = a.pt_stride * a.num_kv_heads;
+    const int slices = wave_split(a.num_kv_heads).slices;
     const int64_t rows = static_cast<int64_t>(a.batch) * num_layers;
-    int64_t gx = (16384 + rows - 1) / rows;
-    gx = std::min<int64_t>(gx, (units + kBlockWaves - 1) / kBlockWaves);
+    int64_t gx = (HCK_BOUNDS_BLOCKS + rows - 1) / rows;
+    gx = std::min<int64_t>(gx, (a.pt_stride + slices - 1) / slices);
     const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>(a.batch), static_cast<unsigned>(num_layers));
     const void* k = dtype == kDtypeBf16
                         ? (head_dim == 128 ? reinterpret_cast<const void*>(&bounds_update_kernel<128, true>)
@@ -782,9 +924,10 @@ hipError_t launch_bounds_update(const BoundsUpdateArgs& a, int head_dim, int dty
 }
 
 hipError_t launch_bounds_read(const BoundsReadArgs& a, int32_t num_layers, hipStream_t s) {
-    const int64_t total = static_cast<int64_t>(a.n) * (a.num_kv_heads * 2 * a.head_dim / 4);
-    const int64_t blocks = std::min<int64_t>((total + kBlockThreads - 1) / kBlockThreads, 65536);
-    if (blocks <= 0) return hipSuccess;
+    if (a.n <= 0) return hipSuccess;
+    const int per = a.num_kv_heads * 2 * a.head_dim / 4;
+    const int side = per < kBlockThreads ? kBlockThreads / per : 1;
+    const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(a.n) + side - 1) / side, 65536);
     hipLaunchKernelGGL(bounds_read_kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(num_layers)),
                        dim3(kBlockThreads), 0, s, a);
     return hipGetLastError();
@@ -804,8 +947,7 @@ hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hip
                                const LaunchEvents& ev_pick) {
     void* args[] = {const_cast<SelectArgs*>(&a)};
     if (a.pt_stride > a.width) {   // else no row has pages to choose from
-        const int head_waves = a.num_kv_heads % 4 == 0 ? 4 : a.num_kv_heads % 2 == 0 ? 2 : 1;
-        const int pages = kWave * (kBlockWaves / head_waves);   // of a block and turn
+        const int pages = kWave * wave_split(a.num_kv_heads).slices;   // of a block and turn
         int64_t gx = (4096 + a.batch - 1) / a.batch;
         gx = std::min<int64_t>(gx, (a.pt_stride + pages - 1) / pages);
         const void* k = dtype == kDtypeBf16

@@ -3,6 +3,7 @@ every operation is a call into the HIP library."""
 
 from __future__ import annotations
 
+import contextlib
 from typing import Optional, Sequence
 
 import torch
@@ -10,6 +11,9 @@ import torch
 from . import hotcold_kv as kv
 
 _DTYPES = {"bf16": (kv.KV_DTYPE_BF16, torch.bfloat16), "f32": (kv.KV_DTYPE_F32, torch.float32)}
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
@@ -254,10 +258,17 @@ class HotColdPool:
         with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
             return torch.cuda.is_current_stream_capturing()
 
+    def _on(self, stream):
+        """The stream whose memory the call takes, as a context.  Entering one costs 6 us on the host, so a
+        call on the current stream of the current device enters none."""
+        if stream is None and torch.cuda.current_device() == self.device.index:
+            return _HERE
+        return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device))
+
     def _memory(self, need, like: Optional[torch.Tensor], stream):
         """An output like `like` and, where `need` is not 0, bytes of workspace, both of the call's
         stream: torch hands out memory that another stream may still be using otherwise."""
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+        with self._on(stream):
             return (None if like is None else torch.empty_like(like),
                     torch.empty(need, dtype=torch.uint8, device=self.device) if need else None)
 
@@ -376,7 +387,7 @@ class HotColdPool:
         """Bounds of the pages (int32 page-table entries [n]) as float32 [num_layers][n][kv_heads][2][head_dim]:
         the lowest and the highest value of each dim, rounded outwards to 8 bits."""
         n = pages.shape[0]
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+        with self._on(stream):
             out = torch.empty((num_layers, n, self.num_kv_heads, 2, self.head_dim), dtype=torch.float32,
                               device=self.device)
         kv.kv_read_bounds(self.handle, layer_begin, num_layers, self._ints(pages, n), n, out.data_ptr(),
@@ -403,7 +414,7 @@ class HotColdPool:
         lens = self._ints(seq_lens, B)
         st = self._raw(stream)
         ws = self._scratch("select", kv.paged_select_workspace_bytes(self.handle, B, pt.shape[1], width), st, stream)
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+        with self._on(stream):
             picks = torch.empty((B, self.num_kv_heads, width), dtype=torch.int32, device=self.device)
             counts = torch.empty((B, self.num_kv_heads), dtype=torch.int32, device=self.device)
         kv.paged_select_pages(self.handle, layer, q.data_ptr(), pt.data_ptr(), pt.shape[1], lens, B, Hq, width, first,
