@@ -29,6 +29,10 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
+// A value that all lanes share, in a scalar register: loads of it go through the vector path, and
+// what depends on it would count as different from lane to lane.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 constexpr int kPowerLimit = 50;  // |e| at most: products of two powers and a sum stay normal numbers
 
 // 2^e for |e| < 127.
@@ -134,14 +138,14 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const Boun
     constexpr int64_t kTile = static_cast<int64_t>(kPageTokens) * D * kElt;
     const int b = blockIdx.y;
     const int layer = a.layer + static_cast<int>(blockIdx.z);
-    const int len = a.lens[b];
+    const int len = uniform(a.lens[b]);
     if (len <= 0 || len > kPageTokens * a.pt_stride) return;
-    int first = a.starts ? a.starts[b] : 0;
+    int first = a.starts ? uniform(a.starts[b]) : 0;
     first = first < 0 ? 0 : first;
     if (first >= len) return;
     const int p0 = first / kPageTokens, p1 = (len - 1) / kPageTokens + 1;
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wave = uniform(threadIdx.x / kWave);
     const WaveSplit ws = wave_split(a.num_kv_heads);
     const int dg = lane / kLanes, sub = lane % kLanes;
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
@@ -154,7 +158,7 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const Boun
     auto fetch = [&](Unit& u, u32x4 (&w)[kLoads]) __attribute__((always_inline)) {
         u.at = -1;
         if (u.page >= p1) return;
-        u.at = page_index(__builtin_amdgcn_readfirstlane(row[u.page]), a.num_hot, a.num_cold);
+        u.at = page_index(uniform(row[u.page]), a.num_hot, a.num_cold);
         if (u.at < 0) return;
         const char* slice = u.at < a.num_hot ? slice_at(a.hot, u.at, layer) : slice_at(a.cold, u.at - a.num_hot, layer);
         const char* tile = slice + u.head * 2 * kTile + dg * 256 + sub * 16;
@@ -398,12 +402,12 @@ __device__ __forceinline__ void round_queries(QueryRows<D>& q, const QueryBits<D
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlockThreads) void page_scores_kernel(const SelectArgs a) {
     const int b = blockIdx.y;
-    const int len = a.lens[b];
+    const int len = uniform(a.lens[b]);
     if (len <= 0 || len > kPageTokens * a.pt_stride) return;
     const int n = (len - 1) / kPageTokens + 1;
     if (n <= a.width) return;
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wave = uniform(threadIdx.x / kWave);
     const WaveSplit ws = wave_split(a.num_kv_heads);
     const int step = kWave * ws.slices * static_cast<int>(gridDim.x);
     const int begin = kWave * (ws.slices * static_cast<int>(blockIdx.x) + wave / ws.heads);
@@ -480,7 +484,7 @@ __global__ __launch_bounds__(THREADS) void page_pick_kernel(const SelectArgs a) 
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
     int32_t* picks = a.picks + seg * a.width;
-    const int len = a.lens[b];
+    const int len = uniform(a.lens[b]);
     const int n = len <= 0 || len > kPageTokens * a.pt_stride ? 0 : (len - 1) / kPageTokens + 1;
     if (n <= a.width) {
         for (int i = tid; i < a.width; i += THREADS) picks[i] = i < n ? i : -1;
@@ -747,13 +751,13 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
     using S = Shape<D, BF16>;
     const int part = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wave = uniform(threadIdx.x / kWave);
     const int qg = lane >> 4;
     const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
-    const int len = a.lens[b];
+    const int len = uniform(a.lens[b]);
     const bool invalid = len < 0 || len > kPageTokens * a.pt_stride;
     const int n = invalid || len == 0 ? 0 : (len - 1) / kPageTokens + 1;
-    int count = a.counts ? a.counts[seg] : a.width;
+    int count = a.counts ? uniform(a.counts[seg]) : a.width;
     count = count < 0 || n == 0 ? 0 : count > a.width ? a.width : count;
     // This wave takes entries k, k + stride, ..: which they are does not wait for the count, and
     // the waves of a block read neighbours at a time.
@@ -763,7 +767,10 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
     const int64_t e_first = k + static_cast<int64_t>(stride) * lane;
     const int p_first = e_first < a.width ? list[e_first] : -1;
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
-    const unsigned head_off = static_cast<unsigned>(g) * 2u * S::kTile;
+    const char* const hot = a.hot + g * 2 * S::kTile;
+    const char* const cold = a.cold + g * 2 * S::kTile;
+    const int64_t hot_stride = a.hot_stride, cold_stride = a.cold_stride;
+    const int num_hot = a.num_hot;
     const unsigned koff = 16u * lane;
     const unsigned voff = BF16 ? (32u * (lane & 15) + 8u * qg) : (64u * (lane & 15) + 16u * qg);
 
@@ -803,8 +810,14 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
             PageAddr pa;
             pa.ok = page >= 0 && tokens > 0;
             const int id = pa.ok ? page : 0;
-            pa.base = (id < a.num_hot ? a.hot + static_cast<int64_t>(id) * a.hot_stride
-                                      : a.cold + static_cast<int64_t>(id - a.num_hot) * a.cold_stride) + head_off;
+            const char* base = hot;
+            int64_t slot = id, pitch = hot_stride;
+            if (id >= num_hot) {
+                base = cold;
+                slot = id - num_hot;
+                pitch = cold_stride;
+            }
+            pa.base = base + slot * pitch;
             const __amdgpu_buffer_rsrc_t rs = page_rsrc<D, BF16>(pa);
             load_page_k<D, BF16>(ring[r], rs, koff);
             load_page_v<D, BF16>(ring[r], rs, voff);
@@ -874,7 +887,7 @@ __global__ __launch_bounds__(kBlockThreads) void sparse_merge_kernel(const Spars
     if (i >= a.group * (D / 4)) return;
     const int h = i / (D / 4), quad = i % (D / 4);
     const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
-    const int len = a.lens[b];
+    const int len = uniform(a.lens[b]);
     const bool invalid = len < 0 || len > kPageTokens * a.pt_stride;
     float M = -INFINITY, den = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
