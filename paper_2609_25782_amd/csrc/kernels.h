@@ -437,16 +437,13 @@ struct SparseArgs {
     float* part_o;               // [lists][parts][group][D]
     float* part_ml;              // [lists][parts][2][group]
 };
-struct SparsePlan {
-    int32_t waves;   // of a workgroup
-    int32_t parts;
-};
-SparsePlan sparse_plan(int cus, int batch, int num_kv_heads, int group, int width);
-inline size_t sparse_workspace_bytes(const SparsePlan& p, int64_t lists, int group, int head_dim) {
-    const size_t n = p.parts > 1 ? static_cast<size_t>(lists) * p.parts * group * (head_dim + 2) * 4 : 0;
+// How many workgroups share a list (host arithmetic only); tile_bytes: K or V of a page and head.
+int32_t sparse_parts(int cus, int batch, int num_kv_heads, int64_t tile_bytes, int width);
+inline size_t sparse_workspace_bytes(int32_t parts, int64_t lists, int group, int head_dim) {
+    const size_t n = parts > 1 ? static_cast<size_t>(lists) * parts * group * (head_dim + 2) * 4 : 0;
     return std::max<size_t>((n + 255) & ~static_cast<size_t>(255), 256);
 }
-hipError_t launch_sparse_attention(const SparseArgs& a, const SparsePlan& p, int head_dim, int dtype, hipStream_t s,
+hipError_t launch_sparse_attention(const SparseArgs& a, int head_dim, int dtype, hipStream_t s,
                                    const LaunchEvents& ev = {}, const LaunchEvents& ev_merge = {});
 
 }  // namespace hck

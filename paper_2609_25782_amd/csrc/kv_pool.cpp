@@ -1862,6 +1862,11 @@ int sparse_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page
     return KV_OK;
 }
 
+int32_t sparse_parts(const kv_pool* pool, int32_t batch, int32_t width) {
+    return hck::sparse_parts(pool->cus, batch, pool->d.num_kv_heads,
+                             pool->slice_bytes / (2 * pool->d.num_kv_heads), width);
+}
+
 int workspace_ok(const void* workspace, size_t bytes, size_t need) {
     if (!workspace) return fail(KV_ERR_INVALID, "NULL workspace");
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KV_ERR_INVALID, "workspace must be 256-byte aligned");
@@ -2118,9 +2123,9 @@ int paged_select_pages(kv_pool* pool, int32_t layer, const void* q, const int32_
 
 size_t paged_sparse_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t width) {
     if (!chunk_shape_ok(pool, batch, num_q_heads) || width < 1) return 0;
-    const int32_t group = num_q_heads / pool->d.num_kv_heads;
-    return hck::sparse_workspace_bytes(hck::sparse_plan(pool->cus, batch, pool->d.num_kv_heads, group, width),
-                                       static_cast<int64_t>(batch) * pool->d.num_kv_heads, group, pool->d.head_dim);
+    return hck::sparse_workspace_bytes(sparse_parts(pool, batch, width),
+                                       static_cast<int64_t>(batch) * pool->d.num_kv_heads,
+                                       num_q_heads / pool->d.num_kv_heads, pool->d.head_dim);
 }
 
 int paged_sparse_attention(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
@@ -2137,9 +2142,9 @@ int paged_sparse_attention(kv_pool* pool, int32_t layer, const void* q, const in
     if (rc != KV_OK) return rc;
     if (!picks || !out) return fail(KV_ERR_INVALID, "NULL picks or out");
     if (reinterpret_cast<uintptr_t>(out) & 15) return fail(KV_ERR_INVALID, "out must be 16-byte aligned");
-    const hck::SparsePlan plan = hck::sparse_plan(pool->cus, batch, a.num_kv_heads, a.group, width);
+    a.parts = sparse_parts(pool, batch, width);
     const int64_t lists = static_cast<int64_t>(batch) * a.num_kv_heads;
-    rc = workspace_ok(workspace, ws_bytes, hck::sparse_workspace_bytes(plan, lists, a.group, pool->d.head_dim));
+    rc = workspace_ok(workspace, ws_bytes, hck::sparse_workspace_bytes(a.parts, lists, a.group, pool->d.head_dim));
     if (rc != KV_OK) return rc;
     DeviceGuard g(pool->d.device);
     hipStream_t st = pool->strm(stream);
@@ -2148,13 +2153,12 @@ int paged_sparse_attention(kv_pool* pool, int32_t layer, const void* q, const in
     a.counts = counts;
     a.width = width;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.parts = plan.parts;
     a.part_o = static_cast<float*>(workspace);
-    a.part_ml = a.part_o + lists * plan.parts * a.group * pool->d.head_dim;
+    a.part_ml = a.part_o + lists * a.parts * a.group * pool->d.head_dim;
     const bool prof = kv_pool::plain_stream(st);
     const hck::LaunchEvents ev = prof ? pool->prof_events() : hck::LaunchEvents{};
-    const hck::LaunchEvents evm = prof && plan.parts > 1 ? pool->prof_events() : hck::LaunchEvents{};
-    const hipError_t e = hck::launch_sparse_attention(a, plan, pool->d.head_dim, pool->d.dtype, st, ev, evm);
+    const hck::LaunchEvents evm = prof && a.parts > 1 ? pool->prof_events() : hck::LaunchEvents{};
+    const hipError_t e = hck::launch_sparse_attention(a, pool->d.head_dim, pool->d.dtype, st, ev, evm);
     pool->prof_done(KV_KERNEL_SPARSE, ev, e);
     pool->prof_done(KV_KERNEL_SPARSE_MERGE, evm, e);
     return e == hipSuccess ? KV_OK : hip_fail(e, "sparse attention launch");

@@ -133,34 +133,30 @@ __global__ __launch_bounds__(kBlockThreads) void page_copy_inline_kernel(
     copy_pages<U>(src, dst, list, n, chunks_per_entry, chunks_per_slice, by_layer, page_table);
 }
 
-// Branches of a session: a page's slice of a layer is read once and written to every branch's
-// page, layer by layer (as copies out of the hot pool are walked).
-template <int U, typename Entries>
-__device__ __forceinline__ void fork_pages(const PoolGeom& pool, const Entries& entries, int32_t n,
-                                           int chunks_per_slice, int64_t total) {
-    const int64_t per_layer = static_cast<int64_t>(n) * chunks_per_slice;
+// Branches of a session: 4 KiB of a page's slice are read once and written to every branch's page,
+// layer by layer (as copies out of the hot pool are walked).  The writes bound it: 2 sessions of
+// 4,000-6,000 tokens, 48 layers, four branches each (4.3 GB written, 1.1 read) 1,041 us a call; with the
+// reads nontemporal as well 1,056, with 16 KiB a block and turn 1,094, page by page 1,150, a
+// branch's page per block 1,518, and cached writes 1,070.
+template <typename Entries>
+__device__ __forceinline__ void fork_pages(const PoolGeom& pool, const Entries& entries, int32_t n, int rows,
+                                           int64_t total) {
+    const int64_t per_layer = static_cast<int64_t>(n) * rows;
     for (int64_t flat = blockIdx.x; flat < total; flat += gridDim.x) {
         const int layer = static_cast<int>(flat / per_layer);
         const int64_t rem = flat % per_layer;
-        const ForkEntry& e = entries[static_cast<int>(rem / chunks_per_slice)];
-        const int64_t off = (rem % chunks_per_slice) * (U * kBlockThreads * 16) + threadIdx.x * 16;
-        const u32x4* s = reinterpret_cast<const u32x4*>(slice_at(pool, e.src, layer) + off);
-        u32x4 buf[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) buf[i] = __builtin_nontemporal_load(s + i * kBlockThreads);
-        for (int k = 0; k < e.n; ++k) {
-            u32x4* d = reinterpret_cast<u32x4*>(slice_at(pool, e.dst[k], layer) + off);
-#pragma unroll
-            for (int i = 0; i < U; ++i) __builtin_nontemporal_store(buf[i], d + i * kBlockThreads);
-        }
+        const ForkEntry& e = entries[static_cast<int>(rem / rows)];
+        const int64_t off = (rem % rows) * (kBlockThreads * 16) + threadIdx.x * 16;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(slice_at(pool, e.src, layer) + off);
+        for (int k = 0; k < e.n; ++k)
+            __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(slice_at(pool, e.dst[k], layer) + off));
     }
 }
 
-template <int U>
 __global__ __launch_bounds__(kBlockThreads) void fork_copy_kernel(const PoolGeom pool,
                                                                   const ForkEntry* __restrict__ entries, int32_t n,
-                                                                  int chunks_per_slice, int64_t total) {
-    fork_pages<U>(pool, entries, n, chunks_per_slice, total);
+                                                                  int rows, int64_t total) {
+    fork_pages(pool, entries, n, rows, total);
 }
 
 struct ForkList {
@@ -168,11 +164,9 @@ struct ForkList {
     __device__ const ForkEntry& operator[](int i) const { return e[i]; }
 };
 
-template <int U>
-__global__ __launch_bounds__(kBlockThreads) void fork_copy_inline_kernel(const PoolGeom pool, int32_t n,
-                                                                         int chunks_per_slice, int64_t total,
-                                                                         const ForkList list) {
-    fork_pages<U>(pool, list, n, chunks_per_slice, total);
+__global__ __launch_bounds__(kBlockThreads) void fork_copy_inline_kernel(const PoolGeom pool, int32_t n, int rows,
+                                                                         int64_t total, const ForkList list) {
+    fork_pages(pool, list, n, rows, total);
 }
 
 __global__ __launch_bounds__(kBlockThreads) void table_writes_kernel(const CopyEntry* __restrict__ entries,
@@ -727,26 +721,19 @@ hipError_t launch_fork_copy(const PoolGeom& pool, int64_t slice_bytes, int32_t l
     constexpr int64_t kRow = static_cast<int64_t>(kBlockThreads) * 16;  // 4 KiB
     if (slice_bytes % kRow || slice_bytes <= 0 || layers < 1) return hipErrorInvalidValue;
     if (on_host && n > kForkInline) return hipErrorInvalidValue;
-    const int64_t rows = slice_bytes / kRow;
-    const int u = rows % 4 == 0 ? 4 : rows % 2 == 0 ? 2 : 1;
-    int cps = static_cast<int>(rows / u);
-    int64_t total = static_cast<int64_t>(cps) * layers * n;
+    int rows = static_cast<int>(slice_bytes / kRow);
+    int64_t total = static_cast<int64_t>(rows) * layers * n;
     const int64_t cap = max_blocks > 0 ? max_blocks : HCK_COPY_FINE_BLOCKS;
     const dim3 grid(static_cast<unsigned>(total < cap ? total : cap));
     if (on_host) {
-        const void* k = u == 4   ? reinterpret_cast<const void*>(&fork_copy_inline_kernel<4>)
-                        : u == 2 ? reinterpret_cast<const void*>(&fork_copy_inline_kernel<2>)
-                                 : reinterpret_cast<const void*>(&fork_copy_inline_kernel<1>);
         ForkList list = {};
         for (int32_t i = 0; i < n; ++i) list.e[i] = entries[i];
-        void* args[] = {const_cast<PoolGeom*>(&pool), &n, &cps, &total, &list};
-        return launch_kernel(k, grid, dim3(kBlockThreads), args, 0, s, ev);
+        void* args[] = {const_cast<PoolGeom*>(&pool), &n, &rows, &total, &list};
+        return launch_kernel(reinterpret_cast<const void*>(&fork_copy_inline_kernel), grid, dim3(kBlockThreads), args, 0,
+                             s, ev);
     }
-    const void* k = u == 4   ? reinterpret_cast<const void*>(&fork_copy_kernel<4>)
-                    : u == 2 ? reinterpret_cast<const void*>(&fork_copy_kernel<2>)
-                             : reinterpret_cast<const void*>(&fork_copy_kernel<1>);
-    void* args[] = {const_cast<PoolGeom*>(&pool), &entries, &n, &cps, &total};
-    return launch_kernel(k, grid, dim3(kBlockThreads), args, 0, s, ev);
+    void* args[] = {const_cast<PoolGeom*>(&pool), &entries, &n, &rows, &total};
+    return launch_kernel(reinterpret_cast<const void*>(&fork_copy_kernel), grid, dim3(kBlockThreads), args, 0, s, ev);
 }
 
 hipError_t launch_table_writes(const CopyEntry* entries, int32_t n, int32_t* page_table, hipStream_t s) {

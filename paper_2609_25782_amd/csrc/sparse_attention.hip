@@ -27,7 +27,6 @@ namespace hck {
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 // A value that all lanes share, in a scalar register: loads of it go through the vector path, and
 // what depends on it would count as different from lane to lane.
@@ -98,44 +97,68 @@ __host__ __device__ __forceinline__ WaveSplit wave_split(int num_kv_heads) {
 // ---------------------------------------------------------------------------
 // Bounds of pages.
 
-// Bit patterns in an order that signed comparisons of whole words (bfloat16: of halves) follow;
-// the map is its own inverse.
+// The lowest and the highest of sign-and-magnitude values from their bits, halves (bfloat16) or
+// whole words: among values without a sign bit integers order them, among those with one backwards.
+// So the highest is the greatest signed integer where that is not negative, else the least unsigned
+// one; the lowest is the greatest unsigned integer where that has a sign bit, else the least.  Three
+// instructions a word of keys.
 template <bool BF16>
-__device__ __forceinline__ unsigned ordered(unsigned w) {
-    if constexpr (BF16) {
-        const s16x2 x = __builtin_bit_cast(s16x2, w);
-        return w ^ (__builtin_bit_cast(unsigned, static_cast<s16x2>(x >> 15)) & 0x7FFF7FFFu);
-    } else {
-        return w ^ (static_cast<unsigned>(static_cast<int>(w) >> 31) & 0x7FFFFFFFu);
+struct Extremes {
+    typedef short s16x2_t __attribute__((ext_vector_type(2)));
+    typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+    unsigned smax, umin, umax;
+    __device__ __forceinline__ explicit Extremes(unsigned w) : smax(w), umin(w), umax(w) {}
+    __device__ __forceinline__ void take(unsigned s, unsigned n, unsigned x) {
+        if constexpr (BF16) {
+            smax = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(s16x2_t, smax),
+                                                                          __builtin_bit_cast(s16x2_t, s)));
+            umin = __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(u16x2_t, umin),
+                                                                          __builtin_bit_cast(u16x2_t, n)));
+            umax = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, umax),
+                                                                          __builtin_bit_cast(u16x2_t, x)));
+        } else {
+            smax = static_cast<unsigned>(max(static_cast<int>(smax), static_cast<int>(s)));
+            umin = min(umin, n);
+            umax = max(umax, x);
+        }
     }
-}
-template <bool BF16, bool MAX>
-__device__ __forceinline__ unsigned pick(unsigned a, unsigned b) {
-    if constexpr (BF16) {
-        const s16x2 x = __builtin_bit_cast(s16x2, a), y = __builtin_bit_cast(s16x2, b);
-        return __builtin_bit_cast(unsigned, MAX ? __builtin_elementwise_max(x, y) : __builtin_elementwise_min(x, y));
-    } else {
-        const int x = static_cast<int>(a), y = static_cast<int>(b);
-        return static_cast<unsigned>(MAX ? max(x, y) : min(x, y));
+    __device__ __forceinline__ void take(unsigned w) { take(w, w, w); }
+    // All ones in every half (word) of x with a sign bit.
+    __device__ __forceinline__ static unsigned signs(unsigned x) {
+        if constexpr (BF16)
+            return __builtin_bit_cast(unsigned, static_cast<s16x2_t>(__builtin_bit_cast(s16x2_t, x) >> 15));
+        else
+            return static_cast<unsigned>(static_cast<int>(x) >> 31);
     }
-}
+    __device__ __forceinline__ unsigned highest() const {
+        const unsigned m = signs(smax);
+        return (smax & ~m) | (umin & m);
+    }
+    __device__ __forceinline__ unsigned lowest() const {
+        const unsigned m = signs(umax);
+        return (umax & m) | (umin & ~m);
+    }
+};
 
 #ifndef HCK_BOUNDS_BLOCKS
 #define HCK_BOUNDS_BLOCKS 4096
 #endif
 
-// One wave takes a (page, KV head) at a time.  A 16-byte group of dims of all 16 tokens is
-// 256 consecutive bytes of the K tile and belongs to kLanes lanes, each with every kLanes-th
-// token of it, so most of the reduction over tokens stays in a lane's registers.
+// One wave takes a (page, KV head) at a time: the K tile is loaded in its own order, whole lines a
+// load, and goes through LDS, from where lane l reads word l of every token (and word l + 64 where a
+// token has 128; where it has 32 the lower lanes read tokens 0 .. 7 and the upper ones the rest).  A
+// group of 16 tokens' 16 bytes takes 272 bytes there: neither side meets a bank twice.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const BoundsUpdateArgs a) {
     constexpr int kElt = BF16 ? 2 : 4;
-    constexpr int kX = 16 / kElt;                     // dims of a group
-    constexpr int kGroups = D / kX;                   // groups of a tile: 8, 16 or 32
-    constexpr int kLanes = kWave / kGroups;           // lanes of a group: 8, 4 or 2
-    constexpr int kLoads = kPageTokens / kLanes;
-    constexpr int kDims = kX / kLanes;                // dims that a lane writes: 1 or 2
-    constexpr int64_t kTile = static_cast<int64_t>(kPageTokens) * D * kElt;
+    constexpr int kTile = kPageTokens * D * kElt;
+    constexpr int kLoads = kTile / (16 * kWave);
+    constexpr int kWords = D * kElt / 4;                        // 4-byte words of a token: 32, 64 or 128
+    constexpr int kRows = kWords > kWave ? kWords / kWave : 1;  // that a lane reduces
+    constexpr int kHalves = kWords < kWave ? kWave / kWords : 1;
+    constexpr int kTokens = kPageTokens / kHalves;
+    constexpr int kDims = 4 / kElt;                             // dims of a word
+    constexpr int kPitch = 16 * kPageTokens + 16;
     const int b = blockIdx.y;
     const int layer = a.layer + static_cast<int>(blockIdx.z);
     const int len = uniform(a.lens[b]);
@@ -147,130 +170,120 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const Boun
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = uniform(threadIdx.x / kWave);
     const WaveSplit ws = wave_split(a.num_kv_heads);
-    const int dg = lane / kLanes, sub = lane % kLanes;
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
     const int step = ws.slices * static_cast<int>(gridDim.x);
-    // this wave's (page, head) pairs, one after the other; the next one's keys are in flight
-    // while the current one's are reduced
     struct Unit {
-        int page, head, at;
+        int at, head;   // the page among the records (-1: none), its KV head
+        int last;       // its last token's slot, which stands in for those behind it
     };
-    auto fetch = [&](Unit& u, u32x4 (&w)[kLoads]) __attribute__((always_inline)) {
-        u.at = -1;
-        if (u.page >= p1) return;
-        u.at = page_index(uniform(row[u.page]), a.num_hot, a.num_cold);
-        if (u.at < 0) return;
-        const char* slice = u.at < a.num_hot ? slice_at(a.hot, u.at, layer) : slice_at(a.cold, u.at - a.num_hot, layer);
-        const char* tile = slice + u.head * 2 * kTile + dg * 256 + sub * 16;
+    __shared__ __align__(16) char s_tile[kBlockWaves][kWords / 4 * kPitch];
+    char* const mem = s_tile[wave];
+    const int word = lane % kWords, half = kHalves > 1 ? lane / kWords : 0;
+    const char* const mine = mem + word / 4 * kPitch + word % 4 * 4 + half * kTokens * 16;
+    auto reduce = [&](const Unit& u, const u32x4 (&tile)[kLoads]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tile + i * kLanes * 16));
-    };
-    Unit next = {p0 + ws.slices * static_cast<int>(blockIdx.x) + wave / ws.heads, wave % ws.heads, -1};
-    u32x4 w_next[kLoads];
-    fetch(next, w_next);
-    while (next.page < p1) {
-        const Unit cur = next;
-        u32x4 w[kLoads];
+            *reinterpret_cast<u32x4*>(mem + (4 * i + lane / 16) * kPitch + lane % 16 * 16) = tile[i];
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        unsigned lo[kRows], hi[kRows];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) w[i] = w_next[i];
-        next.head += ws.heads;
-        if (next.head >= a.num_kv_heads) {
-            next.head = wave % ws.heads;
-            next.page = next.page + step < p1 ? next.page + step : p1;
+        for (int r = 0; r < kRows; ++r) {
+            auto at = [&](int t) { return *reinterpret_cast<const unsigned*>(mine + r * 16 * kPitch + 16 * t); };
+            unsigned w[kTokens];
+            if (u.last == kPageTokens - 1) {
+#pragma unroll
+                for (int t = 0; t < kTokens; ++t) w[t] = at(t);
+            } else {   // the last token once more in the place of those behind it
+#pragma unroll
+                for (int t = 0; t < kTokens; ++t) w[t] = at(min(half * kTokens + t, u.last) - half * kTokens);
+            }
+            Extremes<BF16> x(w[0]);
+#pragma unroll
+            for (int t = 1; t < kTokens; ++t) x.take(w[t]);
+            if constexpr (kHalves == 2)
+                x.take(static_cast<unsigned>(__shfl_xor(static_cast<int>(x.smax), 32)),
+                       static_cast<unsigned>(__shfl_xor(static_cast<int>(x.umin), 32)),
+                       static_cast<unsigned>(__shfl_xor(static_cast<int>(x.umax), 32)));
+            lo[r] = x.lowest();
+            hi[r] = x.highest();
         }
-        fetch(next, w_next);
-        if (cur.at < 0) continue;
-        const int at = cur.at, head = cur.head;
-        const int valid = len - cur.page * kPageTokens;   // tokens of the page, or more than 16
-        unsigned lo[4], hi[4];
-        constexpr unsigned kLeast = BF16 ? 0x80008000u : 0x80000000u, kMost = BF16 ? 0x7FFF7FFFu : 0x7FFFFFFFu;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            lo[j] = kMost;
-            hi[j] = kLeast;
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const bool in = sub + i * kLanes < valid;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const unsigned o = ordered<BF16>(w[i][j]);
-                lo[j] = pick<BF16, false>(lo[j], in ? o : kMost);
-                hi[j] = pick<BF16, true>(hi[j], in ? o : kLeast);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            lo[j] = pick<BF16, false>(lo[j], dpp<kDppXor1>(lo[j]));
-            hi[j] = pick<BF16, true>(hi[j], dpp<kDppXor1>(hi[j]));
-            if constexpr (kLanes >= 4) {
-                lo[j] = pick<BF16, false>(lo[j], dpp<kDppXor2>(lo[j]));
-                hi[j] = pick<BF16, true>(hi[j], dpp<kDppXor2>(hi[j]));
-            }
-            if constexpr (kLanes >= 8) {
-                lo[j] = pick<BF16, false>(lo[j], dpp<kDppMirror8>(lo[j]));
-                hi[j] = pick<BF16, true>(hi[j], dpp<kDppMirror8>(hi[j]));
-            }
-        }
-        // this lane's dims: kDims of its group, from the sub-th on
-        float l[kDims], h[kDims];
-        if constexpr (BF16) {
-            unsigned wl = lo[0], wh = hi[0];
-#pragma unroll
-            for (int j = 1; j < 4; ++j) {
-                wl = sub * kDims / 2 == j ? lo[j] : wl;
-                wh = sub * kDims / 2 == j ? hi[j] : wh;
-            }
-            wl = ordered<true>(wl);
-            wh = ordered<true>(wh);
-            if constexpr (kDims == 2) {
-                l[0] = __uint_as_float(wl << 16);
-                l[1] = __uint_as_float(wl & 0xFFFF0000u);
-                h[0] = __uint_as_float(wh << 16);
-                h[1] = __uint_as_float(wh & 0xFFFF0000u);
-            } else {
-                l[0] = __uint_as_float(sub & 1 ? wl & 0xFFFF0000u : wl << 16);
-                h[0] = __uint_as_float(sub & 1 ? wh & 0xFFFF0000u : wh << 16);
-            }
-        } else {
-#pragma unroll
-            for (int d = 0; d < kDims; ++d) {
-                unsigned wl = lo[d], wh = hi[d];
-#pragma unroll
-                for (int j = 1; j < 4 / kDims; ++j) {
-                    wl = sub == j ? lo[j * kDims + d] : wl;
-                    wh = sub == j ? hi[j * kDims + d] : wh;
-                }
-                l[d] = __uint_as_float(ordered<false>(wl));
-                h[d] = __uint_as_float(ordered<false>(wh));
-            }
-        }
+        __asm__ volatile("" ::: "memory");   // the next tile is written after these reads
+        float l[kRows][kDims], h[kRows][kDims];
         float top = 0.f;
 #pragma unroll
-        for (int d = 0; d < kDims; ++d) {
-            l[d] = no_nan(l[d]);
-            h[d] = no_nan(h[d]);
-            top = fmaxf(top, fmaxf(fabsf(l[d]), fabsf(h[d])));
-        }
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) {
+                l[r][d] = no_nan(__uint_as_float(BF16 ? (d ? lo[r] & 0xFFFF0000u : lo[r] << 16) : lo[r]));
+                h[r][d] = no_nan(__uint_as_float(BF16 ? (d ? hi[r] & 0xFFFF0000u : hi[r] << 16) : hi[r]));
+                top = fmaxf(top, fmaxf(fabsf(l[r][d]), fabsf(h[r][d])));
+            }
         const int e = power_for(wave_max(top));
         const float down = two_to(-e);
-        unsigned ql = 0, qh = 0;
+        // Loads and stores stand under no condition (a pair that is none has resources without
+        // records): the compiler then knows how many of either are in flight and waits for the
+        // next pair's loads alone.
+        const __amdgpu_buffer_rsrc_t rec = __builtin_amdgcn_make_buffer_rsrc(
+            a.bounds + layer * a.layer_stride + static_cast<int64_t>(u.at < 0 ? 0 : u.at) * a.record,
+            static_cast<short>(0), u.at < 0 ? 0 : a.record, kRsrcWord3);
 #pragma unroll
-        for (int d = 0; d < kDims; ++d) {
-            ql |= (static_cast<unsigned>(static_cast<int>(clamp_127(floorf(l[d] * down)))) & 0xFFu) << (8 * d);
-            qh |= (static_cast<unsigned>(static_cast<int>(clamp_127(ceilf(h[d] * down)))) & 0xFFu) << (8 * d);
+        for (int r = 0; r < kRows; ++r) {
+            unsigned ql = 0, qh = 0;
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) {
+                ql |= (static_cast<unsigned>(static_cast<int>(clamp_127(floorf(l[r][d] * down)))) & 0xFFu) << (8 * d);
+                qh |= (static_cast<unsigned>(static_cast<int>(clamp_127(ceilf(h[r][d] * down)))) & 0xFFu) << (8 * d);
+            }
+            const int out = u.head * 2 * D + (r * kWave + word) * kDims;   // (both halves write the same)
+            if constexpr (kDims == 2) {
+                __builtin_amdgcn_raw_buffer_store_b16(static_cast<unsigned short>(ql), rec, out, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b16(static_cast<unsigned short>(qh), rec, out + D, 0, 0);
+            } else {
+                __builtin_amdgcn_raw_buffer_store_b8(static_cast<unsigned char>(ql), rec, out, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b8(static_cast<unsigned char>(qh), rec, out + D, 0, 0);
+            }
         }
-        char* rec = a.bounds + layer * a.layer_stride + static_cast<int64_t>(at) * a.record;
-        char* out = rec + head * 2 * D + dg * kX + sub * kDims;
-        if constexpr (kDims == 2) {
-            *reinterpret_cast<unsigned short*>(out) = static_cast<unsigned short>(ql);
-            *reinterpret_cast<unsigned short*>(out + D) = static_cast<unsigned short>(qh);
-        } else {
-            *out = static_cast<char>(ql);
-            out[D] = static_cast<char>(qh);
+        __builtin_amdgcn_raw_buffer_store_b8(static_cast<unsigned char>(e), rec, a.num_kv_heads * 2 * D + u.head, 0, 0);
+    };
+    // A wave's pages are every step-th from its first on, 64 of them at a time: lane j holds the
+    // j-th's place.  Its (page, head) pairs follow each other with the next one's keys in flight
+    // while one's are reduced.
+    for (int base = p0 + ws.slices * static_cast<int>(blockIdx.x) + wave / ws.heads; base < p1; base += kWave * step) {
+        const int64_t place = base + static_cast<int64_t>(step) * lane;
+        const int places = place < p1 ? page_index(row[place], a.num_hot, a.num_cold) : -1;
+        const int pages = min((p1 - base - 1) / step + 1, kWave);
+        int at_page = 0, at_head = wave % ws.heads;   // the pair fetched next
+        auto fetch = [&](Unit& u, u32x4 (&w)[kLoads]) __attribute__((always_inline)) {
+            u.at = at_page < pages ? __builtin_amdgcn_readlane(places, at_page) : -1;
+            u.head = at_head;
+            const int id = u.at < 0 ? 0 : u.at;
+            const bool cold = id >= a.num_hot;
+            const PoolGeom& pool = cold ? a.cold : a.hot;
+            // every step issues one tile's loads, past the end from a resource without records
+            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                slice_at(pool, cold ? id - a.num_hot : id, layer) + u.head * 2 * kTile, static_cast<short>(0),
+                u.at < 0 ? 0 : kTile, kRsrcWord3);
+            u.last = u.at < 0 ? 0 : min(len - (base + at_page * step) * kPageTokens, kPageTokens) - 1;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                w[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * lane + 1024 * (i % 4), 4096 * (i / 4), 2);
+            at_head += ws.heads;
+            if (at_head >= a.num_kv_heads) {
+                at_head = wave % ws.heads;
+                ++at_page;
+            }
+        };
+        const int pairs = pages * ((a.num_kv_heads - 1) / ws.heads + 1);   // (heads come in whole groups)
+        Unit u0, u1;
+        u32x4 w0[kLoads], w1[kLoads];
+        fetch(u0, w0);
+        for (int k = 0; k < pairs; k += 2) {
+            fetch(u1, w1);
+            reduce(u0, w0);
+            if (k + 1 >= pairs) break;
+            fetch(u0, w0);
+            reduce(u1, w1);
         }
-        if (lane == 0) rec[a.num_kv_heads * 2 * D + head] = static_cast<char>(e);
     }
 }
 
@@ -402,17 +415,18 @@ __device__ __forceinline__ void round_queries(QueryRows<D>& q, const QueryBits<D
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlockThreads) void page_scores_kernel(const SelectArgs a) {
     const int b = blockIdx.y;
-    const int len = uniform(a.lens[b]);
-    if (len <= 0 || len > kPageTokens * a.pt_stride) return;
-    const int n = (len - 1) / kPageTokens + 1;
-    if (n <= a.width) return;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = uniform(threadIdx.x / kWave);
     const WaveSplit ws = wave_split(a.num_kv_heads);
     const int step = kWave * ws.slices * static_cast<int>(gridDim.x);
     const int begin = kWave * (ws.slices * static_cast<int>(blockIdx.x) + wave / ws.heads);
-    if (begin >= n) return;
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
+    // the first page ids do not wait for the length
+    int entry = begin + lane < a.pt_stride ? row[begin + lane] : -1;
+    const int len = uniform(a.lens[b]);
+    if (len <= 0 || len > kPageTokens * a.pt_stride) return;
+    const int n = (len - 1) / kPageTokens + 1;
+    if (n <= a.width || begin >= n) return;
     const char* bounds = a.bounds + a.layer * a.layer_stride;
     const int part = lane >> 4;
     for (int g = wave % ws.heads; g < a.num_kv_heads; g += ws.heads) {
@@ -421,7 +435,8 @@ __global__ __launch_bounds__(kBlockThreads) void page_scores_kernel(const Select
         QueryRows<D> q;
         unsigned* keys = a.keys + (static_cast<int64_t>(b) * a.num_kv_heads + g) * a.pt_stride;
         for (int p0 = begin; p0 < n; p0 += step) {
-            const int at = p0 + lane < n ? page_index(row[p0 + lane], a.num_hot, a.num_cold) : -1;
+            if (p0 != begin || g != wave % ws.heads) entry = p0 + lane < n ? row[p0 + lane] : -1;
+            const int at = p0 + lane < n ? page_index(entry, a.num_hot, a.num_cold) : -1;
             const char* rec = bounds + static_cast<int64_t>(at < 0 ? 0 : at) * a.record;
             const int e = static_cast<signed char>(rec[a.num_kv_heads * 2 * D + g]);
             u32x4 w[4][2 * D / 64];
@@ -746,9 +761,10 @@ __device__ __forceinline__ void store_result(const SparseArgs& a, int64_t head_r
 // Block (s, g, b): part s of row b's list for KV head g, shared by the block's waves and joined
 // in LDS.  With one part the block writes the output, else a
 // partial result.
-template <int D, bool BF16, int WAVES, int R>
-__global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const SparseArgs a) {
+template <int D, bool BF16>
+__global__ __launch_bounds__(kBlockThreads) void sparse_split_kernel(const SparseArgs a) {
     using S = Shape<D, BF16>;
+    constexpr int R = 2;   // pages held: the one computed and the next
     const int part = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = uniform(threadIdx.x / kWave);
@@ -761,7 +777,7 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
     count = count < 0 || n == 0 ? 0 : count > a.width ? a.width : count;
     // This wave takes entries k, k + stride, ..: which they are does not wait for the count, and
     // the waves of a block read neighbours at a time.
-    const int stride = a.parts * WAVES, k = part * WAVES + wave;
+    const int stride = a.parts * kBlockWaves, k = part * kBlockWaves + wave;
     const int entries = count > k ? (count - k - 1) / stride + 1 : 0;
     const int32_t* list = a.picks + seg * a.width;
     const int64_t e_first = k + static_cast<int64_t>(stride) * lane;
@@ -846,7 +862,7 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
     // the waves' results meet in LDS: [wave][head][D], then [wave][max, sum][head]
     extern __shared__ __align__(16) char s_mem[];
     float* s_o = reinterpret_cast<float*>(s_mem);
-    float* s_ml = s_o + WAVES * a.group * D;
+    float* s_ml = s_o + kBlockWaves * a.group * D;
     const int h = lane & 15;
     if (h < a.group) {
         float* o = s_o + (wave * a.group + h) * D + 4 * qg;
@@ -858,12 +874,12 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < a.group * (D / 4); i += WAVES * kWave) {
+    for (int i = threadIdx.x; i < a.group * (D / 4); i += kBlockThreads) {
         const int hh = i / (D / 4), quad = i % (D / 4);
         float M = -INFINITY, den = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w)
+        for (int w = 0; w < kBlockWaves; ++w)
             lse_merge(M, den, acc, s_ml[w * 2 * a.group + hh], s_ml[w * 2 * a.group + a.group + hh],
                       *reinterpret_cast<const f32x4*>(s_o + (w * a.group + hh) * D + 4 * quad));
         if (a.parts == 1) {
@@ -879,39 +895,58 @@ __global__ __launch_bounds__(WAVES * kWave) void sparse_split_kernel(const Spars
     }
 }
 
-// The parts of a list joined: one thread per (head, 4 dims).
+// The parts of a list joined: a lane takes one (head, 4 dims), the block's waves every
+// kBlockWaves-th part each.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlockThreads) void sparse_merge_kernel(const SparseArgs a) {
     const int g = blockIdx.y, b = blockIdx.z;
-    const int i = blockIdx.x * kBlockThreads + threadIdx.x;
-    if (i >= a.group * (D / 4)) return;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = uniform(threadIdx.x / kWave);
+    const int items = a.group * (D / 4);
+    const int i = blockIdx.x * kWave + lane < items ? blockIdx.x * kWave + lane : items - 1;
     const int h = i / (D / 4), quad = i % (D / 4);
     const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
     const int len = uniform(a.lens[b]);
     const bool invalid = len < 0 || len > kPageTokens * a.pt_stride;
     float M = -INFINITY, den = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int p = 0; p < a.parts; ++p) {
-        const int64_t slot = seg * a.parts + p;
-        lse_merge(M, den, acc, a.part_ml[slot * 2 * a.group + h], a.part_ml[slot * 2 * a.group + a.group + h],
-                  *reinterpret_cast<const f32x4*>(a.part_o + (slot * a.group + h) * D + 4 * quad));
+    constexpr int U = 4;   // parts in flight; past the end the last one again, unused
+    for (int p0 = wave; p0 < a.parts; p0 += U * kBlockWaves) {
+        float m[U], l[U];
+        f32x4 o[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int p = p0 + u * kBlockWaves < a.parts ? p0 + u * kBlockWaves : a.parts - 1;
+            const int64_t slot = seg * a.parts + p;
+            m[u] = a.part_ml[slot * 2 * a.group + h];
+            l[u] = a.part_ml[slot * 2 * a.group + a.group + h];
+            o[u] = *reinterpret_cast<const f32x4*>(a.part_o + (slot * a.group + h) * D + 4 * quad);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p0 + u * kBlockWaves < a.parts) lse_merge(M, den, acc, m[u], l[u], o[u]);
     }
-    store_result<D, BF16>(a, seg * a.group + h, quad, M, den, acc, invalid);
+    __shared__ float s_m[kBlockWaves][kWave], s_l[kBlockWaves][kWave];
+    __shared__ f32x4 s_o[kBlockWaves][kWave];
+    s_m[wave][lane] = M;
+    s_l[wave][lane] = den;
+    s_o[wave][lane] = acc;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < kBlockWaves; ++w) lse_merge(M, den, acc, s_m[w][lane], s_l[w][lane], s_o[w][lane]);
+    if (blockIdx.x * kWave + lane < items) store_result<D, BF16>(a, seg * a.group + h, quad, M, den, acc, invalid);
 }
 
 template <int D, bool BF16>
-hipError_t launch_sparse_for(const SparseArgs& a, const SparsePlan& p, hipStream_t s, const LaunchEvents& ev,
-                             const LaunchEvents& ev_merge) {
-    constexpr int R = BF16 ? 3 : 2;
-    const void* k = p.waves == 8 ? reinterpret_cast<const void*>(&sparse_split_kernel<D, BF16, 8, R>)
-                                 : reinterpret_cast<const void*>(&sparse_split_kernel<D, BF16, 4, R>);
-    const size_t lds = static_cast<size_t>(p.waves) * a.group * (D + 2) * sizeof(float);
+hipError_t launch_sparse_for(const SparseArgs& a, hipStream_t s, const LaunchEvents& ev, const LaunchEvents& ev_merge) {
+    const size_t lds = static_cast<size_t>(kBlockWaves) * a.group * (D + 2) * sizeof(float);
     void* args[] = {const_cast<SparseArgs*>(&a)};
     const dim3 grid(static_cast<unsigned>(a.parts), static_cast<unsigned>(a.num_kv_heads), static_cast<unsigned>(a.batch));
-    hipError_t e = launch_kernel(k, grid, dim3(static_cast<unsigned>(p.waves * kWave)), args, lds, s, ev);
+    hipError_t e = launch_kernel(reinterpret_cast<const void*>(&sparse_split_kernel<D, BF16>), grid, dim3(kBlockThreads),
+                                 args, lds, s, ev);
     if (e != hipSuccess || a.parts == 1) return e;
-    const unsigned blocks = static_cast<unsigned>((a.group * (D / 4) + kBlockThreads - 1) / kBlockThreads);
+    const unsigned blocks = static_cast<unsigned>((a.group * (D / 4) + kWave - 1) / kWave);
     return launch_kernel(reinterpret_cast<const void*>(&sparse_merge_kernel<D, BF16>),
                          dim3(blocks, static_cast<unsigned>(a.num_kv_heads), static_cast<unsigned>(a.batch)),
                          dim3(kBlockThreads), args, 0, s, ev_merge);
@@ -991,23 +1026,28 @@ hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hip
                          args, 0, s, ev_pick);
 }
 
-SparsePlan sparse_plan(int cus, int batch, int num_kv_heads, int group, int width) {
-    SparsePlan p;
-    p.waves = group > 8 ? 4 : 8;
-    const int64_t lists = static_cast<int64_t>(batch) * num_kv_heads;
-    const int64_t fill = (cus + lists - 1) / std::max<int64_t>(lists, 1);
-    const int64_t most = (width + 4 * p.waves - 1) / (4 * p.waves);
-    p.parts = static_cast<int>(std::max<int64_t>(1, std::min(fill, most)));
-    return p;
+int32_t sparse_parts(int cus, int batch, int num_kv_heads, int64_t tile_bytes, int width) {
+    const int64_t lists = std::max<int64_t>(static_cast<int64_t>(batch) * num_kv_heads, 1);
+    const int64_t most = std::min<int64_t>((cus + lists - 1) / lists, (width + kBlockWaves - 1) / kBlockWaves);
+    int64_t best = 1, cost = -1;
+    for (int64_t parts = 1; parts <= most; parts = parts < most && 2 * parts > most ? most : 2 * parts) {
+        const int64_t pages = (width + parts * kBlockWaves - 1) / (parts * kBlockWaves);
+        const int64_t c = 45 * pages * tile_bytes / 4096 + (parts > 1 ? 150 + 5 * parts : 0);
+        if (cost < 0 || c < cost) {
+            best = parts;
+            cost = c;
+        }
+    }
+    return static_cast<int32_t>(best);
 }
 
-hipError_t launch_sparse_attention(const SparseArgs& a, const SparsePlan& p, int head_dim, int dtype, hipStream_t s,
-                                   const LaunchEvents& ev, const LaunchEvents& ev_merge) {
+hipError_t launch_sparse_attention(const SparseArgs& a, int head_dim, int dtype, hipStream_t s, const LaunchEvents& ev,
+                                   const LaunchEvents& ev_merge) {
     if (dtype == kDtypeBf16)
-        return head_dim == 128 ? launch_sparse_for<128, true>(a, p, s, ev, ev_merge)
-                               : launch_sparse_for<64, true>(a, p, s, ev, ev_merge);
-    return head_dim == 128 ? launch_sparse_for<128, false>(a, p, s, ev, ev_merge)
-                           : launch_sparse_for<64, false>(a, p, s, ev, ev_merge);
+        return head_dim == 128 ? launch_sparse_for<128, true>(a, s, ev, ev_merge)
+                               : launch_sparse_for<64, true>(a, s, ev, ev_merge);
+    return head_dim == 128 ? launch_sparse_for<128, false>(a, s, ev, ev_merge)
+                           : launch_sparse_for<64, false>(a, s, ev, ev_merge);
 }
 
 }  // namespace hck
