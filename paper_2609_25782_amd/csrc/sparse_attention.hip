@@ -371,25 +371,29 @@ template <int D, bool BF16>
 __device__ __forceinline__ void round_queries(QueryRows<D>& q, const QueryBits<D, BF16>& bits, int group, int lane) {
     const int part = lane >> 4;
     const bool in = (lane & 15) < group;
-    float v[D / 64][16];
+    // unpacked twice, not held: their registers are the records' in the meantime
+    auto value = [&](const QueryBits<D, BF16>& x, int c, int j) {
+        if constexpr (BF16) {
+            const unsigned w = x.w[c][j / 8][(j % 8) / 2];
+            return no_nan(__uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16));
+        } else {
+            return no_nan(__uint_as_float(x.w[c][j / 4][j % 4]));
+        }
+    };
     float top = 0.f;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            if constexpr (BF16) {
-                const unsigned x = bits.w[c][j / 8][(j % 8) / 2];
-                v[c][j] = __uint_as_float(j & 1 ? x & 0xFFFF0000u : x << 16);
-            } else {
-                v[c][j] = __uint_as_float(bits.w[c][j / 4][j % 4]);
-            }
-            v[c][j] = no_nan(v[c][j]);
-            top = fmaxf(top, fabsf(v[c][j]));
-        }
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, fabsf(value(bits, c, j)));
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     const int e = power_for(top);
     const float down = two_to(-e);
+    QueryBits<D, BF16> again = bits;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+        for (int i = 0; i < QueryBits<D, BF16>::kElt; ++i) __asm__("" : "+v"(again.w[c][i]));
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
 #pragma unroll
@@ -397,7 +401,7 @@ __device__ __forceinline__ void round_queries(QueryRows<D>& q, const QueryBits<D
             unsigned n = 0, p = 0;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int x = static_cast<int>(clamp_127(rintf(v[c][4 * j + k] * down)));
+                const int x = static_cast<int>(clamp_127(rintf(value(again, c, 4 * j + k) * down)));
                 n |= (static_cast<unsigned>(min(x, 0)) & 0xFFu) << (8 * k);
                 p |= (static_cast<unsigned>(max(x, 0)) & 0xFFu) << (8 * k);
             }
@@ -413,7 +417,7 @@ __device__ __forceinline__ void round_queries(QueryRows<D>& q, const QueryBits<D
 // takes chunks of 64 pages of a row, its waves a KV head each where the heads come in twos or
 // fours: the records of a page are then read side by side.
 template <int D, bool BF16>
-__global__ __launch_bounds__(kBlockThreads) void page_scores_kernel(const SelectArgs a) {
+__global__ __launch_bounds__(kBlockThreads, BF16 ? 4 : 3) void page_scores_kernel(const SelectArgs a) {
     const int b = blockIdx.y;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = uniform(threadIdx.x / kWave);
