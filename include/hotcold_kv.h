@@ -352,7 +352,7 @@ int kv_session_import_cold(kv_pool* pool, int32_t seq_len, const int32_t* cold_p
  * resident pages of paused sessions where too few are free; spill does not apply: the
  * call fails rather than place a branch in the cold tier), and the parents' pages are
  * copied to them on `stream`, every page read once for all branches of its session and
- * call (up to 14); a spilled page is fetched from the cold tier.  Whole pages are copied,
+ * call (up to 7); a spilled page is fetched from the cold tier.  Whole pages are copied,
  * slots past kept[i] included.  Pages whose 16 tokens are all kept are never written again:
  * the branch shares the parent's valid cold copies of them (an eviction then writes nothing;
  * a spilled page of the parent becomes shared).  Key bounds (kv_pool_set_bounds) go along.

@@ -351,16 +351,19 @@ struct AcceptArgs {
 };
 hipError_t launch_accept_drafts(const AcceptArgs& a, hipStream_t s);
 
-// One hot page copied to several others, all layers: read once, written n times.
-constexpr int kForkDests = 14;
+// One hot page copied to several others, all layers: read once, written n times.  Destination
+// k is also what page-table element at[k] becomes.
+constexpr int kForkDests = 7;
 struct ForkEntry {
     int32_t src;
     int32_t n;                 // destinations in use, 1 .. kForkDests
     int32_t dst[kForkDests];
+    int32_t at[kForkDests];
 };
 constexpr int kForkInline = 48;  // entries that travel in the kernel arguments
 hipError_t launch_fork_copy(const PoolGeom& pool, int64_t slice_bytes, int32_t layers, const ForkEntry* entries,
-                            bool on_host, int32_t n, int32_t max_blocks, hipStream_t s, const LaunchEvents& ev = {});
+                            bool on_host, int32_t n, int32_t* page_table, int32_t max_blocks, hipStream_t s,
+                            const LaunchEvents& ev = {});
 
 // Key bounds of pages.  A record (one page of one layer) is [KV head][lo, hi][head_dim] bytes,
 // then the heads' powers of two in 16 bytes; those of the hot pages come first, then the cold ones.
@@ -409,9 +412,11 @@ struct SelectArgs {
     int32_t* picks;              // [batch][num_kv_heads][width]
     int32_t* counts;             // [batch][num_kv_heads]
 };
-// Bytes of the keys: none where no row can have more pages than are picked.
+// Whether one kernel scores and picks, without a workspace.
+bool select_in_one(int64_t pt_stride);
+// Bytes of the keys: none there, nor where no row can have more pages than are picked.
 inline size_t select_workspace_bytes(int64_t lists, int64_t pt_stride, int32_t width) {
-    const size_t n = pt_stride > width ? static_cast<size_t>(lists) * static_cast<size_t>(pt_stride) * 4 : 0;
+    const size_t n = pt_stride > width && !select_in_one(pt_stride) ? static_cast<size_t>(lists) * static_cast<size_t>(pt_stride) * 4 : 0;
     return std::max<size_t>((n + 255) & ~static_cast<size_t>(255), 256);
 }
 hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hipStream_t s, const LaunchEvents& ev = {},

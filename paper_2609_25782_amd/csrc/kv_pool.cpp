@@ -409,12 +409,12 @@ struct kv_pool {
         return KV_OK;
     }
 
-    // Hot pages to the branches' pages (read once for up to kForkDests of them).
+    // Hot pages to the branches' pages (read once for up to kForkDests of them), and their table entries.
     int submit_fork(const std::vector<hck::ForkEntry>& entries, hipStream_t s) {
         if (!entries.empty() && entries.size() <= static_cast<size_t>(hck::kForkInline)) {
             const hck::LaunchEvents ev = prof_events();
             hipError_t e = hck::launch_fork_copy(hot_geom, slice_bytes, d.num_layers, entries.data(), /*on_host=*/true,
-                                                 static_cast<int32_t>(entries.size()), copy_blocks, s, ev);
+                                                 static_cast<int32_t>(entries.size()), pt, copy_blocks, s, ev);
             prof_done(KV_KERNEL_FORK_COPY, ev, e);
             return e == hipSuccess ? KV_OK : hip_fail(e, "fork copy launch");
         }
@@ -429,7 +429,7 @@ struct kv_pool {
             if (e != hipSuccess) return hip_fail(e, "fork list upload");
             const hck::LaunchEvents ev = prof_events();
             e = hck::launch_fork_copy(hot_geom, slice_bytes, d.num_layers, static_cast<const hck::ForkEntry*>(slot->dev),
-                                      /*on_host=*/false, static_cast<int32_t>(n), copy_blocks, s, ev);
+                                      /*on_host=*/false, static_cast<int32_t>(n), pt, copy_blocks, s, ev);
             prof_done(KV_KERNEL_FORK_COPY, ev, e);
             if (e != hipSuccess) return hip_fail(e, "fork copy launch");
             rc = release_slot(slot, s);
@@ -1125,8 +1125,9 @@ int kv_fork_sessions(kv_pool* pool, const int32_t* sids, const int32_t* kept, in
                     for (int32_t j : mine) {
                         if (p >= made[j].hot.size()) continue;
                         const int32_t dst = made[j].hot[p];
+                        const int32_t entry = ids[j] * pool->d.max_pages_per_session + static_cast<int32_t>(p);
                         if (s.hot[p] < 0) {
-                            fetched.push_back(hck::CopyEntry{s.cold[p], dst, -1, 0});
+                            fetched.push_back(hck::CopyEntry{s.cold[p], dst, entry, dst});
                             continue;
                         }
                         if (pool->bounds) records.push_back(hck::CopyEntry{s.hot[p], dst, -1, 0});
@@ -1135,7 +1136,9 @@ int kv_fork_sessions(kv_pool* pool, const int32_t* sids, const int32_t* kept, in
                             forks.back().src = s.hot[p];
                             fresh = false;
                         }
-                        forks.back().dst[forks.back().n++] = dst;
+                        hck::ForkEntry& e = forks.back();
+                        e.at[e.n] = entry;
+                        e.dst[e.n++] = dst;
                     }
                 }
             }
@@ -1144,8 +1147,6 @@ int kv_fork_sessions(kv_pool* pool, const int32_t* sids, const int32_t* kept, in
             if (!rc) rc = pool->submit_copies(true, fetched, {}, st, KV_KERNEL_PAGE_COPY);
             if (!rc) rc = pool->submit_fork(forks, st);
             if (!rc) rc = pool->submit_bounds_copies(pool->bounds_hot, pool->bounds_hot, records, st);
-            for (int32_t i = 0; i < n && !rc; ++i)
-                rc = pool->submit_row_at(ids[i], 0, made[i].hot.data(), static_cast<int32_t>(made[i].hot.size()), st);
             if (rc) return rc;
         }
         pool->commit_victims(a);
@@ -2113,7 +2114,7 @@ int paged_select_pages(kv_pool* pool, int32_t layer, const void* q, const int32_
     a.picks = picks;
     a.counts = counts;
     const bool prof = kv_pool::plain_stream(st);
-    const hck::LaunchEvents ev = prof && pt_stride > width ? pool->prof_events() : hck::LaunchEvents{};
+    const hck::LaunchEvents ev = prof && pt_stride > width && !hck::select_in_one(pt_stride) ? pool->prof_events() : hck::LaunchEvents{};
     const hck::LaunchEvents evp = prof ? pool->prof_events() : hck::LaunchEvents{};
     const hipError_t e = hck::launch_select_pages(a, pool->d.head_dim, pool->d.dtype, st, ev, evp);
     pool->prof_done(KV_KERNEL_PAGE_SCORES, ev, e);

@@ -140,12 +140,14 @@ __global__ __launch_bounds__(kBlockThreads) void page_copy_inline_kernel(
 // branch's page per block 1,518, and cached writes 1,070.
 template <typename Entries>
 __device__ __forceinline__ void fork_pages(const PoolGeom& pool, const Entries& entries, int32_t n, int rows,
-                                           int64_t total) {
+                                           int64_t total, int32_t* __restrict__ page_table) {
     const int64_t per_layer = static_cast<int64_t>(n) * rows;
     for (int64_t flat = blockIdx.x; flat < total; flat += gridDim.x) {
         const int layer = static_cast<int>(flat / per_layer);
         const int64_t rem = flat % per_layer;
         const ForkEntry& e = entries[static_cast<int>(rem / rows)];
+        if (layer == 0 && rem % rows == 0 && static_cast<int>(threadIdx.x) < e.n)
+            page_table[e.at[threadIdx.x]] = e.dst[threadIdx.x];
         const int64_t off = (rem % rows) * (kBlockThreads * 16) + threadIdx.x * 16;
         const u32x4 w = *reinterpret_cast<const u32x4*>(slice_at(pool, e.src, layer) + off);
         for (int k = 0; k < e.n; ++k)
@@ -155,8 +157,9 @@ __device__ __forceinline__ void fork_pages(const PoolGeom& pool, const Entries& 
 
 __global__ __launch_bounds__(kBlockThreads) void fork_copy_kernel(const PoolGeom pool,
                                                                   const ForkEntry* __restrict__ entries, int32_t n,
-                                                                  int rows, int64_t total) {
-    fork_pages(pool, entries, n, rows, total);
+                                                                  int rows, int64_t total,
+                                                                  int32_t* __restrict__ page_table) {
+    fork_pages(pool, entries, n, rows, total, page_table);
 }
 
 struct ForkList {
@@ -165,8 +168,10 @@ struct ForkList {
 };
 
 __global__ __launch_bounds__(kBlockThreads) void fork_copy_inline_kernel(const PoolGeom pool, int32_t n, int rows,
-                                                                         int64_t total, const ForkList list) {
-    fork_pages(pool, list, n, rows, total);
+                                                                         int64_t total,
+                                                                         int32_t* __restrict__ page_table,
+                                                                         const ForkList list) {
+    fork_pages(pool, list, n, rows, total, page_table);
 }
 
 __global__ __launch_bounds__(kBlockThreads) void table_writes_kernel(const CopyEntry* __restrict__ entries,
@@ -716,7 +721,8 @@ hipError_t launch_page_copy(const PoolGeom& src, const PoolGeom& dst, int64_t sl
 }
 
 hipError_t launch_fork_copy(const PoolGeom& pool, int64_t slice_bytes, int32_t layers, const ForkEntry* entries,
-                            bool on_host, int32_t n, int32_t max_blocks, hipStream_t s, const LaunchEvents& ev) {
+                            bool on_host, int32_t n, int32_t* page_table, int32_t max_blocks, hipStream_t s,
+                            const LaunchEvents& ev) {
     if (n <= 0) return hipSuccess;
     constexpr int64_t kRow = static_cast<int64_t>(kBlockThreads) * 16;  // 4 KiB
     if (slice_bytes % kRow || slice_bytes <= 0 || layers < 1) return hipErrorInvalidValue;
@@ -728,11 +734,11 @@ hipError_t launch_fork_copy(const PoolGeom& pool, int64_t slice_bytes, int32_t l
     if (on_host) {
         ForkList list = {};
         for (int32_t i = 0; i < n; ++i) list.e[i] = entries[i];
-        void* args[] = {const_cast<PoolGeom*>(&pool), &n, &rows, &total, &list};
+        void* args[] = {const_cast<PoolGeom*>(&pool), &n, &rows, &total, &page_table, &list};
         return launch_kernel(reinterpret_cast<const void*>(&fork_copy_inline_kernel), grid, dim3(kBlockThreads), args, 0,
                              s, ev);
     }
-    void* args[] = {const_cast<PoolGeom*>(&pool), &entries, &n, &rows, &total};
+    void* args[] = {const_cast<PoolGeom*>(&pool), &entries, &n, &rows, &total, &page_table};
     return launch_kernel(reinterpret_cast<const void*>(&fork_copy_kernel), grid, dim3(kBlockThreads), args, 0, s, ev);
 }
 

@@ -332,6 +332,13 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_copy_kernel(const PoolGe
 // ---------------------------------------------------------------------------
 // Scores of pages.
 
+// Tables of up to kShortThreads * kShortKeys pages a row take scores and choice in one kernel.
+constexpr int kShortThreads = 512;
+#ifndef HCK_SHORT_KEYS
+#define HCK_SHORT_KEYS 1
+#endif
+constexpr int kShortKeys = HCK_SHORT_KEYS;
+
 constexpr unsigned kKeyBad = 0xFFFFFFFEu;  // above every score: a page that no pool holds
 
 // Scores in an order that unsigned comparisons follow; none maps to 0.
@@ -413,9 +420,44 @@ __device__ __forceinline__ void round_queries(QueryRows<D>& q, const QueryBits<D
     for (int r = 0; r < 4; ++r) q.unit[r] = __shfl(unit, 4 * part + r);
 }
 
-// Keys of the scores of all pages of the rows that have more pages than are picked.  A block
-// takes chunks of 64 pages of a row, its waves a KV head each where the heads come in twos or
-// fours: the records of a page are then read side by side.
+// The keys of 64 pages' scores for KV head g: lane l's page has entry `at` among the records (-1: no
+// page, whose key is above all scores).  `meanwhile` runs while the records come.
+template <int D, typename F>
+__device__ __forceinline__ unsigned score_pages(const QueryRows<D>& q, const char* bounds, const SelectArgs& a, int g,
+                                                int at, int lane, F&& meanwhile) {
+    const int part = lane >> 4, rec = at < 0 ? 0 : at;
+    const int e = static_cast<signed char>(bounds[static_cast<int64_t>(rec) * a.record + a.num_kv_heads * 2 * D + g]);
+    u32x4 w[4][2 * D / 64];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const char* p = bounds + static_cast<int64_t>(__shfl(rec, 16 * t + (lane & 15))) * a.record + g * 2 * D + 16 * part;
+#pragma unroll
+        for (int c = 0; c < 2 * D / 64; ++c) w[t][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
+    }
+    meanwhile();
+    float best = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        i32x4 s = {0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+            s = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.neg[c], __builtin_bit_cast(i32x4, w[t][c]), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.pos[c], __builtin_bit_cast(i32x4, w[t][c + D / 64]), s, 0, 0, 0);
+        }
+        float x = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (q.unit[r] != 0.f) x = fmaxf(x, static_cast<float>(s[r]) * q.unit[r]);
+        x = fmaxf(x, __shfl_xor(x, 16));
+        x = fmaxf(x, __shfl_xor(x, 32));
+        best = part == t ? x : best;
+    }
+    return at < 0 ? kKeyBad : score_key(best * two_to(clamp_power(e)));
+}
+
+// Keys of all pages of the rows that have more pages than are picked.  A block takes chunks of 64
+// pages of a row, its waves a KV head each where the heads come in twos or fours: the records of
+// a page are then read side by side.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlockThreads, BF16 ? 4 : 3) void page_scores_kernel(const SelectArgs a) {
     const int b = blockIdx.y;
@@ -432,7 +474,6 @@ __global__ __launch_bounds__(kBlockThreads, BF16 ? 4 : 3) void page_scores_kerne
     const int n = (len - 1) / kPageTokens + 1;
     if (n <= a.width || begin >= n) return;
     const char* bounds = a.bounds + a.layer * a.layer_stride;
-    const int part = lane >> 4;
     for (int g = wave % ws.heads; g < a.num_kv_heads; g += ws.heads) {
         QueryBits<D, BF16> bits;
         load_query_bits<D, BF16>(bits, a, b, g, lane);
@@ -441,36 +482,10 @@ __global__ __launch_bounds__(kBlockThreads, BF16 ? 4 : 3) void page_scores_kerne
         for (int p0 = begin; p0 < n; p0 += step) {
             if (p0 != begin || g != wave % ws.heads) entry = p0 + lane < n ? row[p0 + lane] : -1;
             const int at = p0 + lane < n ? page_index(entry, a.num_hot, a.num_cold) : -1;
-            const char* rec = bounds + static_cast<int64_t>(at < 0 ? 0 : at) * a.record;
-            const int e = static_cast<signed char>(rec[a.num_kv_heads * 2 * D + g]);
-            u32x4 w[4][2 * D / 64];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int src = __shfl(at < 0 ? 0 : at, 16 * t + (lane & 15));
-                const char* p = bounds + static_cast<int64_t>(src) * a.record + g * 2 * D + 16 * part;
-#pragma unroll
-                for (int c = 0; c < 2 * D / 64; ++c) w[t][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
-            }
-            if (p0 == begin) round_queries<D, BF16>(q, bits, a.group, lane);   // while the records come
-            float best = 0.f;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                i32x4 s = {0, 0, 0, 0};
-#pragma unroll
-                for (int c = 0; c < D / 64; ++c) {
-                    s = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.neg[c], __builtin_bit_cast(i32x4, w[t][c]), s, 0, 0, 0);
-                    s = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.pos[c], __builtin_bit_cast(i32x4, w[t][c + D / 64]), s,
-                                                              0, 0, 0);
-                }
-                float x = -INFINITY;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (q.unit[r] != 0.f) x = fmaxf(x, static_cast<float>(s[r]) * q.unit[r]);
-                x = fmaxf(x, __shfl_xor(x, 16));
-                x = fmaxf(x, __shfl_xor(x, 32));
-                best = part == t ? x : best;
-            }
-            if (p0 + lane < n) keys[p0 + lane] = at < 0 ? kKeyBad : score_key(best * two_to(clamp_power(e)));
+            const unsigned key = score_pages<D>(q, bounds, a, g, at, lane, [&] {
+                if (p0 == begin) round_queries<D, BF16>(q, bits, a.group, lane);
+            });
+            if (p0 + lane < n) keys[p0 + lane] = key;
         }
     }
 }
@@ -488,32 +503,23 @@ __device__ __forceinline__ unsigned wave_max_u32(unsigned x) {
     return static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(x), 63));
 }
 
-// Block (g, b) writes row b's picks for KV head g: all its pages where they are no more than
-// `width`, else the first `first`, the last `recent` and the best of those between.  The keys'
+// Row b's picks for KV head g of its n > width pages: the first `first`, the last `recent` and the best
+// of those between.  The keys'
 // range is cut into bins, the bin that the last place falls into into finer ones, and so on until
 // a bin is wanted whole or is one value, whose places go to the lowest pages.  Bins stand in
 // descending order of their keys.
 template <int THREADS, int KEYS>
-__global__ __launch_bounds__(THREADS) void page_pick_kernel(const SelectArgs a) {
+__device__ __forceinline__ void pick_pages(const SelectArgs& a, int b, int g, int n, const unsigned* keys) {
     constexpr int kWaves = THREADS / kWave;
-    constexpr int kBinBits = THREADS == 256 ? 10 : THREADS == 512 ? 11 : 12;
+    constexpr int kBinBits = THREADS == 1024 ? 12 : 11;
     constexpr int kBins = 1 << kBinBits;
     static_assert(kBins == 4 * THREADS, "four bins a thread");
-    const int g = blockIdx.x, b = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
     int32_t* picks = a.picks + seg * a.width;
-    const int len = uniform(a.lens[b]);
-    const int n = len <= 0 || len > kPageTokens * a.pt_stride ? 0 : (len - 1) / kPageTokens + 1;
-    if (n <= a.width) {
-        for (int i = tid; i < a.width; i += THREADS) picks[i] = i < n ? i : -1;
-        if (tid == 0) a.counts[seg] = n;
-        return;
-    }
     __shared__ __align__(16) int s_bins[kBins];
     __shared__ unsigned s_least[kWaves], s_most[kWaves];
     __shared__ int s_sum[kWaves], s_bin, s_above, s_in;
-    const unsigned* keys = a.keys + seg * a.pt_stride;
     const int lo = a.first, hi = n - a.recent;
     const int want = a.width - a.first - a.recent;   // at least 0, less than hi - lo
     // keys that are no candidates count as 0, which no candidate's is
@@ -671,6 +677,55 @@ __global__ __launch_bounds__(THREADS) void page_pick_kernel(const SelectArgs a) 
         }
     }
     if (tid == 0) a.counts[seg] = a.width;
+}
+
+// Pages of the row, and whether that is more than are picked; else all of them are written here.
+template <int THREADS>
+__device__ __forceinline__ int row_to_pick(const SelectArgs& a, int b, int g, bool& choose) {
+    const int len = uniform(a.lens[b]);
+    const int n = len <= 0 || len > kPageTokens * a.pt_stride ? 0 : (len - 1) / kPageTokens + 1;
+    choose = n > a.width;
+    if (!choose) {
+        const int64_t seg = static_cast<int64_t>(b) * a.num_kv_heads + g;
+        for (int i = threadIdx.x; i < a.width; i += THREADS) a.picks[seg * a.width + i] = i < n ? i : -1;
+        if (threadIdx.x == 0) a.counts[seg] = n;
+    }
+    return n;
+}
+
+// Block (g, b): the choice by the keys that page_scores_kernel wrote.
+template <int THREADS, int KEYS>
+__global__ __launch_bounds__(THREADS) void page_pick_kernel(const SelectArgs a) {
+    const int g = blockIdx.x, b = blockIdx.y;
+    bool choose;
+    const int n = row_to_pick<THREADS>(a, b, g, choose);
+    if (choose)
+        pick_pages<THREADS, KEYS>(a, b, g, n, a.keys + (static_cast<int64_t>(b) * a.num_kv_heads + g) * a.pt_stride);
+}
+
+// Block (g, b): scores and choice in one, the keys in LDS, for rows of few pages.
+template <int D, bool BF16>
+__global__ __launch_bounds__(kShortThreads) void page_select_kernel(const SelectArgs a) {
+    const int g = blockIdx.x, b = blockIdx.y;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = uniform(threadIdx.x / kWave);
+    const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
+    int entry = wave * kWave + lane < a.pt_stride ? row[wave * kWave + lane] : -1;   // does not wait for the length
+    QueryBits<D, BF16> bits;
+    load_query_bits<D, BF16>(bits, a, b, g, lane);
+    bool choose;
+    const int n = row_to_pick<kShortThreads>(a, b, g, choose);
+    if (!choose) return;
+    __shared__ unsigned s_keys[kShortThreads * kShortKeys];
+    QueryRows<D> q;
+    round_queries<D, BF16>(q, bits, a.group, lane);
+    for (int p0 = wave * kWave; p0 < n; p0 += kShortThreads) {
+        if (p0 != wave * kWave) entry = p0 + lane < n ? row[p0 + lane] : -1;
+        const int at = p0 + lane < n ? page_index(entry, a.num_hot, a.num_cold) : -1;
+        s_keys[p0 + lane] = score_pages<D>(q, a.bounds + a.layer * a.layer_stride, a, g, at, lane, [] {});
+    }
+    __syncthreads();
+    pick_pages<kShortThreads, kShortKeys>(a, b, g, n, s_keys);
 }
 
 // ---------------------------------------------------------------------------
@@ -995,12 +1050,23 @@ hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t 
     return hipGetLastError();
 }
 
+bool select_in_one(int64_t pt_stride) { return pt_stride <= kShortThreads * kShortKeys; }
+
 hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hipStream_t s, const LaunchEvents& ev,
                                const LaunchEvents& ev_pick) {
     void* args[] = {const_cast<SelectArgs*>(&a)};
+    if (select_in_one(a.pt_stride)) {
+        const void* k = dtype == kDtypeBf16
+                            ? (head_dim == 128 ? reinterpret_cast<const void*>(&page_select_kernel<128, true>)
+                                               : reinterpret_cast<const void*>(&page_select_kernel<64, true>))
+                            : (head_dim == 128 ? reinterpret_cast<const void*>(&page_select_kernel<128, false>)
+                                               : reinterpret_cast<const void*>(&page_select_kernel<64, false>));
+        return launch_kernel(k, dim3(static_cast<unsigned>(a.num_kv_heads), static_cast<unsigned>(a.batch)),
+                             dim3(kShortThreads), args, 0, s, ev_pick);
+    }
     if (a.pt_stride > a.width) {   // else no row has pages to choose from
         const int pages = kWave * wave_split(a.num_kv_heads).slices;   // of a block and turn
-        int64_t gx = (4096 + a.batch - 1) / a.batch;
+        int64_t gx = (1024 + a.batch - 1) / a.batch;
         gx = std::min<int64_t>(gx, (a.pt_stride + pages - 1) / pages);
         const void* k = dtype == kDtypeBf16
                             ? (head_dim == 128 ? reinterpret_cast<const void*>(&page_scores_kernel<128, true>)
@@ -1013,12 +1079,9 @@ hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hip
     }
     const void* k;
     unsigned threads;
-    if (a.pt_stride <= 1024) {
-        k = reinterpret_cast<const void*>(&page_pick_kernel<256, 4>);
-        threads = 256;
-    } else if (a.pt_stride <= 4096) {
-        k = reinterpret_cast<const void*>(&page_pick_kernel<512, 8>);
-        threads = 512;
+    if (a.pt_stride <= 4096) {
+        k = reinterpret_cast<const void*>(&page_pick_kernel<1024, 4>);
+        threads = 1024;
     } else if (a.pt_stride <= 16384) {
         k = reinterpret_cast<const void*>(&page_pick_kernel<1024, 16>);
         threads = 1024;

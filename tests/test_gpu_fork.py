@@ -41,7 +41,7 @@ def test_branches_hold_the_parents_tokens(hkv, d, dtype):
                        .transpose(0, 1)[torch.tensor(rest, device="cuda")].reshape(len(rest), -1))
 
 
-@pytest.mark.parametrize("branches", [1, 13, 14, 15, 29])
+@pytest.mark.parametrize("branches", [1, 6, 7, 8, 13, 15, 29])
 def test_many_branches_of_one_session(branches):
     """Both sides of how many pages one read serves, and of what fits the kernel's arguments."""
     for n in (40, 16 * 30):

@@ -139,7 +139,8 @@ def test_picks_match_the_definition(hq, hkv, d, dtype, width, first, recent):
     picks_of(s, q, lens, width, first, recent, choices(s, q, lens, width, first, recent))
 
 
-@pytest.mark.parametrize("tokens,stride", [(16 * 1024, 1024), (16 * 1025, 1025), (16 * 5000, 5000), (70001, 20000)])
+@pytest.mark.parametrize("tokens,stride", [(16 * 512, 512), (16 * 1024, 1024), (16 * 1025, 1025), (16 * 4096, 4096), (16 * 5000, 5000),
+                                           (70001, 20000)])
 def test_long_rows(tokens, stride):
     """Both sides of every size at which the choice holds its keys in another way."""
     s = Sessions([tokens, 40], 2, 1, 64, "bf16", seed=8, stride=stride)

@@ -167,6 +167,19 @@ def test_many_rows():
     check(call(s, q, lens, lists, 8), *reference(s, q, lens, lists))
 
 
+@pytest.mark.parametrize("lens,hkv,width", [([9000], 1, 16), ([9000], 1, 17), ([9000], 1, 500), ([9000, 8000], 2, 64),
+                                            ([2000] * 40, 4, 64), ([700] * 70, 4, 32)])
+def test_splits(lens, hkv, width):
+    """Lists in one part, in several, and in as many as there are pages to give away; parts past a
+    short list's end."""
+    s = Sessions(lens, 2 * hkv, hkv, 64, "f32", seed=17)
+    q = s.normal(len(lens), 2 * hkv, 64)
+    lists = random_lists(np.random.default_rng(18), lens, hkv, width)
+    lists[0] = [sorted(np.random.default_rng(g).permutation(pages_for(lens[0]))[:width].tolist()) for g in range(hkv)]
+    lists[-1][0] = lists[-1][0][:1]
+    check(call(s, q, lens, lists, width), *reference(s, q, lens, lists))
+
+
 def test_results_do_not_depend_on_where_pages_sit():
     lens = [3000]
     outs = []
