@@ -22,6 +22,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <cmath>
 
 namespace hck {
 namespace {
@@ -1093,14 +1094,29 @@ hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hip
                          args, 0, s, ev_pick);
 }
 
+// Parts of a list.  More parts mean fewer pages one after the other in a wave, but a second
+// kernel that joins them; past one workgroup a CU they gain nothing (their number is a power of
+// two, or the most that gives every CU one).  The time of each choice, in 10 ns and without what
+// they share, is taken as
+//   - a wave's pages, each 0.15 us and 0.45 more per 4 KiB of K, and all bytes at 6.6 TB/s, joined
+//     as the legs of a right angle: the one hides behind the other, but not whole;
+//   - with several parts 1.8 us for the second kernel, 0.05 a part and 0.007 a list.
+// Of 1, 2, 4, .. 32 parts of 54 calls (1 to 64 rows, 16 to 512 pages a list, 4 and 16 KV heads, bf16 and
+// float32) this takes the fastest or one within 5%.  32 lists of 32 pages 8.5 us a call, in one
+// part 9.2; 4 of 512 pages 11.3 in 32 parts, in one 77.6, in 64 12.6; 16 of 512 16.9 in 16, 18.7
+// in 8; 128 of 64 15.8 in one, 16.9 in two.
 int32_t sparse_parts(int cus, int batch, int num_kv_heads, int64_t tile_bytes, int width) {
     const int64_t lists = std::max<int64_t>(static_cast<int64_t>(batch) * num_kv_heads, 1);
-    const int64_t most = std::min<int64_t>((cus + lists - 1) / lists, (width + kBlockWaves - 1) / kBlockWaves);
-    int64_t best = 1, cost = -1;
+    const int64_t most = std::min<int64_t>(std::max<int64_t>(cus / lists, 1), (width + kBlockWaves - 1) / kBlockWaves);
+    const double all = static_cast<double>(lists) * width * 2 * tile_bytes / 66000;
+    const double page = 15 + 45 * static_cast<double>(tile_bytes) / 4096;
+    int64_t best = 1;
+    double cost = 0;
     for (int64_t parts = 1; parts <= most; parts = parts < most && 2 * parts > most ? most : 2 * parts) {
-        const int64_t pages = (width + parts * kBlockWaves - 1) / (parts * kBlockWaves);
-        const int64_t c = 45 * pages * tile_bytes / 4096 + (parts > 1 ? 150 + 5 * parts : 0);
-        if (cost < 0 || c < cost) {
+        const double wave = page * static_cast<double>((width + parts * kBlockWaves - 1) / (parts * kBlockWaves));
+        const double c = std::sqrt(wave * wave + all * all) +
+                         (parts > 1 ? 180 + 5 * static_cast<double>(parts) + 0.67 * static_cast<double>(lists) : 0);
+        if (parts == 1 || c < cost) {
             best = parts;
             cost = c;
         }
