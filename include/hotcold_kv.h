@@ -900,7 +900,9 @@ int paged_tree_attention(kv_pool* pool, int32_t layer, const void* q, const void
  *   least kv_bounds_bytes; NULL: keep none).  What the buffer holds are the bounds: zeros, or
  *   anything else, until kv_update_bounds has set them.  From then on every copy of a page
  *   between the pools and to a branch (resume, eviction, promotion, kv_fork_sessions) takes
- *   the page's bounds along.  No work of the pool may be running.
+ *   the page's bounds along.  Pages handed to a new session, and cold pages that
+ *   kv_session_import_cold names, have what they had before.  No work of the pool may be
+ *   running.
  *   KV_ERR_INVALID (alignment, size, metadata-only pool).
  */
 size_t kv_bounds_bytes(const kv_pool_desc* desc);

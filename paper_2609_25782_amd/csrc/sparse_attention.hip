@@ -13,6 +13,23 @@
 //
 // Records.  A page's record of one layer is [KV head][lo: D bytes, hi: D bytes], then 16
 // bytes of which byte h is the power of head h: 1/31 of the page's K and V in bfloat16.
+//
+// What bounds them (bf16, 32 query and 4 KV heads of 128 dims, a layer of 32 sessions of 8K-32K
+// tokens on shuffled pages, unless said; the card reads 7.0 TB/s):
+//   bounds     693 MB of keys in 143 us (4.85 TB/s).  Without its stores 100 us (6.6 TB/s): 44 MB
+//              written as records of 1 KB all over the buffer cost as much as 200 MB read, with
+//              pages in order a fifth less.  What did not help: nontemporal or write-through
+//              stores, records of whole lines, sixteen results held and written together
+//              (140 us).  One new token of 8 sessions in 48 layers 5.9 us, a chain of loads
+//              (length, page id, keys).
+//   read back  173 MB of float32 values in 36 us, 6.0 TB/s of reads and writes.
+//   scores     44 MB of records in 12 us, of them 2.4 until the first records are asked for; 1.15
+//              times the records' bytes are fetched (they are no whole lines).
+//   choice     5.2 us, latencies: of its keys, and of two or three rounds of bins at three
+//              barriers each.  Bit by bit (up to 32 rounds) it took 13.4.
+//   attention  135 MB in 23 us and 4 us for the join; 64 sessions of 512 pages a head (1.08 GB) 161 us,
+//              6.7 TB/s.  8 sessions of 2K tokens, 32 pages a head: 5.7 us and the join: of a
+//              block's 5 us the length, the list and the page ids take 1.7, the first page 2.5.
 
 #include "device_common.h"
 #include "kernels.h"
@@ -141,14 +158,18 @@ struct Extremes {
     }
 };
 
-#ifndef HCK_BOUNDS_BLOCKS
-#define HCK_BOUNDS_BLOCKS 4096
-#endif
+// Blocks of a bounds call, over rows and layers.  Few rows with few new pages each want few
+// blocks that find nothing to do, many long rows want many: of one token of 8 sessions in 48 layers,
+// turns of 64-1,024 tokens of 8 sessions, and all pages of 32 sessions (each with reading back)
+// 2,048 blocks take 8.1, 9.7 and 180 us, 4,096 8.8, 8.6 and 178, 16,384 12.7, 11.4 and 172.
+constexpr int64_t kBoundsBlocks = 4096;
 
 // One wave takes a (page, KV head) at a time: the K tile is loaded in its own order, whole lines a
 // load, and goes through LDS, from where lane l reads word l of every token (and word l + 64 where a
 // token has 128; where it has 32 the lower lanes read tokens 0 .. 7 and the upper ones the rest).  A
-// group of 16 tokens' 16 bytes takes 272 bytes there: neither side meets a bank twice.
+// group of 16 tokens' 16 bytes takes 272 bytes there: neither side meets a bank twice.  Loaded
+// straight into the lanes that reduce them, every line was fetched two to four times: 655 MB of
+// keys 158 us, now 131, in float32 226, now 121.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const BoundsUpdateArgs a) {
     constexpr int kElt = BF16 ? 2 : 4;
@@ -333,12 +354,12 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_copy_kernel(const PoolGe
 // ---------------------------------------------------------------------------
 // Scores of pages.
 
-// Tables of up to kShortThreads * kShortKeys pages a row take scores and choice in one kernel.
+// Tables of up to this many pages a row take scores and choice in one kernel, a block per list: one
+// kernel fewer, but a list's records are read by one CU and without the other heads'.  4 rows
+// of 57 pages 4.2 us, in two kernels 7.2; 1, 16, 64 and 256 rows of 512 pages 7.2, 9.0, 13.5 and 41,
+// in two 9.5, 10.4, 14.3 and 45.  With two turns a wave, 16 and 64 rows of 1,024 pages 13.7 and
+// 23.4 us, in two kernels 11.8 and 20.1.
 constexpr int kShortThreads = 512;
-#ifndef HCK_SHORT_KEYS
-#define HCK_SHORT_KEYS 1
-#endif
-constexpr int kShortKeys = HCK_SHORT_KEYS;
 
 constexpr unsigned kKeyBad = 0xFFFFFFFEu;  // above every score: a page that no pool holds
 
@@ -711,22 +732,22 @@ __global__ __launch_bounds__(kShortThreads) void page_select_kernel(const Select
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = uniform(threadIdx.x / kWave);
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.pt_stride;
-    int entry = wave * kWave + lane < a.pt_stride ? row[wave * kWave + lane] : -1;   // does not wait for the length
+    const int page = wave * kWave + lane;
+    const int entry = page < a.pt_stride ? row[page] : -1;   // does not wait for the length
     QueryBits<D, BF16> bits;
     load_query_bits<D, BF16>(bits, a, b, g, lane);
     bool choose;
     const int n = row_to_pick<kShortThreads>(a, b, g, choose);
     if (!choose) return;
-    __shared__ unsigned s_keys[kShortThreads * kShortKeys];
+    __shared__ unsigned s_keys[kShortThreads];
     QueryRows<D> q;
     round_queries<D, BF16>(q, bits, a.group, lane);
-    for (int p0 = wave * kWave; p0 < n; p0 += kShortThreads) {
-        if (p0 != wave * kWave) entry = p0 + lane < n ? row[p0 + lane] : -1;
-        const int at = p0 + lane < n ? page_index(entry, a.num_hot, a.num_cold) : -1;
-        s_keys[p0 + lane] = score_pages<D>(q, a.bounds + a.layer * a.layer_stride, a, g, at, lane, [] {});
+    if (wave * kWave < n) {
+        const int at = page < n ? page_index(entry, a.num_hot, a.num_cold) : -1;
+        s_keys[page] = score_pages<D>(q, a.bounds + a.layer * a.layer_stride, a, g, at, lane, [] {});
     }
     __syncthreads();
-    pick_pages<kShortThreads, kShortKeys>(a, b, g, n, s_keys);
+    pick_pages<kShortThreads, 1>(a, b, g, n, s_keys);
 }
 
 // ---------------------------------------------------------------------------
@@ -800,6 +821,10 @@ __device__ __forceinline__ void sparse_page(SparseState<D, BF16>& st, PageRegs<D
 // it ends in 0 / 0; a list without tokens keeps minus infinity and ends in zeros.
 constexpr float kNoScore = -FLT_MAX;
 
+// Floats of a head's row where a block's waves meet in LDS: rows start in different banks.
+template <int D>
+constexpr int kJoinPitch = D + 4;
+
 template <int D, bool BF16>
 __device__ __forceinline__ void store_result(const SparseArgs& a, int64_t head_row, int quad, float M, float den,
                                              const f32x4& acc, bool invalid) {
@@ -819,8 +844,10 @@ __device__ __forceinline__ void store_result(const SparseArgs& a, int64_t head_r
 }
 
 // Block (s, g, b): part s of row b's list for KV head g, shared by the block's waves and joined
-// in LDS.  With one part the block writes the output, else a
-// partial result.
+// in LDS.  With one part the block writes the output, else a partial result.  A wave holds two
+// pages, the one computed and the next: 8 sessions of 32 and 32 of 128 pages a head 8.3 and 27.1
+// us a call, with three 8.9 and 28.2, four 9.7 and 28.0; eight waves a block, three pages held,
+// 11.1 and 27.8.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlockThreads) void sparse_split_kernel(const SparseArgs a) {
     using S = Shape<D, BF16>;
@@ -919,13 +946,13 @@ __global__ __launch_bounds__(kBlockThreads) void sparse_split_kernel(const Spars
     if (bad) l = __builtin_nanf("");
     float m = st.m == -INFINITY && seen ? kNoScore : st.m;
 
-    // the waves' results meet in LDS: [wave][head][D], then [wave][max, sum][head]
+    // the waves' results meet in LDS: [wave][head][kJoinPitch], then [wave][max, sum][head]
     extern __shared__ __align__(16) char s_mem[];
     float* s_o = reinterpret_cast<float*>(s_mem);
-    float* s_ml = s_o + kBlockWaves * a.group * D;
+    float* s_ml = s_o + kBlockWaves * a.group * kJoinPitch<D>;
     const int h = lane & 15;
     if (h < a.group) {
-        float* o = s_o + (wave * a.group + h) * D + 4 * qg;
+        float* o = s_o + (wave * a.group + h) * kJoinPitch<D> + 4 * qg;
 #pragma unroll
         for (int c = 0; c < S::kChunks; ++c) *reinterpret_cast<f32x4*>(o + 16 * c) = st.o[c];
         if (qg == 0) {
@@ -941,7 +968,7 @@ __global__ __launch_bounds__(kBlockThreads) void sparse_split_kernel(const Spars
 #pragma unroll
         for (int w = 0; w < kBlockWaves; ++w)
             lse_merge(M, den, acc, s_ml[w * 2 * a.group + hh], s_ml[w * 2 * a.group + a.group + hh],
-                      *reinterpret_cast<const f32x4*>(s_o + (w * a.group + hh) * D + 4 * quad));
+                      *reinterpret_cast<const f32x4*>(s_o + (w * a.group + hh) * kJoinPitch<D> + 4 * quad));
         if (a.parts == 1) {
             store_result<D, BF16>(a, seg * a.group + hh, quad, M, den, acc, invalid);
         } else {
@@ -1000,7 +1027,7 @@ __global__ __launch_bounds__(kBlockThreads) void sparse_merge_kernel(const Spars
 
 template <int D, bool BF16>
 hipError_t launch_sparse_for(const SparseArgs& a, hipStream_t s, const LaunchEvents& ev, const LaunchEvents& ev_merge) {
-    const size_t lds = static_cast<size_t>(kBlockWaves) * a.group * (D + 2) * sizeof(float);
+    const size_t lds = static_cast<size_t>(kBlockWaves) * a.group * (kJoinPitch<D> + 2) * sizeof(float);
     void* args[] = {const_cast<SparseArgs*>(&a)};
     const dim3 grid(static_cast<unsigned>(a.parts), static_cast<unsigned>(a.num_kv_heads), static_cast<unsigned>(a.batch));
     hipError_t e = launch_kernel(reinterpret_cast<const void*>(&sparse_split_kernel<D, BF16>), grid, dim3(kBlockThreads),
@@ -1019,7 +1046,7 @@ hipError_t launch_bounds_update(const BoundsUpdateArgs& a, int head_dim, int dty
     // enough blocks for the GPU however few rows there are, no more than the longest row has units
     const int slices = wave_split(a.num_kv_heads).slices;
     const int64_t rows = static_cast<int64_t>(a.batch) * num_layers;
-    int64_t gx = (HCK_BOUNDS_BLOCKS + rows - 1) / rows;
+    int64_t gx = (kBoundsBlocks + rows - 1) / rows;
     gx = std::min<int64_t>(gx, (a.pt_stride + slices - 1) / slices);
     const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>(a.batch), static_cast<unsigned>(num_layers));
     const void* k = dtype == kDtypeBf16
@@ -1051,7 +1078,7 @@ hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t 
     return hipGetLastError();
 }
 
-bool select_in_one(int64_t pt_stride) { return pt_stride <= kShortThreads * kShortKeys; }
+bool select_in_one(int64_t pt_stride) { return pt_stride <= kShortThreads; }
 
 hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hipStream_t s, const LaunchEvents& ev,
                                const LaunchEvents& ev_pick) {
@@ -1067,6 +1094,8 @@ hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hip
     }
     if (a.pt_stride > a.width) {   // else no row has pages to choose from
         const int pages = kWave * wave_split(a.num_kv_heads).slices;   // of a block and turn
+        // 1,024 blocks are resident at once, so waves go on to further pages with their queries
+        // rounded (64 rows of 4,096 pages 68 us a call, with 4,096 blocks 71)
         int64_t gx = (1024 + a.batch - 1) / a.batch;
         gx = std::min<int64_t>(gx, (a.pt_stride + pages - 1) / pages);
         const void* k = dtype == kDtypeBf16
@@ -1080,6 +1109,8 @@ hipError_t launch_select_pages(const SelectArgs& a, int head_dim, int dtype, hip
     }
     const void* k;
     unsigned threads;
+    // The keys are held in registers, as many as the table's rows may have; read again in every
+    // round, 32 rows of 8K-32K tokens take 19.2 us a call instead of 17.7, 4 of 250K 42 instead of 26.
     if (a.pt_stride <= 4096) {
         k = reinterpret_cast<const void*>(&page_pick_kernel<1024, 4>);
         threads = 1024;
