@@ -849,7 +849,7 @@ __device__ __forceinline__ void store_result(const SparseArgs& a, int64_t head_r
 // us a call, with three 8.9 and 28.2, four 9.7 and 28.0; eight waves a block, three pages held,
 // 11.1 and 27.8.
 template <int D, bool BF16>
-__global__ __launch_bounds__(kBlockThreads) void sparse_split_kernel(const SparseArgs a) {
+__global__ __launch_bounds__(kBlockThreads, BF16 ? 3 : 2) void sparse_split_kernel(const SparseArgs a) {
     using S = Shape<D, BF16>;
     constexpr int R = 2;   // pages held: the one computed and the next
     const int part = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
