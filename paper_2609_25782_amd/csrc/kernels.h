@@ -392,9 +392,9 @@ struct BoundsReadArgs {
     float* out;
 };
 hipError_t launch_bounds_read(const BoundsReadArgs& a, int32_t num_layers, hipStream_t s);
-// Records that follow copied pages (n entries on the device; page-table fields are not used).
+// Records that follow copied pages (entries as launch_page_copy's; page-table fields are not used).
 hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t record, int32_t layers,
-                              const CopyEntry* entries, int32_t n, hipStream_t s);
+                              const CopyEntry* entries, bool on_host, int32_t n, hipStream_t s);
 
 // The choice of pages for decode attention.
 struct SelectArgs {

@@ -389,9 +389,17 @@ struct kv_pool {
     // Cold pages that page-table entries may name.
     int32_t named_cold() const { return cold && tiered() ? d.num_cold_pages : 0; }
 
+    int launch_records(const hck::PoolGeom& src, const hck::PoolGeom& dst, const hck::CopyEntry* entries, bool on_host,
+                       int32_t n, hipStream_t s) const {
+        const hipError_t e = hck::launch_bounds_copy(src, dst, bounds_record(), d.num_layers, entries, on_host, n, s);
+        return e == hipSuccess ? KV_OK : hip_fail(e, "bounds copy launch");
+    }
+
     // The records of copied pages, after the copies.
     int submit_bounds_copies(const hck::PoolGeom& src, const hck::PoolGeom& dst,
                              const std::vector<hck::CopyEntry>& copies, hipStream_t s) {
+        if (!copies.empty() && copies.size() <= static_cast<size_t>(hck::kCopyInline))
+            return launch_records(src, dst, copies.data(), /*on_host=*/true, static_cast<int32_t>(copies.size()), s);
         for (size_t off = 0; off < copies.size(); off += kStagingEntries) {
             const int32_t n = static_cast<int32_t>(std::min<size_t>(kStagingEntries, copies.size() - off));
             StagingSlot* slot;
@@ -399,11 +407,9 @@ struct kv_pool {
             if (rc) return rc;
             std::memcpy(slot->host, copies.data() + off, n * sizeof(hck::CopyEntry));
             hipError_t e = hck::launch_upload(slot->mapped, slot->dev, n * sizeof(hck::CopyEntry), s);
-            if (e == hipSuccess)
-                e = hck::launch_bounds_copy(src, dst, bounds_record(), d.num_layers,
-                                            static_cast<const hck::CopyEntry*>(slot->dev), n, s);
-            if (e != hipSuccess) return hip_fail(e, "bounds copy launch");
-            rc = release_slot(slot, s);
+            if (e != hipSuccess) return hip_fail(e, "bounds copy list upload");
+            rc = launch_records(src, dst, static_cast<const hck::CopyEntry*>(slot->dev), /*on_host=*/false, n, s);
+            if (!rc) rc = release_slot(slot, s);
             if (rc) return rc;
         }
         return KV_OK;
@@ -438,27 +444,24 @@ struct kv_pool {
         return KV_OK;
     }
 
-    // Whole-page copies between the pools, and their records where the pool keeps bounds.
-    int submit_copies(bool to_hot, const std::vector<hck::CopyEntry>& copies,
-                      const std::vector<hck::CopyEntry>& writes, hipStream_t s, int kernel_id) {
-        const int rc = submit_page_copies(to_hot, copies, writes, s, kernel_id);
-        if (rc || !bounds || copies.empty()) return rc;
-        return to_hot ? submit_bounds_copies(bounds_cold, bounds_hot, copies, s)
-                      : submit_bounds_copies(bounds_hot, bounds_cold, copies, s);
-    }
-
     // Enqueue whole-page copies between the pools (in chunks that fit a
     // staging slot): cold -> hot when to_hot, else hot -> cold.  `writes` are
     // page-table entries without a copy (rows cleared on eviction, resident
     // pages remapped on resume): they go to the table-write kernel, so the copy
     // grid only walks pages that move.
-    int submit_page_copies(bool to_hot, const std::vector<hck::CopyEntry>& copies,
-                           const std::vector<hck::CopyEntry>& writes, hipStream_t s, int kernel_id) {
+    int submit_copies(bool to_hot, const std::vector<hck::CopyEntry>& copies,
+                      const std::vector<hck::CopyEntry>& writes, hipStream_t s, int kernel_id) {
         if (!writes.empty()) {
             int rc = submit_table_writes(writes, s);
             if (rc) return rc;
         }
-        if (cold_host && host_copy == KV_HOST_COPY_DMA) return submit_dma_copies(to_hot, copies, s, kernel_id);
+        // the pages' key bounds go along, from the same lists
+        const hck::PoolGeom& rec_src = to_hot ? bounds_cold : bounds_hot;
+        const hck::PoolGeom& rec_dst = to_hot ? bounds_hot : bounds_cold;
+        if (cold_host && host_copy == KV_HOST_COPY_DMA) {
+            const int rc = submit_dma_copies(to_hot, copies, s, kernel_id);
+            return rc || !bounds ? rc : submit_bounds_copies(rec_src, rec_dst, copies, s);
+        }
         const hck::PoolGeom& src = to_hot ? cold_geom : hot_geom;
         const hck::PoolGeom& dst = to_hot ? hot_geom : cold_geom;
         if (!copies.empty() && copies.size() <= static_cast<size_t>(hck::kCopyInline)) {
@@ -467,7 +470,9 @@ struct kv_pool {
                                                  copies.data(), /*on_host=*/true, static_cast<int32_t>(copies.size()),
                                                  pt, copy_blocks, s, ev);
             prof_done(kernel_id, ev, e);
-            return e == hipSuccess ? KV_OK : hip_fail(e, "page copy launch");
+            if (e != hipSuccess) return hip_fail(e, "page copy launch");
+            return bounds ? launch_records(rec_src, rec_dst, copies.data(), /*on_host=*/true,
+                                           static_cast<int32_t>(copies.size()), s) : KV_OK;
         }
         for (size_t off = 0; off < copies.size(); off += kStagingEntries) {
             const int32_t n = static_cast<int32_t>(std::min<size_t>(kStagingEntries, copies.size() - off));
@@ -478,7 +483,7 @@ struct kv_pool {
             hipError_t e = hck::launch_upload(slot->mapped, slot->dev, n * sizeof(hck::CopyEntry), s);
             if (e != hipSuccess) return hip_fail(e, "copy list upload");
             hck::LaunchEvents ev = prof_events();
-            const bool own_event = !ev.start && plain_stream(s);
+            const bool own_event = !ev.start && !bounds && plain_stream(s);
             if (own_event) ev.stop = slot->done;  // recorded by the copy's own dispatch
             e = hck::launch_page_copy(src, dst, slice_bytes, d.num_layers, /*by_layer=*/!to_hot,
                                       static_cast<const hck::CopyEntry*>(slot->dev), /*on_host=*/false, n, pt,
@@ -489,7 +494,9 @@ struct kv_pool {
                 slot->pending = true;
                 continue;
             }
-            rc = release_slot(slot, s);
+            if (bounds)
+                rc = launch_records(rec_src, rec_dst, static_cast<const hck::CopyEntry*>(slot->dev), /*on_host=*/false, n, s);
+            if (!rc) rc = release_slot(slot, s);
             if (rc) return rc;
         }
         return KV_OK;

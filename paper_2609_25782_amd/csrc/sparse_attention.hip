@@ -335,20 +335,36 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_read_kernel(const Bounds
 }
 
 // Records of copied pages: entry e's from page e.src of one pool to page e.dst of the other.
-__global__ __launch_bounds__(kBlockThreads) void bounds_copy_kernel(const PoolGeom src, const PoolGeom dst,
-                                                                    const CopyEntry* __restrict__ entries, int32_t n,
-                                                                    int words) {
+template <typename Entries>
+__device__ __forceinline__ void copy_records(const PoolGeom& src, const PoolGeom& dst, const Entries& entries, int32_t n,
+                                             int words) {
     const int layer = static_cast<int>(blockIdx.y);
     const int64_t total = static_cast<int64_t>(n) * words;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlockThreads + threadIdx.x; i < total;
          i += static_cast<int64_t>(gridDim.x) * kBlockThreads) {
-        const int64_t k = i / words;
-        const int word = static_cast<int>(i - k * words);
+        const int k = static_cast<int>(i / words);
+        const int word = static_cast<int>(i - static_cast<int64_t>(k) * words);
         const CopyEntry e = entries[k];
         if (e.src < 0) continue;
         reinterpret_cast<u32x4*>(slice_at(dst, e.dst, layer))[word] =
             reinterpret_cast<const u32x4*>(slice_at(src, e.src, layer))[word];
     }
+}
+
+__global__ __launch_bounds__(kBlockThreads) void bounds_copy_kernel(const PoolGeom src, const PoolGeom dst,
+                                                                    const CopyEntry* __restrict__ entries, int32_t n,
+                                                                    int words) {
+    copy_records(src, dst, entries, n, words);
+}
+
+// The same for a list in the kernel arguments.
+struct RecordList {
+    CopyEntry e[kCopyInline];
+    __device__ const CopyEntry& operator[](int i) const { return e[i]; }
+};
+__global__ __launch_bounds__(kBlockThreads) void bounds_copy_inline_kernel(const PoolGeom src, const PoolGeom dst,
+                                                                           int32_t n, int words, const RecordList list) {
+    copy_records(src, dst, list, n, words);
 }
 
 // ---------------------------------------------------------------------------
@@ -1069,12 +1085,19 @@ hipError_t launch_bounds_read(const BoundsReadArgs& a, int32_t num_layers, hipSt
 }
 
 hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t record, int32_t layers,
-                              const CopyEntry* entries, int32_t n, hipStream_t s) {
+                              const CopyEntry* entries, bool on_host, int32_t n, hipStream_t s) {
     if (n <= 0) return hipSuccess;
+    if (on_host && n > kCopyInline) return hipErrorInvalidValue;
     const int words = record / 16;
     const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(n) * words + kBlockThreads - 1) / kBlockThreads, 65536);
-    hipLaunchKernelGGL(bounds_copy_kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(layers)),
-                       dim3(kBlockThreads), 0, s, src, dst, entries, n, words);
+    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(layers));
+    if (on_host) {
+        RecordList list = {};
+        for (int32_t i = 0; i < n; ++i) list.e[i] = entries[i];
+        hipLaunchKernelGGL(bounds_copy_inline_kernel, grid, dim3(kBlockThreads), 0, s, src, dst, n, words, list);
+    } else {
+        hipLaunchKernelGGL(bounds_copy_kernel, grid, dim3(kBlockThreads), 0, s, src, dst, entries, n, words);
+    }
     return hipGetLastError();
 }
 

@@ -228,6 +228,55 @@ def test_bounds_go_with_evicted_and_resumed_pages():
         p.destroy_session(other)
 
 
+@pytest.mark.parametrize("pages", [100, 128, 129, 300])
+def test_bounds_go_with_lists_of_any_length(pages):
+    """Copy lists in the kernels' arguments and uploaded ones, with and without profiling events."""
+    n = 16 * pages
+    s = Sessions([n], 4, 2, 64, "bf16", seed=18, cold=pages, spare=pages, max_sessions=2)
+    p = s.pool
+    p.set_bounds(True)
+    lens = i32([n])
+    p.update_bounds(0, 1, lens)
+    want = read(s, 0)
+    for prof in (False, True):
+        kv.kv_pool_set_profiling(p.handle, prof)
+        p.evict(0)
+        p.key_bounds(0, 1, i32([0]))
+        other = p.create_session(16 * 7)        # other pages for the resume
+        p.resume(0)
+        s.pages = [p.info(0)[2]]
+        assert np.array_equal(read(s, 0), want)
+        p.write_tokens_layers(0, 0, 0, s.k[0].cuda(), s.v[0].cuda())     # so that the next eviction copies again
+        p.destroy_session(other)
+
+
+def test_bounds_go_with_a_captured_eviction():
+    """Replays after other calls have used the pool's copy lists move the same records."""
+    s = Sessions([200, 300, 100], 4, 2, 64, "bf16", seed=19, cold=60, max_sessions=6, spare=60)
+    p = s.pool
+    p.set_bounds(True)
+    lens = i32([200, 300, 100])
+    p.update_bounds(0, 1, lens)
+    want = read(s, 1)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        p.evict(1, stream=st)
+    cold = i32([c | kv.KV_PAGE_COLD for c in p.info(1)[3]])
+    saved = p.bounds.clone()
+    for turn in range(3):
+        p.bounds.copy_(saved)               # the session's old pages are free: resumes below may take them
+        p.bounds.view(-1)[p.num_hot_pages * (2 * 2 * 64 + 16):] = 0
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(p.key_bounds(0, 1, cold).cpu().double().numpy(), want), turn
+        p.evict(0), p.resume(0)                 # eager calls between the replays
+        p.evict(2), p.resume(2)
+        torch.cuda.synchronize()
+
+
 def test_spilled_pages_have_bounds():
     s = Sessions([200], 8, 2, 64, "bf16", seed=14, cold=40)
     p = s.pool
