@@ -902,7 +902,7 @@ int paged_tree_attention(kv_pool* pool, int32_t layer, const void* q, const void
  *   between the pools and to a branch (resume, eviction, promotion, kv_fork_sessions) takes
  *   the page's bounds along.  Pages handed to a new session, and cold pages that
  *   kv_session_import_cold names, have what they had before.  No work of the pool may be
- *   running.
+ *   running, and calls captured into a HIP graph keep the buffer that they were captured with.
  *   KV_ERR_INVALID (alignment, size, metadata-only pool).
  */
 size_t kv_bounds_bytes(const kv_pool_desc* desc);

@@ -363,7 +363,8 @@ class HotColdPool:
 
     # -- decode over picked pages ---------------------------------------------
     def set_bounds(self, enable: bool) -> None:
-        """Keep key bounds of every page (kv_bounds_bytes of device memory, zeros at first), or none."""
+        """Keep key bounds of every page (kv_bounds_bytes of device memory, zeros at first), or none.  A graph
+        that holds calls captured before is not to be replayed after it: the memory it names is released."""
         torch.cuda.synchronize(self.device)
         bounds = None
         if enable:

@@ -7,7 +7,7 @@ import torch
 
 from chunk_reference import Sessions, check, i32, pages_for
 from paper_2609_25782_amd import hotcold_kv as kv
-from sparse_reference import attend_pages, choose, page_bounds, scores
+from sparse_reference import attend_pages, choose, page_bounds, scores, values
 
 pytestmark = pytest.mark.gpu
 
@@ -283,6 +283,54 @@ def test_captured_steps():
             check(out, *ref, "turn %d" % turn)
         assert torch.equal(run(), outs[0])
         torch.cuda.synchronize()
+
+
+def test_profiling_counts_the_kernels():
+    s = Sessions([9000, 300], 4, 1, 64, "bf16", seed=21, spare=40, max_sessions=4)
+    p, q = s.pool, s.normal(2, 4, 64).cuda()
+    lens = i32(s.lens)
+    p.set_bounds(True)
+    kv.kv_pool_set_profiling(p.handle, True)
+    p.update_bounds(0, 1, lens)
+    picks, counts = p.select_pages(0, q, lens, 40)                                  # a table of over 512 pages a row
+    p.select_pages(0, q, i32([300, 300]), 4, page_table=p.page_table[1].repeat(2, 1)[:, :30].contiguous())
+    p.sparse_decode(0, q, lens, picks, counts)                                      # in parts
+    p.sparse_decode(0, q, lens, picks[:, :, :4].contiguous())                       # in one
+    p.fork([1, 1], [300, 20])
+    torch.cuda.synchronize()
+    for kernel, launches in ((kv.KV_KERNEL_BOUNDS, 1), (kv.KV_KERNEL_PAGE_SCORES, 1), (kv.KV_KERNEL_PAGE_PICK, 2),
+                             (kv.KV_KERNEL_SPARSE, 2), (kv.KV_KERNEL_SPARSE_MERGE, 1), (kv.KV_KERNEL_FORK_COPY, 1)):
+        n, ms = kv.kv_pool_profile_read(p.handle, kernel)
+        assert n == launches and ms > 0, (kernel, n)
+
+
+def test_pages_and_records_past_32_bits():
+    """A row on the last pages of a pool of 71 GB, whose records lie past 2 GiB as well."""
+    from paper_2609_25782_amd.pool import HotColdPool
+    hkv, d, n, pages = 16, 128, 330, 540_000
+    assert pages * (hkv * 2 * d + 16) > 2 ** 31
+    p = HotColdPool(1, hkv, d, "bf16", pages, 0, 2, 30)
+    p.set_bounds(True)
+    rng = np.random.default_rng(22)
+    row = (pages - 1 - rng.permutation(5000)[:pages_for(n)]).astype(np.int32)
+    row[0] = 0
+    table = torch.from_numpy(np.pad(row, (0, 30 - len(row)), constant_values=-1)[None]).cuda()
+    g = torch.Generator().manual_seed(22)
+    k, v, q = (torch.randn(shape, generator=g).to(torch.bfloat16) for shape in ((n, hkv, d), (n, hkv, d), (1, 32, d)))
+    positions = torch.arange(n, dtype=torch.int32, device="cuda")
+    p.append_tokens_table(0, table, torch.zeros_like(positions), positions, k[None].cuda(), v[None].cuda())
+    lens = i32([n])
+    p.update_bounds(0, 1, lens, page_table=table)
+    lo, hi, e = page_bounds(k, n)
+    got = p.key_bounds(0, 1, i32(row.tolist()))[0].cpu().double().numpy()
+    assert np.array_equal(got, values(lo, hi, e))
+    picks, counts = p.select_pages(0, q.cuda(), lens, 7, page_table=table)
+    want = [choose(list(x), 7, 1, 2) for x in scores(q[0], lo, hi, e)]
+    assert picks[0].tolist() == want
+    out, bound = attend_pages(q[0], k, v, n, want, d ** -0.5, "bf16")
+    check(p.sparse_decode(0, q.cuda(), lens, picks, counts, page_table=table), out[None], bound[None])
+    del p
+    torch.cuda.empty_cache()
 
 
 def test_two_streams_at_once():
