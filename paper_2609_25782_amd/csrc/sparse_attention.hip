@@ -862,8 +862,8 @@ __device__ __forceinline__ void store_result(const SparseArgs& a, int64_t head_r
 // Block (s, g, b): part s of row b's list for KV head g, shared by the block's waves and joined
 // in LDS.  With one part the block writes the output, else a partial result.  A wave holds two
 // pages, the one computed and the next: 8 sessions of 32 and 32 of 128 pages a head 8.3 and 27.1
-// us a call, with three 8.9 and 28.2, four 9.7 and 28.0; eight waves a block, three pages held,
-// 11.1 and 27.8.
+// us a call, with three 8.9 and 28.2, four 9.7 and 28.0; eight waves a block and fewer parts 9.5
+// and 27.6, sixteen with one page each 10.2 and 28.8.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kBlockThreads, BF16 ? 3 : 2) void sparse_split_kernel(const SparseArgs a) {
     using S = Shape<D, BF16>;
