@@ -900,8 +900,12 @@ int paged_tree_attention(kv_pool* pool, int32_t layer, const void* q, const void
  *   least kv_bounds_bytes; NULL: keep none).  What the buffer holds are the bounds: zeros, or
  *   anything else, until kv_update_bounds has set them.  From then on every copy of a page
  *   between the pools and to a branch (resume, eviction, promotion, kv_fork_sessions) takes
- *   the page's bounds along.  Pages handed to a new session, and cold pages that
- *   kv_session_import_cold names, have what they had before.  No work of the pool may be
+ *   the page's bounds along, and an eviction that writes nothing because the page's cold copy
+ *   is valid takes along bounds that were set since that copy was made or read (of sessions that
+ *   share the cold page, one whose bounds are older leaves them as they are there).  Pages
+ *   handed to a new session, and cold pages that kv_session_import_cold names, have what they
+ *   had before.  A call on another stream that reads a shared cold page's bounds is to be
+ *   ordered with the eviction of a session that shares it.  No work of the pool may be
  *   running, and calls captured into a HIP graph keep the buffer that they were captured with.
  *   KV_ERR_INVALID (alignment, size, metadata-only pool).
  */

@@ -367,6 +367,8 @@ hipError_t launch_fork_copy(const PoolGeom& pool, int64_t slice_bytes, int32_t l
 
 // Key bounds of pages.  A record (one page of one layer) is [KV head][lo, hi][head_dim] bytes,
 // then the heads' powers of two in 16 bytes; those of the hot pages come first, then the cold ones.
+// A power takes the low 7 bits of its byte.  The top bit says that the head's bounds were set
+// since the record was last copied from the other tier: the other copy's are older.
 inline int32_t bounds_record_bytes(int num_kv_heads, int head_dim) { return num_kv_heads * 2 * head_dim + 16; }
 struct BoundsUpdateArgs {
     PoolGeom hot, cold;
@@ -392,9 +394,13 @@ struct BoundsReadArgs {
     float* out;
 };
 hipError_t launch_bounds_read(const BoundsReadArgs& a, int32_t num_layers, hipStream_t s);
-// Records that follow copied pages (entries as launch_page_copy's; page-table fields are not used).
-hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t record, int32_t layers,
-                              const CopyEntry* entries, bool on_host, int32_t n, hipStream_t s);
+// Records that follow pages (entries as launch_page_copy's; page-table fields are not used): with pages
+// copied between the tiers, with pages copied inside the hot tier, or from hot pages to their valid cold
+// copies, where only bounds that were set since are written (no two entries then name one cold page).
+enum class RecordCopy : int32_t { kTier, kBranch, kRenewed };
+hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t num_kv_heads, int32_t head_dim,
+                              int32_t layers, const CopyEntry* entries, bool on_host, int32_t n, RecordCopy how,
+                              hipStream_t s);
 
 // The choice of pages for decode attention.
 struct SelectArgs {

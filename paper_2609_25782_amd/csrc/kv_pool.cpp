@@ -19,6 +19,7 @@
 #include <map>
 #include <new>
 #include <string>
+#include <unordered_set>
 #include <vector>
 
 namespace {
@@ -390,16 +391,25 @@ struct kv_pool {
     int32_t named_cold() const { return cold && tiered() ? d.num_cold_pages : 0; }
 
     int launch_records(const hck::PoolGeom& src, const hck::PoolGeom& dst, const hck::CopyEntry* entries, bool on_host,
-                       int32_t n, hipStream_t s) const {
-        const hipError_t e = hck::launch_bounds_copy(src, dst, bounds_record(), d.num_layers, entries, on_host, n, s);
+                       int32_t n, hck::RecordCopy how, hipStream_t s) const {
+        const hipError_t e = hck::launch_bounds_copy(src, dst, d.num_kv_heads, d.head_dim, d.num_layers, entries,
+                                                     on_host, n, how, s);
         return e == hipSuccess ? KV_OK : hip_fail(e, "bounds copy launch");
     }
 
-    // The records of copied pages, after the copies.
+    // The records of pages, after the pages' own copies.  Longer lists too go in the kernel arguments,
+    // in several launches, while the stream is captured: a staging slot holds another list by the replay.
     int submit_bounds_copies(const hck::PoolGeom& src, const hck::PoolGeom& dst,
-                             const std::vector<hck::CopyEntry>& copies, hipStream_t s) {
-        if (!copies.empty() && copies.size() <= static_cast<size_t>(hck::kCopyInline))
-            return launch_records(src, dst, copies.data(), /*on_host=*/true, static_cast<int32_t>(copies.size()), s);
+                             const std::vector<hck::CopyEntry>& copies, hck::RecordCopy how, hipStream_t s) {
+        constexpr size_t kInline = static_cast<size_t>(hck::kCopyInline);
+        if (copies.size() <= kInline || !plain_stream(s)) {
+            for (size_t off = 0; off < copies.size(); off += kInline) {
+                const int32_t n = static_cast<int32_t>(std::min(kInline, copies.size() - off));
+                const int rc = launch_records(src, dst, copies.data() + off, /*on_host=*/true, n, how, s);
+                if (rc) return rc;
+            }
+            return KV_OK;
+        }
         for (size_t off = 0; off < copies.size(); off += kStagingEntries) {
             const int32_t n = static_cast<int32_t>(std::min<size_t>(kStagingEntries, copies.size() - off));
             StagingSlot* slot;
@@ -408,11 +418,28 @@ struct kv_pool {
             std::memcpy(slot->host, copies.data() + off, n * sizeof(hck::CopyEntry));
             hipError_t e = hck::launch_upload(slot->mapped, slot->dev, n * sizeof(hck::CopyEntry), s);
             if (e != hipSuccess) return hip_fail(e, "bounds copy list upload");
-            rc = launch_records(src, dst, static_cast<const hck::CopyEntry*>(slot->dev), /*on_host=*/false, n, s);
+            rc = launch_records(src, dst, static_cast<const hck::CopyEntry*>(slot->dev), /*on_host=*/false, n, how, s);
             if (!rc) rc = release_slot(slot, s);
             if (rc) return rc;
         }
         return KV_OK;
+    }
+
+    // Bounds that were set while a page had a valid cold copy (hot -> cold entries of evicted pages that
+    // are not copied).  Sessions that share cold pages may be evicted together: a launch names each once.
+    int submit_renewed_bounds(const std::vector<hck::CopyEntry>& pages, hipStream_t s) {
+        std::vector<hck::CopyEntry> part;
+        std::unordered_set<int32_t> shared;
+        for (const hck::CopyEntry& e : pages) {
+            if (cold_ref[e.dst] > 1 && !shared.insert(e.dst).second) {
+                const int rc = submit_bounds_copies(bounds_hot, bounds_cold, part, hck::RecordCopy::kRenewed, s);
+                if (rc) return rc;
+                part.clear();
+                shared = {e.dst};
+            }
+            part.push_back(e);
+        }
+        return submit_bounds_copies(bounds_hot, bounds_cold, part, hck::RecordCopy::kRenewed, s);
     }
 
     // Hot pages to the branches' pages (read once for up to kForkDests of them), and their table entries.
@@ -460,7 +487,7 @@ struct kv_pool {
         const hck::PoolGeom& rec_dst = to_hot ? bounds_hot : bounds_cold;
         if (cold_host && host_copy == KV_HOST_COPY_DMA) {
             const int rc = submit_dma_copies(to_hot, copies, s, kernel_id);
-            return rc || !bounds ? rc : submit_bounds_copies(rec_src, rec_dst, copies, s);
+            return rc || !bounds ? rc : submit_bounds_copies(rec_src, rec_dst, copies, hck::RecordCopy::kTier, s);
         }
         const hck::PoolGeom& src = to_hot ? cold_geom : hot_geom;
         const hck::PoolGeom& dst = to_hot ? hot_geom : cold_geom;
@@ -472,7 +499,7 @@ struct kv_pool {
             prof_done(kernel_id, ev, e);
             if (e != hipSuccess) return hip_fail(e, "page copy launch");
             return bounds ? launch_records(rec_src, rec_dst, copies.data(), /*on_host=*/true,
-                                           static_cast<int32_t>(copies.size()), s) : KV_OK;
+                                           static_cast<int32_t>(copies.size()), hck::RecordCopy::kTier, s) : KV_OK;
         }
         for (size_t off = 0; off < copies.size(); off += kStagingEntries) {
             const int32_t n = static_cast<int32_t>(std::min<size_t>(kStagingEntries, copies.size() - off));
@@ -495,7 +522,8 @@ struct kv_pool {
                 continue;
             }
             if (bounds)
-                rc = launch_records(rec_src, rec_dst, static_cast<const hck::CopyEntry*>(slot->dev), /*on_host=*/false, n, s);
+                rc = launch_records(rec_src, rec_dst, static_cast<const hck::CopyEntry*>(slot->dev), /*on_host=*/false, n,
+                                    hck::RecordCopy::kTier, s);
             if (!rc) rc = release_slot(slot, s);
             if (rc) return rc;
         }
@@ -707,17 +735,20 @@ struct kv_pool {
     // launch that reuses their hot pages on the same stream.
     int submit_victims(const Alloc& a, hipStream_t s) {
         if (a.victims.empty()) return KV_OK;
-        std::vector<hck::CopyEntry> copies, writes;
+        std::vector<hck::CopyEntry> copies, writes, clean;
         copies.reserve(a.victim_cold.size());
         for (const Victim& v : a.victims) {
             const Session& ss = sessions[v.sid];
             const int32_t at = v.sid * d.max_pages_per_session + v.page;
-            if (ss.cold[v.page] < 0)
+            if (ss.cold[v.page] < 0) {
                 copies.push_back(hck::CopyEntry{ss.hot[v.page], a.victim_cold[copies.size()], at, -1});
-            else
+            } else {
                 writes.push_back(hck::CopyEntry{-1, -1, at, -1});
+                if (bounds) clean.push_back(hck::CopyEntry{ss.hot[v.page], ss.cold[v.page], -1, -1});
+            }
         }
         int rc = submit_copies(false, copies, writes, s, KV_KERNEL_EVICT_COPY);
+        if (!rc) rc = submit_renewed_bounds(clean, s);
         if (!rc) rc = note_frees(s);
         return rc;
     }
@@ -1153,7 +1184,8 @@ int kv_fork_sessions(kv_pool* pool, const int32_t* sids, const int32_t* kept, in
             if (!rc) rc = pool->submit_victims(a, st);
             if (!rc) rc = pool->submit_copies(true, fetched, {}, st, KV_KERNEL_PAGE_COPY);
             if (!rc) rc = pool->submit_fork(forks, st);
-            if (!rc) rc = pool->submit_bounds_copies(pool->bounds_hot, pool->bounds_hot, records, st);
+            if (!rc) rc = pool->submit_bounds_copies(pool->bounds_hot, pool->bounds_hot, records,
+                                                     hck::RecordCopy::kBranch, st);
             if (rc) return rc;
         }
         pool->commit_victims(a);
@@ -1554,15 +1586,21 @@ int kv_evict_sessions(kv_pool* pool, const int32_t* sids, int32_t n, kv_stream_t
     if (!pool->meta) {
         DeviceGuard g(pool->d.device);
         hipStream_t st = pool->strm(stream);
-        // only the dirty pages make a list; the rows are cleared by range
-        std::vector<hck::CopyEntry> entries;
+        // only the dirty pages make a list (and, for their bounds, the others); the rows are cleared
+        // by range
+        std::vector<hck::CopyEntry> entries, clean;
         entries.reserve(dst.size());
         for (int32_t sid : ids) {
             const Session& s = pool->sessions[sid];
-            for (size_t i = 0; i < s.hot.size(); ++i)
-                if (s.cold[i] < 0) entries.push_back(hck::CopyEntry{s.hot[i], dst[entries.size()], -1, -1});
+            for (size_t i = 0; i < s.hot.size(); ++i) {
+                if (s.cold[i] < 0)
+                    entries.push_back(hck::CopyEntry{s.hot[i], dst[entries.size()], -1, -1});
+                else if (pool->bounds && s.hot[i] >= 0)
+                    clean.push_back(hck::CopyEntry{s.hot[i], s.cold[i], -1, -1});
+            }
         }
         int rc = pool->submit_copies(false, entries, {}, st, KV_KERNEL_EVICT_COPY);
+        if (!rc) rc = pool->submit_renewed_bounds(clean, st);
         if (!rc) rc = pool->clear_rows_and_free(ids, st);
         if (rc) return rc;
     }

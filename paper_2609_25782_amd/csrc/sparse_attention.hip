@@ -12,7 +12,8 @@
 // float32.  Which pages are picked therefore does not depend on the order of any sum.
 //
 // Records.  A page's record of one layer is [KV head][lo: D bytes, hi: D bytes], then 16
-// bytes of which byte h is the power of head h: 1/31 of the page's K and V in bfloat16.
+// bytes of which byte h is the power of head h (7 bits) and whether its bounds are newer than those
+// of the page's cold copy (the top bit): 1/31 of the page's K and V in bfloat16.
 //
 // What bounds them (bf16, 32 query and 4 KV heads of 128 dims, a layer of 32 sessions of 8K-32K
 // tokens on shuffled pages, unless said; the card reads 7.0 TB/s):
@@ -63,7 +64,9 @@ __device__ __forceinline__ int power_for(float top) {
     return e;
 }
 
-__device__ __forceinline__ int clamp_power(int e) {
+// The power in a record's byte: its low 7 bits, signed.
+__device__ __forceinline__ int power_of(char byte) {
+    const int e = (static_cast<int>(byte) << 25) >> 25;
     return e < -kPowerLimit ? -kPowerLimit : e > kPowerLimit ? kPowerLimit : e;
 }
 
@@ -265,7 +268,8 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_update_kernel(const Boun
                 __builtin_amdgcn_raw_buffer_store_b8(static_cast<unsigned char>(qh), rec, out + D, 0, 0);
             }
         }
-        __builtin_amdgcn_raw_buffer_store_b8(static_cast<unsigned char>(e), rec, a.num_kv_heads * 2 * D + u.head, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b8(static_cast<unsigned char>((e & 0x7F) | 0x80), rec,
+                                             a.num_kv_heads * 2 * D + u.head, 0, 0);
     };
     // A wave's pages are every step-th from its first on, 64 of them at a time: lane j holds the
     // j-th's place.  Its (page, head) pairs follow each other with the next one's keys in flight
@@ -324,8 +328,7 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_read_kernel(const Bounds
         const char* rec = a.bounds + layer * a.layer_stride + static_cast<int64_t>(at < 0 ? 0 : at) * a.record;
         for (int word = first; word < per; word += kBlockThreads) {
             const unsigned w = reinterpret_cast<const unsigned*>(rec)[word];
-            const int e = static_cast<signed char>(rec[4 * per + word * 2 / a.head_dim]);
-            const float unit = at < 0 ? __builtin_nanf("") : two_to(clamp_power(e));
+            const float unit = at < 0 ? __builtin_nanf("") : two_to(power_of(rec[4 * per + word * 2 / a.head_dim]));
             f32x4 v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = static_cast<float>(static_cast<signed char>(w >> (8 * j))) * unit;
@@ -334,11 +337,14 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_read_kernel(const Bounds
     }
 }
 
-// Records of copied pages: entry e's from page e.src of one pool to page e.dst of the other.
+// Records that follow pages: entry e's from page e.src of one pool to page e.dst of the other.  With
+// kRenewed a head's bounds and power are written only where they were set since the two records were
+// alike: of sessions that share a cold page, one whose bounds are old does not undo another's.
 template <typename Entries>
 __device__ __forceinline__ void copy_records(const PoolGeom& src, const PoolGeom& dst, const Entries& entries, int32_t n,
-                                             int words) {
+                                             int heads, int head_words, RecordCopy how) {
     const int layer = static_cast<int>(blockIdx.y);
+    const int words = heads * head_words + 1;
     const int64_t total = static_cast<int64_t>(n) * words;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlockThreads + threadIdx.x; i < total;
          i += static_cast<int64_t>(gridDim.x) * kBlockThreads) {
@@ -346,15 +352,27 @@ __device__ __forceinline__ void copy_records(const PoolGeom& src, const PoolGeom
         const int word = static_cast<int>(i - static_cast<int64_t>(k) * words);
         const CopyEntry e = entries[k];
         if (e.src < 0) continue;
-        reinterpret_cast<u32x4*>(slice_at(dst, e.dst, layer))[word] =
-            reinterpret_cast<const u32x4*>(slice_at(src, e.src, layer))[word];
+        const char* from = slice_at(src, e.src, layer);
+        char* to = slice_at(dst, e.dst, layer);
+        const char* powers = from + 16 * (words - 1);
+        if (how == RecordCopy::kRenewed) {
+            if (word == words - 1) {
+                for (int h = 0; h < heads; ++h)
+                    if (powers[h] & 0x80) to[16 * word + h] = static_cast<char>(powers[h] & 0x7F);
+                continue;
+            }
+            if (!(powers[word / head_words] & 0x80)) continue;
+        }
+        u32x4 w = reinterpret_cast<const u32x4*>(from)[word];
+        if (word == words - 1 && how == RecordCopy::kTier) w &= 0x7F7F7F7Fu;   // the two are alike now
+        reinterpret_cast<u32x4*>(to)[word] = w;
     }
 }
 
 __global__ __launch_bounds__(kBlockThreads) void bounds_copy_kernel(const PoolGeom src, const PoolGeom dst,
                                                                     const CopyEntry* __restrict__ entries, int32_t n,
-                                                                    int words) {
-    copy_records(src, dst, entries, n, words);
+                                                                    int heads, int head_words, RecordCopy how) {
+    copy_records(src, dst, entries, n, heads, head_words, how);
 }
 
 // The same for a list in the kernel arguments.
@@ -363,8 +381,9 @@ struct RecordList {
     __device__ const CopyEntry& operator[](int i) const { return e[i]; }
 };
 __global__ __launch_bounds__(kBlockThreads) void bounds_copy_inline_kernel(const PoolGeom src, const PoolGeom dst,
-                                                                           int32_t n, int words, const RecordList list) {
-    copy_records(src, dst, list, n, words);
+                                                                           int32_t n, int heads, int head_words,
+                                                                           RecordCopy how, const RecordList list) {
+    copy_records(src, dst, list, n, heads, head_words, how);
 }
 
 // ---------------------------------------------------------------------------
@@ -464,7 +483,7 @@ template <int D, typename F>
 __device__ __forceinline__ unsigned score_pages(const QueryRows<D>& q, const char* bounds, const SelectArgs& a, int g,
                                                 int at, int lane, F&& meanwhile) {
     const int part = lane >> 4, rec = at < 0 ? 0 : at;
-    const int e = static_cast<signed char>(bounds[static_cast<int64_t>(rec) * a.record + a.num_kv_heads * 2 * D + g]);
+    const char e = bounds[static_cast<int64_t>(rec) * a.record + a.num_kv_heads * 2 * D + g];
     u32x4 w[4][2 * D / 64];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -490,7 +509,7 @@ __device__ __forceinline__ unsigned score_pages(const QueryRows<D>& q, const cha
         x = fmaxf(x, __shfl_xor(x, 32));
         best = part == t ? x : best;
     }
-    return at < 0 ? kKeyBad : score_key(best * two_to(clamp_power(e)));
+    return at < 0 ? kKeyBad : score_key(best * two_to(power_of(e)));
 }
 
 // Keys of all pages of the rows that have more pages than are picked.  A block takes chunks of 64
@@ -1084,19 +1103,23 @@ hipError_t launch_bounds_read(const BoundsReadArgs& a, int32_t num_layers, hipSt
     return hipGetLastError();
 }
 
-hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t record, int32_t layers,
-                              const CopyEntry* entries, bool on_host, int32_t n, hipStream_t s) {
+hipError_t launch_bounds_copy(const PoolGeom& src, const PoolGeom& dst, int32_t num_kv_heads, int32_t head_dim,
+                              int32_t layers, const CopyEntry* entries, bool on_host, int32_t n, RecordCopy how,
+                              hipStream_t s) {
     if (n <= 0) return hipSuccess;
     if (on_host && n > kCopyInline) return hipErrorInvalidValue;
-    const int words = record / 16;
-    const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(n) * words + kBlockThreads - 1) / kBlockThreads, 65536);
+    const int heads = num_kv_heads, head_words = 2 * head_dim / 16;
+    const int64_t words = static_cast<int64_t>(n) * (heads * head_words + 1);
+    const int64_t blocks = std::min<int64_t>((words + kBlockThreads - 1) / kBlockThreads, 65536);
     const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(layers));
     if (on_host) {
         RecordList list = {};
         for (int32_t i = 0; i < n; ++i) list.e[i] = entries[i];
-        hipLaunchKernelGGL(bounds_copy_inline_kernel, grid, dim3(kBlockThreads), 0, s, src, dst, n, words, list);
+        hipLaunchKernelGGL(bounds_copy_inline_kernel, grid, dim3(kBlockThreads), 0, s, src, dst, n, heads, head_words, how,
+                           list);
     } else {
-        hipLaunchKernelGGL(bounds_copy_kernel, grid, dim3(kBlockThreads), 0, s, src, dst, entries, n, words);
+        hipLaunchKernelGGL(bounds_copy_kernel, grid, dim3(kBlockThreads), 0, s, src, dst, entries, n, heads, head_words,
+                           how);
     }
     return hipGetLastError();
 }

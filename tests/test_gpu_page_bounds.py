@@ -360,3 +360,233 @@ def test_refusals():
     p.set_bounds(False)
     with pytest.raises(kv.KVError):
         p.update_bounds(0, 1, lens)
+
+
+# -- bounds that are set while a page has a cold copy already ------------------
+
+
+def clean_sessions(n, where="device", dtype="bf16", sessions=1, seed=20, room=None):
+    """Sessions of n tokens each with valid cold copies of all pages, resident: set up before the pool
+    keeps bounds, as a cache that was running already has them."""
+    from paper_2609_25782_amd.pool import HotColdPool
+    pages = pages_for(n)
+    s = Sessions([n] * sessions, 4, 2, 64, dtype, seed=seed, layers=2, max_sessions=sessions + 4)
+    if room is None:
+        room = sessions * pages + pages
+    p = s.pool = HotColdPool(2, 2, 64, dtype, room, 2 * sessions * pages + 8, sessions + 4, pages + 2, cold_location=where)
+    for b in range(sessions):
+        p.create_session(n)
+        p.write_tokens_layers(b, 0, 0, s.k[b].cuda(), s.v[b].cuda())
+    for b in range(sessions):
+        p.evict(b)
+    for b in range(sessions):
+        p.resume(b)
+    p.set_bounds(True)
+    return s
+
+
+def bounds_of(s, b, n):
+    return np.stack([values(*page_bounds(s.k[b][layer], n)) for layer in range(2)])
+
+
+def are(s, sid, want, cold=False):
+    hot, copies = s.pool.info(sid)[2:]
+    entries = [c | kv.KV_PAGE_COLD for c in copies] if cold else hot
+    assert min(entries) >= 0
+    got = s.pool.key_bounds(0, len(want), i32(entries)).cpu().double().numpy()
+    assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("where", ["device", "host"])
+@pytest.mark.parametrize("pages", [5, 128, 129, 300])
+@pytest.mark.parametrize("path", ["evict", "evict_pages", "victims"])
+def test_bounds_of_pages_with_cold_copies_survive(path, pages, where):
+    """An eviction that writes no page takes the bounds along all the same: of a session, of pages of a
+    paused one, and of pages that make room for another session."""
+    n = 16 * pages - 3
+    s = clean_sessions(n, where, room=pages + 4)
+    p, want = s.pool, bounds_of(s, 0, n)
+    p.update_bounds(0, 2, i32([n]))
+    are(s, 0, want)
+    written = p.stats()["pages_to_cold"]
+    if path == "evict":
+        p.evict(0)
+    else:
+        p.pause(0)
+        if path == "evict_pages":
+            assert p.evict_pages(pages - 1) == pages - 1
+            p.evict_pages(pages)
+        else:
+            p.destroy_session(p.create_session(16 * pages))
+            assert p.stats()["lru_evicted_pages"] == pages - 4
+            p.evict_pages(pages)
+    assert p.stats()["pages_to_cold"] == written
+    are(s, 0, want, cold=True)
+    p.create_session(16)                      # a page that the resume then cannot have
+    p.resume(0)
+    are(s, 0, want)
+
+
+def test_bounds_of_imported_pages_survive():
+    n = 200
+    s = clean_sessions(n)
+    p, want = s.pool, bounds_of(s, 0, n)
+    sid = p.import_cold(n, p.info(0)[3])
+    p.destroy_session(0)
+    p.resume(sid)
+    lens = torch.zeros(p.max_sessions, dtype=torch.int32, device="cuda")
+    lens[sid] = n
+    p.update_bounds(0, 2, lens)
+    for _ in range(2):
+        p.evict(sid)
+        p.resume(sid)
+        are(s, sid, want)
+
+
+def test_bounds_that_waited_for_a_resume_survive():
+    """A page that was full before its bounds were renewed, evicted and resumed in between."""
+    n = 16 * 6 + 9
+    s = clean_sessions(n)
+    p = s.pool
+    p.update_bounds(0, 2, i32([n]))
+    more = s.normal(2, 7, 2, 64), s.normal(2, 7, 2, 64)
+    s.k[0] = torch.cat([s.k[0], more[0]], dim=1)
+    p.extend(0, n + 7)
+    p.write_tokens_layers(0, 0, n, more[0].cuda(), more[1].cuda())
+    p.evict(0), p.resume(0)
+    p.update_bounds(0, 2, i32([n + 7]), starts=i32([n]))
+    want = bounds_of(s, 0, n + 7)
+    are(s, 0, want)
+    p.evict(0), p.resume(0)
+    are(s, 0, want)
+
+
+def test_bounds_of_promoted_pages_survive():
+    n = 16 * 9
+    s = clean_sessions(n)
+    p, want = s.pool, bounds_of(s, 0, n)
+    p.set_spill(True)
+    p.evict(0)
+    p.resume_lazy(0)
+    assert p.promote(9) == 9
+    p.update_bounds(0, 2, i32([n]))
+    p.evict(0)
+    p.resume_lazy(0)
+    are(s, 0, want, cold=True)
+    q = s.normal(1, 4, 64)
+    picks_of(s, q, [n], 4, 1, 1, choices(s, q, [n], 4, 1, 1))
+    assert p.promote(9) == 9
+    are(s, 0, want)
+
+
+def test_bounds_of_branches_that_share_cold_copies_survive():
+    n = 16 * 5
+    s = clean_sessions(n, room=20)
+    p, want = s.pool, bounds_of(s, 0, n)
+    p.update_bounds(0, 2, i32([n]))
+    child = p.fork(0)
+    assert p.info(child)[3] == p.info(0)[3]
+    for order in ([child, 0], [0, child]):
+        p.evict(order[0]), p.evict(order[1])
+        p.resume(order)
+        are(s, 0, want), are(s, child, want)
+    p.evict([0, child])
+    p.resume([child, 0])
+    are(s, 0, want), are(s, child, want)
+    twig = p.fork(child)                      # of pages whose records came back from the cold tier
+    are(s, twig, want)
+
+
+def test_a_branch_carries_renewed_bounds_to_the_shared_copies():
+    """The branch alone is evicted after its parent is gone: what it took over is what comes back."""
+    n = 16 * 5
+    s = clean_sessions(n)
+    p, want = s.pool, bounds_of(s, 0, n)
+    p.update_bounds(0, 2, i32([n]))
+    child = p.fork(0)
+    p.destroy_session(0)
+    p.evict(child), p.resume(child)
+    are(s, child, want)
+
+
+@pytest.mark.parametrize("together", [False, True])
+@pytest.mark.parametrize("n", [80, 16 * 150])
+def test_old_bounds_do_not_replace_renewed_ones(n, together):
+    """Two sessions with the same cold pages, of which one had its bounds renewed: the other's eviction
+    leaves the cold record as it is, before, after or in the same call."""
+    s = clean_sessions(n, room=3 * pages_for(n))
+    p, want = s.pool, bounds_of(s, 0, n)
+    twin = p.import_cold(n, p.info(0)[3])
+    p.resume(twin)
+    p.update_bounds(0, 2, i32([n]))
+    for order in ([0, twin], [twin, 0]):
+        if together:
+            p.evict(order)
+        else:
+            for sid in order:
+                p.evict(sid)
+        are(s, 0, want, cold=True)
+        p.resume([0, twin])
+        are(s, 0, want), are(s, twin, want)
+        at = i32(p.info(twin)[2]).long()      # the twin's records grow old again
+        record = 2 * 2 * 64 + 16
+        flat = p.bounds[:2 * record * (p.num_hot_pages + p.num_cold_pages)].view(2, -1, record)
+        flat[:, at] = 0
+        p.update_bounds(0, 2, i32([n]))
+
+
+def test_several_sessions_renew_the_same_cold_pages_at_once():
+    n = 16 * 140
+    s = clean_sessions(n, room=4 * 140)
+    p, want = s.pool, bounds_of(s, 0, n)
+    others = [p.import_cold(n, p.info(0)[3]) for _ in range(2)]
+    p.resume(others)
+    lens = torch.zeros(p.max_sessions, dtype=torch.int32, device="cuda")
+    lens[[0] + others] = n
+    p.update_bounds(0, 2, lens)
+    p.evict([others[1], 0, others[0]])
+    are(s, 0, want, cold=True)
+    p.resume([0] + others)
+    for sid in [0] + others:
+        are(s, sid, want)
+
+
+@pytest.mark.parametrize("pages", [6, 300])
+def test_a_captured_eviction_of_clean_pages_takes_their_bounds(pages):
+    """Replays after other calls have used the pool's copy lists."""
+    n = 16 * pages
+    s = clean_sessions(n, sessions=3, room=4 * pages)
+    p = s.pool
+    p.update_bounds(0, 2, i32([n] * 3))
+    want = bounds_of(s, 1, n)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        p.evict(1, stream=st)
+    saved = p.bounds.clone()
+    cold = i32(p.info(1)[3]).long() + p.num_hot_pages
+    record = 2 * 2 * 64 + 16
+    for turn in range(3):
+        p.bounds.copy_(saved)               # the session's old pages are free: resumes below may take them
+        p.bounds[:2 * record * (p.num_hot_pages + p.num_cold_pages)].view(2, -1, record)[:, cold] = 0
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        are(s, 1, want, cold=True)
+        p.evict(0), p.resume(0)                 # eager calls between the replays
+        p.evict(2), p.resume(2)
+        torch.cuda.synchronize()
+
+
+def test_evictions_without_bounds_leave_the_buffer_alone():
+    n = 16 * 4
+    s = clean_sessions(n)
+    p = s.pool
+    p.update_bounds(0, 2, i32([n]))
+    buf = p.bounds
+    p.set_bounds(False)
+    before = buf.clone()
+    p.evict(0), p.resume(0)
+    torch.cuda.synchronize()
+    assert torch.equal(buf, before)
