@@ -353,9 +353,16 @@ int kv_session_import_cold(kv_pool* pool, int32_t seq_len, const int32_t* cold_p
  * call fails rather than place a branch in the cold tier), and the parents' pages are
  * copied to them on `stream`, every page read once for all branches of its session and
  * call (up to 7); a spilled page is fetched from the cold tier.  Whole pages are copied,
- * slots past kept[i] included.  Pages whose 16 tokens are all kept are never written again:
- * the branch shares the parent's valid cold copies of them (an eviction then writes nothing;
- * a spilled page of the parent becomes shared).  Key bounds (kv_pool_set_bounds) go along.
+ * slots past kept[i] included.  The branch shares the parent's valid cold copies of pages
+ * whose 16 tokens are all kept (an eviction then writes nothing).  A spilled page of the
+ * parent becomes shared only if it lies wholly before the `kept` of the parent's last
+ * kv_session_reserve or kv_session_extend: calls resolved on the device may write the others
+ * in place.  One that is shared now can be written (kv_write_tokens, kv_append_tokens,
+ * a kv_session_reserve that reaches back into it) only once it is promoted: KV_ERR_STATE
+ * before.  Key bounds (kv_pool_set_bounds) go along.
+ * kept[i] counts tokens that are there: a parent's length after kv_session_reserve counts room
+ * as well, and a branch that keeps that length has the same room, to be reserved again from
+ * the number of tokens really held.
  * The new ids (lowest free rows) go to sids_out[0 .. n), host.  The parents stay as they
  * are; their tokens must have been written on `stream` or be ordered before it.
  * Errors: KV_ERR_INVALID (ids, kept outside [0, length], too few free session slots),

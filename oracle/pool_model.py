@@ -41,6 +41,8 @@ Readings where the paper is silent:
   freed.  Extending is reserving from the session's length on.
 * A branch gets hot pages of its own (never spilled ones) with the parent's tokens, and
   shares the parent's cold copies of pages that are full: those are never written again.
+  Spilled pages that hold tokens at or past the `kept` of the parent's last reserve (or
+  extend) may still be written in place and are not shared.
 * Cold pages may be shared by several paused sessions (a virtualised cold
   pool); they are reference counted and freed when the last user lets go.
 * Every failing call leaves the whole state unchanged.
@@ -95,6 +97,7 @@ class _Session:
     hot: List[int] = field(default_factory=list)   # -1 = not resident
     cold: List[int] = field(default_factory=list)  # -1 = no valid cold copy
     spilled: List[bool] = field(default_factory=list)  # row entry names the cold page
+    written: int = 0   # tokens before this one are there; later ones may be room
 
 
 def _pages(seq_len: int) -> int:
@@ -228,7 +231,7 @@ class PoolModel:
         self._take_cold(spill)
         self.sessions[sid] = _Session(ACTIVE, seq_len, 0, list(pages) + [-1] * len(spill),
                                       [-1] * len(pages) + list(spill),
-                                      [False] * len(pages) + [True] * len(spill))
+                                      [False] * len(pages) + [True] * len(spill), seq_len)
         return sid
 
     def extend(self, sid: int, new_len: int) -> None:
@@ -251,6 +254,7 @@ class PoolModel:
         s.hot += list(pages) + [-1] * len(spill)
         s.cold += [-1] * len(pages) + list(spill)
         s.spilled += [False] * len(pages) + [True] * len(spill)
+        s.written = s.seq_len
         s.seq_len = new_len
 
     def fork(self, sids: Sequence[int], kept: Sequence[int]) -> List[int]:
@@ -272,11 +276,12 @@ class PoolModel:
         for sid, s, src, k in zip(free, parents, sids, kept):
             hot = [next(it) for _ in range(_pages(k))]
             whole = k // PAGE_TOKENS         # pages all of whose slots are kept tokens
-            shared = s.cold[:whole]
+            shared = [-1 if s.hot[i] < 0 and (i + 1) * PAGE_TOKENS > s.written else s.cold[i] for i in range(whole)]
             for c in shared:
                 if c >= 0:
                     self.cold_ref[c] += 1
-            self.sessions[sid] = _Session(ACTIVE, k, 0, hot, shared + [-1] * (len(hot) - whole), [False] * len(hot))
+            self.sessions[sid] = _Session(ACTIVE, k, 0, hot, shared + [-1] * (len(hot) - whole), [False] * len(hot),
+                                          min(k, s.written))
             self.last_fork += [(src, i, h) for i, h in enumerate(hot)]
         return free[:len(parents)]
 
@@ -309,7 +314,7 @@ class PoolModel:
             self.cold_free.discard(p)
             self.cold_ref[p] += 1
         self.sessions[sid] = _Session(PAUSED, seq_len, self._tick(), [-1] * n, list(cold_pages),
-                                      [False] * n)
+                                      [False] * n, seq_len)
         return sid
 
     def evict(self, sid: int):
@@ -465,6 +470,7 @@ class PoolModel:
         s.hot += list(pages) + [-1] * len(spill)
         s.cold += [-1] * len(pages) + list(spill)
         s.spilled += [False] * len(pages) + [True] * len(spill)
+        s.written = kept
         s.seq_len = new_len
 
     def promote(self, n: int):

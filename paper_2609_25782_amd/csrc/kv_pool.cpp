@@ -90,6 +90,7 @@ struct Session {
     std::vector<int32_t> hot;   // hot page per logical page, -1 = not resident
     std::vector<int32_t> cold;  // cold page per logical page, -1 = no valid copy
     std::vector<uint8_t> spilled;  // 1: the row entry names the cold page (spill)
+    int32_t written = 0;        // `kept` of the last reserve: later tokens may still be written by the device
 };
 
 // One resident page of a paused session chosen for eviction.
@@ -827,6 +828,7 @@ struct kv_pool {
         s.spilled.resize(stay);
         s.spilled.resize(hot_end, 0);
         s.spilled.resize(n_new, 1);
+        s.written = kept;
         s.seq_len = new_seq_len;
         return KV_OK;
     }
@@ -1014,7 +1016,7 @@ int kv_session_create(kv_pool* pool, int32_t seq_len, const int32_t* hot_pages, 
     Session& ss = pool->sessions[sid];
     ss = Session();
     ss.state = KV_SESSION_ACTIVE;
-    ss.seq_len = seq_len;
+    ss.seq_len = ss.written = seq_len;
     ss.hot = a.pages;
     ss.hot.resize(nh + ns, -1);
     ss.cold.assign(nh, -1);
@@ -1092,7 +1094,7 @@ int kv_session_import_cold(kv_pool* pool, int32_t seq_len, const int32_t* cold_p
     Session& ss = pool->sessions[sid];
     ss = Session();
     ss.state = KV_SESSION_PAUSED;
-    ss.seq_len = seq_len;
+    ss.seq_len = ss.written = seq_len;
     ss.stamp = ++pool->clock;
     ss.hot.assign(n, -1);
     ss.cold = pages;
@@ -1122,9 +1124,10 @@ int kv_fork_sessions(kv_pool* pool, const int32_t* sids, const int32_t* kept, in
         Alloc a;
         int rc = pool->plan_alloc(need, {}, a, /*fresh_spill=*/false, /*allow_spill=*/false, /*all_hot=*/true);
         if (rc) return rc;
-        // The branches, their pages in argument and logical order.  Pages whose slots are all
-        // tokens are never written again, so their cold copies (a spilled page is its own) serve
-        // both sessions; a partly filled one will be, by either.
+        // The branches, their pages in argument and logical order.  Cold copies of pages whose slots
+        // are all tokens serve both sessions; a partly filled page will be written, by either.  A
+        // spilled page is its own cold copy and written in place, where the device's writes cannot be
+        // refused: it is shared only if none is to come.
         std::vector<Session> made(static_cast<size_t>(n));
         int64_t at = 0;
         for (int32_t i = 0; i < n; ++i) {
@@ -1135,7 +1138,10 @@ int kv_fork_sessions(kv_pool* pool, const int32_t* sids, const int32_t* kept, in
             f.seq_len = kept[i];
             f.hot.assign(a.pages.begin() + at, a.pages.begin() + at + pages);
             f.cold.assign(s.cold.begin(), s.cold.begin() + pages);
+            f.written = std::min(kept[i], s.written);
             if (kept[i] % KV_PAGE_TOKENS) f.cold[pages - 1] = -1;
+            for (int32_t p = s.written / KV_PAGE_TOKENS; p < pages; ++p)
+                if (s.hot[p] < 0) f.cold[p] = -1;
             f.spilled.assign(pages, 0);
             at += pages;
         }

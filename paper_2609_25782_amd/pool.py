@@ -118,7 +118,8 @@ class HotColdPool:
 
     def fork(self, sids, kept=None, stream=None):
         """Branches: the id of a new session with the first kept[i] tokens of session sids[i] (the same
-        may stand several times) for each i, or of one for plain numbers; `kept` None: all tokens."""
+        may stand several times) for each i, or of one for plain numbers; `kept` None: their lengths, which
+        after `reserve` count room as well: give the number of tokens then, or `reserve` the branch from it."""
         one = isinstance(sids, int)
         sids = [sids] if one else [int(x) for x in sids]
         if kept is None:

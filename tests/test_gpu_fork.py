@@ -107,6 +107,32 @@ def test_spilled_parents(where):
         assert torch.equal(p.key_bounds(0, 2, i32(p.info(child)[2])), bounds[:, :n])
 
 
+@pytest.mark.parametrize("where", ["device", "host"])
+def test_writes_to_spilled_room_stay_the_parents(where):
+    """Tokens that the device writes in place after the fork do not come back in the branch."""
+    from paper_2609_25782_amd.pool import HotColdPool
+    p = HotColdPool(2, 2, 64, "bf16", 8, 16, 4, 6, cold_location=where)
+    p.set_spill(True)
+    sid, filler = p.create_session(16), p.create_session(16 * 6)
+    p.reserve(sid, 16, 80)                       # of four pages of room one is hot, three are in the cold tier
+    assert [x >= 0 for x in p.info(sid)[2]] == [True, True, False, False, False]
+    p.fill_synthetic(sid, 3, 5, 1e-5)
+    p.destroy_session(filler)
+    child = p.fork(sid)
+    want = p.hot_page_bytes(p.info(child)[2])
+    at = torch.arange(16, 80, dtype=torch.int32, device="cuda")
+    k, v = (torch.full((2, 64, 2, 64), x, dtype=torch.bfloat16, device="cuda") for x in (7.0, 9.0))
+    p.append_tokens_table(0, p.page_table, torch.full_like(at, sid), at, k, v)
+    p.evict(child)
+    p.resume(child)
+    assert torch.equal(page_rows(p, child, 5), want)
+    p.evict(sid)
+    p.destroy_session(child)
+    p.resume(sid)
+    got = page_rows(p, sid, 5)[1:].contiguous().view(torch.bfloat16)
+    assert ((got == 7) | (got == 9)).all()
+
+
 def test_branches_make_room():
     """Pages of paused sessions are evicted for a branch, and come back with their content."""
     s = Sessions([64, 64], 2, 2, 64, "bf16", seed=5, spare=1, cold=8, stride=8, max_sessions=4)

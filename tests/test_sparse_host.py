@@ -138,6 +138,35 @@ def test_spilled_pages_of_a_parent(kv):
     kv.kv_pool_destroy(pool)
 
 
+def test_spilled_room_is_not_shared(kv):
+    """Pages that the device may still write in place (room of kv_session_reserve that found no hot page)
+    stay the parent's alone, also where a branch counts them as tokens; full pages before them are shared."""
+    pool, m = meta_pool(kv, hot=7, cold=8, sessions=6), PoolModel(7, 8, 6, 4, spill=True)
+    kv.kv_pool_set_spill(pool, True)
+    a = kv.kv_session_create(pool, 20)
+    assert m.create(20) == a
+    kv.kv_evict_session(pool, a), m.evict(a)
+    kv.kv_resume_sessions_lazy(pool, [a]), m.resume_lazy([a])       # pages 0 and 1 are in the cold tier,
+    filler = kv.kv_session_create(pool, 48)
+    more = kv.kv_session_create(pool, 64)
+    assert [m.create(48), m.create(64)] == [filler, more]
+    kv.kv_session_reserve(pool, a, 20, 64), m.reserve(a, 20, 64)    # and so are 2 and 3, all of them room
+    for sid in (filler, more):
+        kv.kv_session_destroy(pool, sid), m.destroy(sid)
+    assert m.sessions[a].hot == [-1] * 4 and len(set(m.sessions[a].cold)) == 4
+    child = kv.kv_fork_sessions(pool, [a], [64])
+    assert child == m.fork([a], [64])
+    same(kv, pool, m)
+    assert kv.kv_session_info(pool, child[0])[3] == [kv.kv_session_info(pool, a)[3][0], -1, -1, -1]
+    kv.kv_session_reserve(pool, a, 20, 60), m.reserve(a, 20, 60)    # the parent goes on in place
+    kv.kv_session_reserve(pool, child[0], 20, 50), m.reserve(child[0], 20, 50)
+    same(kv, pool, m)
+    with pytest.raises(kv.KVError) as e:
+        kv.kv_session_reserve(pool, a, 10, 60)                      # back into a page that is shared now
+    assert e.value.status == kv.KV_ERR_STATE
+    kv.kv_pool_destroy(pool)
+
+
 @pytest.mark.parametrize("spill", [False, True])
 def test_random_calls_against_the_model(kv, spill):
     rng = random.Random(11 + spill)
