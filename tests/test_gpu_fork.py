@@ -179,3 +179,25 @@ def test_refusals():
     assert p.stats() == before[2] and torch.equal(p.page_table, before[1])
     assert torch.equal(p.hot.view(torch.int32), before[0].view(torch.int32))
     assert p.fork([], []) == []
+
+
+@pytest.mark.parametrize("kept", [90, 96, 81])
+def test_writes_to_a_branch_leave_its_parent_as_it_is(kept):
+    """In the page that the branch has filled in part, in one that it holds whole, and in new ones."""
+    s = Sessions([100], 8, 2, 128, "bf16", seed=8, layers=2, spare=40, stride=20, max_sessions=4)
+    p = s.pool
+    child = p.fork(0, kept)
+    before = p.hot_page_bytes(s.pages[0])
+    mine = page_rows(p, child, pages_for(kept))
+    assert torch.equal(mine, before[:pages_for(kept)])
+    p.extend(child, kept + 20)
+    k, v = s.normal(2, 40, 2, 128).cuda(), s.normal(2, 40, 2, 128).cuda()
+    p.write_tokens_layers(child, 0, kept - 20, k, v)
+    at = i32([3, 40])
+    p.append_tokens_table(0, p.page_table, torch.full_like(at, child), at, k[:, :2].contiguous(), v[:, :2].contiguous())
+    after = page_rows(p, child, pages_for(kept + 20))
+    written = sorted({0, 2} | {t // 16 for t in range(kept - 20, kept + 20)})
+    for i in range(pages_for(kept)):
+        assert torch.equal(after[i], mine[i]) == (i not in written), i
+    assert torch.equal(p.hot_page_bytes(s.pages[0]), before) and torch.equal(page_rows(p, 0, 7), before)
+    assert p.info(0)[1] == 100

@@ -590,3 +590,99 @@ def test_evictions_without_bounds_leave_the_buffer_alone():
     p.evict(0), p.resume(0)
     torch.cuda.synchronize()
     assert torch.equal(buf, before)
+
+
+# -- the choice of tables of more than 512 pages a row: scores and choice in kernels of their own -------
+
+
+def wide(s, rows, stride=600):
+    """The first rows of the pool's table in one of `stride` pages a row; entries past a row's end name
+    page 0 of the pool, whose keys must not matter."""
+    table = torch.zeros((rows, stride), dtype=torch.int32, device="cuda")
+    own = s.pool.page_table[:rows]
+    for b in range(rows):
+        n = pages_for(s.lens[b])
+        table[b, :n] = own[b, :n]
+    return table
+
+
+@pytest.mark.parametrize("width,first,recent", [(1, 0, 0), (5, 2, 3), (9, 1, 2), (40, 3, 1)])
+@pytest.mark.parametrize("hq,hkv,d,dtype", SHAPES + [(16, 8, 64, "bf16"), (32, 16, 128, "bf16"), (6, 6, 64, "f32"),
+                                                     (16, 16, 128, "f32"), (32, 2, 128, "bf16")])
+def test_picks_of_wide_tables_match_the_definition(hq, hkv, d, dtype, width, first, recent):
+    """Every head layout and type, rows shorter than a block's turn and longer ones."""
+    lens = [1, 0, 16, 150, 333, 16 * 40, 16 * 41, 1000, 16 * 130 + 5]
+    s = spread(Sessions(lens, hq, hkv, d, dtype, seed=21), 22)
+    q = s.normal(len(lens), hq, d)
+    s.pool.set_bounds(True)
+    s.pool.update_bounds(0, 1, i32(lens))
+    assert kv.paged_select_workspace_bytes(s.pool.handle, len(lens), 600, width) > 256
+    picks_of(s, q, lens, width, first, recent, choices(s, q, lens, width, first, recent), page_table=wide(s, len(lens)))
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(8, 4, 128, "bf16"), (2, 2, 64, "f32"), (3, 3, 64, "bf16")])
+def test_wide_tables_of_many_rows(hq, hkv, d, dtype):
+    """So many rows that a block goes on to further pages of its row, some rows far longer than others."""
+    rng = np.random.default_rng(23)
+    lens = [int(x) for x in rng.integers(0, 120, 520)]
+    lens[7], lens[300], lens[519] = 16 * 700, 16 * 1000 + 3, 16 * 257
+    s = Sessions(lens, hq, hkv, d, dtype, seed=23)
+    q = s.normal(len(lens), hq, d)
+    s.pool.set_bounds(True)
+    s.pool.update_bounds(0, 1, i32(lens))
+    assert s.pool.stride > 512
+    picks_of(s, q, lens, 5, 1, 1, choices(s, q, lens, 5, 1, 1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_wide_tables_with_entries_that_name_no_page(dtype):
+    s = Sessions([16 * 50, 16 * 200], 8, 2, 64, dtype, seed=24)
+    q = s.normal(2, 8, 64)
+    lens = [800, 3200]
+    s.pool.set_bounds(True)
+    s.pool.update_bounds(0, 1, i32(lens))
+    table = wide(s, 2)
+    bad = [[20, 33], [0, 64, 199]]
+    sc = [scores(q[b], *page_bounds(s.k[b][0], n)) for b, n in enumerate(lens)]
+    for b, pages in enumerate(bad):
+        table[b, pages] = i32([-1, 1 << 25, (1 << 30) | 3][:len(pages)])
+        sc[b][:, pages] = np.inf
+    for width in (1, 2, 7):
+        want = [[choose(list(sc[b][g]), width, 0, 0) for g in range(2)] for b in range(2)]
+        picks_of(s, q, lens, width, 0, 0, want, page_table=table)
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan"), 2.0 ** 80, 2.0 ** -80])
+@pytest.mark.parametrize("dtype,d", [("f32", 128), ("bf16", 64)])
+def test_wide_tables_with_queries_of_any_size(dtype, d, value):
+    s = Sessions([16 * 60], 4, 2, d, dtype, seed=25)
+    q = s.normal(1, 4, d)
+    if value == value and abs(value) != float("inf"):
+        q = q * value
+    else:
+        q[0, 1, 17] = value
+    s.pool.set_bounds(True)
+    s.pool.update_bounds(0, 1, i32([960]))
+    picks_of(s, q, [960], 11, 1, 1, choices(s, q, [960], 11, 1, 1), page_table=wide(s, 1))
+
+
+def test_ties_of_wide_tables_go_to_the_lowest_pages():
+    s = Sessions([16 * 300], 4, 2, 128, "bf16", seed=26)
+    s.k[0][0] = s.k[0][0, :1]
+    s.k[0][0, 16 * 200:16 * 201] = s.normal(1, 2, 128)
+    q = s.normal(1, 4, 128)
+    s.pool.write_tokens_layers(0, 0, 0, s.k[0].cuda(), s.v[0].cuda())
+    s.pool.set_bounds(True)
+    s.pool.update_bounds(0, 1, i32([4800]))
+    for width, first, recent in ((1, 0, 0), (64, 0, 0), (65, 1, 1), (299, 0, 0)):
+        picks_of(s, q, [4800], width, first, recent, choices(s, q, [4800], width, first, recent), page_table=wide(s, 1))
+
+
+def test_wide_tables_with_lengths_that_do_not_fit():
+    s = Sessions([200, 200, 200, 200], 4, 2, 64, "bf16", seed=27)
+    q = s.normal(4, 4, 64)
+    s.pool.set_bounds(True)
+    s.pool.update_bounds(0, 1, i32([200] * 4))
+    lens = [-1, 0, 16 * 600 + 1, 200]
+    want = [[[], []]] * 3 + choices(s, q, [0, 0, 0, 200], 5, 1, 1)[3:]
+    picks_of(s, q, lens, 5, 1, 1, want, page_table=wide(s, 4))

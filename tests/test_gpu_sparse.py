@@ -376,3 +376,98 @@ def test_refusals():
         p.sparse_decode(0, q, lens, picks.long(), counts)
     with pytest.raises(AssertionError):
         p.sparse_decode(0, q, lens, picks[:, :1].contiguous(), counts)
+
+
+def test_captured_steps_have_workspaces_of_their_own():
+    """Two graphs whose calls need workspaces (scores of a wide table, partial results of a long list), with
+    queries of their own, replayed side by side and between eager calls."""
+    lens = [9000, 7000]
+    s = Sessions(lens, 4, 1, 128, "bf16", seed=23)
+    p = s.pool
+    width, n = 60, i32(lens)
+    assert kv.paged_select_workspace_bytes(p.handle, 2, p.stride, width) > 256
+    assert kv.paged_sparse_workspace_bytes(p.handle, 2, 4, width) > 256
+    p.set_bounds(True)
+    p.update_bounds(0, 1, n)
+    qs = [torch.zeros(2, 4, 128, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+
+    def run(q):
+        picks, counts = p.select_pages(0, q, n, width)
+        return picks, p.sparse_decode(0, q, n, picks, counts)
+    streams, graphs, outs = [torch.cuda.Stream() for _ in range(2)], [], []
+    for q, st in zip(qs, streams):
+        with torch.cuda.stream(st):
+            run(q)
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=st):
+                outs.append(run(q))
+            graphs.append(g)
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for q in qs:
+            q.copy_(s.normal(2, 4, 128))
+        want = [run(q) for q in qs]
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        eager = run(qs[2])
+        torch.cuda.synchronize()
+        for got, ref in zip(outs + [eager], want):
+            assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1]), turn
+    for q, out in zip(qs, outs):
+        lists = []
+        for b, m in enumerate(lens):
+            sc = scores(q[b].cpu(), *page_bounds(s.k[b][0], m))
+            lists.append([choose(list(sc[0]), width, 1, 2)])
+        check(out[1], *reference(s, q.cpu(), lens, lists))
+
+
+def test_two_streams_have_workspaces_of_their_own():
+    s = Sessions([9000] * 2, 4, 1, 128, "f32", seed=24)
+    p, n, width = s.pool, i32([9000] * 2), 60
+    assert kv.paged_select_workspace_bytes(p.handle, 2, p.stride, width) > 256
+    assert kv.paged_sparse_workspace_bytes(p.handle, 2, 4, width) > 256
+    p.set_bounds(True)
+    p.update_bounds(0, 1, n)
+    qs = [s.normal(2, 4, 128).cuda() for _ in range(2)]
+
+    def one(q, stream=None):
+        picks, counts = p.select_pages(0, q, n, width, stream=stream)
+        return picks, p.sparse_decode(0, q, n, picks, counts, stream=stream)
+    want = [one(q) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        got = [one(q, st) for q, st in zip(qs, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_spilled_pages_in_host_memory(dtype):
+    """Bounds, choice and attention over pages that lie in pinned host memory."""
+    from paper_2609_25782_amd.pool import HotColdPool
+    lens = [300, 16 * 20]
+    s = Sessions(lens, 8, 2, 128, dtype, seed=25)
+    p = s.pool = HotColdPool(1, 2, 128, dtype, 44, 44, 3, 24, cold_location="host")
+    for b in range(2):
+        p.create_session(lens[b])
+        p.write_tokens_layers(b, 0, 0, s.k[b].cuda(), s.v[b].cuda())
+    p.set_spill(True)
+    p.evict([0, 1])
+    p.resume_lazy([0, 1])
+    assert p.promote(7) == 7
+    p.set_bounds(True)
+    p.update_bounds(0, 1, i32(lens))
+    q = s.normal(2, 8, 128)
+    picks, counts = p.select_pages(0, q.cuda(), i32(lens), 6)
+    lists = [[choose(list(x), 6, 1, 2) for x in scores(q[b], *page_bounds(s.k[b][0], lens[b]))] for b in range(2)]
+    assert picks.tolist() == lists
+    check(p.sparse_decode(0, q.cuda(), i32(lens), picks, counts), *reference(s, q, lens, lists))
+    entries = p.page_table[1, :20].contiguous()
+    assert (entries & kv.KV_PAGE_COLD != 0).all()
+    assert np.array_equal(p.key_bounds(0, 1, entries)[0].cpu().double().numpy(), values(*page_bounds(s.k[1][0], 320)))
+    all_pages = [[list(range(pages_for(n)))] * 2 for n in lens]
+    check(call(s, q, lens, all_pages, 20), *reference(s, q, lens, all_pages))
