@@ -971,7 +971,7 @@ size_t paged_select_workspace_bytes(const kv_pool* pool, int32_t batch, int64_t 
  *   q          device [batch][num_q_heads][head_dim], pool dtype, 16-byte aligned
  *   page_table, pt_stride, seq_lens   as paged_decode_attention; seq_lens[b] <= 0 or above 16 *
  *              pt_stride picks nothing
- *   width      1 .. ; first, recent >= 0, together at most width
+ *   width      1 .. 2^30; first, recent >= 0, together at most width
  *   picks      device int32 [batch][num_kv_heads][width]: page numbers of the row (not ids),
  *              ascending, then -1
  *   counts     device int32 [batch][num_kv_heads]: how many
@@ -997,6 +997,7 @@ size_t paged_sparse_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t 
  * over the tokens t < seq_lens[b] of pages picks[b][g][0 .. counts[b][g]) of row b.  A page that
  * is listed twice counts twice; an entry outside the row's pages [0, ceil(seq_lens[b] / 16)) is
  * passed over.  The lists may come from paged_select_pages or from any other rule.
+ *   width      1 .. 2^30
  *   counts     device int32 [batch][num_kv_heads] or NULL (width each); outside [0, width] it
  *              counts as the nearer end
  *   out        device [batch][num_q_heads][head_dim], written in full: zeros where a list holds

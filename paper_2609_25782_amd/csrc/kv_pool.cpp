@@ -1883,6 +1883,10 @@ int chunk_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_
     return KV_OK;
 }
 
+// Places of a list of pages: below what a block's threads count past in 32 bits.
+constexpr int32_t kMaxWidth = 1 << 30;
+bool width_ok(int32_t width) { return width >= 1 && width <= kMaxWidth; }
+
 // Checks and arguments that the choice of pages and the attention over them share.
 int sparse_args(kv_pool* pool, int32_t layer, const void* q, const int32_t* page_table, int64_t pt_stride,
                 const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, hck::SparseArgs& a) {
@@ -2117,7 +2121,7 @@ int kv_read_bounds(kv_pool* pool, int32_t layer_begin, int32_t num_layers, const
 }
 
 size_t paged_select_workspace_bytes(const kv_pool* pool, int32_t batch, int64_t pt_stride, int32_t width) {
-    if (!pool || pool->meta || batch < 0 || batch > kMaxDecodeBatch || width < 1 || pt_stride < 1 ||
+    if (!pool || pool->meta || batch < 0 || batch > kMaxDecodeBatch || !width_ok(width) || pt_stride < 1 ||
         static_cast<int64_t>(batch) * pt_stride >= (int64_t(1) << 31))
         return 0;
     return hck::select_workspace_bytes(static_cast<int64_t>(batch) * pool->d.num_kv_heads, pt_stride, width);
@@ -2128,9 +2132,10 @@ int paged_select_pages(kv_pool* pool, int32_t layer, const void* q, const int32_
                        int32_t recent, int32_t* picks, int32_t* counts, void* workspace, size_t ws_bytes,
                        kv_stream_t stream) {
     if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
+    if (!width_ok(width)) return fail(KV_ERR_INVALID, "width %d outside [1, %d]", width, kMaxWidth);
     if (!pool->bounds) return fail(KV_ERR_INVALID, "the pool keeps no bounds (kv_pool_set_bounds)");
-    if (width < 1 || first < 0 || recent < 0 || static_cast<int64_t>(first) + recent > width)
-        return fail(KV_ERR_INVALID, "width %d below 1 or below %d first and %d recent pages", width, first, recent);
+    if (first < 0 || recent < 0 || static_cast<int64_t>(first) + recent > width)
+        return fail(KV_ERR_INVALID, "width %d below %d first and %d recent pages", width, first, recent);
     if (batch < 0 || batch > kMaxDecodeBatch)
         return fail(KV_ERR_INVALID, "batch %d outside [0, %d]", batch, kMaxDecodeBatch);
     if (batch == 0) return KV_OK;
@@ -2174,7 +2179,7 @@ int paged_select_pages(kv_pool* pool, int32_t layer, const void* q, const int32_
 }
 
 size_t paged_sparse_workspace_bytes(const kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t width) {
-    if (!chunk_shape_ok(pool, batch, num_q_heads) || width < 1) return 0;
+    if (!chunk_shape_ok(pool, batch, num_q_heads) || !width_ok(width)) return 0;
     return hck::sparse_workspace_bytes(sparse_parts(pool, batch, width),
                                        static_cast<int64_t>(batch) * pool->d.num_kv_heads,
                                        num_q_heads / pool->d.num_kv_heads, pool->d.head_dim);
@@ -2185,7 +2190,7 @@ int paged_sparse_attention(kv_pool* pool, int32_t layer, const void* q, const in
                            int32_t batch, int32_t num_q_heads, float scale, void* out, void* workspace,
                            size_t ws_bytes, kv_stream_t stream) {
     if (!pool) return fail(KV_ERR_INVALID, "NULL pool");
-    if (width < 1) return fail(KV_ERR_INVALID, "width %d below 1", width);
+    if (!width_ok(width)) return fail(KV_ERR_INVALID, "width %d outside [1, %d]", width, kMaxWidth);
     if (batch < 0 || batch > kMaxDecodeBatch)
         return fail(KV_ERR_INVALID, "batch %d outside [0, %d]", batch, kMaxDecodeBatch);
     if (batch == 0) return KV_OK;

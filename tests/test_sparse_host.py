@@ -39,6 +39,18 @@ def test_metadata_only_pools_are_refused(kv):
     kv.kv_pool_destroy(meta)
 
 
+@pytest.mark.parametrize("width", [-1, 0, (1 << 30) + 1, (1 << 31) - 1])
+def test_widths_that_a_list_cannot_have(kv, width):
+    """Refused before anything else: the kernels count a list's places in 32 bits, a block's threads at a time."""
+    meta = meta_pool(kv)
+    for call in (lambda: kv.paged_sparse_attention(meta, 0, 16, 16, 4, 16, 16, 16, width, 1, 4, 0.1, 16, 256, 1 << 30),
+                 lambda: kv.paged_select_pages(meta, 0, 16, 16, 4, 16, 1, 4, width, 0, 0, 16, 16, 256, 1 << 30)):
+        with pytest.raises(kv.KVError) as e:
+            call()
+        assert e.value.status == kv.KV_ERR_INVALID and "width" in str(e.value)
+    kv.kv_pool_destroy(meta)
+
+
 @pytest.mark.parametrize("heads,d", [(1, 64), (4, 128), (16, 128), (3, 64)])
 def test_bounds_bytes(kv, heads, d):
     desc = kv.kv_pool_desc(3, heads, d, 16, kv.KV_DTYPE_BF16, 5, 7, 0, 1, 1, 0, 0)
