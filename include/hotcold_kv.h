@@ -904,8 +904,9 @@ int paged_tree_attention(kv_pool* pool, int32_t layer, const void* q, const void
  * kv_bounds_bytes: device bytes of a pool's bounds, about 1/31 of its pages in bfloat16 (0 if
  *   the descriptor is invalid).
  * kv_pool_set_bounds: keep bounds in `bounds` (device, caller-owned, 256-byte aligned, of at
- *   least kv_bounds_bytes; NULL: keep none).  What the buffer holds are the bounds: zeros, or
- *   anything else, until kv_update_bounds has set them.  From then on every copy of a page
+ *   least kv_bounds_bytes; NULL: keep none).  What the buffer holds are the bounds until
+ *   kv_update_bounds has set them: zero it first, since other bytes may read as bounds that were
+ *   set (for an eviction, below).  From then on every copy of a page
  *   between the pools and to a branch (resume, eviction, promotion, kv_fork_sessions) takes
  *   the page's bounds along, and an eviction that writes nothing because the page's cold copy
  *   is valid takes along bounds that were set since that copy was made or read (of sessions that

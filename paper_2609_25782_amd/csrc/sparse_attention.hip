@@ -339,7 +339,9 @@ __global__ __launch_bounds__(kBlockThreads) void bounds_read_kernel(const Bounds
 
 // Records that follow pages: entry e's from page e.src of one pool to page e.dst of the other.  With
 // kRenewed a head's bounds and power are written only where they were set since the two records were
-// alike: of sessions that share a cold page, one whose bounds are old does not undo another's.
+// alike: of sessions that share a cold page, one whose bounds are old does not undo another's.  An
+// eviction of 8 sessions of 20,000 tokens in 48 layers whose pages all have valid cold copies takes 26 us
+// of the GPU without bounds, 171 with none of them renewed, 334 with all (1 GB read and written).
 template <typename Entries>
 __device__ __forceinline__ void copy_records(const PoolGeom& src, const PoolGeom& dst, const Entries& entries, int32_t n,
                                              int heads, int head_words, RecordCopy how) {
@@ -561,10 +563,9 @@ __device__ __forceinline__ unsigned wave_max_u32(unsigned x) {
 }
 
 // Row b's picks for KV head g of its n > width pages: the first `first`, the last `recent` and the best
-// of those between.  The keys'
-// range is cut into bins, the bin that the last place falls into into finer ones, and so on until
-// a bin is wanted whole or is one value, whose places go to the lowest pages.  Bins stand in
-// descending order of their keys.
+// of those between.  The keys' range is cut into bins, the bin that the last place falls into into
+// finer ones, and so on until a bin is wanted whole or is one value, whose places go to the lowest
+// pages.  Bins stand in descending order of their keys.
 template <int THREADS, int KEYS>
 __device__ __forceinline__ void pick_pages(const SelectArgs& a, int b, int g, int n, const unsigned* keys) {
     constexpr int kWaves = THREADS / kWave;
@@ -829,7 +830,10 @@ __device__ __forceinline__ void sparse_page(SparseState<D, BF16>& st, PageRegs<D
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - st.shift);
     if constexpr (BF16) {
-        // weights rounded to bf16 for the product, the same rounded ones in the sum
+        // Weights rounded to bf16, which the product with V takes (as the decode over all pages does), and
+        // the same rounded ones in the sum: a common error of theirs cancels.  Outputs are then off by
+        // 0.0018-0.0020 of the values' size against 64 bits, with weights of 32 bits by 0.0016-0.0017:
+        // rounding the output is most of either.
         __bf16 pb[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
